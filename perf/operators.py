@@ -214,7 +214,7 @@ def prepare(case, seed):
         shape = SimpleNamespace(n_layers=1, H=nq * d, nq=nq, nkv=nkv, d=d, F=0, n_experts=0, top_k=0, moe_F=0, page=PAGE, eps=eps,
                                 theta=theta, qk_norm=norm, vocab=case.get("vocab", vocab))
         if case["op"] in ("tables", "attention"):
-            seqs, tokens, longest = len(i.kv), max(sum(i.new), 1), max(k + n for k, n in zip(i.kv, i.new))
+            seqs, tokens, longest = len(i.kv), sum(i.new) + 3, max(k + n for k, n in zip(i.kv, i.new))
         elif case["op"] == "append":
             seqs, tokens, longest = 1, case["tokens"] + case["pad"], 65536
         else:
