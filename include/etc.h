@@ -361,6 +361,139 @@ etc_status etc_graph_launch(etc_ctx *ctx, void *hip_stream);
 #define ETC_ROWSUM_NOALLOC_MAX_N 2048
 etc_status etc_rowsum_launch_noalloc(const float *A, float *C, int32_t n, void *hip_stream);
 
+/* ---- around the decode step: prompts, pages and sampling --------------------------------------
+ * What a serving loop needs beside etc_launch / etc_launch_tokens on the same paged KV pool: page tables and slot maps
+ * grown on the GPU from the requests' lengths, per-head norms + RoPE + KV append of a chunk of new tokens, attention of
+ * that chunk over the paged cache, and sampling of the next token.  One step of a server:
+ *     etc_serving_tables      once: cached and new lengths in; pages, slots and positions out
+ *     etc_serving_append      per layer: rows of the QKV projection in; query rows and cache rows out
+ *     etc_serving_attention   per layer: query rows in; attention rows out
+ *     etc_serving_sample      once: logits in; tokens out (token_in of the next etc_launch_tokens)
+ * A sequence of kv_len cached and n new tokens has its new tokens at positions kv_len .. kv_len + n - 1; with n = 1 this is
+ * the step etc_bind_step describes.  Sequences of one call are ragged and may be idle (n = 0).  RoPE, per-head norms, cache
+ * layout and scale are those of the decoder.
+ *
+ * Lengths and tables are device memory: no call synchronises, allocates or copies, each is one or two kernel launches on
+ * its stream and can be captured into a graph, whose replays then follow whatever the arrays hold.  A handle belongs to the
+ * device that was current at create (a call with another current device is refused) and owns the workspace of its calls:
+ * like a context it is not thread-safe and its calls go to one stream, or the caller orders them (two captured graphs that
+ * may run at the same time need two handles).  Unlike a megakernel launch nothing here waits for other workgroups, so these
+ * calls may share the device with any other work.
+ *
+ * What the kernels find in device memory they check before they use it as an index: a sequence with a length out of range,
+ * a page id or a slot outside the pool is left out (its outputs stay as they were; of a page id alone: its sequence gets
+ * meaningless values), nothing is read or written through it, and the first call, or etc_serving_read_error, that notices
+ * after the launch has finished returns ETC_ETIMEOUT, with the place in the error text.  That report clears it: the handle
+ * stays usable. */
+typedef struct etc_serving etc_serving; /* opaque, library-owned */
+
+typedef enum { ETC_BF16 = 0, ETC_FP32 = 1 } etc_dtype;
+
+typedef struct {
+    int32_t max_seqs;   /* sequences of a call, rows of etc_serving_sample; 1..1024 */
+    int32_t max_tokens; /* new tokens of a call, all sequences together; 1..2^20 */
+    int32_t max_kv_len; /* cached + new tokens of a sequence; 1..2^30 */
+} etc_serving_limits;
+
+/* Of `model` n_q_heads, n_kv_heads (any ratio up to 64), head_dim (64 or 128), page_size (a power of two), rms_eps,
+ * rope_theta, qk_norm and vocab (0: no sampling; <= 2^20) are read.  Allocates all workspace.  A model the kernels have no
+ * form for: ETC_EINVAL. */
+etc_status etc_serving_create(const etc_model_desc *model, const etc_serving_limits *limits, etc_serving **out);
+void etc_serving_destroy(etc_serving *s);                   /* synchronises */
+const char *etc_serving_last_error(const etc_serving *s);   /* s may be NULL: error of this thread's last failed create */
+/* Synchronises; word (host) = code (0: none), operator (1 tables .. 4 sample), index, value of what a kernel refused. */
+etc_status etc_serving_read_error(etc_serving *s, int32_t word[4]);
+
+/* Page tables and slot maps of one step.  Sequence b holds ceil(kv_len[b] / page_size) pages, the first entries of row b of
+ * block_table; it gets the ceil((kv_len[b] + new_len[b]) / page_size) it needs, missing ones from the end of free_pages in
+ * the order of the sequences: the j-th page taken is free_pages[*free_count - 1 - j].  New token i of sequence b is row
+ * q_indptr[b] + i: its position is kv_len[b] + i, its slot (page id) * page_size + position mod page_size.
+ * All or nothing: *status = 0, or the number of pages that free_pages lacks, or -1 (a length out of range, more tokens than
+ * n_tokens, more pages than a row of block_table or page_ids holds).  Other than 0 nothing is taken: block_table stays,
+ * *free_count_out = *free_count, total_len = kv_len, all slots are -1, q_indptr and page_indptr are 0, page_ids stays. */
+typedef struct {
+    int32_t n_seqs, n_tokens;       /* sequences; rows of slots and positions (rows behind the last token: slot -1, position 0) */
+    const int32_t *kv_len;          /* [n_seqs] */
+    const int32_t *new_len;         /* [n_seqs] */
+    int32_t *block_table;           /* [n_seqs][table_stride] in and out; rows at least table_cols long */
+    int64_t table_stride;
+    int32_t table_cols;
+    const int32_t *free_pages;      /* [free_cap] */
+    int32_t free_cap;
+    const int32_t *free_count;      /* [1] */
+    int32_t *free_count_out;        /* [1]; may be free_count */
+    int32_t *q_indptr;              /* [n_seqs + 1] */
+    int32_t *slots;                 /* [n_tokens] */
+    int32_t *positions;             /* [n_tokens] */
+    int32_t *total_len;             /* [n_seqs] kv_len + new_len, or NULL; may be kv_len */
+    int32_t *page_indptr;           /* [n_seqs + 1] and page_ids [page_ids_cap]: the pages as etc_bind_step takes them */
+    int32_t *page_ids;              /* (with new_len = 1 the arrays of the next decode step), or both NULL */
+    int32_t page_ids_cap;
+    int32_t *status;                /* [1] */
+} etc_serving_tables_io;
+etc_status etc_serving_tables(etc_serving *s, const etc_serving_tables_io *io, void *hip_stream);
+
+/* Per-head RMSNorm of q and k (qk_norm models), RoPE, and the append to one layer's pools, in one pass over the rows of the
+ * QKV projection.  Row r goes to slot slots[r]; a row with a negative slot is left out (padding), its q_out row stays as it
+ * was.  A slot may occur once.  q, k, v: row r starts r * stride elements behind the pointer and holds heads * head_dim
+ * values, so the three may be parts of one fused projection output; 16-byte aligned, strides a multiple of 16 bytes.
+ * q_out may be q (bf16 rows without gaps).  The arithmetic is fp32 (angles fp64), rounded once, to bf16. */
+typedef struct {
+    int32_t n_tokens, dtype;        /* rows; etc_dtype of q, k, v */
+    const void *q, *k, *v;
+    int64_t q_stride, k_stride, v_stride;
+    const int32_t *positions;       /* [n_tokens] */
+    const int32_t *slots;           /* [n_tokens] */
+    const void *gq, *gk;            /* bf16 [head_dim]: gains of qk_norm models, else NULL */
+    void *q_out;                    /* bf16 [n_tokens][n_q_heads][head_dim] */
+    void *k_pages, *v_pages;        /* bf16 [n_pages][page_size][n_kv_heads][head_dim]: one layer's part of the pool */
+    int64_t n_pages;                /* n_pages * page_size < 2^31 */
+} etc_serving_append_io;
+etc_status etc_serving_append(etc_serving *s, const etc_serving_append_io *io, void *hip_stream);
+
+/* Attention of the new tokens over the paged cache, which holds their own keys and values already: the query at position p
+ * of a sequence sees its keys 0 .. p.  out = softmax(q . k / sqrt(head_dim)) . v, fp32 sums and softmax statistics.
+ * What lies in the pool outside a row's keys (later tokens of the chunk, slots behind the last token, pages of others) does
+ * not reach it, NaN and infinities included.  q rows behind q_indptr[n_seqs] are left alone. */
+typedef struct {
+    int32_t n_seqs, n_tokens;       /* sequences; rows of q and out */
+    const void *q;                  /* bf16 [n_tokens][n_q_heads][head_dim] */
+    void *out;                      /* bf16 [n_tokens][n_q_heads][head_dim]; not q */
+    const int32_t *q_indptr;        /* [n_seqs + 1]: rows of sequence b */
+    const int32_t *kv_len;          /* [n_seqs] tokens cached in front of the new ones */
+    const int32_t *block_table;     /* [n_seqs][table_stride], rows at least table_cols long */
+    int64_t table_stride;
+    int32_t table_cols;
+    const void *k_pages, *v_pages;  /* one layer's part of the pool, as in etc_serving_append */
+    int64_t n_pages;
+} etc_serving_attention_io;
+etc_status etc_serving_attention(etc_serving *s, const etc_serving_attention_io *io, void *hip_stream);
+
+/* One token per row of logits.  With w_i = exp((x_i - max x) / temperature) and the tokens in the order larger logit first,
+ * equal logits by lower id, three filters each keep a beginning of that order:
+ *   top_k > 0     the first top_k tokens
+ *   top_p < 1     of those, the fewest whose weights sum to top_p of theirs at least (one at least)
+ *   min_p > 0     the tokens with w_i >= min_p (one at least)
+ * The token is the first of what is kept, in that order, at which the running sum of weights passes u times the kept sum.
+ * A temperature that is not > 0 gives the first token of the order (greedy); settings out of range and NaN settings switch
+ * their filter off (top_p <= 0: one token).  NaN and -inf logits are banned, and next to +inf all finite ones; a row with
+ * nothing left gives token -1, kept 0, log-probability -inf.  Weights are summed in 64-bit fixed point (unit 2^-43 of the
+ * largest), so a result does not depend on the order of the sums; a weight below half a unit counts as 0. */
+typedef struct {
+    int32_t n_rows, dtype;          /* etc_dtype of logits */
+    const void *logits;             /* [n_rows][vocab], rows row_stride elements apart; any alignment of the type */
+    int64_t row_stride;
+    const float *u;                 /* [n_rows] random numbers in [0, 1) */
+    const float *temperature;       /* [n_rows], or NULL: 1 */
+    const int32_t *top_k;           /* [n_rows], or NULL: off */
+    const float *top_p;             /* [n_rows], or NULL: off */
+    const float *min_p;             /* [n_rows], or NULL: off */
+    int32_t *token_out;             /* [n_rows] */
+    float *logprob_out;             /* [n_rows] log of the drawn token's share of the kept weights (greedy: 0), or NULL */
+    int32_t *kept_out;              /* [n_rows] number of tokens kept (greedy: 1), or NULL */
+} etc_serving_sample_io;
+etc_status etc_serving_sample(etc_serving *s, const etc_serving_sample_io *io, void *hip_stream);
+
 /* ---- host-only inspection of the scheduling transformation (no device needed) ---------------
  * Instantiates the decoder's event-tensor graph for one sampled batch size exactly as etc_create
  * does and exposes the materialised tasks, static queues (Sec. 3.1), initial event counts (Sec. 2.1)

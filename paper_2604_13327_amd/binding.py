@@ -26,7 +26,9 @@ EXPORTS = ["etc_create", "etc_destroy", "etc_last_error", "etc_bind_layer_weight
            "etc_moe_layer_create", "etc_moe_layer_bind_tokens", "etc_moe_layer_plan_build",
            "etc_get_step_info", "etc_graph_create", "etc_graph_add_event", "etc_graph_add_call",
            "etc_graph_bind_buffer", "etc_graph_bind_shape", "etc_graph_launch", "etc_plan_build", "etc_plan_free",
-           "etc_rowsum_launch_noalloc", "etc_graph_user_fn_count"]
+           "etc_rowsum_launch_noalloc", "etc_graph_user_fn_count", "etc_serving_create", "etc_serving_destroy",
+           "etc_serving_last_error", "etc_serving_read_error", "etc_serving_tables", "etc_serving_append",
+           "etc_serving_attention", "etc_serving_sample"]
 ROWSUM_NOALLOC_MAX_N = 2048
 
 
@@ -85,6 +87,37 @@ class PlanView(C.Structure):
                 ("seed_tasks", C.POINTER(C.c_int32)), ("opaque", C.c_void_p)]
 
 
+class ServingLimits(C.Structure):
+    _fields_ = [("max_seqs", C.c_int32), ("max_tokens", C.c_int32), ("max_kv_len", C.c_int32)]
+
+
+class ServingTablesIo(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("n_tokens", C.c_int32), ("kv_len", C.c_void_p), ("new_len", C.c_void_p),
+                ("block_table", C.c_void_p), ("table_stride", C.c_int64), ("table_cols", C.c_int32), ("free_pages", C.c_void_p),
+                ("free_cap", C.c_int32), ("free_count", C.c_void_p), ("free_count_out", C.c_void_p), ("q_indptr", C.c_void_p),
+                ("slots", C.c_void_p), ("positions", C.c_void_p), ("total_len", C.c_void_p), ("page_indptr", C.c_void_p),
+                ("page_ids", C.c_void_p), ("page_ids_cap", C.c_int32), ("status", C.c_void_p)]
+
+
+class ServingAppendIo(C.Structure):
+    _fields_ = [("n_tokens", C.c_int32), ("dtype", C.c_int32), ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64), ("positions", C.c_void_p),
+                ("slots", C.c_void_p), ("gq", C.c_void_p), ("gk", C.c_void_p), ("q_out", C.c_void_p), ("k_pages", C.c_void_p),
+                ("v_pages", C.c_void_p), ("n_pages", C.c_int64)]
+
+
+class ServingAttentionIo(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("n_tokens", C.c_int32), ("q", C.c_void_p), ("out", C.c_void_p), ("q_indptr", C.c_void_p),
+                ("kv_len", C.c_void_p), ("block_table", C.c_void_p), ("table_stride", C.c_int64), ("table_cols", C.c_int32),
+                ("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("n_pages", C.c_int64)]
+
+
+class ServingSampleIo(C.Structure):
+    _fields_ = [("n_rows", C.c_int32), ("dtype", C.c_int32), ("logits", C.c_void_p), ("row_stride", C.c_int64), ("u", C.c_void_p),
+                ("temperature", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p),
+                ("token_out", C.c_void_p), ("logprob_out", C.c_void_p), ("kept_out", C.c_void_p)]
+
+
 TASK_DTYPE = np.dtype([("fn", "u1"), ("layer", "u1"), ("flags", "<u2"), ("c0", "<i4"), ("c1", "<i4"), ("c2", "<i4"),
                        ("wait0", "<i4"), ("wait1", "<i4"), ("notify0", "<i4"), ("id", "<i4")])
 
@@ -112,8 +145,12 @@ def load_library(path: str):
     L.etc_destroy.restype = None
     L.etc_destroy.argtypes = [C.c_void_p]
     L.etc_plan_free.restype = None
+    L.etc_serving_last_error.restype = C.c_char_p
+    L.etc_serving_last_error.argtypes = [C.c_void_p]
+    L.etc_serving_destroy.restype = None
+    L.etc_serving_destroy.argtypes = [C.c_void_p]
     for name in EXPORTS:
-        if name not in ("etc_last_error", "etc_destroy", "etc_plan_free"):
+        if name not in ("etc_last_error", "etc_destroy", "etc_plan_free", "etc_serving_last_error", "etc_serving_destroy"):
             getattr(L, name).restype = C.c_int
     L.etc_create.argtypes = [C.POINTER(ModelDesc), C.POINTER(TileDesc), C.POINTER(SchedDesc), C.POINTER(C.c_void_p)]
     L.etc_bind_layer_weights.argtypes = [C.c_void_p, C.c_int32, C.POINTER(LayerWeights)]
@@ -143,6 +180,12 @@ def load_library(path: str):
     L.etc_plan_free.argtypes = [C.POINTER(PlanView)]
     L.etc_rowsum_launch_noalloc.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]
     L.etc_graph_user_fn_count.argtypes = [C.POINTER(C.c_int32)]
+    L.etc_serving_create.argtypes = [C.POINTER(ModelDesc), C.POINTER(ServingLimits), C.POINTER(C.c_void_p)]
+    L.etc_serving_read_error.argtypes = [C.c_void_p, C.POINTER(C.c_int32)]
+    L.etc_serving_tables.argtypes = [C.c_void_p, C.POINTER(ServingTablesIo), C.c_void_p]
+    L.etc_serving_append.argtypes = [C.c_void_p, C.POINTER(ServingAppendIo), C.c_void_p]
+    L.etc_serving_attention.argtypes = [C.c_void_p, C.POINTER(ServingAttentionIo), C.c_void_p]
+    L.etc_serving_sample.argtypes = [C.c_void_p, C.POINTER(ServingSampleIo), C.c_void_p]
     return L
 
 
@@ -429,3 +472,134 @@ class EventGraph(_Ctx):
 
     def exec_counts(self):
         return self.read_debug(DBG_TASK_EXEC_COUNT, 0, np.zeros(self.step_info().n_tasks, np.int32))
+
+
+def _tensor(t, name, dtypes, shape, strided=False):
+    """Checks one tensor argument (None in `shape`: any size) and returns its device pointer.  A row of a strided tensor has no gaps."""
+    import torch
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} must be a tensor of the current GPU")
+    if str(t.dtype).replace("torch.", "") not in dtypes:
+        raise ValueError(f"{name} must be one of {dtypes}, not {t.dtype}")
+    if t.dim() != len(shape) or any(n is not None and t.shape[i] != n for i, n in enumerate(shape)):
+        raise ValueError(f"{name} must have the shape {tuple('any' if n is None else n for n in shape)}, not {tuple(t.shape)}")
+    if strided:
+        if t.shape[-1] > 1 and t.stride(-1) != 1:
+            raise ValueError(f"{name}: the elements of a row must be neighbours")
+    elif not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _row_stride(t):
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[-1])
+
+
+class Serving:
+    """The operators around the decode step (include/etc.h, etc_serving_*): page tables and slot maps made on the GPU, norms +
+    RoPE + KV append of a chunk of new tokens, attention of the chunk over the paged cache, sampling.  All arguments are GPU
+    tensors on the handle's device; nothing synchronises, and every call can be captured into a graph.  The handle is for one
+    stream at a time."""
+
+    def __init__(self, shape, max_seqs: int, max_tokens: int, max_kv_len: int):
+        self._L = lib()
+        self._h = C.c_void_p()
+        self.shape = shape
+        md, limits = _model_desc(shape), ServingLimits(max_seqs, max_tokens, max_kv_len)
+        st = self._L.etc_serving_create(C.byref(md), C.byref(limits), C.byref(self._h))
+        if st != 0:
+            raise EtcError(st, self._L.etc_serving_last_error(None).decode())
+
+    def _call(self, fn, io, stream):
+        st = fn(self._h, C.byref(io), _stream_ptr(stream))
+        if st != 0:
+            raise EtcError(st, self._L.etc_serving_last_error(self._h).decode())
+
+    def close(self):
+        if self._h:
+            self._L.etc_serving_destroy(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def read_error(self):
+        """(code, operator, index, value) of what a kernel refused since the last report, or zeros.  Synchronises."""
+        word = (C.c_int32 * 4)()
+        st = self._L.etc_serving_read_error(self._h, word)
+        if st not in (0, -5):
+            raise EtcError(st, self._L.etc_serving_last_error(self._h).decode())
+        return tuple(word)
+
+    def tables(self, kv_len, new_len, block_table, free_pages, free_count, *, q_indptr, slots, positions, status,
+               free_count_out=None, total_len=None, page_indptr=None, page_ids=None, stream=None):
+        """Grows block_table [seqs, pages] (in place) for new_len tokens per sequence and maps every new token to its slot and
+        position; int32 tensors.  free_count_out: free_count unless given."""
+        i32, n = ("int32",), kv_len.shape[0]
+        opt = lambda t, name, shape: None if t is None else _tensor(t, name, i32, shape)      # noqa: E731
+        io = ServingTablesIo(
+            n_seqs=n, n_tokens=slots.shape[0], kv_len=_tensor(kv_len, "kv_len", i32, (n,)), new_len=_tensor(new_len, "new_len", i32, (n,)),
+            block_table=_tensor(block_table, "block_table", i32, (n, None), strided=True), table_stride=_row_stride(block_table),
+            table_cols=block_table.shape[1], free_pages=_tensor(free_pages, "free_pages", i32, (None,)), free_cap=free_pages.shape[0],
+            free_count=_tensor(free_count, "free_count", i32, (1,)),
+            free_count_out=_tensor(free_count if free_count_out is None else free_count_out, "free_count_out", i32, (1,)),
+            q_indptr=_tensor(q_indptr, "q_indptr", i32, (n + 1,)), slots=_tensor(slots, "slots", i32, (None,)),
+            positions=_tensor(positions, "positions", i32, (slots.shape[0],)), total_len=opt(total_len, "total_len", (n,)),
+            page_indptr=opt(page_indptr, "page_indptr", (n + 1,)), page_ids=opt(page_ids, "page_ids", (None,)),
+            page_ids_cap=0 if page_ids is None else page_ids.shape[0], status=_tensor(status, "status", i32, (1,)))
+        self._call(self._L.etc_serving_tables, io, stream)
+
+    def _pool(self, k_pages, v_pages):
+        s = self.shape
+        shape = (None, s.page, s.nkv, s.d)
+        k, v = _tensor(k_pages, "k_pages", ("bfloat16",), shape), _tensor(v_pages, "v_pages", ("bfloat16",), shape)
+        if k_pages.shape != v_pages.shape:
+            raise ValueError("k_pages and v_pages must have the same shape")
+        return k, v, k_pages.shape[0]
+
+    def append(self, q, k, v, positions, slots, q_out, k_pages, v_pages, gq=None, gk=None, stream=None):
+        """Per-head norms (qk_norm models), RoPE and KV append of the rows of a QKV projection: q [tokens, nq * d], k and v
+        [tokens, nkv * d], bf16 or fp32, rows may be parts of wider ones; q_out bf16 [tokens, nq, d]; pools of one layer."""
+        s, n = self.shape, q.shape[0]
+        kinds = ("bfloat16", "float32")
+        if k.dtype != q.dtype or v.dtype != q.dtype:
+            raise ValueError("q, k and v must have the same type")
+        kp, vp, pages = self._pool(k_pages, v_pages)
+        gain = lambda g, name: None if g is None else _tensor(g, name, ("bfloat16",), (s.d,))      # noqa: E731
+        io = ServingAppendIo(
+            n_tokens=n, dtype=1 if q.element_size() == 4 else 0, q=_tensor(q, "q", kinds, (n, s.nq * s.d), strided=True),
+            k=_tensor(k, "k", kinds, (n, s.nkv * s.d), strided=True), v=_tensor(v, "v", kinds, (n, s.nkv * s.d), strided=True),
+            q_stride=_row_stride(q), k_stride=_row_stride(k), v_stride=_row_stride(v),
+            positions=_tensor(positions, "positions", ("int32",), (n,)), slots=_tensor(slots, "slots", ("int32",), (n,)),
+            gq=gain(gq, "gq"), gk=gain(gk, "gk"), q_out=_tensor(q_out, "q_out", ("bfloat16",), (n, s.nq, s.d)),
+            k_pages=kp, v_pages=vp, n_pages=pages)
+        self._call(self._L.etc_serving_append, io, stream)
+
+    def attention(self, q, out, q_indptr, kv_len, block_table, k_pages, v_pages, stream=None):
+        """Attention of the new tokens q [tokens, nq, d] (bf16) of every sequence over its pages, the new tokens' own keys
+        among them; out like q.  q_indptr [seqs + 1], kv_len [seqs] (tokens in front of the new ones), block_table [seqs, pages]."""
+        s, n = self.shape, kv_len.shape[0]
+        kp, vp, pages = self._pool(k_pages, v_pages)
+        io = ServingAttentionIo(
+            n_seqs=n, n_tokens=q.shape[0], q=_tensor(q, "q", ("bfloat16",), (None, s.nq, s.d)),
+            out=_tensor(out, "out", ("bfloat16",), (q.shape[0], s.nq, s.d)), q_indptr=_tensor(q_indptr, "q_indptr", ("int32",), (n + 1,)),
+            kv_len=_tensor(kv_len, "kv_len", ("int32",), (n,)), block_table=_tensor(block_table, "block_table", ("int32",), (n, None), strided=True),
+            table_stride=_row_stride(block_table), table_cols=block_table.shape[1], k_pages=kp, v_pages=vp, n_pages=pages)
+        self._call(self._L.etc_serving_attention, io, stream)
+
+    def sample(self, logits, u, token_out, temperature=None, top_k=None, top_p=None, min_p=None, logprob_out=None, kept_out=None,
+               stream=None):
+        """One token per row of logits [rows, vocab] (fp32 or bf16, rows may be parts of wider ones) from the random numbers
+        u [rows] in [0, 1); settings are tensors [rows] (temperature, top_p, min_p fp32, top_k int32) or None."""
+        n = logits.shape[0]
+        opt = lambda t, name, kind: None if t is None else _tensor(t, name, (kind,), (n,))      # noqa: E731
+        io = ServingSampleIo(
+            n_rows=n, dtype=1 if logits.element_size() == 4 else 0,
+            logits=_tensor(logits, "logits", ("bfloat16", "float32"), (n, int(self.shape.vocab)), strided=True), row_stride=_row_stride(logits),
+            u=_tensor(u, "u", ("float32",), (n,)), temperature=opt(temperature, "temperature", "float32"), top_k=opt(top_k, "top_k", "int32"),
+            top_p=opt(top_p, "top_p", "float32"), min_p=opt(min_p, "min_p", "float32"), token_out=_tensor(token_out, "token_out", ("int32",), (n,)),
+            logprob_out=opt(logprob_out, "logprob_out", "float32"), kept_out=opt(kept_out, "kept_out", "int32"))
+        self._call(self._L.etc_serving_sample, io, stream)

@@ -1,0 +1,35 @@
+// What the serving operators (include/etc.h, etc_serving_*) pass from the host checks to the kernels.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/etc.h"
+
+namespace etc {
+
+constexpr int kServingMaxSeqs = 1024;
+constexpr int kServingMaxTokens = 1 << 20;
+constexpr int kServingMaxKv = 1 << 30;
+constexpr int kServingMaxVocab = 1 << 20;
+
+// Operators in the error word, and what they refuse.
+enum ServingOp { SRV_TABLES = 1, SRV_APPEND = 2, SRV_ATTENTION = 3, SRV_SAMPLE = 4 };
+enum ServingError { SRV_BAD_SLOT = 1, SRV_BAD_LENGTH = 2, SRV_BAD_PAGE = 3 };
+
+// A handle's part in every launch.
+struct ServingDev {
+    int nq, nkv, d, page_shift, qk_norm, vocab;
+    float eps;
+    int max_kv_len;
+    int n_cus;
+    const double *inv_freq;      // [d / 2] theta^(-2i/d)
+    int32_t *error;              // pinned host memory, 4 words
+    int32_t *arrive;             // [2] zero between launches: workgroups of a launch that have read their inputs
+};
+
+hipError_t launch_serving_tables(const ServingDev &S, const etc_serving_tables_io &io, hipStream_t s);
+hipError_t launch_serving_append(const ServingDev &S, const etc_serving_append_io &io, hipStream_t s);
+hipError_t launch_serving_attention(const ServingDev &S, const etc_serving_attention_io &io, hipStream_t s);
+hipError_t launch_serving_sample(const ServingDev &S, const etc_serving_sample_io &io, hipStream_t s);
+
+}  // namespace etc

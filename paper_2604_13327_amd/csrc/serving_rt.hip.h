@@ -1,0 +1,39 @@
+// Device-side helpers of the serving operators.
+#pragma once
+#include "device_rt.hip.h"
+#include "serving.h"
+
+namespace etc {
+
+// Reports something a kernel found in device memory and did not use (pinned host memory; the last report stays, code last).
+__device__ __forceinline__ void refuse(int32_t *error, int code, int op, int index, int value)
+{
+    __hip_atomic_store(as_global(error + 1), op, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+    __hip_atomic_store(as_global(error + 2), index, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+    __hip_atomic_store(as_global(error + 3), value, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+    __hip_atomic_store(as_global(error), code, __ATOMIC_RELEASE, __HIP_MEMORY_SCOPE_SYSTEM);
+}
+
+typedef __attribute__((ext_vector_type(2))) float f32x2_t;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+// Two values to bf16, round to nearest even (NaN stays NaN).
+__device__ __forceinline__ uint32_t to_bf16x2(float a, float b)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), bf16x2_t));
+}
+__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+// Inclusive sum over the lanes of a wavefront.
+__device__ __forceinline__ int wave_scan_i(int v)
+{
+    const int lane = lane_id();
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int t = __shfl_up(v, o, 64);
+        if (lane >= o) v += t;
+    }
+    return v;
+}
+
+}  // namespace etc
