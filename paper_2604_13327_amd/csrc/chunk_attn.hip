@@ -7,12 +7,15 @@
 // right operand of the second product: its 16 keys are merely taken in the order the first product left them, by reading V's
 // rows in that order.
 #ifndef ETC_GENERIC_ONLY
+#include <type_traits>
+
 #include "serving_rt.hip.h"
 
 namespace etc {
 
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((ext_vector_type(2))) short s16x2;
 
 constexpr int kCaWaves = 8, kCaThreads = kCaWaves * 64;
 constexpr int kCaRows = 32 * kCaWaves;      // rows of a block
@@ -28,6 +31,12 @@ __device__ __forceinline__ float partner_sum(float x)
 {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// A bf16 that is no number, as a count (bf16): +inf 1, -inf 2^8, NaN 2^16; 0 for a number.
+__device__ __forceinline__ uint32_t odd_kind(uint32_t e)
+{
+    return (e & 0x7FFFu) > 0x7F80u ? 0x4780u : e == 0x7F80u ? 0x3F80u : e == 0xFF80u ? 0x4380u : 0u;
 }
 
 // Which sequence and block of rows a workgroup has.
@@ -76,6 +85,7 @@ __global__ __launch_bounds__(kCaThreads) void chunk_attention_kernel(ServingDev 
     constexpr int RPT = kCaKeys * CH / kCaThreads;       // pieces of K (and of V) a thread stages
     constexpr int RSTEP = kCaThreads / CH;               // rows between them
     __shared__ __attribute__((aligned(16))) uint16_t s_k[2][kCaKeys * D], s_v[2][kCaKeys * D];
+    __shared__ int s_odd[2];
     const int tid = (int)threadIdx.x, wave = wave_id(), lane = lane_id(), half = lane >> 5, col = lane & 31;
     const Item it = find_item(S, io, (int)blockIdx.x, nullptr);
     if (it.n_new == 0) return;
@@ -90,8 +100,8 @@ __global__ __launch_bounds__(kCaThreads) void chunk_attention_kernel(ServingDev 
     for (int ks = 0; ks < KS; ++ks) qf[ks] = __builtin_bit_cast(bf16x8, gld_16B(qp + ks * 16));
     const int limit = it.kv + t;                         // last key this row sees
     const int t_last = min(r0 + kCaRows - 1, rows - 1) / grp, n_keys = it.kv + t_last + 1;      // keys of the block
-    const int t_first = (r0 + wave * 32) / grp;          // of this wavefront: all its rows see the keys up to kv + t_first
-    const int wave_full = it.kv + min(t_first, it.n_new - 1), wave_last = it.kv + min((r0 + wave * 32 + 31) / grp, it.n_new - 1);
+    const int first_masked = (it.kv + r0 / grp + 1) / kCaKeys;      // tiles in front of it are seen whole by all rows of the block
+    const int wave_last = it.kv + min((r0 + wave * 32 + 31) / grp, it.n_new - 1);
     const bool wave_live = r0 + wave * 32 < rows;
     const int n_tiles = (n_keys + kCaKeys - 1) / kCaKeys;
 
@@ -121,145 +131,174 @@ __global__ __launch_bounds__(kCaThreads) void chunk_attention_kernel(ServingDev 
     // LDS rows: the 16-byte pieces of a row change places with the row (exclusive or), so that lanes reading one piece of
     // neighbouring rows meet different banks: K by the row's low 3 bits (8 lanes an access), V by pairs of pieces (4 rows an access).
     auto store_rows = [&](int tile, int buf) {
+        bool odd = false;
 #pragma unroll
         for (int u = 0; u < RPT; ++u) {
             const int key = key0 + RSTEP * u;
-            const bool in = tile * kCaKeys + key < n_keys;      // rows behind the last key count nothing: zero, whatever the pool holds
-            *reinterpret_cast<u32x4 *>(&s_k[buf][key * D + ((c ^ (key & 7)) * 8)]) = in ? kr[u] : u32x4{0, 0, 0, 0};
-            *reinterpret_cast<u32x4 *>(&s_v[buf][key * D + ((c ^ ((key & 3) * 2)) * 8)]) = in ? vr[u] : u32x4{0, 0, 0, 0};
+            if ((tile + 1) * kCaKeys > n_keys && tile * kCaKeys + key >= n_keys)      // behind the last key: zero, whatever the pool holds
+                kr[u] = vr[u] = u32x4{0, 0, 0, 0};
+            *reinterpret_cast<u32x4 *>(&s_k[buf][key * D + ((c ^ (key & 7)) * 8)]) = kr[u];
+            *reinterpret_cast<u32x4 *>(&s_v[buf][key * D + ((c ^ ((key & 3) * 2)) * 8)]) = vr[u];
+            if (tile >= first_masked) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) odd |= (vr[u][i] & 0x7F80u) == 0x7F80u || (vr[u][i] & 0x7F800000u) == 0x7F800000u;
+            }
         }
+        if (odd) s_odd[buf] = 1;                         // stays: the tiles behind it are masked too
     };
 
     f32x16 o[DT];
 #pragma unroll
     for (int i = 0; i < DT; ++i) o[i] = f32x16{};
-    float m = -INFINITY, l = 0.f;                        // reference of the row's exponentials; sum over this lane's keys
-    const float scale = 1.44269504088896f / sqrtf((float)D);
+    float m = -3e38f, l = 0.f;                           // reference of the row's exponentials; sum over this lane's keys
+    const float scale = 1.44269504088896f / sqrtf((float)D);      // scores and reference count in powers of two
 
+    // Fragments in LDS.  The exchange of pieces touches the low 3 bits of a piece's number, so that every fragment lies at a constant
+    // distance from one of a few addresses: K of step ks at k_at[ks % 4] (and 8 pieces behind for ks >= 4), V of tile dt at v_at[dt % 2].
+    constexpr int ROW = D * 2, BUF = kCaKeys * ROW;      // bytes
+    uint32_t k_at[4], v_at[2];
+    {
+        const uint32_t kb = (uint32_t)(uintptr_t)as_lds(&s_k[0][0]), vb = (uint32_t)(uintptr_t)as_lds(&s_v[0][0]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) k_at[i] = kb + col * ROW + (((i * 2 + half) ^ (col & 7)) * 16);
+        const int vrow = 4 * half + ((lane & 15) >> 2), piece = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) v_at[i] = vb + vrow * ROW + (((i * 4 + piece) ^ ((vrow & 3) * 2)) * 16) + (lane & 1) * 8;
+    }
+    auto k_frag = [&](int buf, int ks, int kt) {
+        return *reinterpret_cast<ETC_AS_LDS const bf16x8 *>(k_at[ks & 3] + buf * BUF + kt * 32 * ROW + (ks >> 2) * 128);
+    };
+    // V^T fragment of 32 elements (tile dt) x 16 keys (step ks), the keys in the order the scores have them: rows 4 half + 0 .. 3
+    // and 8 + 4 half + 0 .. 3 of the step.
+    auto v_frag = [&](int buf, int ks, int dt) {
+        const uint32_t at = v_at[dt & 1] + buf * BUF + ks * 16 * ROW + (dt >> 1) * 128;
+        const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<ETC_AS_LDS s16x4 *>(at)));
+        const u32x2 b = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<ETC_AS_LDS s16x4 *>(at + 8 * ROW)));
+        return u32x4{a.x, a.y, b.x, b.y};
+    };
+    // One tile.  MASKED: some row of the block does not see all of it.
+    auto step = [&](auto masked_c, int tile) {
+        constexpr bool MASKED = decltype(masked_c)::value;
+        const int buf = tile & 1, k0 = tile * kCaKeys;
+        // ---- scores: S^T[key][row], key = 32 kt + 8 (i / 4) + 4 half + i % 4 of register i
+        f32x16 s[2] = {f32x16{}, f32x16{}};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(buf, ks, kt), qf[ks], s[kt], 0, 0, 0);
+        if constexpr (MASKED) {
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (k0 + kt * 32 + 8 * (i >> 2) + 4 * half + (i & 3) > limit) s[kt][i] = -INFINITY;
+        }
+        float mt = s[0][0];
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) mt = fmaxf(mt, s[kt][i]);
+        mt = partner_max(mt) * scale;
+        // The reference follows the maximum only when that has grown by 2^8 (rows of a wavefront together): until then
+        // probabilities up to 2^8 lose nothing, and the running output need not be multiplied.
+        if (__builtin_amdgcn_ballot_w64(mt > m + 8.f) != 0) {
+            const float nm = fmaxf(m, mt), sc = exp2_fast(m - nm);
+            m = nm;
+            l *= sc;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) o[dt] *= sc;
+        }
+        bool odd = false;
+        if constexpr (MASKED) {
+            // Keys some rows do not see: their probability 0 would make a NaN of an infinite or NaN value.  A tile that holds
+            // such values (exponent all ones) has them taken out of the product, and counted by kind in a second one over the
+            // keys each row sees: +inf as 1, -inf as 2^8, NaN as 2^16 (at most 64 of each: exact).
+            odd = s_odd[buf] != 0;
+            if (odd) {
+                auto count = [&](int dt) {
+                    f32x16 n{};
+#pragma unroll 1
+                    for (int ks = 0; ks < 4; ++ks) {
+                        const u32x4 w = v_frag(buf, ks, dt);
+                        u32x4 kind, seen;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int key = k0 + ks * 16 + 4 * half + (i >> 1) * 8 + (i & 1) * 2;
+                            seen[i] = (key <= limit ? 0x3F80u : 0u) | (key + 1 <= limit ? 0x3F800000u : 0u);
+                            kind[i] = odd_kind(w[i] & 0xFFFFu) | odd_kind(w[i] >> 16) << 16;
+                        }
+                        n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kind), __builtin_bit_cast(bf16x8, seen), n, 0, 0, 0);
+                    }
+                    return n;
+                };
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) {
+                    const f32x16 n = count(dt);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const uint32_t c = (uint32_t)n[i];
+                        if (c & 0xFFu) o[dt][i] += INFINITY;
+                        if (c & 0xFF00u) o[dt][i] -= INFINITY;
+                        if (c >> 16) o[dt][i] = __uint_as_float(0x7FC00000u);
+                    }
+                }
+            }
+        }
+        // ---- probabilities of 32 keys, then O^T += V^T . P^T over them
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+            uint32_t p[8];
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                const float a = exp2_fast(__builtin_fmaf(s[kt][i], scale, -m)), b = exp2_fast(__builtin_fmaf(s[kt][i + 1], scale, -m));
+                p[i >> 1] = to_bf16x2(a, b);             // half a unit of bf16 of a probability: below the rounding of the output
+                l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(s16x2, p[i >> 1]), __builtin_bit_cast(s16x2, 0x3F803F80u), l, false);
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const bf16x8 pb = __builtin_bit_cast(bf16x8, u32x4{p[4 * h], p[4 * h + 1], p[4 * h + 2], p[4 * h + 3]});
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) {
+                    u32x4 w = v_frag(buf, kt * 2 + h, dt);
+                    if constexpr (MASKED) {
+                        if (odd) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                w[i] &= ((w[i] & 0x7F80u) == 0x7F80u ? 0u : 0xFFFFu) | ((w[i] & 0x7F800000u) == 0x7F800000u ? 0u : 0xFFFF0000u);
+                        }
+                    }
+                    o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), pb, o[dt], 0, 0, 0);
+                }
+            }
+        }
+    };
+
+    if (tid < 2) s_odd[tid] = 0;
     load_ids(0);
     load_rows(0);
     load_ids(1 < n_tiles ? 1 : 0);
+    __syncthreads();
     store_rows(0, 0);
     if (n_tiles > 1) { load_rows(1); load_ids(2 < n_tiles ? 2 : 0); }
     __syncthreads();
-    for (int tile = 0; tile < n_tiles; ++tile) {
-        const int buf = tile & 1, k0 = tile * kCaKeys;
-        if (wave_live && k0 <= wave_last) {
-            // ---- scores: S^T[key][row], key = 32 kt + 8 (i / 4) + 4 half + i % 4 of register i
-            f32x16 s[2] = {f32x16{}, f32x16{}};
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-                for (int kt = 0; kt < 2; ++kt) {
-                    const int key = kt * 32 + col;
-                    const bf16x8 a = *reinterpret_cast<const bf16x8 *>(&s_k[buf][key * D + (((ks * 2 + half) ^ (key & 7)) * 8)]);
-                    s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[ks], s[kt], 0, 0, 0);
-                }
-            const bool masked = k0 + kCaKeys - 1 > wave_full;      // some row of the wavefront does not see all of the tile
-            float mt = -INFINITY;
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    float x = s[kt][i] * scale;
-                    if (masked) x = k0 + kt * 32 + 8 * (i >> 2) + 4 * half + (i & 3) <= limit ? x : -INFINITY;
-                    s[kt][i] = x;
-                    mt = fmaxf(mt, x);
-                }
-            mt = partner_max(mt);
-            const float nm = fmaxf(m, mt), ref = fmaxf(nm, -1e30f);      // all scores -inf so far: exp2(-inf - ref) = 0, no NaN
-            const float sc = exp2_fast(m - ref);
-            m = nm;
-            float sum = 0.f;
-            uint32_t p[2][8];
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int i = 0; i < 16; i += 2) {
-                    const float a = exp2_fast(s[kt][i] - ref), b = exp2_fast(s[kt][i + 1] - ref);
-                    sum += a + b;
-                    p[kt][i >> 1] = to_bf16x2(a, b);     // half a unit of bf16 of a probability: below the rounding of the output
-                }
-            l = l * sc + sum;
-            if (__builtin_amdgcn_ballot_w64(sc != 1.0f) != 0) {
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt) o[dt] *= sc;
-            }
-            // ---- O^T += V^T . P^T: 16 keys a step, in the order the scores have them: rows 4 half + 0 .. 3 and 8 + 4 half + 0 .. 3
-#pragma unroll
-            for (int ks = 0; ks < 4; ++ks) {
-                const uint32_t *pp = &p[ks >> 1][(ks & 1) * 4];
-                const bf16x8 pb = __builtin_bit_cast(bf16x8, u32x4{pp[0], pp[1], pp[2], pp[3]});
-                const int vrow = ks * 16 + 4 * half + ((lane & 15) >> 2), sw = (vrow & 3) * 2;      // also of row + 8
-                bf16x8 vf[DT];
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt) {
-                    const int piece = dt * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
-                    ETC_AS_LDS uint16_t *at = as_lds(&s_v[buf][vrow * D + ((piece ^ sw) * 8) + (lane & 1) * 4]);
-                    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<ETC_AS_LDS s16x4 *>(at));
-                    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<ETC_AS_LDS s16x4 *>(at + 8 * D));
-                    const u32x2 a = __builtin_bit_cast(u32x2, lo), b = __builtin_bit_cast(u32x2, hi);
-                    vf[dt] = __builtin_bit_cast(bf16x8, u32x4{a.x, a.y, b.x, b.y});
-                }
-                if (masked) {
-                    // Keys some rows of the wavefront do not see: their probability 0 would make a NaN of an infinite or NaN
-                    // value.  Such values (exponent all ones) are taken out of the product and counted by kind in a second
-                    // one over the keys each row sees: +inf as 1, -inf as 2^8, NaN as 2^16 (at most 64 of each: exact).
-                    uint32_t odd = 0;
-#pragma unroll
-                    for (int dt = 0; dt < DT; ++dt) {
-                        const u32x4 w = __builtin_bit_cast(u32x4, vf[dt]);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) odd |= ((w[i] & 0x7F80u) == 0x7F80u) | ((w[i] & 0x7F800000u) == 0x7F800000u);
-                    }
-                    if (__builtin_amdgcn_ballot_w64(odd != 0) != 0) {
-                        uint32_t seen[4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int kk = k0 + ks * 16 + 4 * half + (i >> 1) * 8 + (i & 1) * 2;
-                            seen[i] = (kk <= limit ? 0x3F80u : 0u) | (kk + 1 <= limit ? 0x3F800000u : 0u);
-                        }
-#pragma unroll
-                        for (int dt = 0; dt < DT; ++dt) {
-                            u32x4 w = __builtin_bit_cast(u32x4, vf[dt]), kind;
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                uint32_t out = 0, keep = 0;
-#pragma unroll
-                                for (int h = 0; h < 2; ++h) {
-                                    const uint32_t e = (w[i] >> (16 * h)) & 0xFFFFu;
-                                    const uint32_t code = (e & 0x7FFFu) > 0x7F80u ? 0x4780u : e == 0x7F80u ? 0x3F80u : e == 0xFF80u ? 0x4380u : 0u;
-                                    out |= code << (16 * h);
-                                    keep |= (code ? 0u : e) << (16 * h);
-                                }
-                                kind[i] = out;
-                                w[i] = keep;
-                            }
-                            vf[dt] = __builtin_bit_cast(bf16x8, w);
-                            const f32x16 n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kind),
-                                __builtin_bit_cast(bf16x8, u32x4{seen[0], seen[1], seen[2], seen[3]}), f32x16{}, 0, 0, 0);
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                const uint32_t cnt = (uint32_t)n[i];
-                                if (cnt & 0xFFu) o[dt][i] += INFINITY;
-                                if (cnt & 0xFF00u) o[dt][i] -= INFINITY;
-                                if (cnt >> 16) o[dt][i] = __uint_as_float(0x7FC00000u);
-                            }
-                        }
-                    }
-                }
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[dt], pb, o[dt], 0, 0, 0);
-            }
-        }
+    auto next = [&](int tile) {                          // the tile behind `tile` into the other buffer, the one behind that on its way
         if (tile + 1 < n_tiles) {
-            store_rows(tile + 1, buf ^ 1);
+            store_rows(tile + 1, (tile & 1) ^ 1);
             if (tile + 2 < n_tiles) {
                 load_rows(tile + 2);
                 load_ids(tile + 3 < n_tiles ? tile + 3 : 0);
             }
         }
         __syncthreads();
+    };
+    int tile = 0;
+    for (; tile < min(first_masked, n_tiles); ++tile) {
+        if (wave_live) step(std::false_type(), tile);
+        next(tile);
+    }
+    for (; tile < n_tiles; ++tile) {
+        if (wave_live && tile * kCaKeys <= wave_last) step(std::true_type(), tile);
+        next(tile);
     }
     if (row >= rows) return;
     const float inv = 1.0f / partner_sum(l);
