@@ -20,6 +20,7 @@ typedef __attribute__((ext_vector_type(2))) short s16x2;
 constexpr int kCaWaves = 8, kCaThreads = kCaWaves * 64;
 constexpr int kCaRows = 32 * kCaWaves;      // rows of a block
 constexpr int kCaKeys = 64;                 // keys of a tile
+constexpr int kCaMinTiles = 2;              // of a piece, where keys are cut
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float partner_max(float x)      // with lane + 32
@@ -39,75 +40,182 @@ __device__ __forceinline__ uint32_t odd_kind(uint32_t e)
     return (e & 0x7FFFu) > 0x7F80u ? 0x4780u : e == 0x7F80u ? 0x3F80u : e == 0xFF80u ? 0x4380u : 0u;
 }
 
-// Which sequence and block of rows a workgroup has.
-struct Item { int b, block, row0, n_new, kv; };      // row0: first row of q; n_new == 0: nothing
-
-// Blocks of all sequences back to back; lengths out of range leave their sequence out.
-__device__ Item find_item(const ServingDev &S, const etc_serving_attention_io &io, int want, int *s_sum)
+__device__ __forceinline__ int last_not_above(const int *indptr, int n, int x)      // the last b with indptr[b] <= x
 {
-    __shared__ Item s_item;
-    __shared__ int s_wave[kCaWaves];
-    const int tid = (int)threadIdx.x, grp = S.nq / S.nkv;
-    if (tid == 0) s_item = Item{0, 0, 0, 0, 0};
-    int done = 0;
-    for (int b0 = 0; b0 < io.n_seqs; b0 += kCaThreads) {
-        const int b = b0 + tid;
-        int q0 = 0, n = 0, kv = 0, blocks = 0;
-        if (b < io.n_seqs) {
-            q0 = gld_i32(io.q_indptr + b);
-            const int q1 = gld_i32(io.q_indptr + b + 1);
-            kv = gld_i32(io.kv_len + b);
-            n = q1 - q0;
-            const bool ok = q0 >= 0 && q1 >= q0 && q1 <= io.n_tokens && kv >= 0 && kv <= S.max_kv_len && n <= S.max_kv_len - kv &&
-                            (int)(((unsigned)(kv + n) + (1u << S.page_shift) - 1) >> S.page_shift) <= io.table_cols;
-            if (!ok) {
-                if (blockIdx.x == 0 && blockIdx.y == 0) refuse(S.error, SRV_BAD_LENGTH, SRV_ATTENTION, b, kv);
-                n = 0;
-            }
-            blocks = (n * grp + kCaRows - 1) / kCaRows;      // n * grp <= 2^26
-        }
-        int sum = wave_scan_i(blocks);
-        if (lane_id() == 63) s_wave[wave_id()] = sum;
-        __syncthreads();
-        for (int w = 0; w < wave_id(); ++w) sum += s_wave[w];
-        if (want >= done + sum - blocks && want < done + sum) s_item = Item{b, want - (done + sum - blocks), q0, n, kv};
-        for (int w = 0; w < kCaWaves; ++w) done += s_wave[w];
-        __syncthreads();
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (indptr[mid] <= x) lo = mid; else hi = mid;
     }
-    return lds_get_uniform(&s_item);
+    return lo;
 }
 
+// ---- how a call is cut into pieces ---------------------------------------------------------------------------------------
+// An item is (sequence, block of rows, KV head).  The keys of every item of a sequence are cut into the same number of pieces,
+// whole tiles each; workgroup w of the launch takes the pieces w, w + grid, ...  Every workgroup computes the cut by itself
+// from the lengths, one sequence to a thread: pieces of at most L tiles, with the L out of kCaTries that is estimated to end
+// first.  KV heads are the fastest index of a piece: neighbouring workgroups, on different dies, take different heads, and a
+// die's L2 sees the keys of one or two.
+constexpr int kCaTries = kCaWaves;          // a wavefront estimates one
+
+struct CaLds {
+    int first[kServingMaxSeqs + 1];         // prefix sum: pieces of the sequences
+    int slot[kServingMaxSeqs + 1];          // prefix sum: those that leave a partial result
+    int tiles[kServingMaxSeqs];             // of the last block; 0: nothing to do
+    int blocks[kServingMaxSeqs];
+    int split[kServingMaxSeqs];             // pieces of an item
+    float wave_f[kCaWaves];
+    int wave_i[2][kCaWaves];
+    int odd[2], last;
+};
+
+struct Seq { int q0, n, kv; };
+__device__ __forceinline__ Seq sequence(const ServingDev &S, const etc_serving_attention_io &io, int b, bool *ok)
+{
+    const int q0 = gld_i32(io.q_indptr + b), q1 = gld_i32(io.q_indptr + b + 1), kv = gld_i32(io.kv_len + b), n = q1 - q0;
+    *ok = q0 >= 0 && q1 >= q0 && q1 <= io.n_tokens && kv >= 0 && kv <= S.max_kv_len && n <= S.max_kv_len - kv &&
+          (int)(((unsigned)(kv + n) + (1u << S.page_shift) - 1) >> S.page_shift) <= io.table_cols;
+    return Seq{q0, n, kv};
+}
+
+__device__ __forceinline__ int div_up(int a, int b) { return (a + b - 1) / b; }
+__device__ __forceinline__ float wave_sum_f(float v)
+{
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    return v;
+}
+__device__ __forceinline__ int wave_max_i(int v)
+{
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v = max(v, __shfl_xor(v, o, 64));
+    return v;
+}
+
+// Fills L and returns the number of pieces.
+__device__ int cut(const ServingDev &S, const etc_serving_attention_io &io, CaLds &L)
+{
+    const int tid = (int)threadIdx.x, wave = wave_id(), lane = lane_id(), grp = S.nq / S.nkv, grid = (int)gridDim.x;
+    float work = 0.f;                                    // tiles, all items
+    int tokens = 0;                                      // at most 2^30
+    for (int b = tid; b < io.n_seqs; b += kCaThreads) {
+        bool ok;
+        const Seq q = sequence(S, io, b, &ok);
+        if (!ok && blockIdx.x == 0) refuse(S.error, SRV_BAD_LENGTH, SRV_ATTENTION, b, q.kv);
+        const int rows = ok ? q.n * grp : 0;             // at most 2^26
+        const int blocks = div_up(rows, kCaRows), tiles = rows ? (q.kv + q.n - 1) / kCaKeys + 1 : 0;
+        L.blocks[b] = blocks;
+        L.tiles[b] = tiles;
+        if (ok) tokens += q.n;
+        if (rows) work += (float)S.nkv * blocks * 0.5f * (float)(tiles + (q.kv + min(q.n, kCaRows / grp) - 1) / kCaKeys + 1);
+    }
+    work = wave_sum_f(work);
+    tokens = wave_sum_i(tokens);
+    if (lane == 0) { L.wave_f[wave] = work; L.wave_i[0][wave] = tokens; }
+    __syncthreads();
+    work = 0.f;
+    tokens = 0;
+    for (int w = 0; w < kCaWaves; ++w) { work += L.wave_f[w]; tokens += L.wave_i[0][w]; }
+    __syncthreads();
+    if (tokens > io.n_tokens) {                          // ranges that overlap: no call's lengths
+        if (blockIdx.x == 0 && tid == 0) refuse(S.error, SRV_BAD_LENGTH, SRV_ATTENTION, io.n_seqs, tokens);
+        return 0;
+    }
+    // Candidate of wavefront w: no cut, or pieces of 1.5, 1, 2/3, 1/2, 1/3, 1/4, 1/6 of a workgroup's share, kCaMinTiles at least.  A
+    // piece costs its tiles and 2 more; a partial result is written and read again: 1 more per 64 rows of it.
+    const float share = work / (float)grid;
+    auto tiles_of = [&](int w) {
+        const float f = w == 1 ? 1.5f : w == 2 ? 1.f : w == 3 ? 0.6667f : w == 4 ? 0.5f : w == 5 ? 0.3333f : w == 6 ? 0.25f : 0.1667f;
+        return w == 0 ? 1 << 30 : max(kCaMinTiles, (int)fminf(ceilf(share * f), 1e9f));
+    };
+    float pieces = 0.f, slots = 0.f, cost = 0.f;
+    int longest = 0;
+    const int per = tiles_of(wave);
+    for (int b = lane; b < io.n_seqs; b += 64) {
+        if (L.tiles[b] == 0) continue;
+        const int s = div_up(L.tiles[b], per);
+        const float n = (float)S.nkv * L.blocks[b] * s;
+        pieces += n;
+        if (s > 1) { slots += n; cost += n * (1.f + (L.blocks[b] > 1 ? 4.f : 1.f)); }
+        longest = max(longest, div_up(L.tiles[b], s));
+    }
+    pieces = wave_sum_f(pieces);
+    slots = wave_sum_f(slots);
+    cost = work + wave_sum_f(cost) + 2.f * pieces;
+    longest = wave_max_i(longest);
+    const float rounds = ceilf(pieces / (float)grid);
+    float ends = fmaxf((float)longest + 2.f, rounds * cost / fmaxf(pieces, 1.f));
+    if (wave > 0 && slots > (float)S.attn_slots) ends = INFINITY;
+    if (lane == 0) L.wave_f[wave] = ends;
+    __syncthreads();
+    int best = 0;
+    for (int w = 1; w < kCaTries; ++w)
+        if (L.wave_f[w] < L.wave_f[best]) best = w;
+    const int limit = tiles_of(best);
+    int done = 0, done_slots = 0;
+    for (int b0 = 0; b0 < io.n_seqs; b0 += kCaThreads) {
+        const int b = b0 + tid;
+        int n = 0, sl = 0;
+        if (b < io.n_seqs && L.tiles[b] > 0) {
+            const int s = div_up(L.tiles[b], limit);
+            L.split[b] = s;
+            n = S.nkv * L.blocks[b] * s;                 // all together at most 2^20 tokens * 1024 heads / 256 rows + 2^20, and attn_slots
+            sl = s > 1 ? n : 0;
+        }
+        int sum = wave_scan_i(n), sum_sl = wave_scan_i(sl);
+        if (lane == 63) { L.wave_i[0][wave] = sum; L.wave_i[1][wave] = sum_sl; }
+        __syncthreads();
+        for (int w = 0; w < wave; ++w) { sum += L.wave_i[0][w]; sum_sl += L.wave_i[1][w]; }
+        if (b < io.n_seqs) { L.first[b + 1] = done + sum; L.slot[b + 1] = done_slots + sum_sl; }
+        for (int w = 0; w < kCaWaves; ++w) { done += L.wave_i[0][w]; done_slots += L.wave_i[1][w]; }
+        __syncthreads();
+    }
+    if (tid == 0) L.first[0] = L.slot[0] = 0;
+    __syncthreads();
+    return done;
+}
+
+// Partial results of a slot, wavefront by wavefront: [16-byte piece of a lane][lane] of the output, then m and l of 32 rows.
+template <int D> constexpr int kCaPartO = D / 32 * 4 * 64 * 4;      // floats of a wavefront
+template <int D> constexpr int kCaSlot = kCaWaves * (kCaPartO<D> + 64);
+
 template <int D>
-__global__ __launch_bounds__(kCaThreads) void chunk_attention_kernel(ServingDev S, etc_serving_attention_io io)
+__device__ __forceinline__ void chunk_attention_piece(const ServingDev &S, const etc_serving_attention_io &io, CaLds &L,
+                                                      uint16_t (&s_k)[2][kCaKeys * D], uint16_t (&s_v)[2][kCaKeys * D], int b, int local)
 {
     constexpr int CH = D / 8;                            // 16-byte pieces of a row
     constexpr int KS = D / 16, DT = D / 32;              // steps of the first product, tiles of the output
     constexpr int RPT = kCaKeys * CH / kCaThreads;       // pieces of K (and of V) a thread stages
     constexpr int RSTEP = kCaThreads / CH;               // rows between them
-    __shared__ __attribute__((aligned(16))) uint16_t s_k[2][kCaKeys * D], s_v[2][kCaKeys * D];
-    __shared__ int s_odd[2];
-    const int tid = (int)threadIdx.x, wave = wave_id(), lane = lane_id(), half = lane >> 5, col = lane & 31;
-    const Item it = find_item(S, io, (int)blockIdx.x, nullptr);
-    if (it.n_new == 0) return;
-    const int kvh = (int)blockIdx.y, grp = S.nq / S.nkv, psh = S.page_shift, pmask = (1 << psh) - 1;
-    const int rows = it.n_new * grp, r0 = it.block * kCaRows;
+    const int tid = (int)threadIdx.x, wave = __builtin_amdgcn_readfirstlane(wave_id()), lane = lane_id(), half = lane >> 5, col = lane & 31;
+    const int split = __builtin_amdgcn_readfirstlane(L.split[b]), blocks = __builtin_amdgcn_readfirstlane(L.blocks[b]);
+    const int kvh = local % S.nkv, part = local / S.nkv % split, block = blocks - 1 - local / S.nkv / split;      // long blocks first
+    bool ok;
+    Seq it = sequence(S, io, b, &ok);
+    it = wave_uniform(it);
+    const int grp = S.nq / S.nkv, psh = S.page_shift, pmask = (1 << psh) - 1;
+    const int rows = it.n * grp, r0 = block * kCaRows;
+
+    const int t_last = min(r0 + kCaRows - 1, rows - 1) / grp, n_keys = it.kv + t_last + 1;      // keys of the block
+    const int all_tiles = (n_keys - 1) / kCaKeys + 1;
+    const int tile0 = (int)((int64_t)all_tiles * part / split), n_tiles = (int)((int64_t)all_tiles * (part + 1) / split);      // this piece: [tile0, n_tiles)
+    if (tile0 == n_tiles) return;                        // a block shorter than its sequence's last one may have fewer pieces
+    const int parts = min(split, all_tiles);
 
     // this lane's row: query fragments (right operand: 8 consecutive elements of step ks at ks * 16 + half * 8)
     const int row = r0 + wave * 32 + col, rr = min(row, rows - 1), t = rr / grp, head = kvh * grp + (rr - t * grp);
-    const uint16_t *qp = (const uint16_t *)io.q + ((int64_t)(it.row0 + t) * S.nq + head) * D + half * 8;
+    const uint16_t *qp = (const uint16_t *)io.q + ((int64_t)(it.q0 + t) * S.nq + head) * D + half * 8;
     bf16x8 qf[KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qf[ks] = __builtin_bit_cast(bf16x8, gld_16B(qp + ks * 16));
     const int limit = it.kv + t;                         // last key this row sees
-    const int t_last = min(r0 + kCaRows - 1, rows - 1) / grp, n_keys = it.kv + t_last + 1;      // keys of the block
     const int first_masked = (it.kv + r0 / grp + 1) / kCaKeys;      // tiles in front of it are seen whole by all rows of the block
-    const int wave_last = it.kv + min((r0 + wave * 32 + 31) / grp, it.n_new - 1);
+    const int wave_last = it.kv + min((r0 + wave * 32 + 31) / grp, it.n - 1);
     const bool wave_live = r0 + wave * 32 < rows;
-    const int n_tiles = (n_keys + kCaKeys - 1) / kCaKeys;
 
     // staging: thread has piece c of rows key0 + RSTEP * u of a tile
     const int c = tid % CH, key0 = tid / CH;
-    const int32_t *table = io.block_table + (int64_t)it.b * io.table_stride;
+    const int32_t *table = io.block_table + (int64_t)b * io.table_stride;
     int ids[RPT];
     u32x4 kr[RPT], vr[RPT];
     auto load_ids = [&](int tile) {
@@ -120,7 +228,7 @@ __global__ __launch_bounds__(kCaThreads) void chunk_attention_kernel(ServingDev 
             const int key = min(tile * kCaKeys + key0 + RSTEP * u, n_keys - 1);
             int id = ids[u];
             if ((uint32_t)id >= (uint64_t)io.n_pages) {
-                refuse(S.error, SRV_BAD_PAGE, SRV_ATTENTION, it.b, id);
+                refuse(S.error, SRV_BAD_PAGE, SRV_ATTENTION, b, id);
                 id = 0;
             }
             const int64_t off = (((int64_t)id << psh) + (key & pmask)) * (S.nkv * D) + kvh * D + c * 8;
@@ -144,7 +252,7 @@ __global__ __launch_bounds__(kCaThreads) void chunk_attention_kernel(ServingDev 
                 for (int i = 0; i < 4; ++i) odd |= (vr[u][i] & 0x7F80u) == 0x7F80u || (vr[u][i] & 0x7F800000u) == 0x7F800000u;
             }
         }
-        if (odd) s_odd[buf] = 1;                         // stays: the tiles behind it are masked too
+        if (odd) L.odd[buf] = 1;                         // stays: the tiles behind it are masked too
     };
 
     f32x16 o[DT];
@@ -213,7 +321,7 @@ __global__ __launch_bounds__(kCaThreads) void chunk_attention_kernel(ServingDev 
             // Keys some rows do not see: their probability 0 would make a NaN of an infinite or NaN value.  A tile that holds
             // such values (exponent all ones) has them taken out of the product, and counted by kind in a second one over the
             // keys each row sees: +inf as 1, -inf as 2^8, NaN as 2^16 (at most 64 of each: exact).
-            odd = s_odd[buf] != 0;
+            odd = L.odd[buf] != 0;
             if (odd) {
                 auto count = [&](int dt) {
                     f32x16 n{};
@@ -273,25 +381,26 @@ __global__ __launch_bounds__(kCaThreads) void chunk_attention_kernel(ServingDev 
         }
     };
 
-    if (tid < 2) s_odd[tid] = 0;
-    load_ids(0);
-    load_rows(0);
-    load_ids(1 < n_tiles ? 1 : 0);
+    // Tile t of the sequence goes to buffer t % 2.
+    if (tid < 2) L.odd[tid] = 0;
+    load_ids(tile0);
+    load_rows(tile0);
+    load_ids(tile0 + 1 < n_tiles ? tile0 + 1 : tile0);
     __syncthreads();
-    store_rows(0, 0);
-    if (n_tiles > 1) { load_rows(1); load_ids(2 < n_tiles ? 2 : 0); }
+    store_rows(tile0, tile0 & 1);
+    if (tile0 + 1 < n_tiles) { load_rows(tile0 + 1); load_ids(tile0 + 2 < n_tiles ? tile0 + 2 : tile0); }
     __syncthreads();
     auto next = [&](int tile) {                          // the tile behind `tile` into the other buffer, the one behind that on its way
         if (tile + 1 < n_tiles) {
             store_rows(tile + 1, (tile & 1) ^ 1);
             if (tile + 2 < n_tiles) {
                 load_rows(tile + 2);
-                load_ids(tile + 3 < n_tiles ? tile + 3 : 0);
+                load_ids(tile + 3 < n_tiles ? tile + 3 : tile0);
             }
         }
         __syncthreads();
     };
-    int tile = 0;
+    int tile = tile0;
     for (; tile < min(first_masked, n_tiles); ++tile) {
         if (wave_live) step(std::false_type(), tile);
         next(tile);
@@ -300,22 +409,103 @@ __global__ __launch_bounds__(kCaThreads) void chunk_attention_kernel(ServingDev 
         if (wave_live && tile * kCaKeys <= wave_last) step(std::true_type(), tile);
         next(tile);
     }
-    if (row >= rows) return;
-    const float inv = 1.0f / partner_sum(l);
-    uint16_t *op = (uint16_t *)io.out + ((int64_t)(it.row0 + t) * S.nq + head) * D + half * 4;
+    l = partner_sum(l);
+    auto put = [&](int rw, int cc, f32x4 v) {            // piece cc of a lane's row (row rw of the block): elements 8 cc + 4 half + 0 .. 3
+        const int r = r0 + rw;
+        if (r >= rows) return;
+        const int tt = r / grp;
+        uint16_t *op = (uint16_t *)io.out + ((int64_t)(it.q0 + tt) * S.nq + kvh * grp + (r - tt * grp)) * D + cc * 8 + half * 4;
+        *as_global(reinterpret_cast<u32x2 *>(op)) = u32x2{to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3])};
+    };
+    if (parts == 1) {
+        if (!wave_live) return;
+        const float inv = 1.0f / l;
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
+        for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            *as_global(reinterpret_cast<u32x2 *>(op + dt * 32 + q * 8)) =
-                u32x2{to_bf16x2(o[dt][4 * q] * inv, o[dt][4 * q + 1] * inv), to_bf16x2(o[dt][4 * q + 2] * inv, o[dt][4 * q + 3] * inv)};
+            for (int q = 0; q < 4; ++q)
+                put(wave * 32 + col, dt * 4 + q, f32x4{o[dt][4 * q] * inv, o[dt][4 * q + 1] * inv, o[dt][4 * q + 2] * inv, o[dt][4 * q + 3] * inv});
+        return;
+    }
+    // ---- a part of the keys: the partial result to memory (device scope: the reader may be on another die); who arrives last
+    // ---- at the item joins them, in the order of the keys
+    const int slot0 = __builtin_amdgcn_readfirstlane(L.slot[b]) + local - part * S.nkv;
+    if (wave_live) {
+        float *dst = S.attn_part + (size_t)(slot0 + part * S.nkv) * kCaSlot<D> + (size_t)wave * (kCaPartO<D> + 64);
+        const __amdgpu_buffer_rsrc_t d_b = buf_of(dst);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                buf_st_16B(d_b, (uint32_t)(((dt * 4 + q) * 64 + lane) * 16),
+                           __builtin_bit_cast(u32x4, f32x4{o[dt][4 * q], o[dt][4 * q + 1], o[dt][4 * q + 2], o[dt][4 * q + 3]}));
+        if (half == 0) buf_st_8B(d_b, (uint32_t)(kCaPartO<D> * 4 + col * 8), u32x2{__float_as_uint(m), __float_as_uint(l)});
+    }
+    wg_release();
+    if (tid == 0) {
+        int32_t *ctr = S.attn_arrive + slot0;
+        const int last = __hip_atomic_fetch_add(as_global(ctr), 1, __ATOMIC_RELAXED, ETC_SCOPE) + 1 == parts;
+        if (last) st_i32(ctr, 0);
+        L.last = last;
+    }
+    __syncthreads();
+    if (!L.last) return;
+    const int live = min(kCaWaves, div_up(rows - r0, 32));
+    // which parts exist: all of them, or (fewer tiles than pieces) one per tile, in the pieces part = ceil((t + 1) * split / tiles) - 1
+    for (int cc = wave; cc < live * DT * 4; cc += kCaWaves) {      // a wavefront per (32 rows, piece of them)
+        const int rw = cc / (DT * 4), pc = cc % (DT * 4);
+        float mm = -3e38f, ll = 0.f;
+        f32x4 acc{0.f, 0.f, 0.f, 0.f};
+        for (int j0 = 0; j0 < parts; j0 += 4) {
+            f32x4 ov[4];
+            u32x2 ml[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int j = min(j0 + u, parts - 1), pj = parts == split ? j : (int)(((int64_t)(j + 1) * split + all_tiles - 1) / all_tiles) - 1;
+                const float *src = S.attn_part + (size_t)(slot0 + pj * S.nkv) * kCaSlot<D> + (size_t)rw * (kCaPartO<D> + 64);
+                ov[u] = __builtin_bit_cast(f32x4, buf_ld_16B(buf_of(src), (uint32_t)((pc * 64 + lane) * 16), 0));
+                const uint64_t w = ld_u64(src + kCaPartO<D> + col * 2);
+                ml[u] = u32x2{(uint32_t)w, (uint32_t)(w >> 32)};
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                if (j0 + u >= parts) continue;
+                const float mj = __uint_as_float(ml[u].x), lj = __uint_as_float(ml[u].y);
+                const float nm = fmaxf(mm, mj), sa = exp2_fast(mm - nm), sb = exp2_fast(mj - nm);
+                mm = nm;
+                ll = ll * sa + lj * sb;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[i] = acc[i] * sa + ov[u][i] * sb;
+            }
+        }
+        const float inv = 1.0f / ll;
+        put(rw * 32 + col, pc, f32x4{acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv});
+    }
 }
+
+template <int D>
+__global__ __launch_bounds__(kCaThreads) void chunk_attention_kernel(ServingDev S, etc_serving_attention_io io)
+{
+    __shared__ CaLds L;
+    __shared__ __attribute__((aligned(16))) uint16_t s_k[2][kCaKeys * D], s_v[2][kCaKeys * D];
+    const int n_pieces = cut(S, io, L);
+    for (int p = (int)blockIdx.x; p < n_pieces; p += (int)gridDim.x) {
+        const int b = __builtin_amdgcn_readfirstlane(last_not_above(L.first, io.n_seqs, p));
+        chunk_attention_piece<D>(S, io, L, s_k, s_v, b, p - __builtin_amdgcn_readfirstlane(L.first[b]));
+        __syncthreads();
+    }
+}
+
+int64_t attention_slot_bytes(int head_dim) { return 4ll * (head_dim == 128 ? kCaSlot<128> : kCaSlot<64>); }
 
 hipError_t launch_serving_attention(const ServingDev &S, const etc_serving_attention_io &io, hipStream_t s)
 {
-    const int grp = S.nq / S.nkv;
-    const int64_t blocks = (int64_t)io.n_tokens * grp / kCaRows + (io.n_seqs < io.n_tokens ? io.n_seqs : io.n_tokens);
-    const dim3 grid((unsigned)blocks, (unsigned)S.nkv), block(kCaThreads);
+    // One workgroup per compute unit (its registers fill one); fewer where the call cannot have as many pieces.
+    const int64_t items = ((int64_t)io.n_tokens * (S.nq / S.nkv) / kCaRows + (io.n_seqs < io.n_tokens ? io.n_seqs : io.n_tokens)) * S.nkv;
+    int64_t keys = (int64_t)io.table_cols << S.page_shift;
+    if (keys > S.max_kv_len) keys = S.max_kv_len;
+    const int64_t pieces = items * ((keys - 1) / (kCaKeys * kCaMinTiles) + 1);
+    const dim3 grid((unsigned)(pieces < S.n_cus ? pieces : S.n_cus)), block(kCaThreads);
     if (S.d == 128) hipLaunchKernelGGL((chunk_attention_kernel<128>), grid, block, 0, s, S, io);
     else hipLaunchKernelGGL((chunk_attention_kernel<64>), grid, block, 0, s, S, io);
     return hipGetLastError();

@@ -12,6 +12,7 @@ using namespace etc;
 
 #ifdef ETC_GENERIC_ONLY      // a library generated for one graph has no kernels of these; no handle is ever made there
 namespace etc {
+int64_t attention_slot_bytes(int) { return 0; }
 hipError_t launch_serving_tables(const ServingDev &, const etc_serving_tables_io &, hipStream_t) { return hipErrorInvalidDeviceFunction; }
 hipError_t launch_serving_append(const ServingDev &, const etc_serving_append_io &, hipStream_t) { return hipErrorInvalidDeviceFunction; }
 hipError_t launch_serving_attention(const ServingDev &, const etc_serving_attention_io &, hipStream_t) { return hipErrorInvalidDeviceFunction; }
@@ -24,7 +25,7 @@ struct etc_serving {
     etc_serving_limits limits{};
     int device = 0;
     ServingDev dev{};
-    void *owned[4] = {nullptr, nullptr, nullptr, nullptr};      // device memory
+    void *owned[8] = {nullptr};                                 // device memory
     int n_owned = 0;
     int32_t *h_error = nullptr;                                 // pinned: a kernel's first refusal
     char err[256] = "";
@@ -51,12 +52,12 @@ etc_status fail(etc_serving *s, etc_status st, const char *msg)
     } while (0)
 
 template <class T>
-hipError_t owned_alloc(etc_serving *s, T **p, size_t n)
+hipError_t owned_alloc(etc_serving *s, T **p, size_t n, bool zero = true)
 {
     hipError_t e = hipMalloc((void **)p, n * sizeof(T));
     if (e != hipSuccess) return e;
     s->owned[s->n_owned++] = *p;
-    return hipMemset(*p, 0, n * sizeof(T));
+    return zero ? hipMemset(*p, 0, n * sizeof(T)) : hipSuccess;
 }
 
 // What finished launches refused: reported once, then cleared.
@@ -152,6 +153,9 @@ etc_status etc_serving_create(const etc_model_desc *m, const etc_serving_limits 
         memset(s->h_error, 0, 4 * sizeof(int32_t));
         SRV_TRY(s, hipHostGetDevicePointer((void **)&D.error, s->h_error, 0));
         SRV_TRY(s, owned_alloc(s, &D.arrive, 2));
+        D.attn_slots = kAttnMaxSlots;
+        SRV_TRY(s, owned_alloc(s, &D.attn_arrive, (size_t)kAttnMaxSlots));
+        SRV_TRY(s, owned_alloc(s, (char **)&D.attn_part, (size_t)kAttnMaxSlots * attention_slot_bytes(m->head_dim), false));
         double inv[64], *d_inv = nullptr;
         for (int i = 0; i < m->head_dim / 2; ++i) inv[i] = pow((double)m->rope_theta, -2.0 * i / m->head_dim);
         SRV_TRY(s, owned_alloc(s, &d_inv, m->head_dim / 2));

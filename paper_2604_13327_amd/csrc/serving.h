@@ -25,7 +25,13 @@ struct ServingDev {
     const double *inv_freq;      // [d / 2] theta^(-2i/d)
     int32_t *error;              // pinned host memory, 4 words
     int32_t *arrive;             // [2] zero between launches: workgroups of a launch that have read their inputs
+    // attention: partial results of items whose keys are cut, a slot each, and per item how many have arrived (zero between launches)
+    float *attn_part;
+    int32_t *attn_arrive;
+    int attn_slots;
 };
+constexpr int kAttnMaxSlots = 1024;
+int64_t attention_slot_bytes(int head_dim);
 
 hipError_t launch_serving_tables(const ServingDev &S, const etc_serving_tables_io &io, hipStream_t s);
 hipError_t launch_serving_append(const ServingDev &S, const etc_serving_append_io &io, hipStream_t s);
