@@ -40,7 +40,7 @@ __device__ __forceinline__ uint32_t odd_kind(uint32_t e)
     return (e & 0x7FFFu) > 0x7F80u ? 0x4780u : e == 0x7F80u ? 0x3F80u : e == 0xFF80u ? 0x4380u : 0u;
 }
 
-__device__ __forceinline__ int last_not_above(const int *indptr, int n, int x)      // the last b with indptr[b] <= x
+__device__ __forceinline__ int last_not_above(ETC_AS_LDS const int *indptr, int n, int x)      // the last b with indptr[b] <= x
 {
     int lo = 0, hi = n;
     while (hi - lo > 1) {
@@ -66,7 +66,7 @@ struct CaLds {
     int split[kServingMaxSeqs];             // pieces of an item
     float wave_f[kCaWaves];
     int wave_i[2][kCaWaves];
-    int odd[2], last;
+    int odd, last;
 };
 
 struct Seq { int q0, n, kv; };
@@ -93,7 +93,7 @@ __device__ __forceinline__ int wave_max_i(int v)
 }
 
 // Fills L and returns the number of pieces.
-__device__ int cut(const ServingDev &S, const etc_serving_attention_io &io, CaLds &L)
+__device__ int cut(const ServingDev &S, const etc_serving_attention_io &io, ETC_AS_LDS CaLds &L)
 {
     const int tid = (int)threadIdx.x, wave = wave_id(), lane = lane_id(), grp = S.nq / S.nkv, grid = (int)gridDim.x;
     float work = 0.f;                                    // tiles, all items
@@ -179,15 +179,188 @@ __device__ int cut(const ServingDev &S, const etc_serving_attention_io &io, CaLd
 template <int D> constexpr int kCaPartO = D / 32 * 4 * 64 * 4;      // floats of a wavefront
 template <int D> constexpr int kCaSlot = kCaWaves * (kCaPartO<D> + 64);
 
+// ---- the products --------------------------------------------------------------------------------------------------------
+// Rows of K and V in LDS, D elements without gaps; their 16-byte pieces change places with the row (exclusive or), so that the
+// lanes of an access meet different banks (64 of 4 bytes): 16 rows of one piece of K, 4 rows of 4 pieces of V.  Rows of 64
+// elements are half as wide as the banks: there two neighbouring rows share their places.
+template <int D> __device__ __forceinline__ int k_swap(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
+template <int D> __device__ __forceinline__ int v_swap(int row) { return D == 128 ? (row & 3) * 4 : (row & 2) * 2; }
+
 template <int D>
-__device__ __forceinline__ void chunk_attention_piece(const ServingDev &S, const etc_serving_attention_io &io, CaLds &L,
-                                                      uint16_t (&s_k)[2][kCaKeys * D], uint16_t (&s_v)[2][kCaKeys * D], int b, int local)
+struct Fragments {                          // LDS byte addresses of this lane's pieces in a tile that starts at 0
+    uint32_t k[D / 16], v[D / 32];
+    __device__ __forceinline__ Fragments(int lane)
+    {
+        const int half = lane >> 5, col = lane & 31, vrow = 4 * half + ((lane & 15) >> 2), piece = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) k[ks] = col * D * 2 + ((ks * 2 + half) ^ k_swap<D>(col)) * 16;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt) v[dt] = vrow * D * 2 + ((dt * 4 + piece) ^ v_swap<D>(vrow)) * 16 + (lane & 1) * 8;
+    }
+    // V^T fragment of 32 elements (tile dt) x 16 keys (step ks), the keys in the order the scores have them: rows 4 half + 0 .. 3
+    // and 8 + 4 half + 0 .. 3 of the step.
+    __device__ __forceinline__ u32x4 v_frag(uint32_t base, int ks, int dt) const
+    {
+        ETC_AS_LDS char *at = reinterpret_cast<ETC_AS_LDS char *>(v[dt] + base) + ks * 16 * D * 2;
+        const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<ETC_AS_LDS s16x4 *>(at)));
+        const u32x2 b = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<ETC_AS_LDS s16x4 *>(at + 8 * D * 2)));
+        return u32x4{a.x, a.y, b.x, b.y};
+    }
+};
+
+// S^T = K . Q^T over 32 KT keys: register i of tile kt is key 32 kt + 8 (i / 4) + 4 half + i % 4, the lane's row.
+template <int D, int KT>
+__device__ __forceinline__ void scores(f32x16 (&s)[KT], const Fragments<D> &F, uint32_t base, const bf16x8 (&qf)[D / 16])
+{
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) s[kt] = f32x16{};
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) {
+            const bf16x8 a = *reinterpret_cast<ETC_AS_LDS const bf16x8 *>(reinterpret_cast<ETC_AS_LDS const char *>(F.k[ks] + base) + kt * 32 * D * 2);
+            s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[ks], s[kt], 0, 0, 0);
+        }
+}
+
+// Softmax of a tile's scores and O^T += V^T . P^T.  l is this lane's sum, over half of the keys.
+// MASKED: keys behind `limit` do not count; their rows of V hold numbers (odd_values has seen to that).
+template <int D, int KT, bool MASKED>
+__device__ __forceinline__ void attend(f32x16 (&s)[KT], f32x16 (&o)[D / 32], float &m, float &l, const Fragments<D> &F, uint32_t base,
+                                       int half, float scale, int k0, int limit)
+{
+    constexpr int DT = D / 32;
+    if constexpr (MASKED) {
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (k0 + kt * 32 + 8 * (i >> 2) + 4 * half + (i & 3) > limit) s[kt][i] = -INFINITY;
+    }
+    float mt = s[0][0];
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mt = fmaxf(mt, s[kt][i]);
+    mt = partner_max(mt) * scale;
+    // The reference follows the maximum only when that has grown by 2^8 (rows of a wavefront together): until then
+    // probabilities up to 2^8 lose nothing, and the running output need not be multiplied.
+    if (__builtin_amdgcn_ballot_w64(mt > m + 8.f) != 0) {
+        const float nm = fmaxf(m, mt), sc = exp2_fast(m - nm);
+        m = nm;
+        l *= sc;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[dt] *= sc;
+    }
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) {
+        uint32_t p[8];
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) {
+            const float a = exp2_fast(__builtin_fmaf(s[kt][i], scale, -m)), b = exp2_fast(__builtin_fmaf(s[kt][i + 1], scale, -m));
+            p[i >> 1] = to_bf16x2(a, b);                 // half a unit of bf16 of a probability: below the rounding of the output
+            l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(s16x2, p[i >> 1]), __builtin_bit_cast(s16x2, 0x3F803F80u), l, false);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const bf16x8 pb = __builtin_bit_cast(bf16x8, u32x4{p[4 * h], p[4 * h + 1], p[4 * h + 2], p[4 * h + 3]});
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                const u32x4 w = F.v_frag(base, kt * 2 + h, dt);
+                o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), pb, o[dt], 0, 0, 0);
+            }
+        }
+    }
+}
+
+// Values of V that are no numbers, in a tile that some rows see a part of: the probability 0 of what a row does not see would make a
+// NaN of them.  They are counted by kind, in a product over the keys each row sees (+inf as 1, -inf as 2^8, NaN as 2^16, at most 64 of
+// each: exact), which goes to the output as infinities and NaN; the tile then holds zeros in their place.  `mine` are the pieces of the tile this
+// thread looks after, at the LDS addresses at[]; for the whole workgroup.
+template <int D, int N>
+__device__ __forceinline__ void odd_values(const u32x4 (&mine)[N], const uint32_t (&at)[N], f32x16 (&o)[D / 32], const Fragments<D> &F, uint32_t base, int half, int k0, int limit, bool live)
+{
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+        u32x4 kind;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) kind[i] = odd_kind(mine[u][i] & 0xFFFFu) | odd_kind(mine[u][i] >> 16) << 16;
+        *reinterpret_cast<ETC_AS_LDS u32x4 *>(at[u]) = kind;
+    }
+    __syncthreads();
+    if (live) {
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt) {
+            f32x16 n{};
+#pragma unroll 1
+            for (int ks = 0; ks < kCaKeys / 16; ++ks) {
+                const u32x4 w = F.v_frag(base, ks, dt);
+                u32x4 seen;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int key = k0 + ks * 16 + 4 * half + (i >> 1) * 8 + (i & 1) * 2;
+                    seen[i] = (key <= limit ? 0x3F80u : 0u) | (key + 1 <= limit ? 0x3F800000u : 0u);
+                }
+                n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, seen), n, 0, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const uint32_t c = (uint32_t)n[i];
+                if (c & 0xFFu) o[dt][i] += INFINITY;
+                if (c & 0xFF00u) o[dt][i] -= INFINITY;
+                if (c >> 16) o[dt][i] = __uint_as_float(0x7FC00000u);
+            }
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+        u32x4 w = mine[u];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            w[i] &= ((w[i] & 0x7F80u) == 0x7F80u ? 0u : 0xFFFFu) | ((w[i] & 0x7F800000u) == 0x7F800000u ? 0u : 0xFFFF0000u);
+        *reinterpret_cast<ETC_AS_LDS u32x4 *>(at[u]) = w;
+    }
+    __syncthreads();
+}
+
+__device__ __forceinline__ bool any_odd(u32x4 v)          // an exponent of all ones among 8 values
+{
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) odd |= (v[i] & 0x7F80u) == 0x7F80u || (v[i] & 0x7F800000u) == 0x7F800000u;
+    return odd;
+}
+
+// Rows go from memory to LDS without a stop in registers: 64 lanes, 16 bytes each, to 1 KB of LDS from `to` on (the same for the
+// whole wavefront).  The compiler would have every LDS read wait for all such loads in flight; here their order is the
+// program's own: arrived(n) waits until at most n of this wavefront's are on their way, a barrier then covers everyone's.
+__device__ __forceinline__ void fetch_1k(const char *from, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory");
+}
+template <int N> __device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(%0)" : : "i"(N) : "memory"); }
+
+// Tile t of a piece has K in ring slot t % 3 and V in t % 4: while the rows of t + 2 are on their way, t + 1 has arrived or is about
+// to, t is being read, and so is, by half the wavefronts, V of t - 1.
+constexpr int kCaKSlots = 3, kCaVSlots = 4;
+constexpr int kCaIds = 2048;                // page ids in LDS, a window of a piece's at a time
+template <int D>
+struct Tiles {
+    uint16_t k[kCaKSlots][kCaKeys * D], v[kCaVSlots][kCaKeys * D];
+    int ids[kCaIds];
+};
+
+template <int D>
+__device__ __forceinline__ void chunk_attention_piece(const ServingDev &S, const etc_serving_attention_io &io, ETC_AS_LDS CaLds &L, ETC_AS_LDS Tiles<D> &B, int b, int local)
 {
     constexpr int CH = D / 8;                            // 16-byte pieces of a row
     constexpr int KS = D / 16, DT = D / 32;              // steps of the first product, tiles of the output
-    constexpr int RPT = kCaKeys * CH / kCaThreads;       // pieces of K (and of V) a thread stages
-    constexpr int RSTEP = kCaThreads / CH;               // rows between them
-    const int tid = (int)threadIdx.x, wave = __builtin_amdgcn_readfirstlane(wave_id()), lane = lane_id(), half = lane >> 5, col = lane & 31;
+    constexpr int RPL = 64 / CH, LOADS = kCaKeys / RPL / kCaWaves;      // rows of a load; loads of K (and of V) a wavefront has in a tile
+    constexpr uint32_t BUF = kCaKeys * D * 2;            // bytes of a tile
+    int tid = (int)threadIdx.x;
+    asm volatile("" : "+v"(tid));                        // of this piece: what is computed from it does not stay in registers across pieces
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, half = lane >> 5, col = lane & 31;
     const int split = __builtin_amdgcn_readfirstlane(L.split[b]), blocks = __builtin_amdgcn_readfirstlane(L.blocks[b]);
     const int kvh = local % S.nkv, part = local / S.nkv % split, block = blocks - 1 - local / S.nkv / split;      // long blocks first
     bool ok;
@@ -202,6 +375,24 @@ __device__ __forceinline__ void chunk_attention_piece(const ServingDev &S, const
     if (tile0 == n_tiles) return;                        // a block shorter than its sequence's last one may have fewer pieces
     const int parts = min(split, all_tiles);
 
+    // page ids of the tiles [., ids_end), from page ids0 on
+    const int32_t *table = io.block_table + (int64_t)b * io.table_stride;
+    int ids0 = 0, ids_end = tile0;
+    auto load_ids = [&](int tile) {                      // between barriers
+        ids0 = tile * kCaKeys >> psh;
+        const int last_page = (min(n_tiles * kCaKeys, n_keys) - 1) >> psh, n = min(last_page - ids0 + 1, kCaIds);
+        ids_end = last_page - ids0 < kCaIds ? n_tiles : (int)((((int64_t)(ids0 + kCaIds)) << psh) / kCaKeys);      // whole tiles only
+        for (int i = tid; i < n; i += kCaThreads) {
+            int id = gld_i32(table + ids0 + i);
+            if ((uint32_t)id >= (uint64_t)io.n_pages) {
+                refuse(S.error, SRV_BAD_PAGE, SRV_ATTENTION, b, id);
+                id = 0;
+            }
+            B.ids[i] = id;
+        }
+    };
+    load_ids(tile0);
+
     // this lane's row: query fragments (right operand: 8 consecutive elements of step ks at ks * 16 + half * 8)
     const int row = r0 + wave * 32 + col, rr = min(row, rows - 1), t = rr / grp, head = kvh * grp + (rr - t * grp);
     const uint16_t *qp = (const uint16_t *)io.q + ((int64_t)(it.q0 + t) * S.nq + head) * D + half * 8;
@@ -212,47 +403,22 @@ __device__ __forceinline__ void chunk_attention_piece(const ServingDev &S, const
     const int first_masked = (it.kv + r0 / grp + 1) / kCaKeys;      // tiles in front of it are seen whole by all rows of the block
     const int wave_last = it.kv + min((r0 + wave * 32 + 31) / grp, it.n - 1);
     const bool wave_live = r0 + wave * 32 < rows;
+    const uint32_t k_base = (uint32_t)(uintptr_t)&B.k[0][0], v_base = (uint32_t)(uintptr_t)&B.v[0][0];
 
-    // staging: thread has piece c of rows key0 + RSTEP * u of a tile
-    const int c = tid % CH, key0 = tid / CH;
-    const int32_t *table = io.block_table + (int64_t)b * io.table_stride;
-    int ids[RPT];
-    u32x4 kr[RPT], vr[RPT];
-    auto load_ids = [&](int tile) {
+    // Load u of this wavefront brings the rows row_of(u) + 0 .. RPL - 1 of a tile; the lane's place in LDS is given, so it is the piece of
+    // memory that belongs there which it chooses.  Rows behind the last key are that key's again (their scores are masked).
+    const uint32_t row_bytes = (uint32_t)(S.nkv * D * 2);
+    const uint64_t page_bytes = (uint64_t)row_bytes << psh;
+    const int lrow = lane / CH, c = lane % CH;
+    auto fetch = [&](int tile, uint32_t kb, uint32_t vb) {
 #pragma unroll
-        for (int u = 0; u < RPT; ++u) ids[u] = gld_i32(table + (min(tile * kCaKeys + key0 + RSTEP * u, n_keys - 1) >> psh));
-    };
-    auto load_rows = [&](int tile) {
-#pragma unroll
-        for (int u = 0; u < RPT; ++u) {
-            const int key = min(tile * kCaKeys + key0 + RSTEP * u, n_keys - 1);
-            int id = ids[u];
-            if ((uint32_t)id >= (uint64_t)io.n_pages) {
-                refuse(S.error, SRV_BAD_PAGE, SRV_ATTENTION, b, id);
-                id = 0;
-            }
-            const int64_t off = (((int64_t)id << psh) + (key & pmask)) * (S.nkv * D) + kvh * D + c * 8;
-            kr[u] = gld_16B((const uint16_t *)io.k_pages + off);
-            vr[u] = gld_16B((const uint16_t *)io.v_pages + off);
+        for (int u = 0; u < LOADS; ++u) {
+            const int r = (wave * LOADS + u) * RPL, key = min(tile * kCaKeys + r + lrow, n_keys - 1);
+            const uint32_t id = (uint32_t)B.ids[(key >> psh) - ids0];
+            const uint64_t off = id * page_bytes + (uint64_t)((uint32_t)(key & pmask)) * row_bytes + kvh * D * 2;
+            fetch_1k((const char *)io.k_pages + (off + (uint32_t)((c ^ k_swap<D>(r + lrow)) * 16)), k_base + kb + r * D * 2);
+            fetch_1k((const char *)io.v_pages + (off + (uint32_t)((c ^ v_swap<D>(r + lrow)) * 16)), v_base + vb + r * D * 2);
         }
-    };
-    // LDS rows: the 16-byte pieces of a row change places with the row (exclusive or), so that lanes reading one piece of
-    // neighbouring rows meet different banks: K by the row's low 3 bits (8 lanes an access), V by pairs of pieces (4 rows an access).
-    auto store_rows = [&](int tile, int buf) {
-        bool odd = false;
-#pragma unroll
-        for (int u = 0; u < RPT; ++u) {
-            const int key = key0 + RSTEP * u;
-            if ((tile + 1) * kCaKeys > n_keys && tile * kCaKeys + key >= n_keys)      // behind the last key: zero, whatever the pool holds
-                kr[u] = vr[u] = u32x4{0, 0, 0, 0};
-            *reinterpret_cast<u32x4 *>(&s_k[buf][key * D + ((c ^ (key & 7)) * 8)]) = kr[u];
-            *reinterpret_cast<u32x4 *>(&s_v[buf][key * D + ((c ^ ((key & 3) * 2)) * 8)]) = vr[u];
-            if (tile >= first_masked) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) odd |= (vr[u][i] & 0x7F80u) == 0x7F80u || (vr[u][i] & 0x7F800000u) == 0x7F800000u;
-            }
-        }
-        if (odd) L.odd[buf] = 1;                         // stays: the tiles behind it are masked too
     };
 
     f32x16 o[DT];
@@ -260,153 +426,80 @@ __device__ __forceinline__ void chunk_attention_piece(const ServingDev &S, const
     for (int i = 0; i < DT; ++i) o[i] = f32x16{};
     float m = -3e38f, l = 0.f;                           // reference of the row's exponentials; sum over this lane's keys
     const float scale = 1.44269504088896f / sqrtf((float)D);      // scores and reference count in powers of two
+    const Fragments<D> F(lane);
+    f32x16 s[2];
 
-    // Fragments in LDS.  The exchange of pieces touches the low 3 bits of a piece's number, so that every fragment lies at a constant
-    // distance from one of a few addresses: K of step ks at k_at[ks % 4] (and 8 pieces behind for ks >= 4), V of tile dt at v_at[dt % 2].
-    constexpr int ROW = D * 2, BUF = kCaKeys * ROW;      // bytes
-    uint32_t k_at[4], v_at[2];
-    {
-        const uint32_t kb = (uint32_t)(uintptr_t)as_lds(&s_k[0][0]), vb = (uint32_t)(uintptr_t)as_lds(&s_v[0][0]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) k_at[i] = kb + col * ROW + (((i * 2 + half) ^ (col & 7)) * 16);
-        const int vrow = 4 * half + ((lane & 15) >> 2), piece = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) v_at[i] = vb + vrow * ROW + (((i * 4 + piece) ^ ((vrow & 3) * 2)) * 16) + (lane & 1) * 8;
-    }
-    auto k_frag = [&](int buf, int ks, int kt) {
-        return *reinterpret_cast<ETC_AS_LDS const bf16x8 *>(k_at[ks & 3] + buf * BUF + kt * 32 * ROW + (ks >> 2) * 128);
-    };
-    // V^T fragment of 32 elements (tile dt) x 16 keys (step ks), the keys in the order the scores have them: rows 4 half + 0 .. 3
-    // and 8 + 4 half + 0 .. 3 of the step.
-    auto v_frag = [&](int buf, int ks, int dt) {
-        const uint32_t at = v_at[dt & 1] + buf * BUF + ks * 16 * ROW + (dt >> 1) * 128;
-        const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<ETC_AS_LDS s16x4 *>(at)));
-        const u32x2 b = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<ETC_AS_LDS s16x4 *>(at + 8 * ROW)));
-        return u32x4{a.x, a.y, b.x, b.y};
-    };
-    // One tile.  MASKED: some row of the block does not see all of it.
-    auto step = [&](auto masked_c, int tile) {
-        constexpr bool MASKED = decltype(masked_c)::value;
-        const int buf = tile & 1, k0 = tile * kCaKeys;
-        // ---- scores: S^T[key][row], key = 32 kt + 8 (i / 4) + 4 half + i % 4 of register i
-        f32x16 s[2] = {f32x16{}, f32x16{}};
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt) s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(buf, ks, kt), qf[ks], s[kt], 0, 0, 0);
-        if constexpr (MASKED) {
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (k0 + kt * 32 + 8 * (i >> 2) + 4 * half + (i & 3) > limit) s[kt][i] = -INFINITY;
-        }
-        float mt = s[0][0];
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) mt = fmaxf(mt, s[kt][i]);
-        mt = partner_max(mt) * scale;
-        // The reference follows the maximum only when that has grown by 2^8 (rows of a wavefront together): until then
-        // probabilities up to 2^8 lose nothing, and the running output need not be multiplied.
-        if (__builtin_amdgcn_ballot_w64(mt > m + 8.f) != 0) {
-            const float nm = fmaxf(m, mt), sc = exp2_fast(m - nm);
-            m = nm;
-            l *= sc;
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt) o[dt] *= sc;
-        }
-        bool odd = false;
-        if constexpr (MASKED) {
-            // Keys some rows do not see: their probability 0 would make a NaN of an infinite or NaN value.  A tile that holds
-            // such values (exponent all ones) has them taken out of the product, and counted by kind in a second one over the
-            // keys each row sees: +inf as 1, -inf as 2^8, NaN as 2^16 (at most 64 of each: exact).
-            odd = L.odd[buf] != 0;
-            if (odd) {
-                auto count = [&](int dt) {
-                    f32x16 n{};
-#pragma unroll 1
-                    for (int ks = 0; ks < 4; ++ks) {
-                        const u32x4 w = v_frag(buf, ks, dt);
-                        u32x4 kind, seen;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int key = k0 + ks * 16 + 4 * half + (i >> 1) * 8 + (i & 1) * 2;
-                            seen[i] = (key <= limit ? 0x3F80u : 0u) | (key + 1 <= limit ? 0x3F800000u : 0u);
-                            kind[i] = odd_kind(w[i] & 0xFFFFu) | odd_kind(w[i] >> 16) << 16;
-                        }
-                        n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kind), __builtin_bit_cast(bf16x8, seen), n, 0, 0, 0);
-                    }
-                    return n;
-                };
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt) {
-                    const f32x16 n = count(dt);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const uint32_t c = (uint32_t)n[i];
-                        if (c & 0xFFu) o[dt][i] += INFINITY;
-                        if (c & 0xFF00u) o[dt][i] -= INFINITY;
-                        if (c >> 16) o[dt][i] = __uint_as_float(0x7FC00000u);
-                    }
-                }
-            }
-        }
-        // ---- probabilities of 32 keys, then O^T += V^T . P^T over them
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
-            uint32_t p[8];
-#pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-                const float a = exp2_fast(__builtin_fmaf(s[kt][i], scale, -m)), b = exp2_fast(__builtin_fmaf(s[kt][i + 1], scale, -m));
-                p[i >> 1] = to_bf16x2(a, b);             // half a unit of bf16 of a probability: below the rounding of the output
-                l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(s16x2, p[i >> 1]), __builtin_bit_cast(s16x2, 0x3F803F80u), l, false);
-            }
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const bf16x8 pb = __builtin_bit_cast(bf16x8, u32x4{p[4 * h], p[4 * h + 1], p[4 * h + 2], p[4 * h + 3]});
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt) {
-                    u32x4 w = v_frag(buf, kt * 2 + h, dt);
-                    if constexpr (MASKED) {
-                        if (odd) {
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                w[i] &= ((w[i] & 0x7F80u) == 0x7F80u ? 0u : 0xFFFFu) | ((w[i] & 0x7F800000u) == 0x7F800000u ? 0u : 0xFFFF0000u);
-                        }
-                    }
-                    o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), pb, o[dt], 0, 0, 0);
-                }
-            }
-        }
-    };
-
-    // Tile t of the sequence goes to buffer t % 2.
-    if (tid < 2) L.odd[tid] = 0;
-    load_ids(tile0);
-    load_rows(tile0);
-    load_ids(tile0 + 1 < n_tiles ? tile0 + 1 : tile0);
+    if (tid == 0) L.odd = -1;
+    drain_vmem();                                        // nothing but tiles on their way from here on
     __syncthreads();
-    store_rows(tile0, tile0 & 1);
-    if (tile0 + 1 < n_tiles) { load_rows(tile0 + 1); load_ids(tile0 + 2 < n_tiles ? tile0 + 2 : tile0); }
+    uint32_t kb = 0, vb = 0, vb_before = 0;              // ring slots of the tile at hand; of V also of the one before
+    auto after = [](uint32_t at, int slots) { return at == (slots - 1) * BUF ? 0u : at + BUF; };
+    fetch(tile0, 0, 0);
+    if (tile0 + 1 < n_tiles && tile0 + 1 < ids_end) { fetch(tile0 + 1, BUF, BUF); arrived<2 * LOADS>(); }
+    else arrived<0>();
     __syncthreads();
-    auto next = [&](int tile) {                          // the tile behind `tile` into the other buffer, the one behind that on its way
-        if (tile + 1 < n_tiles) {
-            store_rows(tile + 1, (tile & 1) ^ 1);
-            if (tile + 2 < n_tiles) {
-                load_rows(tile + 2);
-                load_ids(tile + 3 < n_tiles ? tile + 3 : tile0);
+    // In front of a tile's work: the rows of the tile two behind it go on their way.  Behind it: the next tile's have arrived, for all.
+    auto ahead = [&](int tile) {
+        if (tile + 2 < n_tiles) {
+            if (tile + 2 >= ids_end) {                   // its page ids are not here: a new window, with all loads at rest
+                __syncthreads();
+                load_ids(tile + 2);
+                drain_vmem();
+                __syncthreads();
             }
+            fetch(tile + 2, after(after(kb, kCaKSlots), kCaKSlots), after(after(vb, kCaVSlots), kCaVSlots));
         }
+    };
+    auto next = [&](int tile) {
+        if (tile + 2 < n_tiles) arrived<2 * LOADS>(); else arrived<0>();
         __syncthreads();
+        kb = after(kb, kCaKSlots);
+        vb_before = vb;
+        vb = after(vb, kCaVSlots);
     };
+    // Two wavefronts share a SIMD, w and w + 4.  The barrier of every tile would have both at their products and both at their
+    // exponentials at the same time; so the second four are half a tile behind: they end a tile in front of the scores of the next.
     int tile = tile0;
-    for (; tile < min(first_masked, n_tiles); ++tile) {
-        if (wave_live) step(std::false_type(), tile);
-        next(tile);
+    const int n_seen = min(first_masked, n_tiles);
+    if (wave < kCaWaves / 2) {
+        for (; tile < n_seen; ++tile) {
+            ahead(tile);
+            if (wave_live) {
+                scores<D, 2>(s, F, k_base + kb, qf);
+                attend<D, 2, false>(s, o, m, l, F, v_base + vb, half, scale, 0, 0);
+            }
+            next(tile);
+        }
+    } else {
+        for (; tile < n_seen; ++tile) {
+            ahead(tile);
+            if (wave_live) {
+                if (tile > tile0) attend<D, 2, false>(s, o, m, l, F, v_base + vb_before, half, scale, 0, 0);
+                scores<D, 2>(s, F, k_base + kb, qf);
+            }
+            next(tile);
+        }
+        if (wave_live && tile > tile0) attend<D, 2, false>(s, o, m, l, F, v_base + vb_before, half, scale, 0, 0);
     }
     for (; tile < n_tiles; ++tile) {
-        if (wave_live && tile * kCaKeys <= wave_last) step(std::true_type(), tile);
+        ahead(tile);
+        u32x4 mine[LOADS];
+        uint32_t at[LOADS];
+        bool odd = false;                                // values that are no numbers, in any row of the tile
+#pragma unroll
+        for (int u = 0; u < LOADS; ++u) {
+            at[u] = v_base + vb + (wave * LOADS + u) * RPL * D * 2 + lane * 16;
+            mine[u] = *reinterpret_cast<ETC_AS_LDS const u32x4 *>(at[u]);
+            odd |= any_odd(mine[u]);
+        }
+        if (odd) L.odd = tile;
+        __syncthreads();
+        const bool live = wave_live && tile * kCaKeys <= wave_last;
+        if (__builtin_expect(L.odd == tile, 0)) odd_values<D, LOADS>(mine, at, o, F, v_base + vb, half, tile * kCaKeys, limit, live);
+        if (live) {
+            scores<D, 2>(s, F, k_base + kb, qf);
+            attend<D, 2, true>(s, o, m, l, F, v_base + vb, half, scale, tile * kCaKeys, limit);
+        }
         next(tile);
     }
     l = partner_sum(l);
@@ -486,12 +579,14 @@ __device__ __forceinline__ void chunk_attention_piece(const ServingDev &S, const
 template <int D>
 __global__ __launch_bounds__(kCaThreads) void chunk_attention_kernel(ServingDev S, etc_serving_attention_io io)
 {
-    __shared__ CaLds L;
-    __shared__ __attribute__((aligned(16))) uint16_t s_k[2][kCaKeys * D], s_v[2][kCaKeys * D];
+    __shared__ CaLds s_cut;
+    __shared__ __attribute__((aligned(16))) Tiles<D> s_tiles;
+    ETC_AS_LDS CaLds &L = *as_lds(&s_cut);
+    ETC_AS_LDS Tiles<D> &B = *as_lds(&s_tiles);
     const int n_pieces = cut(S, io, L);
     for (int p = (int)blockIdx.x; p < n_pieces; p += (int)gridDim.x) {
         const int b = __builtin_amdgcn_readfirstlane(last_not_above(L.first, io.n_seqs, p));
-        chunk_attention_piece<D>(S, io, L, s_k, s_v, b, p - __builtin_amdgcn_readfirstlane(L.first[b]));
+        chunk_attention_piece<D>(S, io, L, B, b, p - __builtin_amdgcn_readfirstlane(L.first[b]));
         __syncthreads();
     }
 }
