@@ -58,117 +58,114 @@ __device__ __forceinline__ int last_not_above(ETC_AS_LDS const int *indptr, int 
 // die's L2 sees the keys of one or two.
 constexpr int kCaTries = kCaWaves;          // a wavefront estimates one
 
+struct Seq { int q0, n, kv; };             // first row, new tokens, cached ones
+
 struct CaLds {
+    int q0[kServingMaxSeqs], n[kServingMaxSeqs], kv[kServingMaxSeqs];      // n == 0: nothing to do
+    int split[kServingMaxSeqs];             // pieces of an item
     int first[kServingMaxSeqs + 1];         // prefix sum: pieces of the sequences
     int slot[kServingMaxSeqs + 1];          // prefix sum: those that leave a partial result
-    int tiles[kServingMaxSeqs];             // of the last block; 0: nothing to do
-    int blocks[kServingMaxSeqs];
-    int split[kServingMaxSeqs];             // pieces of an item
     float wave_f[kCaWaves];
     int wave_i[2][kCaWaves];
     int odd, last;
 };
 
-struct Seq { int q0, n, kv; };
-__device__ __forceinline__ Seq sequence(const ServingDev &S, const etc_serving_attention_io &io, int b, bool *ok)
-{
-    const int q0 = gld_i32(io.q_indptr + b), q1 = gld_i32(io.q_indptr + b + 1), kv = gld_i32(io.kv_len + b), n = q1 - q0;
-    *ok = q0 >= 0 && q1 >= q0 && q1 <= io.n_tokens && kv >= 0 && kv <= S.max_kv_len && n <= S.max_kv_len - kv &&
-          (int)(((unsigned)(kv + n) + (1u << S.page_shift) - 1) >> S.page_shift) <= io.table_cols;
-    return Seq{q0, n, kv};
-}
-
 __device__ __forceinline__ int div_up(int a, int b) { return (a + b - 1) / b; }
-__device__ __forceinline__ float wave_sum_f(float v)
-{
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    return v;
-}
+__device__ __forceinline__ int blocks_of(int n, int grp) { return div_up(n * grp, kCaRows); }                    // n * grp <= 2^26
+__device__ __forceinline__ int tiles_of(int kv, int n) { return n > 0 ? (kv + n - 1) / kCaKeys + 1 : 0; }        // of the last block
 __device__ __forceinline__ int wave_max_i(int v)
 {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = max(v, __shfl_xor(v, o, 64));
-    return v;
+    v = max(v, dpp_i32<0xB1>(v));
+    v = max(v, dpp_i32<0x4E>(v));
+    v = max(v, dpp_i32<0x141>(v));
+    v = max(v, dpp_i32<0x140>(v));
+    return max(max(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16)), max(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
 }
 
 // Fills L and returns the number of pieces.
-__device__ int cut(const ServingDev &S, const etc_serving_attention_io &io, ETC_AS_LDS CaLds &L)
+__device__ __forceinline__ int cut(const ServingDev &S, const etc_serving_attention_io &io, ETC_AS_LDS CaLds &L)
 {
-    const int tid = (int)threadIdx.x, wave = wave_id(), lane = lane_id(), grp = S.nq / S.nkv, grid = (int)gridDim.x;
+    const int tid = (int)threadIdx.x, wave = __builtin_amdgcn_readfirstlane(wave_id()), lane = lane_id(), grp = S.nq / S.nkv, grid = (int)gridDim.x;
     float work = 0.f;                                    // tiles, all items
     int tokens = 0;                                      // at most 2^30
     for (int b = tid; b < io.n_seqs; b += kCaThreads) {
-        bool ok;
-        const Seq q = sequence(S, io, b, &ok);
-        if (!ok && blockIdx.x == 0) refuse(S.error, SRV_BAD_LENGTH, SRV_ATTENTION, b, q.kv);
-        const int rows = ok ? q.n * grp : 0;             // at most 2^26
-        const int blocks = div_up(rows, kCaRows), tiles = rows ? (q.kv + q.n - 1) / kCaKeys + 1 : 0;
-        L.blocks[b] = blocks;
-        L.tiles[b] = tiles;
-        if (ok) tokens += q.n;
-        if (rows) work += (float)S.nkv * blocks * 0.5f * (float)(tiles + (q.kv + min(q.n, kCaRows / grp) - 1) / kCaKeys + 1);
+        const int q0 = gld_i32(io.q_indptr + b), q1 = gld_i32(io.q_indptr + b + 1), kv = gld_i32(io.kv_len + b);
+        int n = q1 - q0;
+        if (q0 < 0 || q1 < q0 || q1 > io.n_tokens || kv < 0 || kv > S.max_kv_len || n > S.max_kv_len - kv ||
+            (int)(((unsigned)(kv + n) + (1u << S.page_shift) - 1) >> S.page_shift) > io.table_cols) {
+            if (blockIdx.x == 0) refuse(S.error, SRV_BAD_LENGTH, SRV_ATTENTION, b, kv);
+            n = 0;
+        }
+        L.q0[b] = q0;
+        L.n[b] = n;
+        L.kv[b] = kv;
+        tokens += n;
+        if (n > 0) work += (float)S.nkv * blocks_of(n, grp) * 0.5f * (float)(tiles_of(kv, n) + tiles_of(kv, min(n, kCaRows / grp)));
     }
-    work = wave_sum_f(work);
+    work = wave_sum(work);
     tokens = wave_sum_i(tokens);
     if (lane == 0) { L.wave_f[wave] = work; L.wave_i[0][wave] = tokens; }
     __syncthreads();
     work = 0.f;
     tokens = 0;
+#pragma unroll
     for (int w = 0; w < kCaWaves; ++w) { work += L.wave_f[w]; tokens += L.wave_i[0][w]; }
-    __syncthreads();
     if (tokens > io.n_tokens) {                          // ranges that overlap: no call's lengths
         if (blockIdx.x == 0 && tid == 0) refuse(S.error, SRV_BAD_LENGTH, SRV_ATTENTION, io.n_seqs, tokens);
         return 0;
     }
-    // Candidate of wavefront w: no cut, or pieces of 1.5, 1, 2/3, 1/2, 1/3, 1/4, 1/6 of a workgroup's share, kCaMinTiles at least.  A
-    // piece costs its tiles and 2 more; a partial result is written and read again: 1 more per 64 rows of it.
+    // Candidate of wavefront w: no cut, or pieces of 1.5, 1, 2/3, 1/2, 1/3, 1/4, 1/6 of a workgroup's share, kCaMinTiles at least.  All in
+    // tiles: a piece costs its tiles and 3 more; a partial result is written and read again, 1 or (a whole block) 5 more, and where there
+    // are any the end waits for the last join, 5 more.
     const float share = work / (float)grid;
-    auto tiles_of = [&](int w) {
+    auto limit_of = [&](int w) {
         const float f = w == 1 ? 1.5f : w == 2 ? 1.f : w == 3 ? 0.6667f : w == 4 ? 0.5f : w == 5 ? 0.3333f : w == 6 ? 0.25f : 0.1667f;
         return w == 0 ? 1 << 30 : max(kCaMinTiles, (int)fminf(ceilf(share * f), 1e9f));
     };
     float pieces = 0.f, slots = 0.f, cost = 0.f;
     int longest = 0;
-    const int per = tiles_of(wave);
+    const int per = limit_of(wave);
     for (int b = lane; b < io.n_seqs; b += 64) {
-        if (L.tiles[b] == 0) continue;
-        const int s = div_up(L.tiles[b], per);
-        const float n = (float)S.nkv * L.blocks[b] * s;
-        pieces += n;
-        if (s > 1) { slots += n; cost += n * (1.f + (L.blocks[b] > 1 ? 4.f : 1.f)); }
-        longest = max(longest, div_up(L.tiles[b], s));
+        const int n = L.n[b], tiles = tiles_of(L.kv[b], n);
+        if (n == 0) continue;
+        const int blocks = blocks_of(n, grp), s = div_up(tiles, per);
+        const float k = (float)S.nkv * blocks * s;
+        pieces += k;
+        if (s > 1) { slots += k; cost += k * (blocks > 1 ? 5.f : 1.f); }
+        longest = max(longest, div_up(tiles, s));
     }
-    pieces = wave_sum_f(pieces);
-    slots = wave_sum_f(slots);
-    cost = work + wave_sum_f(cost) + 2.f * pieces;
+    pieces = wave_sum(pieces);
+    slots = wave_sum(slots);
+    cost = work + wave_sum(cost) + 3.f * pieces;
     longest = wave_max_i(longest);
-    const float rounds = ceilf(pieces / (float)grid);
-    float ends = fmaxf((float)longest + 2.f, rounds * cost / fmaxf(pieces, 1.f));
+    float ends = fmaxf((float)longest + 3.f, ceilf(pieces / (float)grid) * cost / fmaxf(pieces, 1.f)) + (slots > 0.f ? 5.f : 0.f);
     if (wave > 0 && slots > (float)S.attn_slots) ends = INFINITY;
+    __syncthreads();
     if (lane == 0) L.wave_f[wave] = ends;
     __syncthreads();
     int best = 0;
+    float best_ends = L.wave_f[0];
+#pragma unroll
     for (int w = 1; w < kCaTries; ++w)
-        if (L.wave_f[w] < L.wave_f[best]) best = w;
-    const int limit = tiles_of(best);
+        if (L.wave_f[w] < best_ends) { best = w; best_ends = L.wave_f[w]; }
+    const int limit = limit_of(best);
     int done = 0, done_slots = 0;
     for (int b0 = 0; b0 < io.n_seqs; b0 += kCaThreads) {
         const int b = b0 + tid;
-        int n = 0, sl = 0;
-        if (b < io.n_seqs && L.tiles[b] > 0) {
-            const int s = div_up(L.tiles[b], limit);
+        int k = 0, sl = 0;
+        if (b < io.n_seqs && L.n[b] > 0) {
+            const int s = div_up(tiles_of(L.kv[b], L.n[b]), limit);
             L.split[b] = s;
-            n = S.nkv * L.blocks[b] * s;                 // all together at most 2^20 tokens * 1024 heads / 256 rows + 2^20, and attn_slots
-            sl = s > 1 ? n : 0;
+            k = S.nkv * blocks_of(L.n[b], grp) * s;      // all together at most 2^20 tokens * 1024 heads / 256 rows + 2^20, and attn_slots
+            sl = s > 1 ? k : 0;
         }
-        int sum = wave_scan_i(n), sum_sl = wave_scan_i(sl);
+        int sum = wave_scan_i(k), sum_sl = wave_scan_i(sl);
         if (lane == 63) { L.wave_i[0][wave] = sum; L.wave_i[1][wave] = sum_sl; }
         __syncthreads();
         for (int w = 0; w < wave; ++w) { sum += L.wave_i[0][w]; sum_sl += L.wave_i[1][w]; }
         if (b < io.n_seqs) { L.first[b + 1] = done + sum; L.slot[b + 1] = done_slots + sum_sl; }
         for (int w = 0; w < kCaWaves; ++w) { done += L.wave_i[0][w]; done_slots += L.wave_i[1][w]; }
-        __syncthreads();
+        if (b0 + kCaThreads < io.n_seqs) __syncthreads();
     }
     if (tid == 0) L.first[0] = L.slot[0] = 0;
     __syncthreads();
@@ -276,8 +273,8 @@ __device__ __forceinline__ void attend(f32x16 (&s)[KT], f32x16 (&o)[D / 32], flo
 // Values of V that are no numbers, in a tile that some rows see a part of: the probability 0 of what a row does not see would make a
 // NaN of them.  They are counted by kind, in a product over the keys each row sees (+inf as 1, -inf as 2^8, NaN as 2^16, at most 64 of
 // each: exact), which goes to the output as infinities and NaN; the tile then holds zeros in their place.  `mine` are the pieces of the tile this
-// thread looks after, at the LDS addresses at[]; for the whole workgroup.
-template <int D, int N>
+// thread looks after, at the LDS addresses at[]; the wavefront's rows see the KEYS keys from k0 on, at `base`.  For the whole workgroup.
+template <int D, int KEYS, int N>
 __device__ __forceinline__ void odd_values(const u32x4 (&mine)[N], const uint32_t (&at)[N], f32x16 (&o)[D / 32], const Fragments<D> &F, uint32_t base, int half, int k0, int limit, bool live)
 {
 #pragma unroll
@@ -293,7 +290,7 @@ __device__ __forceinline__ void odd_values(const u32x4 (&mine)[N], const uint32_
         for (int dt = 0; dt < D / 32; ++dt) {
             f32x16 n{};
 #pragma unroll 1
-            for (int ks = 0; ks < kCaKeys / 16; ++ks) {
+            for (int ks = 0; ks < KEYS / 16; ++ks) {
                 const u32x4 w = F.v_frag(base, ks, dt);
                 u32x4 seen;
 #pragma unroll
@@ -341,84 +338,187 @@ __device__ __forceinline__ void fetch_1k(const char *from, uint32_t to)
 }
 template <int N> __device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(%0)" : : "i"(N) : "memory"); }
 
-// Tile t of a piece has K in ring slot t % 3 and V in t % 4: while the rows of t + 2 are on their way, t + 1 has arrived or is about
-// to, t is being read, and so is, by half the wavefronts, V of t - 1.
-constexpr int kCaKSlots = 3, kCaVSlots = 4;
-constexpr int kCaIds = 2048;                // page ids in LDS, a window of a piece's at a time
+// LDS of a piece: rows of K and V, and the ids of its pages, a window of them at a time.
+constexpr int kCaIds = 1024;
 template <int D>
 struct Tiles {
-    uint16_t k[kCaKSlots][kCaKeys * D], v[kCaVSlots][kCaKeys * D];
+    uint16_t rows[512 * D];                 // 128 KB for heads of 128
     int ids[kCaIds];
 };
 
-template <int D>
-__device__ __forceinline__ void chunk_attention_piece(const ServingDev &S, const etc_serving_attention_io &io, ETC_AS_LDS CaLds &L, ETC_AS_LDS Tiles<D> &B, int b, int local)
+struct Piece {
+    int b, local, kvh, part, split, parts;  // part `part` of an item that has `parts` of them; of a sequence whose longest items have `split`
+    int tile0, tile1;                       // of the piece: [tile0, tile1)
+    int n_keys;                             // that the last row of the block sees
+    int grp, rows, r0;                      // query heads per KV head; rows of (sequence, KV head); first one of the block
+    Seq seq;
+};
+
+__device__ __forceinline__ Piece piece_of(const ServingDev &S, const etc_serving_attention_io &io, ETC_AS_LDS const CaLds &L, int b, int local)
 {
-    constexpr int CH = D / 8;                            // 16-byte pieces of a row
-    constexpr int KS = D / 16, DT = D / 32;              // steps of the first product, tiles of the output
-    constexpr int RPL = 64 / CH, LOADS = kCaKeys / RPL / kCaWaves;      // rows of a load; loads of K (and of V) a wavefront has in a tile
-    constexpr uint32_t BUF = kCaKeys * D * 2;            // bytes of a tile
-    int tid = (int)threadIdx.x;
-    asm volatile("" : "+v"(tid));                        // of this piece: what is computed from it does not stay in registers across pieces
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, half = lane >> 5, col = lane & 31;
-    const int split = __builtin_amdgcn_readfirstlane(L.split[b]), blocks = __builtin_amdgcn_readfirstlane(L.blocks[b]);
-    const int kvh = local % S.nkv, part = local / S.nkv % split, block = blocks - 1 - local / S.nkv / split;      // long blocks first
-    bool ok;
-    Seq it = sequence(S, io, b, &ok);
-    it = wave_uniform(it);
-    const int grp = S.nq / S.nkv, psh = S.page_shift, pmask = (1 << psh) - 1;
-    const int rows = it.n * grp, r0 = block * kCaRows;
+    Piece P;
+    P.b = b;
+    P.local = local;
+    P.seq = wave_uniform(Seq{L.q0[b], L.n[b], L.kv[b]});
+    P.split = __builtin_amdgcn_readfirstlane(L.split[b]);
+    P.kvh = local % S.nkv;
+    P.part = local / S.nkv % P.split;
+    P.grp = S.nq / S.nkv;
+    P.rows = P.seq.n * P.grp;
+    P.r0 = (blocks_of(P.seq.n, P.grp) - 1 - local / S.nkv / P.split) * kCaRows;      // long blocks first
+    P.n_keys = P.seq.kv + min(P.r0 + kCaRows - 1, P.rows - 1) / P.grp + 1;
+    const int tiles = (P.n_keys - 1) / kCaKeys + 1, each = tiles / P.split, more = tiles - each * P.split;      // the first `more` have one more
+    P.parts = min(P.split, tiles);          // a block shorter than its sequence's last one may have fewer
+    P.tile0 = P.part * each + min(P.part, more);
+    P.tile1 = P.tile0 + each + (P.part < more);
+    return P;
+}
 
-    const int t_last = min(r0 + kCaRows - 1, rows - 1) / grp, n_keys = it.kv + t_last + 1;      // keys of the block
-    const int all_tiles = (n_keys - 1) / kCaKeys + 1;
-    const int tile0 = (int)((int64_t)all_tiles * part / split), n_tiles = (int)((int64_t)all_tiles * (part + 1) / split);      // this piece: [tile0, n_tiles)
-    if (tile0 == n_tiles) return;                        // a block shorter than its sequence's last one may have fewer pieces
-    const int parts = min(split, all_tiles);
-
-    // page ids of the tiles [., ids_end), from page ids0 on
-    const int32_t *table = io.block_table + (int64_t)b * io.table_stride;
-    int ids0 = 0, ids_end = tile0;
-    auto load_ids = [&](int tile) {                      // between barriers
-        ids0 = tile * kCaKeys >> psh;
-        const int last_page = (min(n_tiles * kCaKeys, n_keys) - 1) >> psh, n = min(last_page - ids0 + 1, kCaIds);
-        ids_end = last_page - ids0 < kCaIds ? n_tiles : (int)((((int64_t)(ids0 + kCaIds)) << psh) / kCaKeys);      // whole tiles only
+// The ids of a piece's pages for the keys [key, ., .): a window, valid in front of key `end`.  Between barriers.
+template <int D>
+struct PageWindow {
+    const int32_t *table;
+    int first, end;                         // first page; first key that is not covered
+    __device__ __forceinline__ void load(const ServingDev &S, const etc_serving_attention_io &io, ETC_AS_LDS Tiles<D> &B, int b, int key, int key_end, int tid)
+    {
+        first = key >> S.page_shift;
+        const int last = (key_end - 1) >> S.page_shift, n = min(last - first + 1, kCaIds);
+        end = last - first < kCaIds ? key_end : (int)(((int64_t)(first + kCaIds)) << S.page_shift);
         for (int i = tid; i < n; i += kCaThreads) {
-            int id = gld_i32(table + ids0 + i);
+            int id = gld_i32(table + first + i);
             if ((uint32_t)id >= (uint64_t)io.n_pages) {
                 refuse(S.error, SRV_BAD_PAGE, SRV_ATTENTION, b, id);
                 id = 0;
             }
             B.ids[i] = id;
         }
-    };
-    load_ids(tile0);
+    }
+};
+
+// Fetches a tile's rows, KEYS of K to LDS at kb and of V at vb: load u of a wavefront brings RPL rows of each.  A lane's place in LDS is
+// given, so it is the piece of memory that belongs there which it chooses.  Rows behind the last key are that key's again (their
+// scores are masked).
+template <int D, int KEYS>
+__device__ __forceinline__ void fetch_rows(const ServingDev &S, const etc_serving_attention_io &io, ETC_AS_LDS const Tiles<D> &B, int first_page, int key0, int last_key,
+                                           int kvh, int wave, int lane, uint32_t kb, uint32_t vb)
+{
+    constexpr int CH = D / 8, RPL = 64 / CH, LOADS = KEYS / RPL / kCaWaves;
+    const uint32_t row_bytes = (uint32_t)(S.nkv * D * 2);
+    const uint64_t page_bytes = (uint64_t)row_bytes << S.page_shift;
+    const int lrow = lane / CH, c = lane % CH, pmask = (1 << S.page_shift) - 1;
+#pragma unroll
+    for (int u = 0; u < LOADS; ++u) {
+        const int r = (wave * LOADS + u) * RPL, key = min(key0 + r + lrow, last_key);
+        const uint32_t id = (uint32_t)B.ids[(key >> S.page_shift) - first_page];
+        const uint64_t off = id * page_bytes + (uint64_t)((uint32_t)(key & pmask)) * row_bytes + kvh * D * 2;
+        fetch_1k((const char *)io.k_pages + (off + (uint32_t)((c ^ k_swap<D>(r + lrow)) * 16)), kb + r * D * 2);
+        fetch_1k((const char *)io.v_pages + (off + (uint32_t)((c ^ v_swap<D>(r + lrow)) * 16)), vb + r * D * 2);
+    }
+}
+
+// Piece cc (of D / 8) of a lane's row: elements 8 cc + 4 half + 0 .. 3 of row r of the sequence and KV head.
+template <int D>
+__device__ __forceinline__ void put_out(const ServingDev &S, const etc_serving_attention_io &io, const Piece &P, int r, int cc, int half, f32x4 v)
+{
+    if (r >= P.rows) return;
+    const int t = r / P.grp;
+    uint16_t *op = (uint16_t *)io.out + ((int64_t)(P.seq.q0 + t) * S.nq + P.kvh * P.grp + (r - t * P.grp)) * D + cc * 8 + half * 4;
+    *as_global(reinterpret_cast<u32x2 *>(op)) = u32x2{to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3])};
+}
+
+// Where the 32 rows rw of a part leave their partial result (device scope: the reader may be on another die).
+template <int D>
+__device__ __forceinline__ float *partial(const ServingDev &S, int slot, int rw)
+{
+    return S.attn_part + (size_t)slot * kCaSlot<D> + (size_t)rw * (kCaPartO<D> + 64);
+}
+
+// Running join of partial results (reference, sum, 4 elements of the output).
+struct Join {
+    float m = -3e38f, l = 0.f;
+    f32x4 o{0.f, 0.f, 0.f, 0.f};
+    __device__ __forceinline__ void add(float mj, float lj, f32x4 oj)
+    {
+        const float nm = fmaxf(m, mj), a = exp2_fast(m - nm), b = exp2_fast(mj - nm);
+        m = nm;
+        l = l * a + lj * b;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = o[i] * a + oj[i] * b;
+    }
+    __device__ __forceinline__ f32x4 result() const
+    {
+        const float inv = 1.0f / l;
+        return f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+    }
+};
+
+// Behind a part's partial result: who arrives last at the item joins its parts, in the order of the keys.
+template <int D>
+__device__ __forceinline__ void join_parts(const ServingDev &S, const etc_serving_attention_io &io, ETC_AS_LDS CaLds &L, const Piece &P, int slot0, int tid, int wave, int lane)
+{
+    const int half = lane >> 5, col = lane & 31;
+    wg_release();
+    if (tid == 0) {
+        int32_t *ctr = S.attn_arrive + slot0;
+        const int last = __hip_atomic_fetch_add(as_global(ctr), 1, __ATOMIC_RELAXED, ETC_SCOPE) + 1 == P.parts;
+        if (last) st_i32(ctr, 0);
+        L.last = last;
+    }
+    __syncthreads();
+    if (!L.last) return;
+    const int live = min(kCaWaves, div_up(P.rows - P.r0, 32));
+    for (int cc = wave; cc < live * (D / 8); cc += kCaWaves) {      // a wavefront per (32 rows, piece of them)
+        const int rw = cc / (D / 8), pc = cc % (D / 8);
+        Join J;
+        for (int j0 = 0; j0 < P.parts; j0 += 4) {
+            f32x4 ov[4];
+            uint64_t ml[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const float *src = partial<D>(S, slot0 + min(j0 + u, P.parts - 1) * S.nkv, rw);
+                ov[u] = __builtin_bit_cast(f32x4, buf_ld_16B(buf_of(src), (uint32_t)((pc * 64 + lane) * 16), 0));
+                ml[u] = ld_u64(src + kCaPartO<D> + col * 2);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (j0 + u < P.parts) J.add(__uint_as_float((uint32_t)ml[u]), __uint_as_float((uint32_t)(ml[u] >> 32)), ov[u]);
+        }
+        put_out<D>(S, io, P, P.r0 + rw * 32 + col, pc, half, J.result());
+    }
+}
+
+// A block of more than 64 rows: 32 of them to a wavefront, all wavefronts over the same tiles of 64 keys.
+// Tile t has K in ring slot t % 3 and V in t % 4: while the rows of t + 2 are on their way, t + 1 has arrived or is about to, t is being
+// read, and so is, by half the wavefronts, V of t - 1.
+constexpr int kCaKSlots = 3, kCaVSlots = 4;
+
+template <int D>
+__device__ __forceinline__ void wide_piece(const ServingDev &S, const etc_serving_attention_io &io, ETC_AS_LDS CaLds &L, ETC_AS_LDS Tiles<D> &B, const Piece &P)
+{
+    constexpr int KS = D / 16, DT = D / 32;              // steps of the first product, tiles of the output
+    constexpr int RPL = 512 / D, LOADS = kCaKeys / RPL / kCaWaves;      // rows of a load; loads of K (and of V) a wavefront has in a tile
+    constexpr uint32_t BUF = kCaKeys * D * 2;            // bytes of a tile
+    static_assert((kCaKSlots + kCaVSlots) * kCaKeys <= 512, "LDS");
+    int tid = (int)threadIdx.x;
+    asm volatile("" : "+v"(tid));                        // of this piece: what is computed from it does not stay in registers across pieces
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, half = lane >> 5, col = lane & 31;
+    const int tile0 = P.tile0, n_tiles = P.tile1, key_end = min(n_tiles * kCaKeys, P.n_keys);
+    PageWindow<D> W{io.block_table + (int64_t)P.b * io.table_stride, 0, 0};
+    W.load(S, io, B, P.b, tile0 * kCaKeys, key_end, tid);
 
     // this lane's row: query fragments (right operand: 8 consecutive elements of step ks at ks * 16 + half * 8)
-    const int row = r0 + wave * 32 + col, rr = min(row, rows - 1), t = rr / grp, head = kvh * grp + (rr - t * grp);
-    const uint16_t *qp = (const uint16_t *)io.q + ((int64_t)(it.q0 + t) * S.nq + head) * D + half * 8;
+    const int row = P.r0 + wave * 32 + col, rr = min(row, P.rows - 1), t = rr / P.grp, head = P.kvh * P.grp + (rr - t * P.grp);
+    const uint16_t *qp = (const uint16_t *)io.q + ((int64_t)(P.seq.q0 + t) * S.nq + head) * D + half * 8;
     bf16x8 qf[KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qf[ks] = __builtin_bit_cast(bf16x8, gld_16B(qp + ks * 16));
-    const int limit = it.kv + t;                         // last key this row sees
-    const int first_masked = (it.kv + r0 / grp + 1) / kCaKeys;      // tiles in front of it are seen whole by all rows of the block
-    const int wave_last = it.kv + min((r0 + wave * 32 + 31) / grp, it.n - 1);
-    const bool wave_live = r0 + wave * 32 < rows;
-    const uint32_t k_base = (uint32_t)(uintptr_t)&B.k[0][0], v_base = (uint32_t)(uintptr_t)&B.v[0][0];
-
-    // Load u of this wavefront brings the rows row_of(u) + 0 .. RPL - 1 of a tile; the lane's place in LDS is given, so it is the piece of
-    // memory that belongs there which it chooses.  Rows behind the last key are that key's again (their scores are masked).
-    const uint32_t row_bytes = (uint32_t)(S.nkv * D * 2);
-    const uint64_t page_bytes = (uint64_t)row_bytes << psh;
-    const int lrow = lane / CH, c = lane % CH;
+    const int limit = P.seq.kv + t;                      // last key this row sees
+    const int first_masked = (P.seq.kv + P.r0 / P.grp + 1) / kCaKeys;      // tiles in front of it are seen whole by all rows of the block
+    const int wave_last = P.seq.kv + min((P.r0 + wave * 32 + 31) / P.grp, P.seq.n - 1);
+    const bool wave_live = P.r0 + wave * 32 < P.rows;
+    const uint32_t k_base = (uint32_t)(uintptr_t)&B.rows[0], v_base = k_base + kCaKSlots * BUF;
     auto fetch = [&](int tile, uint32_t kb, uint32_t vb) {
-#pragma unroll
-        for (int u = 0; u < LOADS; ++u) {
-            const int r = (wave * LOADS + u) * RPL, key = min(tile * kCaKeys + r + lrow, n_keys - 1);
-            const uint32_t id = (uint32_t)B.ids[(key >> psh) - ids0];
-            const uint64_t off = id * page_bytes + (uint64_t)((uint32_t)(key & pmask)) * row_bytes + kvh * D * 2;
-            fetch_1k((const char *)io.k_pages + (off + (uint32_t)((c ^ k_swap<D>(r + lrow)) * 16)), k_base + kb + r * D * 2);
-            fetch_1k((const char *)io.v_pages + (off + (uint32_t)((c ^ v_swap<D>(r + lrow)) * 16)), v_base + vb + r * D * 2);
-        }
+        fetch_rows<D, kCaKeys>(S, io, B, W.first, tile * kCaKeys, P.n_keys - 1, P.kvh, wave, lane, k_base + kb, v_base + vb);
     };
 
     f32x16 o[DT];
@@ -433,17 +533,18 @@ __device__ __forceinline__ void chunk_attention_piece(const ServingDev &S, const
     drain_vmem();                                        // nothing but tiles on their way from here on
     __syncthreads();
     uint32_t kb = 0, vb = 0, vb_before = 0;              // ring slots of the tile at hand; of V also of the one before
+    auto covered = [&](int tile) { return min((tile + 1) * kCaKeys, key_end) <= W.end; };
     auto after = [](uint32_t at, int slots) { return at == (slots - 1) * BUF ? 0u : at + BUF; };
     fetch(tile0, 0, 0);
-    if (tile0 + 1 < n_tiles && tile0 + 1 < ids_end) { fetch(tile0 + 1, BUF, BUF); arrived<2 * LOADS>(); }
+    if (tile0 + 1 < n_tiles && covered(tile0 + 1)) { fetch(tile0 + 1, BUF, BUF); arrived<2 * LOADS>(); }
     else arrived<0>();
     __syncthreads();
     // In front of a tile's work: the rows of the tile two behind it go on their way.  Behind it: the next tile's have arrived, for all.
     auto ahead = [&](int tile) {
         if (tile + 2 < n_tiles) {
-            if (tile + 2 >= ids_end) {                   // its page ids are not here: a new window, with all loads at rest
+            if (!covered(tile + 2)) {                    // its page ids are not here: a new window, with all loads at rest
                 __syncthreads();
-                load_ids(tile + 2);
+                W.load(S, io, B, P.b, (tile + 2) * kCaKeys, key_end, tid);
                 drain_vmem();
                 __syncthreads();
             }
@@ -495,7 +596,7 @@ __device__ __forceinline__ void chunk_attention_piece(const ServingDev &S, const
         if (odd) L.odd = tile;
         __syncthreads();
         const bool live = wave_live && tile * kCaKeys <= wave_last;
-        if (__builtin_expect(L.odd == tile, 0)) odd_values<D, LOADS>(mine, at, o, F, v_base + vb, half, tile * kCaKeys, limit, live);
+        if (__builtin_expect(L.odd == tile, 0)) odd_values<D, kCaKeys, LOADS>(mine, at, o, F, v_base + vb, half, tile * kCaKeys, limit, live);
         if (live) {
             scores<D, 2>(s, F, k_base + kb, qf);
             attend<D, 2, true>(s, o, m, l, F, v_base + vb, half, scale, tile * kCaKeys, limit);
@@ -503,29 +604,19 @@ __device__ __forceinline__ void chunk_attention_piece(const ServingDev &S, const
         next(tile);
     }
     l = partner_sum(l);
-    auto put = [&](int rw, int cc, f32x4 v) {            // piece cc of a lane's row (row rw of the block): elements 8 cc + 4 half + 0 .. 3
-        const int r = r0 + rw;
-        if (r >= rows) return;
-        const int tt = r / grp;
-        uint16_t *op = (uint16_t *)io.out + ((int64_t)(it.q0 + tt) * S.nq + kvh * grp + (r - tt * grp)) * D + cc * 8 + half * 4;
-        *as_global(reinterpret_cast<u32x2 *>(op)) = u32x2{to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3])};
-    };
-    if (parts == 1) {
+    if (P.parts == 1) {
         if (!wave_live) return;
         const float inv = 1.0f / l;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-                put(wave * 32 + col, dt * 4 + q, f32x4{o[dt][4 * q] * inv, o[dt][4 * q + 1] * inv, o[dt][4 * q + 2] * inv, o[dt][4 * q + 3] * inv});
+                put_out<D>(S, io, P, row, dt * 4 + q, half, f32x4{o[dt][4 * q] * inv, o[dt][4 * q + 1] * inv, o[dt][4 * q + 2] * inv, o[dt][4 * q + 3] * inv});
         return;
     }
-    // ---- a part of the keys: the partial result to memory (device scope: the reader may be on another die); who arrives last
-    // ---- at the item joins them, in the order of the keys
-    const int slot0 = __builtin_amdgcn_readfirstlane(L.slot[b]) + local - part * S.nkv;
+    const int slot0 = __builtin_amdgcn_readfirstlane(L.slot[P.b]) + P.local - P.part * S.nkv;
     if (wave_live) {
-        float *dst = S.attn_part + (size_t)(slot0 + part * S.nkv) * kCaSlot<D> + (size_t)wave * (kCaPartO<D> + 64);
-        const __amdgpu_buffer_rsrc_t d_b = buf_of(dst);
+        const __amdgpu_buffer_rsrc_t d_b = buf_of(partial<D>(S, slot0 + P.part * S.nkv, wave));
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -534,46 +625,131 @@ __device__ __forceinline__ void chunk_attention_piece(const ServingDev &S, const
                            __builtin_bit_cast(u32x4, f32x4{o[dt][4 * q], o[dt][4 * q + 1], o[dt][4 * q + 2], o[dt][4 * q + 3]}));
         if (half == 0) buf_st_8B(d_b, (uint32_t)(kCaPartO<D> * 4 + col * 8), u32x2{__float_as_uint(m), __float_as_uint(l)});
     }
-    wg_release();
-    if (tid == 0) {
-        int32_t *ctr = S.attn_arrive + slot0;
-        const int last = __hip_atomic_fetch_add(as_global(ctr), 1, __ATOMIC_RELAXED, ETC_SCOPE) + 1 == parts;
-        if (last) st_i32(ctr, 0);
-        L.last = last;
-    }
+    join_parts<D>(S, io, L, P, slot0, tid, wave, lane);
+}
+
+// A block of at most 64 rows is bound by the rows of the cache: all wavefronts work on the same keys' arrival, four to 128 keys (32 each)
+// for the first 32 rows and four for the rest, and the keys' results are joined in LDS.  Two buffers of 128 keys: one on its
+// way, or both, at any time.
+constexpr int kCaNarrowRows = 64, kCaNarrowKeys = 128;
+
+template <int D>
+__device__ __forceinline__ void narrow_piece(const ServingDev &S, const etc_serving_attention_io &io, ETC_AS_LDS CaLds &L, ETC_AS_LDS Tiles<D> &B, const Piece &P)
+{
+    constexpr int KS = D / 16, DT = D / 32, KEYS = kCaNarrowKeys;
+    constexpr int RPL = 512 / D, LOADS = KEYS / RPL / kCaWaves;
+    constexpr uint32_t BUF = KEYS * D * 2;               // bytes of a step's K, and of its V behind that
+    static_assert(4 * KEYS <= 512, "LDS");
+    int tid = (int)threadIdx.x;
+    asm volatile("" : "+v"(tid));
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, half = lane >> 5, col = lane & 31;
+    const int rw = wave >> 2, kg = wave & 3;             // rows 32 rw + 0 .. 31, keys 32 kg + 0 .. 31 of a step
+    const int key0 = P.tile0 * kCaKeys, key_end = min(P.tile1 * kCaKeys, P.n_keys), n_steps = div_up(key_end - key0, KEYS);
+    PageWindow<D> W{io.block_table + (int64_t)P.b * io.table_stride, 0, 0};
+    W.load(S, io, B, P.b, key0, key_end, tid);
+
+    const int row = rw * 32 + col, rr = min(row, P.rows - 1), t = rr / P.grp, head = P.kvh * P.grp + (rr - t * P.grp);
+    const uint16_t *qp = (const uint16_t *)io.q + ((int64_t)(P.seq.q0 + t) * S.nq + head) * D + half * 8;
+    bf16x8 qf[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = __builtin_bit_cast(bf16x8, gld_16B(qp + ks * 16));
+    const int limit = min(P.seq.kv + t, key_end - 1);    // last key this row sees in this piece
+    const int all_see = min(P.seq.kv + 1, key_end);      // keys in front of it are seen by all rows
+    const bool live = rw * 32 < P.rows;
+    const uint32_t base = (uint32_t)(uintptr_t)&B.rows[0];
+    auto fetch = [&](int step) {
+        const uint32_t at = base + (step & 1) * 2 * BUF;
+        fetch_rows<D, KEYS>(S, io, B, W.first, key0 + step * KEYS, key_end - 1, P.kvh, wave, lane, at, at + BUF);
+    };
+    auto covered = [&](int step) { return min(key0 + (step + 1) * KEYS, key_end) <= W.end; };
+
+    f32x16 o[DT];
+#pragma unroll
+    for (int i = 0; i < DT; ++i) o[i] = f32x16{};
+    float m = -3e38f, l = 0.f;
+    const float scale = 1.44269504088896f / sqrtf((float)D);
+    const Fragments<D> F(lane);
+    f32x16 s[1];
+    if (tid == 0) L.odd = -1;
+    drain_vmem();                                        // nothing but rows on their way from here on
     __syncthreads();
-    if (!L.last) return;
-    const int live = min(kCaWaves, div_up(rows - r0, 32));
-    // which parts exist: all of them, or (fewer tiles than pieces) one per tile, in the pieces part = ceil((t + 1) * split / tiles) - 1
-    for (int cc = wave; cc < live * DT * 4; cc += kCaWaves) {      // a wavefront per (32 rows, piece of them)
-        const int rw = cc / (DT * 4), pc = cc % (DT * 4);
-        float mm = -3e38f, ll = 0.f;
-        f32x4 acc{0.f, 0.f, 0.f, 0.f};
-        for (int j0 = 0; j0 < parts; j0 += 4) {
-            f32x4 ov[4];
-            u32x2 ml[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int j = min(j0 + u, parts - 1), pj = parts == split ? j : (int)(((int64_t)(j + 1) * split + all_tiles - 1) / all_tiles) - 1;
-                const float *src = S.attn_part + (size_t)(slot0 + pj * S.nkv) * kCaSlot<D> + (size_t)rw * (kCaPartO<D> + 64);
-                ov[u] = __builtin_bit_cast(f32x4, buf_ld_16B(buf_of(src), (uint32_t)((pc * 64 + lane) * 16), 0));
-                const uint64_t w = ld_u64(src + kCaPartO<D> + col * 2);
-                ml[u] = u32x2{(uint32_t)w, (uint32_t)(w >> 32)};
+    fetch(0);
+    if (n_steps > 1 && covered(1)) { fetch(1); arrived<2 * LOADS>(); }
+    else arrived<0>();
+    __syncthreads();
+    for (int step = 0; step < n_steps; ++step) {
+        const int k0 = key0 + step * KEYS;
+        const uint32_t kb = base + (step & 1) * 2 * BUF, kw = kb + kg * 32 * D * 2, vw = kw + BUF;
+        const bool mine_live = live && k0 + kg * 32 < key_end;
+        if (k0 + KEYS <= all_see) {
+            if (mine_live) {
+                scores<D, 1>(s, F, kw, qf);
+                attend<D, 1, false>(s, o, m, l, F, vw, half, scale, 0, 0);
             }
+        } else {
+            u32x4 mine[LOADS];
+            uint32_t at[LOADS];
+            bool odd = false;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                if (j0 + u >= parts) continue;
-                const float mj = __uint_as_float(ml[u].x), lj = __uint_as_float(ml[u].y);
-                const float nm = fmaxf(mm, mj), sa = exp2_fast(mm - nm), sb = exp2_fast(mj - nm);
-                mm = nm;
-                ll = ll * sa + lj * sb;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[i] = acc[i] * sa + ov[u][i] * sb;
+            for (int u = 0; u < LOADS; ++u) {
+                at[u] = kb + BUF + (wave * LOADS + u) * RPL * D * 2 + lane * 16;
+                mine[u] = *reinterpret_cast<ETC_AS_LDS const u32x4 *>(at[u]);
+                odd |= any_odd(mine[u]);
+            }
+            if (odd) L.odd = step;
+            __syncthreads();
+            if (__builtin_expect(L.odd == step, 0)) odd_values<D, 32, LOADS>(mine, at, o, F, vw, half, k0 + kg * 32, limit, mine_live);
+            if (mine_live) {
+                scores<D, 1>(s, F, kw, qf);
+                attend<D, 1, true>(s, o, m, l, F, vw, half, scale, k0 + kg * 32, limit);
             }
         }
-        const float inv = 1.0f / ll;
-        put(rw * 32 + col, pc, f32x4{acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv});
+        __syncthreads();                                 // the buffer is free
+        if (step + 2 < n_steps) {
+            if (!covered(step + 2)) {                    // a new window of page ids, with all loads at rest
+                arrived<0>();
+                __syncthreads();
+                W.load(S, io, B, P.b, k0 + 2 * KEYS, key_end, tid);
+                drain_vmem();
+                __syncthreads();
+            }
+            fetch(step + 2);
+            arrived<2 * LOADS>();
+        } else {
+            arrived<0>();
+        }
+        __syncthreads();                                 // the next step's rows are here, for all
     }
+
+    // ---- the four wavefronts of a row, in the order of the keys: output pieces of a lane as in a partial result, then m and l
+    l = partner_sum(l);
+    const uint32_t mine_at = base + wave * (kCaPartO<D> * 4), ml_at = (uint32_t)(uintptr_t)&B.ids[0];
+    static_assert(kCaWaves * kCaPartO<D> * 4 <= 512 * D * 2, "LDS");
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            *reinterpret_cast<ETC_AS_LDS f32x4 *>(mine_at + ((dt * 4 + q) * 64 + lane) * 16) = f32x4{o[dt][4 * q], o[dt][4 * q + 1], o[dt][4 * q + 2], o[dt][4 * q + 3]};
+    if (half == 0) *reinterpret_cast<ETC_AS_LDS f32x2_t *>(ml_at + (wave * 32 + col) * 8) = f32x2_t{m, l};
+    __syncthreads();
+    const int slot0 = __builtin_amdgcn_readfirstlane(L.slot[P.b]) + P.local - P.part * S.nkv;
+    for (int cc = wave; cc < div_up(P.rows, 32) * (D / 8); cc += kCaWaves) {
+        const int jr = cc / (D / 8), pc = cc % (D / 8);
+        Join J;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const f32x2_t ml = *reinterpret_cast<ETC_AS_LDS const f32x2_t *>(ml_at + ((jr * 4 + g) * 32 + col) * 8);
+            J.add(ml[0], ml[1], *reinterpret_cast<ETC_AS_LDS const f32x4 *>(base + (jr * 4 + g) * (kCaPartO<D> * 4) + (pc * 64 + lane) * 16));
+        }
+        if (P.parts == 1) {
+            put_out<D>(S, io, P, jr * 32 + col, pc, half, J.result());
+        } else {
+            const __amdgpu_buffer_rsrc_t d_b = buf_of(partial<D>(S, slot0 + P.part * S.nkv, jr));
+            buf_st_16B(d_b, (uint32_t)((pc * 64 + lane) * 16), __builtin_bit_cast(u32x4, J.o));
+            if (pc == 0 && half == 0) buf_st_8B(d_b, (uint32_t)(kCaPartO<D> * 4 + col * 8), u32x2{__float_as_uint(J.m), __float_as_uint(J.l)});
+        }
+    }
+    if (P.parts > 1) join_parts<D>(S, io, L, P, slot0, tid, wave, lane);
 }
 
 template <int D>
@@ -586,7 +762,11 @@ __global__ __launch_bounds__(kCaThreads) void chunk_attention_kernel(ServingDev 
     const int n_pieces = cut(S, io, L);
     for (int p = (int)blockIdx.x; p < n_pieces; p += (int)gridDim.x) {
         const int b = __builtin_amdgcn_readfirstlane(last_not_above(L.first, io.n_seqs, p));
-        chunk_attention_piece<D>(S, io, L, B, b, p - __builtin_amdgcn_readfirstlane(L.first[b]));
+        const Piece P = piece_of(S, io, L, b, p - __builtin_amdgcn_readfirstlane(L.first[b]));
+        if (P.tile0 < P.tile1) {
+            if (P.rows <= kCaNarrowRows) narrow_piece<D>(S, io, L, B, P);
+            else wide_piece<D>(S, io, L, B, P);
+        }
         __syncthreads();
     }
 }
