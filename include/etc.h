@@ -477,8 +477,8 @@ etc_status etc_serving_attention(etc_serving *s, const etc_serving_attention_io 
  * The token is the first of what is kept, in that order, at which the running sum of weights passes u times the kept sum.
  * A temperature that is not > 0 gives the first token of the order (greedy); settings out of range and NaN settings switch
  * their filter off (top_p <= 0: one token).  NaN and -inf logits are banned, and next to +inf all finite ones; a row with
- * nothing left gives token -1, kept 0, log-probability -inf.  Weights are summed in 64-bit fixed point (unit 2^-43 of the
- * largest), so a result does not depend on the order of the sums; a weight below half a unit counts as 0. */
+ * nothing left gives token -1, kept 0, log-probability -inf.  Weights are whole numbers of 2^-35 of the largest (a
+ * weight below half of that counts as 0) and their sums exact, so a result does not depend on an order of additions. */
 typedef struct {
     int32_t n_rows, dtype;          /* etc_dtype of logits */
     const void *logits;             /* [n_rows][vocab], rows row_stride elements apart; any alignment of the type */

@@ -13,6 +13,9 @@ using namespace etc;
 #ifdef ETC_GENERIC_ONLY      // a library generated for one graph has no kernels of these; no handle is ever made there
 namespace etc {
 int64_t attention_slot_bytes(int) { return 0; }
+int64_t sample_slices(int, int) { return 0; }
+int64_t sample_stat_bytes() { return 0; }
+int64_t sample_bins_bytes() { return 0; }
 hipError_t launch_serving_tables(const ServingDev &, const etc_serving_tables_io &, hipStream_t) { return hipErrorInvalidDeviceFunction; }
 hipError_t launch_serving_append(const ServingDev &, const etc_serving_append_io &, hipStream_t) { return hipErrorInvalidDeviceFunction; }
 hipError_t launch_serving_attention(const ServingDev &, const etc_serving_attention_io &, hipStream_t) { return hipErrorInvalidDeviceFunction; }
@@ -156,6 +159,13 @@ etc_status etc_serving_create(const etc_model_desc *m, const etc_serving_limits 
         D.attn_slots = kAttnMaxSlots;
         SRV_TRY(s, owned_alloc(s, &D.attn_arrive, (size_t)kAttnMaxSlots));
         SRV_TRY(s, owned_alloc(s, (char **)&D.attn_part, (size_t)kAttnMaxSlots * attention_slot_bytes(m->head_dim), false));
+        if (m->vocab > 0) {
+            const size_t n = (size_t)sample_slices(m->vocab, l->max_seqs);
+            if (n > 0) {
+                SRV_TRY(s, owned_alloc(s, (char **)&D.smp_stats, n * (size_t)sample_stat_bytes(), false));
+                SRV_TRY(s, owned_alloc(s, (char **)&D.smp_bins, n * (size_t)sample_bins_bytes(), false));
+            }
+        }
         double inv[64], *d_inv = nullptr;
         for (int i = 0; i < m->head_dim / 2; ++i) inv[i] = pow((double)m->rope_theta, -2.0 * i / m->head_dim);
         SRV_TRY(s, owned_alloc(s, &d_inv, m->head_dim / 2));

@@ -29,9 +29,15 @@ struct ServingDev {
     float *attn_part;
     int32_t *attn_arrive;
     int attn_slots;
+    // sampling of long rows: statistics and bins of the slices
+    void *smp_stats;
+    uint64_t *smp_bins;
 };
 constexpr int kAttnMaxSlots = 1024;
 int64_t attention_slot_bytes(int head_dim);
+int64_t sample_slices(int vocab, int max_rows);
+int64_t sample_stat_bytes();
+int64_t sample_bins_bytes();
 
 hipError_t launch_serving_tables(const ServingDev &S, const etc_serving_tables_io &io, hipStream_t s);
 hipError_t launch_serving_append(const ServingDev &S, const etc_serving_append_io &io, hipStream_t s);

@@ -242,13 +242,25 @@ hipError_t launch_serving_append(const ServingDev &S, const etc_serving_append_i
 }
 
 // ---- sampling ----------------------------------------------------------------------------------------------------------
-// Everything the filters and the draw ask for is a beginning of the tokens in the order (larger logit, lower id), named by
-// the key of its last logit and how many of that key's tokens belong to it.  It is found by descending through the 32 bits
-// of the (order-preserving) key, 11 + 11 + 10 of them at a time, over counts or over sums of weights.  Weights are computed in
-// double and summed as 64-bit integers: sums are exact, so no result depends on an order of additions, and equal keys have
-// equal weights, so ties are settled by a division.  One workgroup per row.
-constexpr int kSmpThreads = 1024;
-constexpr int kSmpBins = 2048;
+// Everything the filters and the draw ask for is a beginning of the tokens in the order (larger logit, lower id): the first k, the
+// first that weigh so much.  A row is sorted into kSmpBins bins by its logits' distance from the largest, with the tokens and the
+// weight of each bin; running sums over the bins say in which bin a beginning ends.  The tokens of the few bins in question go
+// to a list in LDS, where the same is done once more within a bin, and the handful left is compared one by one.
+// Weights are whole numbers of 2^-35 of the largest and summed as such: sums are exact, so no result depends on an order of additions.
+// Long rows: sample_scan (largest and smallest logit) and sample_bins over slices of the rows, as many as fill the chip, then
+// sample_row; short ones: sample_row does it all.  Rows with more tokens in the bins in question than the list holds (flat or with
+// many ties, in the wrong place) and rows with +inf take slow_row, which descends through the bits of the logits' keys instead.
+constexpr int kSmpThreads = 1024;           // of sample_row
+constexpr int kSliceThreads = 512;
+constexpr int kSmpBins = 1024;              // a bin: 1 / 1024 of min(32 temperatures, the row's range); a weight below 2^-36 is 0
+constexpr int kSmpList = 8192;              // tokens
+constexpr int kSmpFew = 1024;               // compared one by one
+constexpr int kUnitBits = 35;
+constexpr uint64_t kTopWeight = 1ull << kUnitBits;
+constexpr int kBinTokens = 1 << 14;         // tokens whose count and weight fit the 64 bits of a bin: 15 and 49
+constexpr int kCountShift = 49;
+constexpr int kSmpWgs = 512;                // workgroups over slices
+constexpr int kSmpWhole = kBinTokens;       // longest row that sample_row does alone
 
 template <bool F32>
 __device__ __forceinline__ float logit_at(const void *row, int i)
@@ -257,6 +269,36 @@ __device__ __forceinline__ float logit_at(const void *row, int i)
     x = x != x ? -INFINITY : x;                              // NaN: banned
     return x + 0.f;                                          // -0 is +0: equal logits
 }
+// f(logit, id) for the tokens [i0, i1) of a row, by the workgroup: 16 bytes a load and four loads in flight (one after the other
+// a row of 128256 took 73 us instead of 14), single tokens in front of and behind what is aligned.
+template <bool F32, int THREADS, class Fn>
+__device__ __forceinline__ void for_tokens(const void *row, int i0, int i1, Fn f)
+{
+    constexpr int SIZE = F32 ? 4 : 2, E = 16 / SIZE, U = 4;
+    const int tid = (int)threadIdx.x;
+    const char *from = (const char *)row + (int64_t)i0 * SIZE;
+    const int a0 = min(i1, i0 + (int)((16 - ((uintptr_t)from & 15)) & 15) / SIZE), nv = (i1 - a0) / E, t0 = a0 + nv * E;
+    if (i0 + tid < a0) f(logit_at<F32>(row, i0 + tid), i0 + tid);
+    if (t0 + tid < i1) f(logit_at<F32>(row, t0 + tid), t0 + tid);
+    const char *body = (const char *)row + (int64_t)a0 * SIZE;
+    for (int v0 = tid; v0 < nv; v0 += THREADS * U) {
+        u32x4 w[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) w[u] = gld_16B(body + (int64_t)min(v0 + u * THREADS, nv - 1) * 16);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (v0 + u * THREADS >= nv) break;
+            const int i = a0 + (v0 + u * THREADS) * E;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                float x = F32 ? __uint_as_float(w[u][e]) : (e & 1) ? bf16_hi(w[u][e >> 1]) : bf16_lo(w[u][e >> 1]);
+                x = x != x ? -INFINITY : x;
+                f(x + 0.f, i + e);
+            }
+        }
+    }
+}
+
 __device__ __forceinline__ uint32_t order_key(float x)
 {
     const uint32_t u = __float_as_uint(x);
@@ -265,28 +307,167 @@ __device__ __forceinline__ uint32_t order_key(float x)
 __device__ __forceinline__ float key_logit(uint32_t k) { return __uint_as_float(k ^ ((k >> 31) ? 0x80000000u : 0xFFFFFFFFu)); }
 constexpr uint32_t kBannedKey = 0x007FFFFFu;                 // of -inf
 
-struct RowScale { float top; double inv_t; };
-__device__ __forceinline__ uint64_t weight_of(const RowScale &R, float x)      // exp((x - top) / T), unit 2^-43
+// A token in the order: larger is earlier.
+__device__ __forceinline__ uint64_t entry_of(float x, int id) { return ((uint64_t)order_key(x) << 32) | (uint32_t)~(uint32_t)id; }
+__device__ __forceinline__ float entry_logit(uint64_t e) { return key_logit((uint32_t)(e >> 32)); }
+
+struct RowScale {
+    float top;               // largest logit
+    double inv_t;
+    double per;              // 2^20 / width of the bins together
+    double steps;            // 1024 log2(e) / T: a weight is 2^(-distance * steps / 1024)
+};
+
+// 2^(35 - j / 1024): a weight is one of these, times a polynomial in the rest of its exponent (below 2^-10: three terms in fp32
+// leave 2^-34 of it), times a power of two.  Eleven operations in 64 bits; exp() took three times as long.
+__device__ __forceinline__ void fill_powers(double *table)
 {
-    if (x == R.top) return 1ull << 43;
-    if (R.top == INFINITY) return 0;
-    const double w = exp(((double)x - (double)R.top) * R.inv_t);
-    return (uint64_t)rint(w * 8796093022208.0);
+    for (int j = (int)threadIdx.x; j < 1024; j += (int)blockDim.x) table[j] = exp2((double)kUnitBits - (double)j * 0x1p-10);
+}
+__device__ __forceinline__ uint64_t weight_of(const RowScale &R, const double *table, float x)      // exp((x - top) / T) in units
+{
+    if (x == R.top) return kTopWeight;                       // +inf among them
+    const double t = ((double)R.top - (double)x) * R.steps;
+    if (!(t < 37.0 * 1024.0)) return 0;                      // below half a unit; next to +inf (all but which are banned)
+    const double fl = floor(t);
+    const int n = (int)fl;
+    const float r = (float)(t - fl) * (float)(0.69314718055994531 / 1024.0);
+    const float s = -r + r * r * (0.5f - r * 0.16666667f);
+    const double base = table[n & 1023];
+    const double w = __builtin_ldexp(__builtin_fma(base, (double)s, base), -(n >> 10));
+    return (uint64_t)__double_as_longlong(w + 0x1p52) & ((1ull << 52) - 1);      // rounded to a whole number
+}
+__device__ __forceinline__ uint32_t place_of(const RowScale &R, float x)      // bin << 10 | place within it; does not decrease with the distance from the top
+{
+    const double d = ((double)R.top - (double)x) * R.per;
+    return d < 1048575.0 ? (uint32_t)d : 1048575u;
 }
 
+struct RowStats { float top, low; uint32_t first, live; };      // largest logit and its first token; smallest; tokens that are not banned
+
+template <class T> __device__ __forceinline__ T wave_all_sum(T v)
+{
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    return v;
+}
+template <class T> __device__ __forceinline__ T wave_all_max(T v)
+{
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) { const T t = __shfl_xor(v, o, 64); v = t > v ? t : v; }
+    return v;
+}
+
+__device__ __forceinline__ void join(RowStats &st, const RowStats &t)
+{
+    if (t.top > st.top || (t.top == st.top && t.first < st.first)) { st.top = t.top; st.first = t.first; }
+    st.low = fminf(st.low, t.low);
+    st.live += t.live;
+}
+__device__ __forceinline__ RowStats wave_join(RowStats st)
+{
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1)
+        join(st, RowStats{__shfl_xor(st.top, o, 64), __shfl_xor(st.low, o, 64), (uint32_t)__shfl_xor((int)st.first, o, 64), (uint32_t)__shfl_xor((int)st.live, o, 64)});
+    return st;
+}
+
+// One pass over the tokens [i0, i1) of a row by the workgroup; the same in every thread.
+template <bool F32, int THREADS>
+__device__ __forceinline__ RowStats row_stats(const void *row, int i0, int i1, RowStats *s_red)
+{
+    RowStats st{-INFINITY, INFINITY, 0xFFFFFFFFu, 0};
+    for_tokens<F32, THREADS>(row, i0, i1, [&](float x, int i) {
+        if (x > st.top || (x == st.top && (uint32_t)i < st.first)) { st.top = x; st.first = (uint32_t)i; }
+        const bool banned = x == -INFINITY;
+        st.low = fminf(st.low, banned ? INFINITY : x);
+        st.live += !banned;
+    });
+    st = wave_join(st);
+    if (lane_id() == 0) s_red[wave_id()] = st;
+    __syncthreads();
+    st = s_red[0];
+    for (int w = 1; w < THREADS / 64; ++w) join(st, s_red[w]);
+    __syncthreads();
+    return st;
+}
+
+__device__ __forceinline__ RowScale scale_of(const RowStats &st, float T)
+{
+    RowScale R{st.top, 1.0 / (double)T, 0.0, 1024.0 * 1.4426950408889634 / (double)T};
+    const double range = fmin((double)st.top - (double)st.low, 32.0 * (double)T);
+    R.per = range > 0.0 ? fmin(1048576.0 / range, 1e300) : 0.0;
+    return R;
+}
+
+// A slice's bins, or a row's: weight, and tokens in the upper bits.
+template <bool F32, int THREADS>
+__device__ __forceinline__ void fill_bins(const void *row, int i0, int i1, const RowScale &R, const double *table, unsigned long long *bins)
+{
+    for_tokens<F32, THREADS>(row, i0, i1, [&](float x, int) {
+        if (x != -INFINITY) atomicAdd(&bins[place_of(R, x) >> 10], (unsigned long long)(weight_of(R, table, x) | 1ull << kCountShift));
+    });
+}
+
+struct SampleArgs {
+    ServingDev S;
+    etc_serving_sample_io io;
+    int slices, per_slice;   // of a row; tokens of one
+};
+template <bool F32> __device__ __forceinline__ const void *row_of(const SampleArgs &a, int r)
+{
+    return (const char *)a.io.logits + (int64_t)r * a.io.row_stride * (F32 ? 4 : 2);
+}
+
+template <bool F32>
+__global__ __launch_bounds__(kSliceThreads) void sample_scan_kernel(SampleArgs a)
+{
+    __shared__ RowStats s_red[kSliceThreads / 64];
+    const int r = (int)blockIdx.y, sl = (int)blockIdx.x, i0 = sl * a.per_slice, i1 = min(a.S.vocab, i0 + a.per_slice);
+    const RowStats st = row_stats<F32, kSliceThreads>(row_of<F32>(a, r), i0, i1, s_red);
+    if (threadIdx.x == 0) ((RowStats *)a.S.smp_stats)[(size_t)r * a.slices + sl] = st;
+}
+
+// The row's statistics from its slices', in every thread.
+__device__ __forceinline__ RowStats join_stats(const SampleArgs &a, int r)
+{
+    RowStats st{-INFINITY, INFINITY, 0xFFFFFFFFu, 0};
+    const RowStats *p = (const RowStats *)a.S.smp_stats + (size_t)r * a.slices;
+    for (int i = lane_id(); i < a.slices; i += 64) join(st, p[i]);
+    return wave_join(st);
+}
+
+template <bool F32>
+__global__ __launch_bounds__(kSliceThreads) void sample_bins_kernel(SampleArgs a)
+{
+    __shared__ unsigned long long s_bins[kSmpBins];
+    __shared__ double s_powers[1024];
+    const int r = (int)blockIdx.y, sl = (int)blockIdx.x, i0 = sl * a.per_slice, i1 = min(a.S.vocab, i0 + a.per_slice);
+    const float T = a.io.temperature ? *as_global(a.io.temperature + r) : 1.f;
+    const RowStats st = join_stats(a, r);
+    if (!(T > 0.f) || st.live == 0 || st.top == INFINITY) return;      // sample_row needs no bins
+    for (int i = (int)threadIdx.x; i < kSmpBins; i += kSliceThreads) s_bins[i] = 0;
+    fill_powers(s_powers);
+    __syncthreads();
+    fill_bins<F32, kSliceThreads>(row_of<F32>(a, r), i0, i1, scale_of(st, T), s_powers, s_bins);
+    __syncthreads();
+    uint64_t *bins = a.S.smp_bins + ((size_t)r * a.slices + sl) * kSmpBins;
+    for (int i = (int)threadIdx.x; i < kSmpBins; i += kSliceThreads) bins[i] = s_bins[i];
+}
+
+// ---- the slow way ------------------------------------------------------------------------------------------------------
 struct Prefix {              // a beginning of the order
     uint32_t key;            // of its last token
     uint32_t ties;           // how many tokens of that key belong to it
     uint32_t before;         // tokens of larger keys
     uint64_t mass;           // weight of all of it
-    uint64_t mass_before;    // weight of the tokens of larger keys
 };
 
 // Sum over the workgroup, the same in every thread.
 template <class T>
 __device__ T wg_sum(T v, T *s_red)
 {
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    v = wave_all_sum(v);
     __syncthreads();
     if (lane_id() == 0) s_red[wave_id()] = v;
     __syncthreads();
@@ -295,19 +476,22 @@ __device__ T wg_sum(T v, T *s_red)
     return t;
 }
 
-struct SampleLds {
-    uint32_t count[kSmpBins];
-    uint64_t mass[kSmpBins];
+constexpr int kSlowBins = 2048;
+struct SlowLds {
+    uint32_t count[kSlowBins];
+    uint64_t mass[kSlowBins];
     uint64_t red[kSmpThreads / 64];
     uint32_t red_i[kSmpThreads / 64];
     uint32_t bin;
     uint32_t before;
     uint64_t mass_before;
+    uint32_t id;
 };
 
-// The shortest beginning of the order that holds `want_count` tokens, or (want_count == 0) weighs `want_mass` at least; the row has it.
+// The shortest beginning of the order that holds `want_count` tokens, or (want_count == 0) weighs `want_mass` at least; the row has
+// it.  11 + 11 + 10 bits of the key at a time; equal keys have equal weights, so ties are settled by a division.
 template <bool F32>
-__device__ Prefix find_prefix(SampleLds &L, const void *row, int vocab, const RowScale &R, uint32_t want_count, uint64_t want_mass)
+__device__ Prefix find_prefix(SlowLds &L, const void *row, int vocab, const RowScale &R, const double *table, uint32_t want_count, uint64_t want_mass)
 {
     const int tid = (int)threadIdx.x;
     uint32_t prefix = 0, before = 0;
@@ -318,7 +502,7 @@ __device__ Prefix find_prefix(SampleLds &L, const void *row, int vocab, const Ro
         const int high = shift;                              // bits above are fixed
         shift -= bits[level];
         const uint32_t bins = 1u << bits[level];
-        for (int i = tid; i < kSmpBins; i += kSmpThreads) { L.count[i] = 0; L.mass[i] = 0; }
+        for (int i = tid; i < kSlowBins; i += kSmpThreads) { L.count[i] = 0; L.mass[i] = 0; }
         __syncthreads();
         for (int i = tid; i < vocab; i += kSmpThreads) {
             const float x = logit_at<F32>(row, i);
@@ -326,12 +510,12 @@ __device__ Prefix find_prefix(SampleLds &L, const void *row, int vocab, const Ro
             if (k == kBannedKey || (level > 0 && (k >> high) != (prefix >> high))) continue;
             const uint32_t b = (k >> shift) & (bins - 1);
             atomicAdd(&L.count[b], 1u);
-            const uint64_t w = weight_of(R, x);
+            const uint64_t w = weight_of(R, table, x);
             if (w) atomicAdd((unsigned long long *)&L.mass[b], (unsigned long long)w);
         }
         __syncthreads();
         // two bins a thread, from the largest key down: prefix sums across the workgroup
-        const int hi = kSmpBins - 1 - 2 * tid, lo = hi - 1;
+        const int hi = kSlowBins - 1 - 2 * tid, lo = hi - 1;
         const uint32_t c0 = L.count[hi], c1 = L.count[lo];
         const uint64_t m0 = L.mass[hi], m1 = L.mass[lo];
         uint32_t c = c0 + c1;
@@ -344,9 +528,8 @@ __device__ Prefix find_prefix(SampleLds &L, const void *row, int vocab, const Ro
         if (lane_id() == 63) { L.red_i[wave_id()] = c; L.red[wave_id()] = m; }
         __syncthreads();
         for (int w = 0; w < wave_id(); ++w) { c += L.red_i[w]; m += L.red[w]; }
-        // exclusive sums in front of this thread's bins
-        uint32_t cb = before + c - (c0 + c1);
-        uint64_t mb = mass_before + m - (m0 + m1);
+        const uint32_t cb = before + c - (c0 + c1);          // in front of this thread's bins
+        const uint64_t mb = mass_before + m - (m0 + m1);
         auto holds = [&](uint32_t cc, uint64_t mm) { return want_count ? cc >= want_count : mm >= want_mass; };
         if (!holds(cb, mb)) {                                // one thread and one bin: the sums do not decrease
             if (holds(cb + c0, mb + m0)) { L.bin = hi; L.before = cb; L.mass_before = mb; }
@@ -361,127 +544,392 @@ __device__ Prefix find_prefix(SampleLds &L, const void *row, int vocab, const Ro
     Prefix p;
     p.key = prefix;
     p.before = before;
-    p.mass_before = mass_before;
-    const uint64_t w = weight_of(R, key_logit(prefix));
+    const uint64_t w = weight_of(R, table, key_logit(prefix));
     p.ties = want_count ? want_count - before : (uint32_t)((want_mass - mass_before + w - 1) / w);
     p.mass = mass_before + p.ties * w;
     return p;
 }
 
-template <bool F32>
-__global__ __launch_bounds__(kSmpThreads) void serving_sample_kernel(ServingDev S, etc_serving_sample_io io)
-{
-    __shared__ SampleLds L;
-    __shared__ uint32_t s_id;
-    const int tid = (int)threadIdx.x, r = (int)blockIdx.x, vocab = S.vocab;
-    const void *row = (const char *)io.logits + (int64_t)r * io.row_stride * (F32 ? 4 : 2);
-    const float T = io.temperature ? *as_global(io.temperature + r) : 1.f;
-    const int top_k = io.top_k ? gld_i32(io.top_k + r) : 0;
-    const float top_p = io.top_p ? *as_global(io.top_p + r) : 1.f, min_p = io.min_p ? *as_global(io.min_p + r) : 0.f;
+struct Drawn { uint32_t id, kept; float logprob; };
+struct Settings { float T, top_p, min_p, u; int top_k; };
 
-    // the largest logit, and the tokens that are not banned
-    uint32_t best = 0, live = 0;
-    for (int i = tid; i < vocab; i += kSmpThreads) {
-        const uint32_t k = order_key(logit_at<F32>(row, i));
-        best = max(best, k);
-        live += k != kBannedKey;
+__device__ __forceinline__ uint64_t mass_wanted(float p, uint64_t mass)      // by a top_p below 1; sums are whole numbers
+{
+    const uint64_t want = (uint64_t)ceil(fmax((double)p, 0.0) * (double)mass);
+    return want < 1 ? 1 : want > mass ? mass : want;
+}
+__device__ __forceinline__ uint64_t draw_wanted(float u, uint64_t mass)      // the first running sum above u * mass
+{
+    u = u > 0.f ? fminf(u, 1.f) : 0.f;
+    const uint64_t want = (uint64_t)((double)u * (double)mass) + 1;
+    return want > mass ? mass : want;
+}
+__device__ __forceinline__ bool above_min_p(const RowScale &R, float x, float min_p)
+{
+    return x == R.top || (R.top != INFINITY && exp(((double)x - (double)R.top) * R.inv_t) >= (double)min_p);
+}
+__device__ __forceinline__ float log_share(const RowScale &R, float x, uint64_t mass)      // from the logit, not from its weight in fixed point
+{
+    return (float)((x == R.top ? 0.0 : ((double)x - (double)R.top) * R.inv_t) - log((double)mass * 0x1p-35));
+}
+
+template <bool F32>
+__device__ Drawn slow_row(SlowLds &L, const void *row, int vocab, const RowScale &R, const double *table, uint32_t live, const Settings &q)
+{
+    const int tid = (int)threadIdx.x;
+    uint32_t n_live = live;
+    if (R.top == INFINITY) {                                 // next to +inf the finite ones are banned
+        uint32_t inf = 0;
+        for (int i = tid; i < vocab; i += kSmpThreads) inf += logit_at<F32>(row, i) == INFINITY;
+        n_live = wg_sum<uint32_t>(inf, L.red_i);
     }
-    for (int o = 32; o > 0; o >>= 1) best = max(best, (uint32_t)__shfl_xor((int)best, o, 64));
-    if (lane_id() == 0) L.red_i[wave_id()] = best;
-    __syncthreads();
-    for (int w = 0; w < kSmpThreads / 64; ++w) best = max(best, L.red_i[w]);
-    live = wg_sum<uint32_t>(live, L.red_i);
-    RowScale R{key_logit(best), 0.0};
-    if (live == 0) {
-        if (tid == 0) {
-            *as_global(io.token_out + r) = -1;
-            if (io.logprob_out) gst_f32(io.logprob_out + r, -INFINITY);
-            if (io.kept_out) *as_global(io.kept_out + r) = 0;
-        }
-        return;
+    uint32_t kept = q.top_k > 0 ? min((uint32_t)q.top_k, n_live) : n_live;
+    uint64_t mass = find_prefix<F32>(L, row, vocab, R, table, kept, 0).mass;
+    if (q.top_p < 1.f) {
+        const Prefix p = find_prefix<F32>(L, row, vocab, R, table, 0, mass_wanted(q.top_p, mass));
+        kept = p.before + p.ties;
+        mass = p.mass;
     }
-    Prefix drawn{best, 1, 0, 1, 0};
-    uint32_t kept = 1;
-    float logprob = 0.f;
-    if (T > 0.f) {
-        R.inv_t = 1.0 / (double)T;
-        uint32_t n_live = live;
-        if (R.top == INFINITY) {                             // next to +inf the finite ones are banned
-            uint32_t inf = 0;
-            for (int i = tid; i < vocab; i += kSmpThreads) inf += logit_at<F32>(row, i) == INFINITY;
-            n_live = wg_sum<uint32_t>(inf, L.red_i);
+    if (q.min_p > 0.f) {
+        uint32_t above = 0;
+        uint64_t m = 0;
+        for (int i = tid; i < vocab; i += kSmpThreads) {
+            const float x = logit_at<F32>(row, i);
+            if (x != -INFINITY && above_min_p(R, x, q.min_p)) { above++; m += weight_of(R, table, x); }
         }
-        kept = top_k > 0 ? min((uint32_t)top_k, n_live) : n_live;
-        uint64_t mass;
-        if (kept < live) {
-            mass = find_prefix<F32>(L, row, vocab, R, kept, 0).mass;
-        } else {
-            uint64_t m = 0;
-            for (int i = tid; i < vocab; i += kSmpThreads) {
-                const float x = logit_at<F32>(row, i);
-                if (x != -INFINITY) m += weight_of(R, x);
-            }
-            mass = wg_sum<uint64_t>(m, L.red);
-        }
-        if (top_p < 1.f) {
-            const double target = fmax((double)top_p, 0.0) * (double)mass;
-            uint64_t want = (uint64_t)ceil(target);          // the sums are whole numbers
-            want = want < 1 ? 1 : want > mass ? mass : want;
-            const Prefix p = find_prefix<F32>(L, row, vocab, R, 0, want);
-            kept = p.before + p.ties;
-            mass = p.mass;
-        }
-        if (min_p > 0.f) {
-            uint32_t above = 0;
-            uint64_t m = 0;
-            for (int i = tid; i < vocab; i += kSmpThreads) {
-                const float x = logit_at<F32>(row, i);
-                if (x == -INFINITY) continue;
-                if (x == R.top || exp(((double)x - (double)R.top) * R.inv_t) >= (double)min_p) { above++; m += weight_of(R, x); }
-            }
-            above = wg_sum<uint32_t>(above, L.red_i);
-            m = wg_sum<uint64_t>(m, L.red);
-            if (min_p > 1.f) { above = 1; m = 1ull << 43; }
-            if (above < kept) { kept = above; mass = m; }
-        }
-        float u = *as_global(io.u + r);
-        u = u > 0.f ? fminf(u, 1.f) : 0.f;
-        uint64_t want = (uint64_t)((double)u * (double)mass) + 1;      // first running sum above u * mass
-        want = want > mass ? mass : want;
-        drawn = find_prefix<F32>(L, row, vocab, R, 0, want);
-        const float x = key_logit(drawn.key);                // from the logit, not from its weight in fixed point
-        logprob = (float)((x == R.top ? 0.0 : ((double)x - (double)R.top) * R.inv_t) - log((double)mass * 0x1p-43));
+        above = wg_sum<uint32_t>(above, L.red_i);
+        m = wg_sum<uint64_t>(m, L.red);
+        if (q.min_p > 1.f) { above = 1; m = kTopWeight; }
+        if (above < kept) { kept = above; mass = m; }
     }
+    const Prefix d = find_prefix<F32>(L, row, vocab, R, table, 0, draw_wanted(q.u, mass));
     // the ties-th token of the key, by id: a count in front of each thread's stretch of ids
-    __syncthreads();
     const int per = (vocab + kSmpThreads - 1) / kSmpThreads, i0 = min(vocab, tid * per), i1 = min(vocab, i0 + per);
     uint32_t n = 0;
-    for (int i = i0; i < i1; ++i) n += order_key(logit_at<F32>(row, i)) == drawn.key;
+    for (int i = i0; i < i1; ++i) n += order_key(logit_at<F32>(row, i)) == d.key;
     uint32_t upto = (uint32_t)wave_scan_i((int)n);
     if (lane_id() == 63) L.red_i[wave_id()] = upto;
     __syncthreads();
     for (int w = 0; w < wave_id(); ++w) upto += L.red_i[w];
-    uint32_t left = drawn.ties - (upto - n);                 // which of this stretch's, from 1
-    if (upto - n < drawn.ties && drawn.ties <= upto) {
+    uint32_t left = d.ties - (upto - n);                     // which of this stretch's, from 1
+    if (upto - n < d.ties && d.ties <= upto) {
         int i = i0;
         for (; i < i1; ++i)
-            if (order_key(logit_at<F32>(row, i)) == drawn.key && --left == 0) break;
-        s_id = (uint32_t)i;
+            if (order_key(logit_at<F32>(row, i)) == d.key && --left == 0) break;
+        L.id = (uint32_t)i;
     }
     __syncthreads();
-    if (tid == 0) {
-        *as_global(io.token_out + r) = (int32_t)s_id;
+    return Drawn{L.id, kept, log_share(R, key_logit(d.key), mass)};
+}
+
+// ---- a row -------------------------------------------------------------------------------------------------------------
+struct FastLds {
+    uint32_t upto[kSmpBins];                                 // tokens up to and with a bin
+    uint64_t mass_upto[kSmpBins], sub[kSmpBins];             // their weight; the places within a bin
+    uint64_t list[kSmpList], few[kSmpFew];
+    uint32_t n_list, n_few, found[8];
+    uint64_t red[kSmpThreads / 64];
+    uint32_t red_i[kSmpThreads / 64];
+    uint64_t end_mass, end_entry;
+    uint32_t end_count;
+};
+union RowLds {
+    FastLds f;
+    SlowLds s;
+    RowStats stats[kSmpThreads / 64];
+};
+
+template <int CTRL, int ROWS> __device__ __forceinline__ uint64_t dpp_u64(uint64_t v)
+{
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xF, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROWS, 0xF, false);
+    return (uint64_t)hi << 32 | lo;
+}
+__device__ __forceinline__ uint64_t row_scan_u64(uint64_t v)      // over rows of 16 lanes
+{
+    v += dpp_u64<0x111, 0xF>(v);
+    v += dpp_u64<0x112, 0xF>(v);
+    v += dpp_u64<0x114, 0xF>(v);
+    v += dpp_u64<0x118, 0xF>(v);
+    return v;
+}
+__device__ __forceinline__ uint64_t wave_scan_u64(uint64_t v)
+{
+    v = row_scan_u64(v);
+    v += dpp_u64<0x142, 0xA>(v);
+    v += dpp_u64<0x143, 0xC>(v);
+    return v;
+}
+__device__ __forceinline__ uint64_t lane_u64(uint64_t v, int lane)
+{
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
+}
+
+// Running sums over the workgroup, of one value a thread: a wavefront's by lane moves, the 16 wavefronts' by the lanes of a row.
+__device__ __forceinline__ void wg_scan(FastLds &L, uint32_t &c, uint64_t &m)
+{
+    static_assert(kSmpThreads / 64 == 16, "a row of lanes");
+    c = (uint32_t)wave_scan_i((int)c);
+    m = wave_scan_u64(m);
+    const int wave = __builtin_amdgcn_readfirstlane(wave_id()), lane = lane_id();
+    __syncthreads();
+    if (lane == 63) { L.red_i[wave] = c; L.red[wave] = m; }
+    __syncthreads();
+    const uint32_t cw = (uint32_t)wave_scan_i(lane < 16 ? (int)L.red_i[lane & 15] : 0);
+    const uint64_t mw = row_scan_u64(L.red[lane & 15]);
+    if (wave > 0) {
+        c += (uint32_t)__builtin_amdgcn_readlane((int)cw, wave - 1);
+        m += lane_u64(mw, wave - 1);
+    }
+}
+
+struct End { uint32_t count; uint64_t mass, entry; bool ok; };      // of a beginning: its tokens, its weight, its last token
+
+// The beginning that ends in `bin` (whose tokens are in the list), holds `want_count` tokens or weighs `want_mass` at least.
+__device__ End end_in_bin(FastLds &L, const RowScale &R, const double *table, uint32_t bin, uint32_t want_count, uint64_t want_mass)
+{
+    const int tid = (int)threadIdx.x;
+    uint32_t before = bin ? L.upto[bin - 1] : 0;
+    uint64_t mass_before = bin ? L.mass_upto[bin - 1] : 0;
+    auto holds = [&](uint32_t c, uint64_t m) { return want_count ? c >= want_count : m >= want_mass; };
+    L.sub[tid] = 0;
+    if (tid == 0) { L.n_few = 0; L.found[7] = 0; }
+    __syncthreads();
+    const uint32_t n = L.n_list;
+    for (uint32_t i = tid; i < n; i += kSmpThreads) {
+        const float x = entry_logit(L.list[i]);
+        const uint32_t p = place_of(R, x);
+        if (p >> 10 == bin) atomicAdd((unsigned long long *)&L.sub[p & 1023], (unsigned long long)(weight_of(R, table, x) | 1ull << kCountShift));
+    }
+    __syncthreads();
+    const uint32_t c_own = (uint32_t)(L.sub[tid] >> kCountShift);
+    const uint64_t m_own = L.sub[tid] & ((1ull << kCountShift) - 1);
+    uint32_t c = c_own;
+    uint64_t m = m_own;
+    wg_scan(L, c, m);
+    c += before;
+    m += mass_before;
+    if (!holds(c - c_own, m - m_own) && holds(c, m)) { L.found[7] = tid; L.end_count = c - c_own; L.end_mass = m - m_own; }
+    __syncthreads();
+    const uint32_t place = bin << 10 | L.found[7];
+    before = L.end_count;
+    mass_before = L.end_mass;
+    const uint32_t few = (uint32_t)(L.sub[L.found[7]] >> kCountShift);
+    if (few > kSmpFew) return End{0, 0, 0, false};
+    for (uint32_t i = tid; i < n; i += kSmpThreads)
+        if (place_of(R, entry_logit(L.list[i])) == place) L.few[atomicAdd(&L.n_few, 1u)] = L.list[i];
+    __syncthreads();
+    if (tid < (int)few) {                                    // what is in front of this thread's token, and with it
+        const uint64_t e = L.few[tid], own = weight_of(R, table, entry_logit(e));
+        uint32_t cc = before;
+        uint64_t mm = mass_before;
+        for (uint32_t j = 0; j < few; ++j) {
+            const uint64_t t = L.few[j];
+            if (t > e) { cc++; mm += weight_of(R, table, entry_logit(t)); }
+        }
+        if (!holds(cc, mm) && holds(cc + 1, mm + own)) { L.end_count = cc + 1; L.end_mass = mm + own; L.end_entry = e; }
+    }
+    __syncthreads();
+    const End e{L.end_count, L.end_mass, L.end_entry, true};
+    __syncthreads();
+    return e;
+}
+
+template <bool F32, bool WHOLE>
+__global__ __launch_bounds__(kSmpThreads) void sample_row_kernel(SampleArgs a)
+{
+    __shared__ RowLds lds;
+    __shared__ double table[1024];
+    FastLds &L = lds.f;
+    fill_powers(table);                                      // (the first barrier is in front of its first use)
+    const int tid = (int)threadIdx.x, r = (int)blockIdx.x, vocab = a.S.vocab;
+    const etc_serving_sample_io &io = a.io;
+    const void *row = row_of<F32>(a, r);
+    Settings q;
+    q.T = io.temperature ? *as_global(io.temperature + r) : 1.f;
+    q.top_k = io.top_k ? gld_i32(io.top_k + r) : 0;
+    q.top_p = io.top_p ? *as_global(io.top_p + r) : 1.f;
+    q.min_p = io.min_p ? *as_global(io.min_p + r) : 0.f;
+    q.u = *as_global(io.u + r);
+    auto answer = [&](int32_t token, float logprob, uint32_t kept) {
+        if (tid != 0) return;
+        *as_global(io.token_out + r) = token;
         if (io.logprob_out) gst_f32(io.logprob_out + r, logprob);
         if (io.kept_out) *as_global(io.kept_out + r) = (int32_t)kept;
+    };
+    RowStats st;
+    if constexpr (WHOLE) st = row_stats<F32, kSmpThreads>(row, 0, vocab, lds.stats);
+    else st = join_stats(a, r);
+    if (st.live == 0) return answer(-1, -INFINITY, 0);
+    if (!(q.T > 0.f)) return answer((int32_t)st.first, 0.f, 1);
+    const RowScale R = scale_of(st, q.T);
+    auto slow = [&]() {
+        __syncthreads();
+        const Drawn d = slow_row<F32>(lds.s, row, vocab, R, table, st.live, q);
+        answer((int32_t)d.id, d.logprob, d.kept);
+    };
+    if (R.top == INFINITY) return slow();
+
+    // ---- the bins, one a thread, and their running sums
+    uint32_t c_own = 0;
+    uint64_t m_own = 0;
+    auto unpack = [&](uint64_t v) { c_own += (uint32_t)(v >> kCountShift); m_own += v & ((1ull << kCountShift) - 1); };
+    if constexpr (WHOLE) {
+        L.sub[tid] = 0;
+        __syncthreads();
+        fill_bins<F32, kSmpThreads>(row, 0, vocab, R, table, (unsigned long long *)L.sub);
+        __syncthreads();
+        unpack(L.sub[tid]);
+    } else {
+        const uint64_t *bins = a.S.smp_bins + (size_t)r * a.slices * kSmpBins + tid;
+#pragma unroll 8
+        for (int sl = 0; sl < a.slices; ++sl) unpack(bins[(size_t)sl * kSmpBins]);
     }
+    uint32_t c = c_own;
+    uint64_t m = m_own;
+    if (tid < 8) L.found[tid] = 0;
+    if (tid == 0) L.n_list = 0;
+    wg_scan(L, c, m);
+    L.upto[tid] = c;
+    L.mass_upto[tid] = m;
+    __syncthreads();
+    const uint64_t total = L.mass_upto[kSmpBins - 1];
+    const uint32_t n_live = L.upto[kSmpBins - 1];
+
+    // ---- where the beginnings can end: the bins in question.  found: 0 top_k; 1, 2 top_p at its least and most; 3, 4 the draw's
+    const bool use_k = q.top_k > 0 && (uint32_t)q.top_k < n_live, use_p = q.top_p < 1.f, use_m = q.min_p > 0.f;
+    auto holds_mass = [&](uint64_t want) { return m - m_own < want && want <= m; };
+    auto mass_in_front = [&](uint32_t b) { return b ? L.mass_upto[b - 1] : 0ull; };
+    if (use_k && c - c_own < (uint32_t)q.top_k && (uint32_t)q.top_k <= c) L.found[0] = tid;
+    __syncthreads();
+    const uint32_t bin_k = L.found[0];
+    uint64_t least = use_k ? mass_in_front(bin_k) : total, most = use_k ? L.mass_upto[bin_k] : total;
+    if (use_p) {
+        if (holds_mass(mass_wanted(q.top_p, least > 0 ? least : 1))) L.found[1] = tid;
+        if (holds_mass(mass_wanted(q.top_p, most))) L.found[2] = tid;
+        __syncthreads();
+        least = min(least, mass_in_front(L.found[1]));
+        most = min(most, L.mass_upto[L.found[2]]);
+    }
+    uint32_t bin_m0 = 0, bin_m1 = 0;
+    if (use_m) {                                             // its border, and a bin to either side for the rounding of the logarithm
+        const double at = q.min_p < 1.f ? -log((double)q.min_p) * (double)q.T * R.per * 0.0009765625 : 0.0;
+        const uint32_t b = at < (double)(kSmpBins - 1) ? (uint32_t)at : kSmpBins - 1;
+        bin_m0 = b ? b - 1 : 0;
+        bin_m1 = min(b + 1, (uint32_t)kSmpBins - 1);
+        least = min(least, mass_in_front(bin_m0));
+        most = min(most, L.mass_upto[bin_m1]);
+    }
+    if (holds_mass(draw_wanted(q.u, least > 0 ? least : 1))) L.found[3] = tid;
+    if (holds_mass(draw_wanted(q.u, most))) L.found[4] = tid;
+    __syncthreads();
+    const uint32_t p0 = L.found[1], p1 = L.found[2], d0 = L.found[3], d1 = L.found[4];
+    auto in_question = [&](uint32_t b) {
+        return (use_k && b == bin_k) || (use_p && b >= p0 && b <= p1) || (use_m && b >= bin_m0 && b <= bin_m1) || (b >= d0 && b <= d1);
+    };
+    {
+        const uint32_t n = wave_all_sum(in_question(tid) ? c_own : 0u);
+        if (lane_id() == 0) L.red_i[wave_id()] = n;
+        __syncthreads();
+        uint32_t all = 0;
+        for (int w = 0; w < kSmpThreads / 64; ++w) all += L.red_i[w];
+        if (all > kSmpList) return slow();
+    }
+    // a first look in fp32: the logits between the first and the last of these bins, and a hundredth of a bin more
+    uint32_t b0 = d0, b1 = d1;
+    if (use_k) { b0 = min(b0, bin_k); b1 = max(b1, bin_k); }
+    if (use_p) { b0 = min(b0, p0); b1 = max(b1, p1); }
+    if (use_m) { b0 = min(b0, bin_m0); b1 = max(b1, bin_m1); }
+    const double wide = R.per > 0.0 ? 1024.0 / R.per : 0.0;
+    const float hi = b0 == 0 ? R.top : (float)((double)R.top - ((double)b0 - 0.01) * wide) + fabsf(R.top) * 0x1p-22f;
+    const float lo = R.per == 0.0 || b1 == kSmpBins - 1 ? -3.402823466e38f : (float)((double)R.top - ((double)b1 + 1.01) * wide) - fabsf(R.top) * 0x1p-22f;
+    for_tokens<F32, kSmpThreads>(row, 0, vocab, [&](float x, int i) {
+        if (x <= hi && x >= lo && in_question(place_of(R, x) >> 10)) L.list[atomicAdd(&L.n_list, 1u)] = entry_of(x, i);
+    });
+    __syncthreads();
+
+    // ---- the filters, exactly
+    uint32_t kept = n_live;
+    uint64_t mass = total;
+    if (use_k) {
+        const End e = end_in_bin(L, R, table, bin_k, (uint32_t)q.top_k, 0);
+        if (!e.ok) return slow();
+        kept = e.count;
+        mass = e.mass;
+    }
+    auto bin_of_mass = [&](uint64_t want) {                  // by all threads
+        if (holds_mass(want)) L.found[5] = tid;
+        __syncthreads();
+        const uint32_t b = L.found[5];
+        __syncthreads();
+        return b;
+    };
+    if (use_p) {
+        const uint64_t want = mass_wanted(q.top_p, mass);
+        const End e = end_in_bin(L, R, table, bin_of_mass(want), 0, want);
+        if (!e.ok) return slow();
+        kept = e.count;
+        mass = e.mass;
+    }
+    if (use_m) {
+        uint32_t above = 0;
+        uint64_t am = 0;
+        for (uint32_t i = tid; i < L.n_list; i += kSmpThreads) {
+            const float x = entry_logit(L.list[i]);
+            const uint32_t b = place_of(R, x) >> 10;
+            if (b >= bin_m0 && b <= bin_m1 && above_min_p(R, x, q.min_p)) { above++; am += weight_of(R, table, x); }
+        }
+        above = wg_sum<uint32_t>(above, L.red_i) + (bin_m0 ? L.upto[bin_m0 - 1] : 0);
+        am = wg_sum<uint64_t>(am, L.red) + mass_in_front(bin_m0);
+        if (q.min_p > 1.f) { above = 1; am = kTopWeight; }
+        if (above < kept) { kept = above; mass = am; }
+        __syncthreads();
+    }
+    const uint64_t want = draw_wanted(q.u, mass);
+    const End e = end_in_bin(L, R, table, bin_of_mass(want), 0, want);
+    if (!e.ok) return slow();
+    answer((int32_t)~(uint32_t)e.entry, log_share(R, entry_logit(e.entry), mass), kept);
+}
+
+// Slices of a row: as many as give kSmpWgs workgroups, of 2048 tokens at least, and of kBinTokens at most.
+static int slices_of(int vocab, int rows)
+{
+    const int most = (vocab + 2047) / 2048, least = (vocab + kBinTokens - 1) / kBinTokens;
+    int s = kSmpWgs / rows;
+    if (s > most) s = most;
+    return s < least ? least : s;
+}
+
+template <bool F32>
+static void launch_sample(const SampleArgs &a, hipStream_t s)
+{
+    if (a.S.vocab <= kSmpWhole) {
+        hipLaunchKernelGGL((sample_row_kernel<F32, true>), dim3(a.io.n_rows), dim3(kSmpThreads), 0, s, a);
+        return;
+    }
+    const dim3 grid((unsigned)a.slices, (unsigned)a.io.n_rows);
+    hipLaunchKernelGGL((sample_scan_kernel<F32>), grid, dim3(kSliceThreads), 0, s, a);
+    hipLaunchKernelGGL((sample_bins_kernel<F32>), grid, dim3(kSliceThreads), 0, s, a);
+    hipLaunchKernelGGL((sample_row_kernel<F32, false>), dim3(a.io.n_rows), dim3(kSmpThreads), 0, s, a);
 }
 
 hipError_t launch_serving_sample(const ServingDev &S, const etc_serving_sample_io &io, hipStream_t s)
 {
-    if (io.dtype == ETC_FP32) hipLaunchKernelGGL((serving_sample_kernel<true>), dim3(io.n_rows), dim3(kSmpThreads), 0, s, S, io);
-    else hipLaunchKernelGGL((serving_sample_kernel<false>), dim3(io.n_rows), dim3(kSmpThreads), 0, s, S, io);
+    SampleArgs a{S, io, slices_of(S.vocab, io.n_rows), 0};
+    a.per_slice = (S.vocab + a.slices - 1) / a.slices;
+    if (io.dtype == ETC_FP32) launch_sample<true>(a, s); else launch_sample<false>(a, s);
     return hipGetLastError();
 }
+
+// Workspace of a handle: slices of a launch, all rows together.
+int64_t sample_slices(int vocab, int max_rows)
+{
+    if (vocab <= kSmpWhole) return 0;
+    const int64_t least = (int64_t)max_rows * ((vocab + kBinTokens - 1) / kBinTokens);
+    return least > kSmpWgs ? least : kSmpWgs;
+}
+int64_t sample_stat_bytes() { return (int64_t)sizeof(RowStats); }
+int64_t sample_bins_bytes() { return kSmpBins * 8; }
 
 }  // namespace etc
 #endif  // ETC_GENERIC_ONLY

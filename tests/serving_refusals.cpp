@@ -29,6 +29,9 @@ const char *hipGetErrorString(hipError_t) { return "stub"; }
 }
 namespace etc {
 int64_t attention_slot_bytes(int) { return 64; }
+int64_t sample_slices(int, int) { return 4; }
+int64_t sample_stat_bytes() { return 16; }
+int64_t sample_bins_bytes() { return 64; }
 hipError_t launch_serving_tables(const ServingDev &, const etc_serving_tables_io &, hipStream_t) { ++g_launches; return hipSuccess; }
 hipError_t launch_serving_append(const ServingDev &, const etc_serving_append_io &, hipStream_t) { ++g_launches; return hipSuccess; }
 hipError_t launch_serving_attention(const ServingDev &, const etc_serving_attention_io &, hipStream_t) { ++g_launches; return hipSuccess; }
@@ -79,7 +82,7 @@ int main()
         CHECK(bad([](M, L b) { b.max_kv_len = 0; }));
         CHECK(etc_serving_create(nullptr, &l, &s) == ETC_EINVAL && etc_serving_create(&m, nullptr, &s) == ETC_EINVAL);
         CHECK(etc_serving_create(&m, &l, nullptr) == ETC_EINVAL);
-        for (int k = 0; k < 4; ++k) {                     // no memory: everything is given back
+        for (int k = 0; k < 6; ++k) {                     // no memory: everything is given back
             g_fail_malloc = k;
             CHECK(etc_serving_create(&m, &l, &s) == ETC_ENOMEM && s == nullptr && g_allocs == 0 && etc_serving_last_error(nullptr)[0]);
             g_fail_malloc = -1;

@@ -287,7 +287,7 @@ def test_attention_bad_pages_and_lengths(etc):
 
 # ---- sampling -----------------------------------------------------------------------------------------------------------
 def _sample(etc, x, u, stride_pad=0, **settings):
-    """Checks every row, and returns how many rows stood next to a border (gap below 1e-9) and were not compared."""
+    """Checks every row, and returns how many rows stood next to a border (gap below 1e-7) and were not compared."""
     rows, vocab = x.shape
     sv = etc.Serving(ref.shape(vocab=vocab), max_seqs=rows, max_tokens=1, max_kv_len=1)
     wide = torch.full((rows, vocab + stride_pad), 1e30, dtype=x.dtype)
@@ -303,12 +303,12 @@ def _sample(etc, x, u, stride_pad=0, **settings):
     for r in range(rows):
         own = {k: float(np.float32(v[r])) if k != "top_k" else int(v[r]) for k, v in settings.items()}
         t, p, n, gap = ref.sample_row(xs[r], float(np.float32(u[r])), **own)
-        if gap < 1e-9:                                    # sums here: 2^-44 a token, 2^20 tokens; there: fp64
+        if gap < 1e-7:                                    # a weight is off by 2^-34 of it and half of 2^-35: 128256 of them by 6 sigma = 2e-8 of a sum
             skipped += 1
             continue
         assert int(tok[r]) == t and int(kept[r]) == n, (r, own, int(tok[r]), t, int(kept[r]), n)
-        # fp32 rounding of the result; the sum of weights: 2^-44 of each token's at most, relative to a sum of 1 at least
-        assert abs(float(lp[r]) - p) <= 2.0 ** -24 * abs(p) + 2.0 ** -43 * vocab + 1e-12 or float(lp[r]) == p
+        # fp32 rounding of the result; the sum of weights is at least 1, each of them off by half of 2^-35 and 2^-34 of itself at most
+        assert abs(float(lp[r]) - p) <= 2.0 ** -24 * abs(p) + 2.0 ** -36 * vocab + 2.0 ** -34 or float(lp[r]) == p
     return skipped
 
 

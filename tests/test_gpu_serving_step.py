@@ -137,7 +137,7 @@ def test_prompt_in_chunks_then_decode_with_sampling(etc):
         for b in range(B):
             t, _, _, gap = ref.sample_row(host[b], float(u[step + 1, b]), float(np.float32(setting["temperature"][b].item())),
                                           int(setting["top_k"][b]), float(np.float32(setting["top_p"][b].item())))
-            assert gap < 1e-9 or int(out[b]) == t
+            assert gap < 1e-7 or int(out[b]) == t
         assert int(out[0]) == int(scratch[0])             # greedy: the megakernel's own token
         token = out.clone()
     assert sv.read_error()[0] == 0
