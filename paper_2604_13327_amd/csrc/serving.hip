@@ -259,44 +259,44 @@ constexpr int kUnitBits = 35;
 constexpr uint64_t kTopWeight = 1ull << kUnitBits;
 constexpr int kBinTokens = 1 << 14;         // tokens whose count and weight fit the 64 bits of a bin: 15 and 49
 constexpr int kCountShift = 49;
-constexpr int kSmpWgs = 512;                // workgroups over slices
+constexpr int kSmpWgs = 256;                // workgroups over slices
 constexpr int kSmpWhole = kBinTokens;       // longest row that sample_row does alone
 
 template <bool F32>
+__device__ __forceinline__ float raw_logit(const void *row, int i)
+{
+    return F32 ? *as_global((const float *)row + i) : bf16_bits_to_f32(gld_u16((const uint16_t *)row + i));
+}
+template <bool F32>
 __device__ __forceinline__ float logit_at(const void *row, int i)
 {
-    float x = F32 ? *as_global((const float *)row + i) : bf16_bits_to_f32(gld_u16((const uint16_t *)row + i));
+    float x = raw_logit<F32>(row, i);
     x = x != x ? -INFINITY : x;                              // NaN: banned
     return x + 0.f;                                          // -0 is +0: equal logits
 }
-// f(logit, id) for the tokens [i0, i1) of a row, by the workgroup: 16 bytes a load and four loads in flight (one after the other
-// a row of 128256 took 73 us instead of 14), single tokens in front of and behind what is aligned.
-template <bool F32, int THREADS, class Fn>
-__device__ __forceinline__ void for_tokens(const void *row, int i0, int i1, Fn f)
+// The tokens [i0, i1) of a row, by the workgroup, a thread's ids ascending; NaN as it stands.  16 bytes a load and U loads in flight
+// (one after the other a row of 128256 took 73 us instead of 14): vectors(w, n, id) gets U vectors of which n are of this row, the
+// first one's ids from `id` on, the next ones' THREADS * 16 bytes behind.  single(logit, id): in front of and behind what is aligned.
+template <bool F32, int THREADS, int U, class Vectors, class Single>
+__device__ __forceinline__ void for_tokens(const void *row, int i0, int i1, Vectors vectors, Single single)
 {
-    constexpr int SIZE = F32 ? 4 : 2, E = 16 / SIZE, U = 4;
+    constexpr int SIZE = F32 ? 4 : 2, E = 16 / SIZE;
     const int tid = (int)threadIdx.x;
     const char *from = (const char *)row + (int64_t)i0 * SIZE;
     const int a0 = min(i1, i0 + (int)((16 - ((uintptr_t)from & 15)) & 15) / SIZE), nv = (i1 - a0) / E, t0 = a0 + nv * E;
-    if (i0 + tid < a0) f(logit_at<F32>(row, i0 + tid), i0 + tid);
-    if (t0 + tid < i1) f(logit_at<F32>(row, t0 + tid), t0 + tid);
+    if (i0 + tid < a0) single(raw_logit<F32>(row, i0 + tid), i0 + tid);
     const char *body = (const char *)row + (int64_t)a0 * SIZE;
     for (int v0 = tid; v0 < nv; v0 += THREADS * U) {
         u32x4 w[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) w[u] = gld_16B(body + (int64_t)min(v0 + u * THREADS, nv - 1) * 16);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (v0 + u * THREADS >= nv) break;
-            const int i = a0 + (v0 + u * THREADS) * E;
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                float x = F32 ? __uint_as_float(w[u][e]) : (e & 1) ? bf16_hi(w[u][e >> 1]) : bf16_lo(w[u][e >> 1]);
-                x = x != x ? -INFINITY : x;
-                f(x + 0.f, i + e);
-            }
-        }
+        vectors(w, min(U, (nv - v0 + THREADS - 1) / THREADS), a0 + v0 * E);
     }
+    if (t0 + tid < i1) single(raw_logit<F32>(row, t0 + tid), t0 + tid);
+}
+template <bool F32> __device__ __forceinline__ float element(u32x4 w, int e)
+{
+    return F32 ? __uint_as_float(w[e & 3]) : (e & 1) ? bf16_hi(w[e >> 1]) : bf16_lo(w[e >> 1]);
 }
 
 __device__ __forceinline__ uint32_t order_key(float x)
@@ -308,7 +308,6 @@ __device__ __forceinline__ float key_logit(uint32_t k) { return __uint_as_float(
 constexpr uint32_t kBannedKey = 0x007FFFFFu;                 // of -inf
 
 // A token in the order: larger is earlier.
-__device__ __forceinline__ uint64_t entry_of(float x, int id) { return ((uint64_t)order_key(x) << 32) | (uint32_t)~(uint32_t)id; }
 __device__ __forceinline__ float entry_logit(uint64_t e) { return key_logit((uint32_t)(e >> 32)); }
 
 struct RowScale {
@@ -377,12 +376,21 @@ template <bool F32, int THREADS>
 __device__ __forceinline__ RowStats row_stats(const void *row, int i0, int i1, RowStats *s_red)
 {
     RowStats st{-INFINITY, INFINITY, 0xFFFFFFFFu, 0};
-    for_tokens<F32, THREADS>(row, i0, i1, [&](float x, int i) {
-        if (x > st.top || (x == st.top && (uint32_t)i < st.first)) { st.top = x; st.first = (uint32_t)i; }
-        const bool banned = x == -INFINITY;
-        st.low = fminf(st.low, banned ? INFINITY : x);
-        st.live += !banned;
-    });
+    auto one = [&](float x, int i) {
+        if (x > st.top) { st.top = x; st.first = (uint32_t)i; }
+        const bool live = x > -INFINITY;                     // no NaN either
+        st.low = live ? fminf(st.low, x) : st.low;
+        st.live += live;
+    };
+    for_tokens<F32, THREADS, 4>(row, i0, i1, [&](const u32x4 (&w)[4], int n, int id) {
+        constexpr int E = F32 ? 4 : 8;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (u >= n) break;
+#pragma unroll
+            for (int e = 0; e < E; ++e) one(element<F32>(w[u], e), id + u * THREADS * E + e);
+        }
+    }, one);
     st = wave_join(st);
     if (lane_id() == 0) s_red[wave_id()] = st;
     __syncthreads();
@@ -404,9 +412,23 @@ __device__ __forceinline__ RowScale scale_of(const RowStats &st, float T)
 template <bool F32, int THREADS>
 __device__ __forceinline__ void fill_bins(const void *row, int i0, int i1, const RowScale &R, const double *table, unsigned long long *bins)
 {
-    for_tokens<F32, THREADS>(row, i0, i1, [&](float x, int) {
-        if (x != -INFINITY) atomicAdd(&bins[place_of(R, x) >> 10], (unsigned long long)(weight_of(R, table, x) | 1ull << kCountShift));
-    });
+    auto one = [&](float x, int) {
+        if (x > -INFINITY) atomicAdd(&bins[place_of(R, x) >> 10], (unsigned long long)(weight_of(R, table, x) | 1ull << kCountShift));
+    };
+    // word by word, in a loop: written out for all, the code does not stay in the instruction cache
+    for_tokens<F32, THREADS, 2>(row, i0, i1, [&](const u32x4 (&w)[2], int n, int) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            if (u >= n) break;
+            u32x4 v = w[u];
+#pragma unroll 1
+            for (int k = 0; k < 4; ++k) {
+                if (F32) one(__uint_as_float(v.x), 0);
+                else { one(bf16_lo(v.x), 0); one(bf16_hi(v.x), 0); }
+                v = u32x4{v.y, v.z, v.w, v.x};
+            }
+        }
+    }, one);
 }
 
 struct SampleArgs {
@@ -491,7 +513,7 @@ struct SlowLds {
 // The shortest beginning of the order that holds `want_count` tokens, or (want_count == 0) weighs `want_mass` at least; the row has
 // it.  11 + 11 + 10 bits of the key at a time; equal keys have equal weights, so ties are settled by a division.
 template <bool F32>
-__device__ Prefix find_prefix(SlowLds &L, const void *row, int vocab, const RowScale &R, const double *table, uint32_t want_count, uint64_t want_mass)
+__device__ __noinline__ Prefix find_prefix(SlowLds &L, const void *row, int vocab, const RowScale &R, const double *table, uint32_t want_count, uint64_t want_mass)
 {
     const int tid = (int)threadIdx.x;
     uint32_t prefix = 0, before = 0;
@@ -574,7 +596,7 @@ __device__ __forceinline__ float log_share(const RowScale &R, float x, uint64_t 
 }
 
 template <bool F32>
-__device__ Drawn slow_row(SlowLds &L, const void *row, int vocab, const RowScale &R, const double *table, uint32_t live, const Settings &q)
+__device__ __noinline__ Drawn slow_row(SlowLds &L, const void *row, int vocab, const RowScale &R, const double *table, uint32_t live, const Settings &q)
 {
     const int tid = (int)threadIdx.x;
     uint32_t n_live = live;
@@ -626,7 +648,8 @@ __device__ Drawn slow_row(SlowLds &L, const void *row, int vocab, const RowScale
 struct FastLds {
     uint32_t upto[kSmpBins];                                 // tokens up to and with a bin
     uint64_t mass_upto[kSmpBins], sub[kSmpBins];             // their weight; the places within a bin
-    uint64_t list[kSmpList], few[kSmpFew];
+    uint32_t id[kSmpList], key[kSmpList], place[kSmpList];   // the tokens in question (and some next to them)
+    uint64_t few[kSmpFew], few_mass[kSmpFew];
     uint32_t n_list, n_few, found[8];
     uint64_t red[kSmpThreads / 64];
     uint32_t red_i[kSmpThreads / 64];
@@ -685,22 +708,54 @@ __device__ __forceinline__ void wg_scan(FastLds &L, uint32_t &c, uint64_t &m)
 
 struct End { uint32_t count; uint64_t mass, entry; bool ok; };      // of a beginning: its tokens, its weight, its last token
 
-// The beginning that ends in `bin` (whose tokens are in the list), holds `want_count` tokens or weighs `want_mass` at least.
-__device__ End end_in_bin(FastLds &L, const RowScale &R, const double *table, uint32_t bin, uint32_t want_count, uint64_t want_mass)
+// The r-th token (from 1), by id, of those in the list that lie in `place`, which have one key.  Sorted by id into 1024 bins, the right
+// one's counted one by one.
+__device__ __forceinline__ uint64_t tied_token(FastLds &L, uint32_t place, uint32_t r, uint32_t vocab)
+{
+    const int tid = (int)threadIdx.x;
+    const uint32_t n = L.n_list, per = (vocab + 1023) / 1024;
+    L.sub[tid] = 0;
+    if (tid == 0) L.n_few = 0;
+    __syncthreads();
+    for (uint32_t i = tid; i < n; i += kSmpThreads)
+        if (L.place[i] == place) atomicAdd((unsigned long long *)&L.sub[L.id[i] / per], 1ull);
+    __syncthreads();
+    uint32_t c = (uint32_t)L.sub[tid];
+    const uint32_t own = c;
+    uint64_t none = 0;
+    wg_scan(L, c, none);
+    if (c - own < r && r <= c) { L.found[7] = tid; L.end_count = c - own; }
+    __syncthreads();
+    const uint32_t bin = L.found[7], left = r - L.end_count;      // at most `per` <= 1024 tokens
+    for (uint32_t i = tid; i < n; i += kSmpThreads)
+        if (L.place[i] == place && L.id[i] / per == bin) L.few[atomicAdd(&L.n_few, 1u)] = (uint64_t)L.key[i] << 32 | ~L.id[i];
+    __syncthreads();
+    const uint32_t few = L.n_few;
+    if (tid < (int)few) {
+        const uint64_t e = L.few[tid];
+        uint32_t rank = 1;
+        for (uint32_t j = 0; j < few; ++j) rank += L.few[j] > e;
+        if (rank == left) L.end_entry = e;
+    }
+    __syncthreads();
+    return L.end_entry;
+}
+
+// The beginning that ends in `bin` (whose tokens are in the list), holds `want_count` tokens or weighs `want_mass` at least.  Its last
+// token is named for the draw only.
+__device__ __forceinline__ End end_in_bin(FastLds &L, const RowScale &R, const double *table, uint32_t vocab, uint32_t bin, uint32_t want_count, uint64_t want_mass, bool draw)
 {
     const int tid = (int)threadIdx.x;
     uint32_t before = bin ? L.upto[bin - 1] : 0;
     uint64_t mass_before = bin ? L.mass_upto[bin - 1] : 0;
     auto holds = [&](uint32_t c, uint64_t m) { return want_count ? c >= want_count : m >= want_mass; };
     L.sub[tid] = 0;
-    if (tid == 0) { L.n_few = 0; L.found[7] = 0; }
+    if (tid == 0) { L.n_few = 0; L.found[6] = 0; }
     __syncthreads();
     const uint32_t n = L.n_list;
-    for (uint32_t i = tid; i < n; i += kSmpThreads) {
-        const float x = entry_logit(L.list[i]);
-        const uint32_t p = place_of(R, x);
-        if (p >> 10 == bin) atomicAdd((unsigned long long *)&L.sub[p & 1023], (unsigned long long)(weight_of(R, table, x) | 1ull << kCountShift));
-    }
+    for (uint32_t i = tid; i < n; i += kSmpThreads)
+        if (L.place[i] >> 10 == bin)
+            atomicAdd((unsigned long long *)&L.sub[L.place[i] & 1023], (unsigned long long)(weight_of(R, table, key_logit(L.key[i])) | 1ull << kCountShift));
     __syncthreads();
     const uint32_t c_own = (uint32_t)(L.sub[tid] >> kCountShift);
     const uint64_t m_own = L.sub[tid] & ((1ull << kCountShift) - 1);
@@ -709,24 +764,46 @@ __device__ End end_in_bin(FastLds &L, const RowScale &R, const double *table, ui
     wg_scan(L, c, m);
     c += before;
     m += mass_before;
-    if (!holds(c - c_own, m - m_own) && holds(c, m)) { L.found[7] = tid; L.end_count = c - c_own; L.end_mass = m - m_own; }
+    if (!holds(c - c_own, m - m_own) && holds(c, m)) {
+        L.found[7] = tid;
+        L.end_count = c - c_own;
+        L.end_mass = m - m_own;
+    }
     __syncthreads();
-    const uint32_t place = bin << 10 | L.found[7];
+    const uint32_t place = bin << 10 | L.found[7], few = (uint32_t)(L.sub[L.found[7]] >> kCountShift);
     before = L.end_count;
     mass_before = L.end_mass;
-    const uint32_t few = (uint32_t)(L.sub[L.found[7]] >> kCountShift);
-    if (few > kSmpFew) return End{0, 0, 0, false};
-    for (uint32_t i = tid; i < n; i += kSmpThreads)
-        if (place_of(R, entry_logit(L.list[i])) == place) L.few[atomicAdd(&L.n_few, 1u)] = L.list[i];
+    for (uint32_t i = tid; i < n; i += kSmpThreads)          // the tokens of the place
+        if (L.place[i] == place) {
+            const uint32_t at = atomicAdd(&L.n_few, 1u);
+            if (at < kSmpFew) L.few[at] = (uint64_t)L.key[i] << 32 | ~L.id[i];
+        }
     __syncthreads();
+    const uint64_t one = L.few[0];                           // have they one key?
+    if (few <= kSmpFew) {
+        if (tid < (int)few) {
+            if ((uint32_t)(L.few[tid] >> 32) != (uint32_t)(one >> 32)) L.found[6] = 1;
+            L.few_mass[tid] = weight_of(R, table, entry_logit(L.few[tid]));
+        }
+    } else {
+        for (uint32_t i = tid; i < n; i += kSmpThreads)
+            if (L.place[i] == place && L.key[i] != (uint32_t)(one >> 32)) L.found[6] = 1;
+    }
+    __syncthreads();
+    if (!L.found[6] && few > 1) {                            // equal keys: equal weights
+        const uint64_t w = weight_of(R, table, entry_logit(one));
+        const uint32_t r = want_count ? want_count - before : (uint32_t)((want_mass - mass_before + w - 1) / w);
+        const End e{before + r, mass_before + r * w, draw ? tied_token(L, place, r, vocab) : one, true};
+        __syncthreads();
+        return e;
+    }
+    if (few > kSmpFew) return End{0, 0, 0, false};
     if (tid < (int)few) {                                    // what is in front of this thread's token, and with it
-        const uint64_t e = L.few[tid], own = weight_of(R, table, entry_logit(e));
+        const uint64_t e = L.few[tid], own = L.few_mass[tid];
         uint32_t cc = before;
         uint64_t mm = mass_before;
-        for (uint32_t j = 0; j < few; ++j) {
-            const uint64_t t = L.few[j];
-            if (t > e) { cc++; mm += weight_of(R, table, entry_logit(t)); }
-        }
+        for (uint32_t j = 0; j < few; ++j)
+            if (L.few[j] > e) { cc++; mm += L.few_mass[j]; }
         if (!holds(cc, mm) && holds(cc + 1, mm + own)) { L.end_count = cc + 1; L.end_mass = mm + own; L.end_entry = e; }
     }
     __syncthreads();
@@ -735,41 +812,11 @@ __device__ End end_in_bin(FastLds &L, const RowScale &R, const double *table, ui
     return e;
 }
 
+// The row by its bins.  False: more tokens are in question than the list holds.
 template <bool F32, bool WHOLE>
-__global__ __launch_bounds__(kSmpThreads) void sample_row_kernel(SampleArgs a)
+__device__ __forceinline__ bool fast_row(const SampleArgs &a, FastLds &L, const void *row, const RowScale &R, const double *table, const Settings &q, int r, Drawn *out)
 {
-    __shared__ RowLds lds;
-    __shared__ double table[1024];
-    FastLds &L = lds.f;
-    fill_powers(table);                                      // (the first barrier is in front of its first use)
-    const int tid = (int)threadIdx.x, r = (int)blockIdx.x, vocab = a.S.vocab;
-    const etc_serving_sample_io &io = a.io;
-    const void *row = row_of<F32>(a, r);
-    Settings q;
-    q.T = io.temperature ? *as_global(io.temperature + r) : 1.f;
-    q.top_k = io.top_k ? gld_i32(io.top_k + r) : 0;
-    q.top_p = io.top_p ? *as_global(io.top_p + r) : 1.f;
-    q.min_p = io.min_p ? *as_global(io.min_p + r) : 0.f;
-    q.u = *as_global(io.u + r);
-    auto answer = [&](int32_t token, float logprob, uint32_t kept) {
-        if (tid != 0) return;
-        *as_global(io.token_out + r) = token;
-        if (io.logprob_out) gst_f32(io.logprob_out + r, logprob);
-        if (io.kept_out) *as_global(io.kept_out + r) = (int32_t)kept;
-    };
-    RowStats st;
-    if constexpr (WHOLE) st = row_stats<F32, kSmpThreads>(row, 0, vocab, lds.stats);
-    else st = join_stats(a, r);
-    if (st.live == 0) return answer(-1, -INFINITY, 0);
-    if (!(q.T > 0.f)) return answer((int32_t)st.first, 0.f, 1);
-    const RowScale R = scale_of(st, q.T);
-    auto slow = [&]() {
-        __syncthreads();
-        const Drawn d = slow_row<F32>(lds.s, row, vocab, R, table, st.live, q);
-        answer((int32_t)d.id, d.logprob, d.kept);
-    };
-    if (R.top == INFINITY) return slow();
-
+    const int tid = (int)threadIdx.x, vocab = a.S.vocab;
     // ---- the bins, one a thread, and their running sums
     uint32_t c_own = 0;
     uint64_t m_own = 0;
@@ -824,71 +871,132 @@ __global__ __launch_bounds__(kSmpThreads) void sample_row_kernel(SampleArgs a)
     if (holds_mass(draw_wanted(q.u, most))) L.found[4] = tid;
     __syncthreads();
     const uint32_t p0 = L.found[1], p1 = L.found[2], d0 = L.found[3], d1 = L.found[4];
-    auto in_question = [&](uint32_t b) {
-        return (use_k && b == bin_k) || (use_p && b >= p0 && b <= p1) || (use_m && b >= bin_m0 && b <= bin_m1) || (b >= d0 && b <= d1);
-    };
+    // The tokens of the bins in question, by four intervals of logits a hundredth of a bin wider, in fp32: their ids first, then all their
+    // logits at once.
+    float lo[4], hi[4];
     {
-        const uint32_t n = wave_all_sum(in_question(tid) ? c_own : 0u);
-        if (lane_id() == 0) L.red_i[wave_id()] = n;
-        __syncthreads();
-        uint32_t all = 0;
-        for (int w = 0; w < kSmpThreads / 64; ++w) all += L.red_i[w];
-        if (all > kSmpList) return slow();
+        const double wide = R.per > 0.0 ? 1024.0 / R.per : 0.0;
+        const float slack = fabsf(R.top) * 0x1p-22f;
+        auto interval = [&](int i, bool use, uint32_t b0, uint32_t b1) {
+            hi[i] = !use ? -INFINITY : b0 == 0 ? R.top : (float)((double)R.top - ((double)b0 - 0.01) * wide) + slack;
+            lo[i] = !use ? INFINITY : R.per == 0.0 || b1 == kSmpBins - 1 ? -3.402823466e38f : (float)((double)R.top - ((double)b1 + 1.01) * wide) - slack;
+        };
+        interval(0, true, d0, d1);
+        interval(1, use_p, p0, p1);
+        interval(2, use_k, bin_k, bin_k);
+        interval(3, use_m, bin_m0, bin_m1);
     }
-    // a first look in fp32: the logits between the first and the last of these bins, and a hundredth of a bin more
-    uint32_t b0 = d0, b1 = d1;
-    if (use_k) { b0 = min(b0, bin_k); b1 = max(b1, bin_k); }
-    if (use_p) { b0 = min(b0, p0); b1 = max(b1, p1); }
-    if (use_m) { b0 = min(b0, bin_m0); b1 = max(b1, bin_m1); }
-    const double wide = R.per > 0.0 ? 1024.0 / R.per : 0.0;
-    const float hi = b0 == 0 ? R.top : (float)((double)R.top - ((double)b0 - 0.01) * wide) + fabsf(R.top) * 0x1p-22f;
-    const float lo = R.per == 0.0 || b1 == kSmpBins - 1 ? -3.402823466e38f : (float)((double)R.top - ((double)b1 + 1.01) * wide) - fabsf(R.top) * 0x1p-22f;
-    for_tokens<F32, kSmpThreads>(row, 0, vocab, [&](float x, int i) {
-        if (x <= hi && x >= lo && in_question(place_of(R, x) >> 10)) L.list[atomicAdd(&L.n_list, 1u)] = entry_of(x, i);
+    auto look = [&](float x) {
+        bool yes = x <= hi[0] && x >= lo[0];
+        if (use_p) yes |= x <= hi[1] && x >= lo[1];
+        if (use_k) yes |= x <= hi[2] && x >= lo[2];
+        if (use_m) yes |= x <= hi[3] && x >= lo[3];
+        return yes;
+    };
+    for_tokens<F32, kSmpThreads, 8>(row, 0, vocab, [&](const u32x4 (&w)[8], int n, int id) {
+        constexpr int E = F32 ? 4 : 8;
+        uint64_t hits = 0;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            uint32_t h = 0;
+#pragma unroll
+            for (int e = 0; e < E; ++e) h |= (uint32_t)look(element<F32>(w[u], e)) << e;
+            if (u < n) hits |= (uint64_t)h << (u * E);
+        }
+        const int mine = __builtin_popcountll(hits);
+        if (mine == 0) return;
+        uint32_t at = atomicAdd(&L.n_list, (uint32_t)mine);
+        for (; hits; hits &= hits - 1, ++at) {
+            const int k = __builtin_ctzll(hits);
+            if (at < kSmpList) L.id[at] = (uint32_t)(id + (k / E) * kSmpThreads * E + k % E);
+        }
+    }, [&](float x, int i) {
+        if (!look(x)) return;
+        const uint32_t at = atomicAdd(&L.n_list, 1u);
+        if (at < kSmpList) L.id[at] = (uint32_t)i;
     });
     __syncthreads();
+    if (L.n_list > kSmpList) return false;
+    for (uint32_t j = tid; j < L.n_list; j += kSmpThreads) {
+        const float x = logit_at<F32>(row, (int)L.id[j]);
+        L.key[j] = order_key(x);
+        L.place[j] = place_of(R, x);
+    }
+    __syncthreads();
 
-    // ---- the filters, exactly
+    // ---- exactly: top_k, top_p and, behind min_p, the draw; one after the other through the same code
     uint32_t kept = n_live;
     uint64_t mass = total;
-    if (use_k) {
-        const End e = end_in_bin(L, R, table, bin_k, (uint32_t)q.top_k, 0);
-        if (!e.ok) return slow();
-        kept = e.count;
-        mass = e.mass;
-    }
-    auto bin_of_mass = [&](uint64_t want) {                  // by all threads
-        if (holds_mass(want)) L.found[5] = tid;
-        __syncthreads();
-        const uint32_t b = L.found[5];
-        __syncthreads();
-        return b;
-    };
-    if (use_p) {
-        const uint64_t want = mass_wanted(q.top_p, mass);
-        const End e = end_in_bin(L, R, table, bin_of_mass(want), 0, want);
-        if (!e.ok) return slow();
-        kept = e.count;
-        mass = e.mass;
-    }
-    if (use_m) {
-        uint32_t above = 0;
-        uint64_t am = 0;
-        for (uint32_t i = tid; i < L.n_list; i += kSmpThreads) {
-            const float x = entry_logit(L.list[i]);
-            const uint32_t b = place_of(R, x) >> 10;
-            if (b >= bin_m0 && b <= bin_m1 && above_min_p(R, x, q.min_p)) { above++; am += weight_of(R, table, x); }
+#pragma unroll 1
+    for (int stage = use_k ? 0 : use_p ? 1 : 2; stage < 3; stage += stage == 0 && !use_p ? 2 : 1) {
+        uint64_t want = 0;
+        uint32_t bin = bin_k;
+        if (stage == 2 && use_m) {
+            uint32_t above = 0;
+            uint64_t am = 0;
+            for (uint32_t i = tid; i < L.n_list; i += kSmpThreads) {
+                const float x = key_logit(L.key[i]);
+                const uint32_t b = L.place[i] >> 10;
+                if (b >= bin_m0 && b <= bin_m1 && above_min_p(R, x, q.min_p)) { above++; am += weight_of(R, table, x); }
+            }
+            above = wg_sum<uint32_t>(above, L.red_i) + (bin_m0 ? L.upto[bin_m0 - 1] : 0);
+            am = wg_sum<uint64_t>(am, L.red) + mass_in_front(bin_m0);
+            if (q.min_p > 1.f) { above = 1; am = kTopWeight; }
+            if (above < kept) { kept = above; mass = am; }
         }
-        above = wg_sum<uint32_t>(above, L.red_i) + (bin_m0 ? L.upto[bin_m0 - 1] : 0);
-        am = wg_sum<uint64_t>(am, L.red) + mass_in_front(bin_m0);
-        if (q.min_p > 1.f) { above = 1; am = kTopWeight; }
-        if (above < kept) { kept = above; mass = am; }
-        __syncthreads();
+        if (stage > 0) {
+            want = stage == 1 ? mass_wanted(q.top_p, mass) : draw_wanted(q.u, mass);
+            __syncthreads();
+            if (holds_mass(want)) L.found[5] = tid;
+            __syncthreads();
+            bin = L.found[5];
+        }
+        const End e = end_in_bin(L, R, table, vocab, bin, stage == 0 ? (uint32_t)q.top_k : 0, want, stage == 2);
+        if (!e.ok) return false;
+        if (stage == 2) {
+            *out = Drawn{~(uint32_t)e.entry, kept, log_share(R, entry_logit(e.entry), mass)};
+        } else {
+            kept = e.count;
+            mass = e.mass;
+        }
     }
-    const uint64_t want = draw_wanted(q.u, mass);
-    const End e = end_in_bin(L, R, table, bin_of_mass(want), 0, want);
-    if (!e.ok) return slow();
-    answer((int32_t)~(uint32_t)e.entry, log_share(R, entry_logit(e.entry), mass), kept);
+    return true;
+}
+
+template <bool F32, bool WHOLE>
+__global__ __launch_bounds__(kSmpThreads) void sample_row_kernel(SampleArgs a)
+{
+    __shared__ RowLds lds;
+    __shared__ double table[1024];
+    FastLds &L = lds.f;
+    fill_powers(table);                                      // (the first barrier is in front of its first use)
+    const int tid = (int)threadIdx.x, r = (int)blockIdx.x, vocab = a.S.vocab;
+    const etc_serving_sample_io &io = a.io;
+    const void *row = row_of<F32>(a, r);
+    Settings q;
+    q.T = io.temperature ? *as_global(io.temperature + r) : 1.f;
+    q.top_k = io.top_k ? gld_i32(io.top_k + r) : 0;
+    q.top_p = io.top_p ? *as_global(io.top_p + r) : 1.f;
+    q.min_p = io.min_p ? *as_global(io.min_p + r) : 0.f;
+    q.u = *as_global(io.u + r);
+    auto answer = [&](int32_t token, float logprob, uint32_t kept) {
+        if (tid != 0) return;
+        *as_global(io.token_out + r) = token;
+        if (io.logprob_out) gst_f32(io.logprob_out + r, logprob);
+        if (io.kept_out) *as_global(io.kept_out + r) = (int32_t)kept;
+    };
+    RowStats st;
+    if constexpr (WHOLE) st = row_stats<F32, kSmpThreads>(row, 0, vocab, lds.stats);
+    else st = join_stats(a, r);
+    if (st.live == 0) return answer(-1, -INFINITY, 0);
+    if (!(q.T > 0.f)) return answer((int32_t)st.first, 0.f, 1);
+    const RowScale R = scale_of(st, q.T);
+    Drawn drawn;
+    if (R.top == INFINITY || !fast_row<F32, WHOLE>(a, L, row, R, table, q, r, &drawn)) {
+        __syncthreads();
+        drawn = slow_row<F32>(lds.s, row, vocab, R, table, st.live, q);
+    }
+    answer((int32_t)drawn.id, drawn.logprob, drawn.kept);
 }
 
 // Slices of a row: as many as give kSmpWgs workgroups, of 2048 tokens at least, and of kBinTokens at most.
