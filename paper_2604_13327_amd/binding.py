@@ -474,25 +474,23 @@ class EventGraph(_Ctx):
         return self.read_debug(DBG_TASK_EXEC_COUNT, 0, np.zeros(self.step_info().n_tasks, np.int32))
 
 
-def _tensor(t, name, dtypes, shape, strided=False):
-    """Checks one tensor argument (None in `shape`: any size) and returns its device pointer.  A row of a strided tensor has no gaps."""
-    import torch
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} must be a tensor of the current GPU")
-    if str(t.dtype).replace("torch.", "") not in dtypes:
-        raise ValueError(f"{name} must be one of {dtypes}, not {t.dtype}")
-    if t.dim() != len(shape) or any(n is not None and t.shape[i] != n for i, n in enumerate(shape)):
-        raise ValueError(f"{name} must have the shape {tuple('any' if n is None else n for n in shape)}, not {tuple(t.shape)}")
-    if strided:
-        if t.shape[-1] > 1 and t.stride(-1) != 1:
-            raise ValueError(f"{name}: the elements of a row must be neighbours")
-    elif not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    return t.data_ptr()
+def _tensor(t, name, dtype, shape, device):
+    """Checks a tensor argument and returns its device pointer: contiguous, of one of the types `dtype` (a tuple) and of the shape, on
+    the handle's device.  The checks of a call's tensors are most of its host time, so the good case is one expression."""
+    if t.dtype in dtype and t.shape == shape and t.get_device() == device and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name} must be a contiguous tensor of shape {tuple(shape)} and one of the types {dtype} on the current GPU, not "
+                     f"{tuple(t.shape)} (strides {t.stride()}), {t.dtype}, on {t.device}")
 
 
-def _row_stride(t):
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[-1])
+def _rows(t, name, dtype, shape, device):
+    """The same for a matrix whose rows may be parts of wider ones: (pointer, distance of the rows in elements)."""
+    if t.dtype in dtype and t.shape == shape and t.get_device() == device:
+        rows, step = t.stride()
+        if step == 1 or shape[1] == 1:
+            return t.data_ptr(), rows if shape[0] > 1 else max(rows, shape[1])
+    raise ValueError(f"{name} must be a matrix of shape {tuple(shape)} and one of the types {dtype}, the elements of a row neighbours, on "
+                     f"the current GPU, not {tuple(t.shape)} (strides {t.stride()}), {t.dtype}, on {t.device}")
 
 
 class Serving:
@@ -502,6 +500,7 @@ class Serving:
     stream at a time."""
 
     def __init__(self, shape, max_seqs: int, max_tokens: int, max_kv_len: int):
+        import torch
         self._L = lib()
         self._h = C.c_void_p()
         self.shape = shape
@@ -509,9 +508,14 @@ class Serving:
         st = self._L.etc_serving_create(C.byref(md), C.byref(limits), C.byref(self._h))
         if st != 0:
             raise EtcError(st, self._L.etc_serving_last_error(None).decode())
+        self._device = torch.cuda.current_device()
+        self._stream = torch._C._cuda_getCurrentRawStream
+        self._i32, self._f32, self._bf16 = (torch.int32,), (torch.float32,), (torch.bfloat16,)
+        self._float = (torch.bfloat16, torch.float32)
+        self._code = {torch.bfloat16: 0, torch.float32: 1}
 
     def _call(self, fn, io, stream):
-        st = fn(self._h, C.byref(io), _stream_ptr(stream))
+        st = fn(self._h, C.byref(io), self._stream(self._device) if stream is None else stream.cuda_stream)
         if st != 0:
             raise EtcError(st, self._L.etc_serving_last_error(self._h).decode())
 
@@ -538,68 +542,61 @@ class Serving:
                free_count_out=None, total_len=None, page_indptr=None, page_ids=None, stream=None):
         """Grows block_table [seqs, pages] (in place) for new_len tokens per sequence and maps every new token to its slot and
         position; int32 tensors.  free_count_out: free_count unless given."""
-        i32, n = ("int32",), kv_len.shape[0]
-        opt = lambda t, name, shape: None if t is None else _tensor(t, name, i32, shape)      # noqa: E731
+        i32, dev, n, rows = self._i32, self._device, kv_len.shape[0], slots.shape[0]
+        cols, free, ids = block_table.shape[-1], free_pages.shape[0], 0 if page_ids is None else page_ids.shape[0]
+        table, stride = _rows(block_table, "block_table", i32, (n, cols), dev)
         io = ServingTablesIo(
-            n_seqs=n, n_tokens=slots.shape[0], kv_len=_tensor(kv_len, "kv_len", i32, (n,)), new_len=_tensor(new_len, "new_len", i32, (n,)),
-            block_table=_tensor(block_table, "block_table", i32, (n, None), strided=True), table_stride=_row_stride(block_table),
-            table_cols=block_table.shape[1], free_pages=_tensor(free_pages, "free_pages", i32, (None,)), free_cap=free_pages.shape[0],
-            free_count=_tensor(free_count, "free_count", i32, (1,)),
-            free_count_out=_tensor(free_count if free_count_out is None else free_count_out, "free_count_out", i32, (1,)),
-            q_indptr=_tensor(q_indptr, "q_indptr", i32, (n + 1,)), slots=_tensor(slots, "slots", i32, (None,)),
-            positions=_tensor(positions, "positions", i32, (slots.shape[0],)), total_len=opt(total_len, "total_len", (n,)),
-            page_indptr=opt(page_indptr, "page_indptr", (n + 1,)), page_ids=opt(page_ids, "page_ids", (None,)),
-            page_ids_cap=0 if page_ids is None else page_ids.shape[0], status=_tensor(status, "status", i32, (1,)))
+            n, rows, _tensor(kv_len, "kv_len", i32, (n,), dev), _tensor(new_len, "new_len", i32, (n,), dev), table, stride, cols,
+            _tensor(free_pages, "free_pages", i32, (free,), dev), free, _tensor(free_count, "free_count", i32, (1,), dev),
+            _tensor(free_count if free_count_out is None else free_count_out, "free_count_out", i32, (1,), dev),
+            _tensor(q_indptr, "q_indptr", i32, (n + 1,), dev), _tensor(slots, "slots", i32, (rows,), dev),
+            _tensor(positions, "positions", i32, (rows,), dev), None if total_len is None else _tensor(total_len, "total_len", i32, (n,), dev),
+            None if page_indptr is None else _tensor(page_indptr, "page_indptr", i32, (n + 1,), dev),
+            None if page_ids is None else _tensor(page_ids, "page_ids", i32, (ids,), dev), ids, _tensor(status, "status", i32, (1,), dev))
         self._call(self._L.etc_serving_tables, io, stream)
 
     def _pool(self, k_pages, v_pages):
-        s = self.shape
-        shape = (None, s.page, s.nkv, s.d)
-        k, v = _tensor(k_pages, "k_pages", ("bfloat16",), shape), _tensor(v_pages, "v_pages", ("bfloat16",), shape)
-        if k_pages.shape != v_pages.shape:
-            raise ValueError("k_pages and v_pages must have the same shape")
-        return k, v, k_pages.shape[0]
+        s, pages = self.shape, k_pages.shape[0]
+        shape = (pages, s.page, s.nkv, s.d)
+        return _tensor(k_pages, "k_pages", self._bf16, shape, self._device), _tensor(v_pages, "v_pages", self._bf16, shape, self._device), pages
 
     def append(self, q, k, v, positions, slots, q_out, k_pages, v_pages, gq=None, gk=None, stream=None):
         """Per-head norms (qk_norm models), RoPE and KV append of the rows of a QKV projection: q [tokens, nq * d], k and v
         [tokens, nkv * d], bf16 or fp32, rows may be parts of wider ones; q_out bf16 [tokens, nq, d]; pools of one layer."""
-        s, n = self.shape, q.shape[0]
-        kinds = ("bfloat16", "float32")
-        if k.dtype != q.dtype or v.dtype != q.dtype:
-            raise ValueError("q, k and v must have the same type")
+        s, n, dev, kind = self.shape, q.shape[0], self._device, (q.dtype,)
+        if q.dtype not in self._float:
+            raise ValueError(f"q, k and v must be bf16 or fp32, not {q.dtype}")
         kp, vp, pages = self._pool(k_pages, v_pages)
-        gain = lambda g, name: None if g is None else _tensor(g, name, ("bfloat16",), (s.d,))      # noqa: E731
+        qp, qs = _rows(q, "q", kind, (n, s.nq * s.d), dev)
+        kk, ks = _rows(k, "k", kind, (n, s.nkv * s.d), dev)
+        vv, vs = _rows(v, "v", kind, (n, s.nkv * s.d), dev)
         io = ServingAppendIo(
-            n_tokens=n, dtype=1 if q.element_size() == 4 else 0, q=_tensor(q, "q", kinds, (n, s.nq * s.d), strided=True),
-            k=_tensor(k, "k", kinds, (n, s.nkv * s.d), strided=True), v=_tensor(v, "v", kinds, (n, s.nkv * s.d), strided=True),
-            q_stride=_row_stride(q), k_stride=_row_stride(k), v_stride=_row_stride(v),
-            positions=_tensor(positions, "positions", ("int32",), (n,)), slots=_tensor(slots, "slots", ("int32",), (n,)),
-            gq=gain(gq, "gq"), gk=gain(gk, "gk"), q_out=_tensor(q_out, "q_out", ("bfloat16",), (n, s.nq, s.d)),
-            k_pages=kp, v_pages=vp, n_pages=pages)
+            n, self._code[q.dtype], qp, kk, vv, qs, ks, vs, _tensor(positions, "positions", self._i32, (n,), dev),
+            _tensor(slots, "slots", self._i32, (n,), dev), None if gq is None else _tensor(gq, "gq", self._bf16, (s.d,), dev),
+            None if gk is None else _tensor(gk, "gk", self._bf16, (s.d,), dev), _tensor(q_out, "q_out", self._bf16, (n, s.nq, s.d), dev),
+            kp, vp, pages)
         self._call(self._L.etc_serving_append, io, stream)
 
     def attention(self, q, out, q_indptr, kv_len, block_table, k_pages, v_pages, stream=None):
         """Attention of the new tokens q [tokens, nq, d] (bf16) of every sequence over its pages, the new tokens' own keys
         among them; out like q.  q_indptr [seqs + 1], kv_len [seqs] (tokens in front of the new ones), block_table [seqs, pages]."""
-        s, n = self.shape, kv_len.shape[0]
+        s, n, rows, dev, cols = self.shape, kv_len.shape[0], q.shape[0], self._device, block_table.shape[-1]
         kp, vp, pages = self._pool(k_pages, v_pages)
+        table, stride = _rows(block_table, "block_table", self._i32, (n, cols), dev)
         io = ServingAttentionIo(
-            n_seqs=n, n_tokens=q.shape[0], q=_tensor(q, "q", ("bfloat16",), (None, s.nq, s.d)),
-            out=_tensor(out, "out", ("bfloat16",), (q.shape[0], s.nq, s.d)), q_indptr=_tensor(q_indptr, "q_indptr", ("int32",), (n + 1,)),
-            kv_len=_tensor(kv_len, "kv_len", ("int32",), (n,)), block_table=_tensor(block_table, "block_table", ("int32",), (n, None), strided=True),
-            table_stride=_row_stride(block_table), table_cols=block_table.shape[1], k_pages=kp, v_pages=vp, n_pages=pages)
+            n, rows, _tensor(q, "q", self._bf16, (rows, s.nq, s.d), dev), _tensor(out, "out", self._bf16, (rows, s.nq, s.d), dev),
+            _tensor(q_indptr, "q_indptr", self._i32, (n + 1,), dev), _tensor(kv_len, "kv_len", self._i32, (n,), dev), table, stride, cols, kp, vp, pages)
         self._call(self._L.etc_serving_attention, io, stream)
 
     def sample(self, logits, u, token_out, temperature=None, top_k=None, top_p=None, min_p=None, logprob_out=None, kept_out=None,
                stream=None):
         """One token per row of logits [rows, vocab] (fp32 or bf16, rows may be parts of wider ones) from the random numbers
         u [rows] in [0, 1); settings are tensors [rows] (temperature, top_p, min_p fp32, top_k int32) or None."""
-        n = logits.shape[0]
-        opt = lambda t, name, kind: None if t is None else _tensor(t, name, (kind,), (n,))      # noqa: E731
+        n, dev, f32 = logits.shape[0], self._device, self._f32
+        opt = lambda t, name, kind: None if t is None else _tensor(t, name, kind, (n,), dev)      # noqa: E731
+        rows, stride = _rows(logits, "logits", self._float, (n, int(self.shape.vocab)), dev)
         io = ServingSampleIo(
-            n_rows=n, dtype=1 if logits.element_size() == 4 else 0,
-            logits=_tensor(logits, "logits", ("bfloat16", "float32"), (n, int(self.shape.vocab)), strided=True), row_stride=_row_stride(logits),
-            u=_tensor(u, "u", ("float32",), (n,)), temperature=opt(temperature, "temperature", "float32"), top_k=opt(top_k, "top_k", "int32"),
-            top_p=opt(top_p, "top_p", "float32"), min_p=opt(min_p, "min_p", "float32"), token_out=_tensor(token_out, "token_out", ("int32",), (n,)),
-            logprob_out=opt(logprob_out, "logprob_out", "float32"), kept_out=opt(kept_out, "kept_out", "int32"))
+            n, self._code[logits.dtype], rows, stride, _tensor(u, "u", f32, (n,), dev), opt(temperature, "temperature", f32),
+            opt(top_k, "top_k", self._i32), opt(top_p, "top_p", f32), opt(min_p, "min_p", f32),
+            _tensor(token_out, "token_out", self._i32, (n,), dev), opt(logprob_out, "logprob_out", f32), opt(kept_out, "kept_out", self._i32))
         self._call(self._L.etc_serving_sample, io, stream)

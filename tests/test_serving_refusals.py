@@ -34,25 +34,32 @@ def test_create_refuses_before_any_device_call():
             etc.Serving(ref.shape(), *limits)
 
 
-def test_binding_takes_gpu_tensors_only():
-    from paper_2604_13327_amd.binding import _tensor
-    with pytest.raises(ValueError, match="current GPU"):
-        _tensor(torch.zeros(3), "x", ("float32",), (3,))
+class OnGpu:
+    """A CPU tensor that says it is on GPU 0."""
+
+    def __init__(self, t):
+        self.t = t
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+    def get_device(self):
+        return 0
 
 
-def test_binding_checks(monkeypatch):
-    from paper_2604_13327_amd import binding
-
-    class Fake:
-        """A CPU tensor that says it is on the GPU."""
-        def __init__(self, t):
-            self.t, self.is_cuda, self.device = t, True, type("D", (), {"index": 0})
-        def __getattr__(self, name):
-            return getattr(self.t, name)
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+def test_binding_checks():
+    from paper_2604_13327_amd.binding import _rows, _tensor
+    f32 = (torch.float32,)
     t = torch.zeros(4, 6)
-    assert binding._tensor(Fake(t), "x", ("float32",), (4, 6)) == t.data_ptr()
-    assert binding._tensor(Fake(t[:, :3]), "x", ("float32",), (None, 3), strided=True) == t.data_ptr()
-    for bad, kw in ((t.double(), {}), (t[:3], {}), (t.t().contiguous().t(), {}), (t[:, None], {}), (t[:, ::2], {"shape": (4, 3), "strided": True})):
+    assert _tensor(OnGpu(t), "x", f32, (4, 6), 0) == t.data_ptr()
+    for bad in (t, OnGpu(t.double()), OnGpu(t[:3]), OnGpu(torch.zeros(6, 4).t()), OnGpu(t[:, None]), OnGpu(torch.zeros(4, 12)[:, ::2])):
         with pytest.raises(ValueError):
-            binding._tensor(Fake(bad), "x", ("float32",), kw.pop("shape", (4, 6)), **kw)
+            _tensor(bad, "x", f32, (4, 6), 0)
+    with pytest.raises(ValueError):
+        _tensor(OnGpu(t), "x", f32, (4, 6), 1)
+    wide = torch.zeros(4, 9)
+    assert _rows(OnGpu(wide[:, 1:4]), "x", f32, (4, 3), 0) == (wide.data_ptr() + 4, 9)
+    assert _rows(OnGpu(wide[:1, :3]), "x", f32, (1, 3), 0)[1] >= 3
+    for bad in (wide[:, :3], OnGpu(wide[:, ::3]), OnGpu(wide[:, :4]), OnGpu(wide[:, :3].int())):
+        with pytest.raises(ValueError):
+            _rows(bad, "x", f32, (4, 3), 0)
