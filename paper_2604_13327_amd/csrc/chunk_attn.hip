@@ -336,6 +336,10 @@ __device__ __forceinline__ void fetch_1k(const char *from, uint32_t to)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory");
 }
+__device__ __forceinline__ void fetch_1k(const char *base, uint32_t lane_off, uint32_t to)      // base the same for the wavefront
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(lane_off), "s"(base) : "memory");
+}
 template <int N> __device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(%0)" : : "i"(N) : "memory"); }
 
 // LDS of a piece: rows of K and V, and the ids of its pages, a window of them at a time.
@@ -395,26 +399,62 @@ struct PageWindow {
     }
 };
 
-// Fetches a tile's rows, KEYS of K to LDS at kb and of V at vb: load u of a wavefront brings RPL rows of each.  A lane's place in LDS is
-// given, so it is the piece of memory that belongs there which it chooses.  Rows behind the last key are that key's again (their
-// scores are masked).
+// Fetches rows of the cache, KEYS of K and of V at a time, the first key a multiple of 64: load u of a wavefront brings RPL rows of
+// each.  A lane's place in LDS is given, so it is the piece of memory that belongs there which it chooses.  Rows behind the last key
+// are that key's again (their scores are masked).
+// Where the rows of a load lie in one page (pages of RPL tokens and more) its address is a scalar and a constant of the lane: no vector
+// instruction at all.  (With addresses per lane, and their page ids read from LDS on the spot, the fetches cost the long prompt 16 %.)
 template <int D, int KEYS>
-__device__ __forceinline__ void fetch_rows(const ServingDev &S, const etc_serving_attention_io &io, ETC_AS_LDS const Tiles<D> &B, int first_page, int key0, int last_key,
-                                           int kvh, int wave, int lane, uint32_t kb, uint32_t vb)
-{
-    constexpr int CH = D / 8, RPL = 64 / CH, LOADS = KEYS / RPL / kCaWaves;
-    const uint32_t row_bytes = (uint32_t)(S.nkv * D * 2);
-    const uint64_t page_bytes = (uint64_t)row_bytes << S.page_shift;
-    const int lrow = lane / CH, c = lane % CH, pmask = (1 << S.page_shift) - 1;
+struct Fetch {
+    static constexpr int CH = D / 8, RPL = 64 / CH, LOADS = KEYS / RPL / kCaWaves;
+    const etc_serving_attention_io &io;
+    ETC_AS_LDS const Tiles<D> &B;
+    int psh, pmask, wave, lrow, c, last_key;
+    uint32_t row_bytes, head_off;
+    uint32_t k_off[LOADS], v_off[LOADS];    // of the lane, from the page's row of the load's 64 keys on
+    int id[LOADS];                          // page ids of the next fetch, asked for ahead of it
+    __device__ __forceinline__ Fetch(const ServingDev &S, const etc_serving_attention_io &io_, ETC_AS_LDS const Tiles<D> &B_, int kvh, int last, int wave_, int lane)
+        : io(io_), B(B_), psh(S.page_shift), pmask((1 << S.page_shift) - 1), wave(wave_), lrow(lane / CH), c(lane % CH), last_key(last),
+          row_bytes((uint32_t)(S.nkv * D * 2)), head_off((uint32_t)(kvh * D * 2))
+    {
 #pragma unroll
-    for (int u = 0; u < LOADS; ++u) {
-        const int r = (wave * LOADS + u) * RPL, key = min(key0 + r + lrow, last_key);
-        const uint32_t id = (uint32_t)B.ids[(key >> S.page_shift) - first_page];
-        const uint64_t off = id * page_bytes + (uint64_t)((uint32_t)(key & pmask)) * row_bytes + kvh * D * 2;
-        fetch_1k((const char *)io.k_pages + (off + (uint32_t)((c ^ k_swap<D>(r + lrow)) * 16)), kb + r * D * 2);
-        fetch_1k((const char *)io.v_pages + (off + (uint32_t)((c ^ v_swap<D>(r + lrow)) * 16)), vb + r * D * 2);
+        for (int u = 0; u < LOADS; ++u) {
+            const int r = row_of(u) + lrow;
+            const uint32_t in_page = (uint32_t)((r & 63) & pmask) * row_bytes + head_off;
+            k_off[u] = in_page + (uint32_t)((c ^ k_swap<D>(r)) * 16);
+            v_off[u] = in_page + (uint32_t)((c ^ v_swap<D>(r)) * 16);
+        }
     }
-}
+    __device__ __forceinline__ int row_of(int u) const { return (wave * LOADS + u) * RPL; }
+    __device__ __forceinline__ bool whole(int key0) const { return pmask + 1 >= RPL && key0 + KEYS - 1 <= last_key; }
+    __device__ __forceinline__ void ask(int key0, int first_page)      // (nothing where each lane looks up its own)
+    {
+        if (!whole(key0)) return;
+#pragma unroll
+        for (int u = 0; u < LOADS; ++u) id[u] = B.ids[((key0 + row_of(u)) >> psh) - first_page];
+    }
+    __device__ __forceinline__ void fetch(int key0, int first_page, uint32_t kb, uint32_t vb)
+    {
+        const uint64_t page_bytes = (uint64_t)row_bytes << psh;
+        if (whole(key0)) {
+#pragma unroll
+            for (int u = 0; u < LOADS; ++u) {
+                const int r = row_of(u);
+                const uint64_t off = (uint32_t)__builtin_amdgcn_readfirstlane(id[u]) * page_bytes + (uint64_t)(uint32_t)((key0 + (r & ~63)) & pmask) * row_bytes;
+                fetch_1k((const char *)io.k_pages + off, k_off[u], kb + r * D * 2);
+                fetch_1k((const char *)io.v_pages + off, v_off[u], vb + r * D * 2);
+            }
+        } else {
+#pragma unroll 1
+            for (int u = 0; u < LOADS; ++u) {
+                const int r = row_of(u), key = min(key0 + r + lrow, last_key);
+                const uint64_t off = (uint32_t)B.ids[(key >> psh) - first_page] * page_bytes + (uint64_t)((uint32_t)(key & pmask)) * row_bytes + head_off;
+                fetch_1k((const char *)io.k_pages + (off + (uint32_t)((c ^ k_swap<D>(r + lrow)) * 16)), kb + r * D * 2);
+                fetch_1k((const char *)io.v_pages + (off + (uint32_t)((c ^ v_swap<D>(r + lrow)) * 16)), vb + r * D * 2);
+            }
+        }
+    }
+};
 
 // Piece cc (of D / 8) of a lane's row: elements 8 cc + 4 half + 0 .. 3 of row r of the sequence and KV head.
 template <int D>
@@ -487,10 +527,9 @@ __device__ __forceinline__ void join_parts(const ServingDev &S, const etc_servin
     }
 }
 
-// A block of more than 64 rows: 32 of them to a wavefront, all wavefronts over the same tiles of 64 keys.
-// Tile t has K in ring slot t % 3 and V in t % 4: while the rows of t + 2 are on their way, t + 1 has arrived or is about to, t is being
-// read, and so is, by half the wavefronts, V of t - 1.
-constexpr int kCaKSlots = 3, kCaVSlots = 4;
+// A block of more than 64 rows: 32 of them to a wavefront, all wavefronts over the same tiles of 64 keys, in ring slot t % 3: while
+// tile t is being read, t + 1 has arrived or is about to, and the rows of t + 2 are on their way.
+constexpr int kCaSlots = 3;
 
 template <int D>
 __device__ __forceinline__ void wide_piece(const ServingDev &S, const etc_serving_attention_io &io, ETC_AS_LDS CaLds &L, ETC_AS_LDS Tiles<D> &B, const Piece &P)
@@ -498,7 +537,7 @@ __device__ __forceinline__ void wide_piece(const ServingDev &S, const etc_servin
     constexpr int KS = D / 16, DT = D / 32;              // steps of the first product, tiles of the output
     constexpr int RPL = 512 / D, LOADS = kCaKeys / RPL / kCaWaves;      // rows of a load; loads of K (and of V) a wavefront has in a tile
     constexpr uint32_t BUF = kCaKeys * D * 2;            // bytes of a tile
-    static_assert((kCaKSlots + kCaVSlots) * kCaKeys <= 512, "LDS");
+    static_assert(2 * kCaSlots * kCaKeys <= 512, "LDS");
     int tid = (int)threadIdx.x;
     asm volatile("" : "+v"(tid));                        // of this piece: what is computed from it does not stay in registers across pieces
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, half = lane >> 5, col = lane & 31;
@@ -516,10 +555,8 @@ __device__ __forceinline__ void wide_piece(const ServingDev &S, const etc_servin
     const int first_masked = (P.seq.kv + P.r0 / P.grp + 1) / kCaKeys;      // tiles in front of it are seen whole by all rows of the block
     const int wave_last = P.seq.kv + min((P.r0 + wave * 32 + 31) / P.grp, P.seq.n - 1);
     const bool wave_live = P.r0 + wave * 32 < P.rows;
-    const uint32_t k_base = (uint32_t)(uintptr_t)&B.rows[0], v_base = k_base + kCaKSlots * BUF;
-    auto fetch = [&](int tile, uint32_t kb, uint32_t vb) {
-        fetch_rows<D, kCaKeys>(S, io, B, W.first, tile * kCaKeys, P.n_keys - 1, P.kvh, wave, lane, k_base + kb, v_base + vb);
-    };
+    const uint32_t k_base = (uint32_t)(uintptr_t)&B.rows[0], v_base = k_base + kCaSlots * BUF;
+    Fetch<D, kCaKeys> G(S, io, B, P.kvh, P.n_keys - 1, wave, lane);
 
     f32x16 o[DT];
 #pragma unroll
@@ -532,12 +569,19 @@ __device__ __forceinline__ void wide_piece(const ServingDev &S, const etc_servin
     if (tid == 0) L.odd = -1;
     drain_vmem();                                        // nothing but tiles on their way from here on
     __syncthreads();
-    uint32_t kb = 0, vb = 0, vb_before = 0;              // ring slots of the tile at hand; of V also of the one before
+    uint32_t at = 0;                                     // ring slot of the tile at hand
     auto covered = [&](int tile) { return min((tile + 1) * kCaKeys, key_end) <= W.end; };
-    auto after = [](uint32_t at, int slots) { return at == (slots - 1) * BUF ? 0u : at + BUF; };
-    fetch(tile0, 0, 0);
-    if (tile0 + 1 < n_tiles && covered(tile0 + 1)) { fetch(tile0 + 1, BUF, BUF); arrived<2 * LOADS>(); }
-    else arrived<0>();
+    auto after = [](uint32_t a) { return a == (kCaSlots - 1) * BUF ? 0u : a + BUF; };
+    G.ask(tile0 * kCaKeys, W.first);
+    G.fetch(tile0 * kCaKeys, W.first, k_base, v_base);
+    if (tile0 + 1 < n_tiles && covered(tile0 + 1)) {
+        G.ask((tile0 + 1) * kCaKeys, W.first);
+        G.fetch((tile0 + 1) * kCaKeys, W.first, k_base + BUF, v_base + BUF);
+        arrived<2 * LOADS>();
+    } else {
+        arrived<0>();
+    }
+    if (tile0 + 2 < n_tiles && covered(tile0 + 2)) G.ask((tile0 + 2) * kCaKeys, W.first);
     __syncthreads();
     // In front of a tile's work: the rows of the tile two behind it go on their way.  Behind it: the next tile's have arrived, for all.
     auto ahead = [&](int tile) {
@@ -547,59 +591,46 @@ __device__ __forceinline__ void wide_piece(const ServingDev &S, const etc_servin
                 W.load(S, io, B, P.b, (tile + 2) * kCaKeys, key_end, tid);
                 drain_vmem();
                 __syncthreads();
+                G.ask((tile + 2) * kCaKeys, W.first);
             }
-            fetch(tile + 2, after(after(kb, kCaKSlots), kCaKSlots), after(after(vb, kCaVSlots), kCaVSlots));
+            const uint32_t to = after(after(at));
+            G.fetch((tile + 2) * kCaKeys, W.first, k_base + to, v_base + to);
+            if (tile + 3 < n_tiles && covered(tile + 3)) G.ask((tile + 3) * kCaKeys, W.first);
         }
     };
     auto next = [&](int tile) {
         if (tile + 2 < n_tiles) arrived<2 * LOADS>(); else arrived<0>();
         __syncthreads();
-        kb = after(kb, kCaKSlots);
-        vb_before = vb;
-        vb = after(vb, kCaVSlots);
+        at = after(at);
     };
-    // Two wavefronts share a SIMD, w and w + 4.  The barrier of every tile would have both at their products and both at their
-    // exponentials at the same time; so the second four are half a tile behind: they end a tile in front of the scores of the next.
     int tile = tile0;
     const int n_seen = min(first_masked, n_tiles);
-    if (wave < kCaWaves / 2) {
-        for (; tile < n_seen; ++tile) {
-            ahead(tile);
-            if (wave_live) {
-                scores<D, 2>(s, F, k_base + kb, qf);
-                attend<D, 2, false>(s, o, m, l, F, v_base + vb, half, scale, 0, 0);
-            }
-            next(tile);
+    for (; tile < n_seen; ++tile) {
+        ahead(tile);
+        if (wave_live) {
+            scores<D, 2>(s, F, k_base + at, qf);
+            attend<D, 2, false>(s, o, m, l, F, v_base + at, half, scale, 0, 0);
         }
-    } else {
-        for (; tile < n_seen; ++tile) {
-            ahead(tile);
-            if (wave_live) {
-                if (tile > tile0) attend<D, 2, false>(s, o, m, l, F, v_base + vb_before, half, scale, 0, 0);
-                scores<D, 2>(s, F, k_base + kb, qf);
-            }
-            next(tile);
-        }
-        if (wave_live && tile > tile0) attend<D, 2, false>(s, o, m, l, F, v_base + vb_before, half, scale, 0, 0);
+        next(tile);
     }
     for (; tile < n_tiles; ++tile) {
         ahead(tile);
         u32x4 mine[LOADS];
-        uint32_t at[LOADS];
+        uint32_t mine_at[LOADS];
         bool odd = false;                                // values that are no numbers, in any row of the tile
 #pragma unroll
         for (int u = 0; u < LOADS; ++u) {
-            at[u] = v_base + vb + (wave * LOADS + u) * RPL * D * 2 + lane * 16;
-            mine[u] = *reinterpret_cast<ETC_AS_LDS const u32x4 *>(at[u]);
+            mine_at[u] = v_base + at + (wave * LOADS + u) * RPL * D * 2 + lane * 16;
+            mine[u] = *reinterpret_cast<ETC_AS_LDS const u32x4 *>(mine_at[u]);
             odd |= any_odd(mine[u]);
         }
         if (odd) L.odd = tile;
         __syncthreads();
         const bool live = wave_live && tile * kCaKeys <= wave_last;
-        if (__builtin_expect(L.odd == tile, 0)) odd_values<D, kCaKeys, LOADS>(mine, at, o, F, v_base + vb, half, tile * kCaKeys, limit, live);
+        if (__builtin_expect(L.odd == tile, 0)) odd_values<D, kCaKeys, LOADS>(mine, mine_at, o, F, v_base + at, half, tile * kCaKeys, limit, live);
         if (live) {
-            scores<D, 2>(s, F, k_base + kb, qf);
-            attend<D, 2, true>(s, o, m, l, F, v_base + vb, half, scale, tile * kCaKeys, limit);
+            scores<D, 2>(s, F, k_base + at, qf);
+            attend<D, 2, true>(s, o, m, l, F, v_base + at, half, scale, tile * kCaKeys, limit);
         }
         next(tile);
     }
@@ -657,10 +688,12 @@ __device__ __forceinline__ void narrow_piece(const ServingDev &S, const etc_serv
     const int all_see = min(P.seq.kv + 1, key_end);      // keys in front of it are seen by all rows
     const bool live = rw * 32 < P.rows;
     const uint32_t base = (uint32_t)(uintptr_t)&B.rows[0];
+    Fetch<D, KEYS> G(S, io, B, P.kvh, key_end - 1, wave, lane);
     auto fetch = [&](int step) {
-        const uint32_t at = base + (step & 1) * 2 * BUF;
-        fetch_rows<D, KEYS>(S, io, B, W.first, key0 + step * KEYS, key_end - 1, P.kvh, wave, lane, at, at + BUF);
+        const uint32_t to = base + (step & 1) * 2 * BUF;
+        G.fetch(key0 + step * KEYS, W.first, to, to + BUF);
     };
+    auto ask = [&](int step) { G.ask(key0 + step * KEYS, W.first); };
     auto covered = [&](int step) { return min(key0 + (step + 1) * KEYS, key_end) <= W.end; };
 
     f32x16 o[DT];
@@ -673,9 +706,11 @@ __device__ __forceinline__ void narrow_piece(const ServingDev &S, const etc_serv
     if (tid == 0) L.odd = -1;
     drain_vmem();                                        // nothing but rows on their way from here on
     __syncthreads();
+    ask(0);
     fetch(0);
-    if (n_steps > 1 && covered(1)) { fetch(1); arrived<2 * LOADS>(); }
+    if (n_steps > 1 && covered(1)) { ask(1); fetch(1); arrived<2 * LOADS>(); }
     else arrived<0>();
+    if (n_steps > 2 && covered(2)) ask(2);
     __syncthreads();
     for (int step = 0; step < n_steps; ++step) {
         const int k0 = key0 + step * KEYS;
@@ -712,8 +747,10 @@ __device__ __forceinline__ void narrow_piece(const ServingDev &S, const etc_serv
                 W.load(S, io, B, P.b, k0 + 2 * KEYS, key_end, tid);
                 drain_vmem();
                 __syncthreads();
+                ask(step + 2);
             }
             fetch(step + 2);
+            if (step + 3 < n_steps && covered(step + 3)) ask(step + 3);
             arrived<2 * LOADS>();
         } else {
             arrived<0>();
