@@ -21,6 +21,7 @@ constexpr int kCaWaves = 8, kCaThreads = kCaWaves * 64;
 constexpr int kCaRows = 32 * kCaWaves;      // rows of a block
 constexpr int kCaKeys = 64;                 // keys of a tile
 constexpr int kCaMinTiles = 2;              // of a piece, where keys are cut
+constexpr int kCaNarrowRows = 64, kCaNarrowKeys = 128;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float partner_max(float x)      // with lane + 32
@@ -51,22 +52,24 @@ __device__ __forceinline__ int last_not_above(ETC_AS_LDS const int *indptr, int 
 }
 
 // ---- how a call is cut into pieces ---------------------------------------------------------------------------------------
-// An item is (sequence, block of rows, KV head).  The keys of every item of a sequence are cut into the same number of pieces,
-// whole tiles each; workgroup w of the launch takes the pieces w, w + grid, ...  Every workgroup computes the cut by itself
-// from the lengths, one sequence to a thread: pieces of at most L tiles, with the L out of kCaTries that is estimated to end
-// first.  KV heads are the fastest index of a piece: neighbouring workgroups, on different dies, take different heads, and a
-// die's L2 sees the keys of one or two.
+// An item is (sequence, block of rows, KV head).  Its keys are cut into pieces of at most L tiles, about equal ones, with the L out of
+// kCaTries that is estimated to end first; every workgroup computes this by itself from the lengths, one sequence to a thread.  A
+// sequence's long blocks come first, and workgroups take pieces forwards and backwards in turn, so that their sums come out about
+// equal: a chunk of 4096 (512 pieces of 1 to 64 tiles) takes 146 us, 188 where every workgroup takes piece w + 256 after piece w, 164
+// from a queue of pieces.  KV heads are the fastest index of a piece: neighbouring workgroups, on different dies, take different heads,
+// and a die's L2 sees the keys of one or two.
 constexpr int kCaTries = kCaWaves;          // a wavefront estimates one
 
 struct Seq { int q0, n, kv; };             // first row, new tokens, cached ones
 
 struct CaLds {
     int q0[kServingMaxSeqs], n[kServingMaxSeqs], kv[kServingMaxSeqs];      // n == 0: nothing to do
-    int split[kServingMaxSeqs];             // pieces of an item
+    int split[kServingMaxSeqs];             // pieces of the longest item
     int first[kServingMaxSeqs + 1];         // prefix sum: pieces of the sequences
     int slot[kServingMaxSeqs + 1];          // prefix sum: those that leave a partial result
     float wave_f[kCaWaves];
     int wave_i[2][kCaWaves];
+    int limit;                              // tiles of a piece
     int odd, last;
 };
 
@@ -114,31 +117,36 @@ __device__ __forceinline__ int cut(const ServingDev &S, const etc_serving_attent
         if (blockIdx.x == 0 && tid == 0) refuse(S.error, SRV_BAD_LENGTH, SRV_ATTENTION, io.n_seqs, tokens);
         return 0;
     }
-    // Candidate of wavefront w: no cut, or pieces of 1.5, 1, 2/3, 1/2, 1/3, 1/4, 1/6 of a workgroup's share, kCaMinTiles at least.  All in
-    // tiles: a piece costs its tiles and 3 more; a partial result is written and read again, 1 or (a whole block) 5 more, and where there
-    // are any the end waits for the last join, 5 more.
+    // Candidate of wavefront w: no cut, or pieces of 4, 3, 2, 1.5, 1.25, 1.1, 1 times a workgroup's share, kCaMinTiles at least.  In tiles
+    // (1.8 us): a piece costs its tiles and 1 more; a call ends with its longest piece or, where some workgroup takes several, after as
+    // many of them; the last join then reads half a tile's time a part, and 9 more where a whole block is joined.  Fitted to the times of
+    // all candidates in 17 calls (1 to 64 sequences, chunks of 1 to 8192, caches to 32768): what it chooses is 0.8 % behind the fastest
+    // in the mean, 3 % at worst.  The shortest pieces are the fastest for 30 sequences with two prompts (66 us, 81 without a cut), the
+    // longest for one token of one sequence (18 and 58), 1.1 for a chunk of 512 behind 8000 keys (89 and 242).
     const float share = work / (float)grid;
     auto limit_of = [&](int w) {
-        const float f = w == 1 ? 1.5f : w == 2 ? 1.f : w == 3 ? 0.6667f : w == 4 ? 0.5f : w == 5 ? 0.3333f : w == 6 ? 0.25f : 0.1667f;
+        const float f = w == 1 ? 4.f : w == 2 ? 3.f : w == 3 ? 2.f : w == 4 ? 1.5f : w == 5 ? 1.25f : w == 6 ? 1.1f : 1.f;
         return w == 0 ? 1 << 30 : max(kCaMinTiles, (int)fminf(ceilf(share * f), 1e9f));
     };
-    float pieces = 0.f, slots = 0.f, cost = 0.f;
-    int longest = 0;
+    float pieces = 0.f, slots = 0.f;
+    int longest = 0, parts = 1;
+    bool whole = false;
     const int per = limit_of(wave);
     for (int b = lane; b < io.n_seqs; b += 64) {
         const int n = L.n[b], tiles = tiles_of(L.kv[b], n);
         if (n == 0) continue;
         const int blocks = blocks_of(n, grp), s = div_up(tiles, per);
-        const float k = (float)S.nkv * blocks * s;
-        pieces += k;
-        if (s > 1) { slots += k; cost += k * (blocks > 1 ? 5.f : 1.f); }
+        const float k = (float)S.nkv * blocks, some = 0.5f * (float)(s + div_up(tiles_of(L.kv[b], min(n, div_up(kCaRows, grp))), per));
+        pieces += k * some;
+        if (s > 1) { slots += k * s; whole |= n * grp > kCaNarrowRows; }
+        parts = max(parts, s);
         longest = max(longest, div_up(tiles, s));
     }
     pieces = wave_sum(pieces);
     slots = wave_sum(slots);
-    cost = work + wave_sum(cost) + 3.f * pieces;
     longest = wave_max_i(longest);
-    float ends = fmaxf((float)longest + 3.f, ceilf(pieces / (float)grid) * cost / fmaxf(pieces, 1.f)) + (slots > 0.f ? 5.f : 0.f);
+    parts = wave_max_i(parts);
+    float ends = fmaxf((float)longest + 1.f, ceilf(pieces / (float)grid) * ((work + pieces) / fmaxf(pieces, 1.f))) + 0.5f * (float)parts + (__any(whole) ? 9.f : 0.f);
     if (wave > 0 && slots > (float)S.attn_slots) ends = INFINITY;
     __syncthreads();
     if (lane == 0) L.wave_f[wave] = ends;
@@ -167,7 +175,7 @@ __device__ __forceinline__ int cut(const ServingDev &S, const etc_serving_attent
         for (int w = 0; w < kCaWaves; ++w) { done += L.wave_i[0][w]; done_slots += L.wave_i[1][w]; }
         if (b0 + kCaThreads < io.n_seqs) __syncthreads();
     }
-    if (tid == 0) L.first[0] = L.slot[0] = 0;
+    if (tid == 0) { L.first[0] = L.slot[0] = 0; L.limit = limit; }
     __syncthreads();
     return done;
 }
@@ -234,6 +242,10 @@ __device__ __forceinline__ void attend(f32x16 (&s)[KT], f32x16 (&o)[D / 32], flo
             for (int i = 0; i < 16; ++i)
                 if (k0 + kt * 32 + 8 * (i >> 2) + 4 * half + (i & 3) > limit) s[kt][i] = -INFINITY;
     }
+    // V's fragments a step ahead of their products: the first ones while the maximum is found
+    u32x4 w[2][DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) w[0][dt] = F.v_frag(base, 0, dt);
     float mt = s[0][0];
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
@@ -260,12 +272,14 @@ __device__ __forceinline__ void attend(f32x16 (&s)[KT], f32x16 (&o)[D / 32], flo
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
+            const int step = kt * 2 + h;
             const bf16x8 pb = __builtin_bit_cast(bf16x8, u32x4{p[4 * h], p[4 * h + 1], p[4 * h + 2], p[4 * h + 3]});
+            if (step + 1 < 2 * KT) {
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) {
-                const u32x4 w = F.v_frag(base, kt * 2 + h, dt);
-                o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), pb, o[dt], 0, 0, 0);
+                for (int dt = 0; dt < DT; ++dt) w[(step + 1) & 1][dt] = F.v_frag(base, step + 1, dt);
             }
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w[step & 1][dt]), pb, o[dt], 0, 0, 0);
         }
     }
 }
@@ -306,7 +320,8 @@ __device__ __forceinline__ void odd_values(const u32x4 (&mine)[N], const uint32_
                 if (c & 0xFFu) o[dt][i] += INFINITY;
                 if (c & 0xFF00u) o[dt][i] -= INFINITY;
                 if (c >> 16) o[dt][i] = __uint_as_float(0x7FC00000u);
-            }
+                __builtin_amdgcn_sched_barrier(0);           // one after the other: the conditions of all at once fill 600 scalar registers, and
+            }                                                // the lanes of eleven vector registers of the whole kernel with them (10 % of a long prompt)
         }
     }
     __syncthreads();
@@ -371,10 +386,11 @@ __device__ __forceinline__ Piece piece_of(const ServingDev &S, const etc_serving
     P.rows = P.seq.n * P.grp;
     P.r0 = (blocks_of(P.seq.n, P.grp) - 1 - local / S.nkv / P.split) * kCaRows;      // long blocks first
     P.n_keys = P.seq.kv + min(P.r0 + kCaRows - 1, P.rows - 1) / P.grp + 1;
-    const int tiles = (P.n_keys - 1) / kCaKeys + 1, each = tiles / P.split, more = tiles - each * P.split;      // the first `more` have one more
-    P.parts = min(P.split, tiles);          // a block shorter than its sequence's last one may have fewer
+    const int tiles = (P.n_keys - 1) / kCaKeys + 1;
+    P.parts = div_up(tiles, __builtin_amdgcn_readfirstlane(L.limit));      // of a block shorter than its sequence's last one maybe fewer than `split`
+    const int each = tiles / P.parts, more = tiles - each * P.parts;      // the first `more` have one more
     P.tile0 = P.part * each + min(P.part, more);
-    P.tile1 = P.tile0 + each + (P.part < more);
+    P.tile1 = P.part < P.parts ? P.tile0 + each + (P.part < more) : P.tile0;
     return P;
 }
 
@@ -606,11 +622,9 @@ __device__ __forceinline__ void wide_piece(const ServingDev &S, const etc_servin
     int tile = tile0;
     const int n_seen = min(first_masked, n_tiles);
     for (; tile < n_seen; ++tile) {
-        ahead(tile);
-        if (wave_live) {
-            scores<D, 2>(s, F, k_base + at, qf);
-            attend<D, 2, false>(s, o, m, l, F, v_base + at, half, scale, 0, 0);
-        }
+        if (wave_live) scores<D, 2>(s, F, k_base + at, qf);
+        ahead(tile);                                     // while the products run: in front of them all wavefronts' fetches queue up (1 %)
+        if (wave_live) attend<D, 2, false>(s, o, m, l, F, v_base + at, half, scale, 0, 0);
         next(tile);
     }
     for (; tile < n_tiles; ++tile) {
@@ -662,7 +676,6 @@ __device__ __forceinline__ void wide_piece(const ServingDev &S, const etc_servin
 // A block of at most 64 rows is bound by the rows of the cache: all wavefronts work on the same keys' arrival, four to 128 keys (32 each)
 // for the first 32 rows and four for the rest, and the keys' results are joined in LDS.  Two buffers of 128 keys: one on its
 // way, or both, at any time.
-constexpr int kCaNarrowRows = 64, kCaNarrowKeys = 128;
 
 template <int D>
 __device__ __forceinline__ void narrow_piece(const ServingDev &S, const etc_serving_attention_io &io, ETC_AS_LDS CaLds &L, ETC_AS_LDS Tiles<D> &B, const Piece &P)
@@ -796,8 +809,11 @@ __global__ __launch_bounds__(kCaThreads) void chunk_attention_kernel(ServingDev 
     __shared__ __attribute__((aligned(16))) Tiles<D> s_tiles;
     ETC_AS_LDS CaLds &L = *as_lds(&s_cut);
     ETC_AS_LDS Tiles<D> &B = *as_lds(&s_tiles);
-    const int n_pieces = cut(S, io, L);
-    for (int p = (int)blockIdx.x; p < n_pieces; p += (int)gridDim.x) {
+    const int n_pieces = cut(S, io, L), grid = (int)gridDim.x;
+    // In every other round of the launch in reverse, by groups of kXcds workgroups, so that piece p stays with die p % kXcds.
+    const int w = (int)blockIdx.x, all = grid & ~(kXcds - 1), back = w < all ? all - kXcds - (w & ~(kXcds - 1)) + (w & (kXcds - 1)) : w;
+    for (int round = 0; round * grid + ((round & 1) ? back : w) < n_pieces; ++round) {
+        const int p = round * grid + ((round & 1) ? back : w);
         const int b = __builtin_amdgcn_readfirstlane(last_not_above(L.first, io.n_seqs, p));
         const Piece P = piece_of(S, io, L, b, p - __builtin_amdgcn_readfirstlane(L.first[b]));
         if (P.tile0 < P.tile1) {
