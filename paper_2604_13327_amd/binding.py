@@ -488,7 +488,7 @@ def _rows(t, name, dtype, shape, device):
     if t.dtype in dtype and t.shape == shape and t.get_device() == device:
         rows, step = t.stride()
         if step == 1 or shape[1] == 1:
-            return t.data_ptr(), rows if shape[0] > 1 else max(rows, shape[1])
+            return t.data_ptr(), rows if shape[0] > 1 else shape[1]
     raise ValueError(f"{name} must be a matrix of shape {tuple(shape)} and one of the types {dtype}, the elements of a row neighbours, on "
                      f"the current GPU, not {tuple(t.shape)} (strides {t.stride()}), {t.dtype}, on {t.device}")
 

@@ -257,8 +257,9 @@ constexpr int kSmpList = 8192;              // tokens
 constexpr int kSmpFew = 1024;               // compared one by one
 constexpr int kUnitBits = 35;
 constexpr uint64_t kTopWeight = 1ull << kUnitBits;
-constexpr int kBinTokens = 1 << 14;         // tokens whose count and weight fit the 64 bits of a bin: 15 and 49
 constexpr int kCountShift = 49;
+constexpr int kBinTokens = (1 << 14) - 1;   // tokens whose count and weight fit the 64 bits of a bin, 15 and 49, all of them the largest's
+static_assert((uint64_t)kBinTokens * kTopWeight < 1ull << kCountShift && kSmpList <= kBinTokens, "a bin");
 constexpr int kSmpWgs = 256;                // workgroups over slices
 constexpr int kSmpWhole = kBinTokens;       // longest row that sample_row does alone
 

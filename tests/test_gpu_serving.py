@@ -225,6 +225,46 @@ def test_attention_many_sequences(etc):
     _attention(etc, ref.shape(2, 1, 64), rng.integers(0, 90, 700).tolist(), new, pad=1)
 
 
+def test_attention_most_sequences(etc):
+    rng = np.random.default_rng(2)
+    new = rng.choice([0, 1, 1, 1, 2, 30], 1024).tolist()
+    _attention(etc, ref.shape(4, 2, 64, page=8), rng.integers(0, 300, 1024).tolist(), new)
+
+
+@pytest.mark.parametrize("new", [1, 70])
+def test_attention_more_pages_than_a_window(etc, new):
+    """Pages of one token, and as many sequences as workgroups take without cutting their keys: page ids come 1024 at a time."""
+    _attention(etc, ref.shape(8, 8, 64, page=1), [1600] * 33, [new] * 33)
+    _attention(etc, ref.shape(8, 8, 64, page=1), [1023 + 5 * i for i in range(32)], [new] * 32)
+
+
+def test_far_pages(etc):
+    """Pools of more than 4 GiB: append and attention at their end."""
+    s = ref.shape(16, 8, 128, page=16)
+    n_pages, used = 150000, 12
+    pools = [torch.zeros(n_pages, 16, 8, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    assert pools[0].numel() * 2 > 1 << 32
+    for i, p in enumerate(pools):
+        p[-used:] = randn(i, used, 16, 8, 128).cuda()
+    table = np.arange(n_pages - used, n_pages, dtype=np.int32)[::-1].copy().reshape(2, used // 2)
+    kv, new = [60, 3], [30, 80]
+    slots = [int(table[b, p // 16]) * 16 + p % 16 for b in range(2) for p in range(kv[b], kv[b] + new[b])]
+    pos = [p for b in range(2) for p in range(kv[b], kv[b] + new[b])]
+    qkv = randn(5, 110, 32 * 128).cuda()
+    q, out = torch.zeros(110, 16, 128, dtype=torch.bfloat16, device="cuda"), torch.zeros(110, 16, 128, dtype=torch.bfloat16, device="cuda")
+    sv = etc.Serving(s, max_seqs=2, max_tokens=110, max_kv_len=96)
+    sv.append(qkv[:, :2048], qkv[:, 2048:3072], qkv[:, 3072:], i32(pos), i32(slots), q, *pools)
+    sv.attention(q, out, i32([0, 30, 110]), i32(kv), i32(table), *pools)
+    torch.cuda.synchronize()
+    assert sv.read_error() == (0, 0, 0, 0)
+    sv.close()
+    near = [p[-used:].cpu() for p in pools]
+    assert torch.equal(near[1].view(-1, 8, 128)[torch.as_tensor(slots) - (n_pages - used) * 16], qkv[:, 3072:].cpu().view(-1, 8, 128))
+    want, size = ref.attention(s, q, *near, [0, 30, 110], kv, table - (n_pages - used))
+    ref.check_attention(out, want, size)
+    assert not any(bool(p[:-used].any()) for p in pools)
+
+
 def test_attention_large_scores(etc):
     _attention(etc, ref.shape(4, 2, 64), [300, 0], [20, 65], sigma=12.0)
 
@@ -345,6 +385,29 @@ def test_sample_ties_and_flat_rows(etc, dtype):
     _sample(etc, x, u, top_k=[1500] * 12, top_p=[0.50001] * 12)
     _sample(etc, x, u, min_p=[0.9] * 12)
     _sample(etc, x, u, temperature=[0.0] * 12)
+
+
+@pytest.mark.parametrize("vocab", [16382, 16383, 16384, 16385])
+def test_sample_longest_rows_of_one_launch(etc, vocab):
+    """All tokens in one bin, each with the largest weight: counts and weights of a bin share a word."""
+    x = torch.zeros(4, vocab)
+    x[1, 5:] = -60.0                                      # beyond the bins
+    x[2] = _logits(2, 1, vocab, torch.float32)[0]
+    x[3, ::2] = 1.0
+    u = [0.50001, 0.3, 0.7, 0.99]
+    _sample(etc, x, u)
+    _sample(etc, x, u, top_k=[vocab - 1, 9000, 9000, 8100], top_p=[0.75001] * 4)
+
+
+def test_sample_a_slice_of_equal_logits(etc):
+    """The largest vocabulary in as many slices as there are with 4 rows: the first tokens all weigh as much as the largest."""
+    vocab = 1 << 20
+    x = _logits(9, 4, vocab, torch.float32, sigma=1.0) - 12.0
+    x[:, :16384] = 0.0
+    x[2, 16000:] -= 5.0
+    u = [0.2, 0.9999, 0.9995, 0.99999]
+    assert _sample(etc, x, u) < 4
+    _sample(etc, x, u, top_p=[0.5, 0.99999, 0.999, 1.0], top_k=[0, 0, 300000, 17000])
 
 
 def test_sample_banned_and_infinite(etc):

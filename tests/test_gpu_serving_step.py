@@ -242,3 +242,29 @@ def test_on_another_stream(etc):
     st.synchronize()
     assert torch.equal(out, again)
     sv.close()
+
+
+def test_two_handles_at_once(etc):
+    """Two handles on two streams, in turn and without waiting for each other: every call has its own workspace."""
+    s = ref.shape(8, 2, 128, vocab=20000)
+    q, k, v = ref.randn(1, 70, 8, 128).cuda(), ref.randn(2, 400, 16, 2, 128).cuda(), ref.randn(3, 400, 16, 2, 128).cuda()
+    qi, kv, table = i32([0, 1, 70]), i32([3000, 3000]), i32(np.random.default_rng(1).permutation(400).reshape(2, 200))
+    logits, u = ref.randn(4, 2, 20000, dtype=torch.float32).cuda(), torch.tensor([0.3, 0.9], device="cuda")
+    svs = [etc.Serving(s, max_seqs=2, max_tokens=70, max_kv_len=3200) for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    want, token = torch.zeros_like(q), i32([0, 0])
+    svs[0].attention(q, want, qi, kv, table, k, v)
+    svs[0].sample(logits, u, token)
+    outs = [[torch.zeros_like(q) for _ in range(2)] for _ in range(8)]
+    tokens = [[i32([-5, -5]) for _ in range(2)] for _ in range(8)]
+    torch.cuda.synchronize()
+    for i in range(8):
+        for j in range(2):
+            svs[j].attention(q, outs[i][j], qi, kv, table, k, v, stream=streams[j])
+            svs[j].sample(logits, u, tokens[i][j], stream=streams[j])
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for pair in outs for o in pair)
+    assert all(torch.equal(t, token) for pair in tokens for t in pair)
+    for sv in svs:
+        assert sv.read_error()[0] == 0
+        sv.close()
