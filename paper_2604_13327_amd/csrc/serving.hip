@@ -250,6 +250,9 @@ hipError_t launch_serving_append(const ServingDev &S, const etc_serving_append_i
 // Long rows: sample_scan (largest and smallest logit) and sample_bins over slices of the rows, as many as fill the chip, then
 // sample_row; short ones: sample_row does it all.  Rows with more tokens in the bins in question than the list holds (flat or with
 // many ties, in the wrong place) and rows with +inf take slow_row, which descends through the bits of the logits' keys instead.
+// Measured: one row of 1024 in 14 us (a quarter of it the first pass, over code that no cache holds yet), 16 rows of 128256 without
+// filters in 33 us (scan 4, bins 7, row 21), 64 in bf16 with all of them in 55 (7, 14, 33).  A third of sample_row is one compute unit's
+// look at a row of 128256, 30 bytes a cycle; the same by slices, with a hand-over, was 2 us less for 16 rows and 12 more for 64.
 constexpr int kSmpThreads = 1024;           // of sample_row
 constexpr int kSliceThreads = 512;
 constexpr int kSmpBins = 1024;              // a bin: 1 / 1024 of min(32 temperatures, the row's range); a weight below 2^-36 is 0
@@ -278,20 +281,31 @@ __device__ __forceinline__ float logit_at(const void *row, int i)
 // The tokens [i0, i1) of a row, by the workgroup, a thread's ids ascending; NaN as it stands.  16 bytes a load and U loads in flight
 // (one after the other a row of 128256 took 73 us instead of 14): vectors(w, n, id) gets U vectors of which n are of this row, the
 // first one's ids from `id` on, the next ones' THREADS * 16 bytes behind.  single(logit, id): in front of and behind what is aligned.
-template <bool F32, int THREADS, int U, class Vectors, class Single>
-__device__ __forceinline__ void for_tokens(const void *row, int i0, int i1, Vectors vectors, Single single)
+// meanwhile() runs while the first ones are on their way.
+struct Nothing { __device__ __forceinline__ void operator()() const {} };
+template <bool F32, int THREADS, int U, class Vectors, class Single, class Meanwhile = Nothing>
+__device__ __forceinline__ void for_tokens(const void *row, int i0, int i1, Vectors vectors, Single single, Meanwhile meanwhile = Nothing())
 {
     constexpr int SIZE = F32 ? 4 : 2, E = 16 / SIZE;
     const int tid = (int)threadIdx.x;
     const char *from = (const char *)row + (int64_t)i0 * SIZE;
     const int a0 = min(i1, i0 + (int)((16 - ((uintptr_t)from & 15)) & 15) / SIZE), nv = (i1 - a0) / E, t0 = a0 + nv * E;
-    if (i0 + tid < a0) single(raw_logit<F32>(row, i0 + tid), i0 + tid);
     const char *body = (const char *)row + (int64_t)a0 * SIZE;
-    for (int v0 = tid; v0 < nv; v0 += THREADS * U) {
-        u32x4 w[U];
+    u32x4 w[U], behind[U];
+    auto load = [&](u32x4 (&to)[U], int v0) {
+        if (v0 < nv) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) w[u] = gld_16B(body + (int64_t)min(v0 + u * THREADS, nv - 1) * 16);
+            for (int u = 0; u < U; ++u) to[u] = gld_16B(body + (int64_t)min(v0 + u * THREADS, nv - 1) * 16);
+        }
+    };
+    load(w, tid);
+    meanwhile();
+    if (i0 + tid < a0) single(raw_logit<F32>(row, i0 + tid), i0 + tid);
+    for (int v0 = tid; v0 < nv; v0 += THREADS * U) {
+        load(behind, v0 + THREADS * U);
         vectors(w, min(U, (nv - v0 + THREADS - 1) / THREADS), a0 + v0 * E);
+#pragma unroll
+        for (int u = 0; u < U; ++u) w[u] = behind[u];
     }
     if (t0 + tid < i1) single(raw_logit<F32>(row, t0 + tid), t0 + tid);
 }
@@ -373,8 +387,8 @@ __device__ __forceinline__ RowStats wave_join(RowStats st)
 }
 
 // One pass over the tokens [i0, i1) of a row by the workgroup; the same in every thread.
-template <bool F32, int THREADS>
-__device__ __forceinline__ RowStats row_stats(const void *row, int i0, int i1, RowStats *s_red)
+template <bool F32, int THREADS, class Meanwhile = Nothing>
+__device__ __forceinline__ RowStats row_stats(const void *row, int i0, int i1, RowStats *s_red, Meanwhile meanwhile = Nothing())
 {
     RowStats st{-INFINITY, INFINITY, 0xFFFFFFFFu, 0};
     auto one = [&](float x, int i) {
@@ -391,7 +405,7 @@ __device__ __forceinline__ RowStats row_stats(const void *row, int i0, int i1, R
 #pragma unroll
             for (int e = 0; e < E; ++e) one(element<F32>(w[u], e), id + u * THREADS * E + e);
         }
-    }, one);
+    }, one, meanwhile);
     st = wave_join(st);
     if (lane_id() == 0) s_red[wave_id()] = st;
     __syncthreads();
@@ -514,7 +528,7 @@ struct SlowLds {
 // The shortest beginning of the order that holds `want_count` tokens, or (want_count == 0) weighs `want_mass` at least; the row has
 // it.  11 + 11 + 10 bits of the key at a time; equal keys have equal weights, so ties are settled by a division.
 template <bool F32>
-__device__ __noinline__ Prefix find_prefix(SlowLds &L, const void *row, int vocab, const RowScale &R, const double *table, uint32_t want_count, uint64_t want_mass)
+__device__ __forceinline__ Prefix find_prefix(SlowLds &L, const void *row, int vocab, const RowScale &R, const double *table, uint32_t want_count, uint64_t want_mass)
 {
     const int tid = (int)threadIdx.x;
     uint32_t prefix = 0, before = 0;
@@ -597,7 +611,7 @@ __device__ __forceinline__ float log_share(const RowScale &R, float x, uint64_t 
 }
 
 template <bool F32>
-__device__ __noinline__ Drawn slow_row(SlowLds &L, const void *row, int vocab, const RowScale &R, const double *table, uint32_t live, const Settings &q)
+__device__ __forceinline__ Drawn slow_row(SlowLds &L, const void *row, int vocab, const RowScale &R, const double *table, uint32_t live, const Settings &q)
 {
     const int tid = (int)threadIdx.x;
     uint32_t n_live = live;
@@ -813,6 +827,24 @@ __device__ __forceinline__ End end_in_bin(FastLds &L, const RowScale &R, const d
     return e;
 }
 
+// The same by every wavefront for itself, where the tokens fit its lanes (entry, bin and weight `w` of the lane's): no barrier, no bins.
+struct Few { uint64_t entry, w; uint32_t bin; int n; };
+__device__ __forceinline__ End end_among_few(const FastLds &L, const Few &F, uint32_t bin, uint32_t want_count, uint64_t want_mass)
+{
+    auto holds = [&](uint32_t c, uint64_t m) { return want_count ? c >= want_count : m >= want_mass; };
+    const bool in = lane_id() < F.n && F.bin == bin;
+    uint32_t c = bin ? L.upto[bin - 1] : 0;
+    uint64_t m = bin ? L.mass_upto[bin - 1] : 0;
+    for (uint64_t left = __ballot(in); left; left &= left - 1) {
+        const int j = __builtin_ctzll(left);
+        const uint64_t w = lane_u64(F.w, j);
+        if (lane_u64(F.entry, j) > F.entry) { c++; m += w; }
+    }
+    const uint64_t here = __ballot(in && !holds(c, m) && holds(c + 1, m + F.w));
+    const int at = here ? __builtin_ctzll(here) : 0;        // there is one
+    return End{(uint32_t)__builtin_amdgcn_readlane((int)c + 1, at), lane_u64(m + F.w, at), lane_u64(F.entry, at), true};
+}
+
 // The row by its bins.  False: more tokens are in question than the list holds.
 template <bool F32, bool WHOLE>
 __device__ __forceinline__ bool fast_row(const SampleArgs &a, FastLds &L, const void *row, const RowScale &R, const double *table, const Settings &q, int r, Drawn *out)
@@ -830,7 +862,7 @@ __device__ __forceinline__ bool fast_row(const SampleArgs &a, FastLds &L, const 
         unpack(L.sub[tid]);
     } else {
         const uint64_t *bins = a.S.smp_bins + (size_t)r * a.slices * kSmpBins + tid;
-#pragma unroll 8
+#pragma unroll 16
         for (int sl = 0; sl < a.slices; ++sl) unpack(bins[(size_t)sl * kSmpBins]);
     }
     uint32_t c = c_own;
@@ -872,58 +904,73 @@ __device__ __forceinline__ bool fast_row(const SampleArgs &a, FastLds &L, const 
     if (holds_mass(draw_wanted(q.u, most))) L.found[4] = tid;
     __syncthreads();
     const uint32_t p0 = L.found[1], p1 = L.found[2], d0 = L.found[3], d1 = L.found[4];
-    // The tokens of the bins in question, by four intervals of logits a hundredth of a bin wider, in fp32: their ids first, then all their
-    // logits at once.
+    // The tokens of the bins in question, by intervals of logits a hundredth of a bin wider, in fp32: their ids first, then all their
+    // logits at once.  One interval from the first of the bins to the last where that holds few tokens (with filters the ends lie close
+    // together: 64 rows of 128256 with all filters: 55 us for 64, with what follows), else one for each end.
+    const uint32_t b0[4] = {d0, p0, bin_k, bin_m0}, b1[4] = {d1, p1, bin_k, bin_m1};
+    bool use[4] = {true, use_p, use_k, use_m};
+    uint32_t first = d0, last = d1;
+#pragma unroll
+    for (int i = 1; i < 4; ++i)
+        if (use[i]) { first = min(first, b0[i]); last = max(last, b1[i]); }
+    const bool one = L.upto[last] - (first ? L.upto[first - 1] : 0) <= kSmpList / 4;
     float lo[4], hi[4];
     {
         const double wide = R.per > 0.0 ? 1024.0 / R.per : 0.0;
         const float slack = fabsf(R.top) * 0x1p-22f;
-        auto interval = [&](int i, bool use, uint32_t b0, uint32_t b1) {
-            hi[i] = !use ? -INFINITY : b0 == 0 ? R.top : (float)((double)R.top - ((double)b0 - 0.01) * wide) + slack;
-            lo[i] = !use ? INFINITY : R.per == 0.0 || b1 == kSmpBins - 1 ? -3.402823466e38f : (float)((double)R.top - ((double)b1 + 1.01) * wide) - slack;
-        };
-        interval(0, true, d0, d1);
-        interval(1, use_p, p0, p1);
-        interval(2, use_k, bin_k, bin_k);
-        interval(3, use_m, bin_m0, bin_m1);
-    }
-    auto look = [&](float x) {
-        bool yes = x <= hi[0] && x >= lo[0];
-        if (use_p) yes |= x <= hi[1] && x >= lo[1];
-        if (use_k) yes |= x <= hi[2] && x >= lo[2];
-        if (use_m) yes |= x <= hi[3] && x >= lo[3];
-        return yes;
-    };
-    for_tokens<F32, kSmpThreads, 8>(row, 0, vocab, [&](const u32x4 (&w)[8], int n, int id) {
-        constexpr int E = F32 ? 4 : 8;
-        uint64_t hits = 0;
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t from = one ? first : b0[i], to = one ? last : b1[i];
+            use[i] &= i == 0 || !one;
+            hi[i] = from == 0 ? R.top : (float)((double)R.top - ((double)from - 0.01) * wide) + slack;
+            lo[i] = R.per == 0.0 || to == kSmpBins - 1 ? -3.402823466e38f : (float)((double)R.top - ((double)to + 1.01) * wide) - slack;
+        }
+    }
+    auto inside = [&](float x, int i) { return __builtin_amdgcn_fmed3f(x, lo[i], hi[i]) == x; };      // NaN: no
+    for_tokens<F32, kSmpThreads, 4>(row, 0, vocab, [&](const u32x4 (&w)[4], int n, int id) {
+        constexpr int E = F32 ? 4 : 8, ALL = 4 * E;
+        uint32_t hits = 0;                                   // the first element's is the highest of ALL bits
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (!use[i]) continue;
             uint32_t h = 0;
 #pragma unroll
-            for (int e = 0; e < E; ++e) h |= (uint32_t)look(element<F32>(w[u], e)) << e;
-            if (u < n) hits |= (uint64_t)h << (u * E);
+            for (int e = 0; e < ALL; ++e) h = h + h + (uint32_t)inside(element<F32>(w[e / E], e % E), i);
+            hits |= h;
         }
-        const int mine = __builtin_popcountll(hits);
+        hits &= ~0u << ((4 - n) * E);
+        const int mine = __builtin_popcount(hits);
         if (mine == 0) return;
         uint32_t at = atomicAdd(&L.n_list, (uint32_t)mine);
         for (; hits; hits &= hits - 1, ++at) {
-            const int k = __builtin_ctzll(hits);
+            const int k = ALL - 1 - __builtin_ctz(hits);
             if (at < kSmpList) L.id[at] = (uint32_t)(id + (k / E) * kSmpThreads * E + k % E);
         }
-    }, [&](float x, int i) {
-        if (!look(x)) return;
+    }, [&](float x, int id) {
+        if (!(inside(x, 0) || (use[1] && inside(x, 1)) || (use[2] && inside(x, 2)) || (use[3] && inside(x, 3)))) return;
         const uint32_t at = atomicAdd(&L.n_list, 1u);
-        if (at < kSmpList) L.id[at] = (uint32_t)i;
+        if (at < kSmpList) L.id[at] = (uint32_t)id;
     });
     __syncthreads();
     if (L.n_list > kSmpList) return false;
-    for (uint32_t j = tid; j < L.n_list; j += kSmpThreads) {
-        const float x = logit_at<F32>(row, (int)L.id[j]);
-        L.key[j] = order_key(x);
-        L.place[j] = place_of(R, x);
+    const bool is_few = L.n_list <= 64;
+    Few F{0, 0, 0, (int)L.n_list};
+    if (is_few) {
+        if (lane_id() < F.n) {
+            const uint32_t id = L.id[lane_id()];
+            const float x = logit_at<F32>(row, (int)id);
+            F.entry = (uint64_t)order_key(x) << 32 | (uint32_t)~id;
+            F.w = weight_of(R, table, x);
+            F.bin = place_of(R, x) >> 10;
+        }
+    } else {
+        for (uint32_t j = tid; j < L.n_list; j += kSmpThreads) {
+            const float x = logit_at<F32>(row, (int)L.id[j]);
+            L.key[j] = order_key(x);
+            L.place[j] = place_of(R, x);
+        }
+        __syncthreads();
     }
-    __syncthreads();
 
     // ---- exactly: top_k, top_p and, behind min_p, the draw; one after the other through the same code
     uint32_t kept = n_live;
@@ -935,13 +982,21 @@ __device__ __forceinline__ bool fast_row(const SampleArgs &a, FastLds &L, const 
         if (stage == 2 && use_m) {
             uint32_t above = 0;
             uint64_t am = 0;
-            for (uint32_t i = tid; i < L.n_list; i += kSmpThreads) {
-                const float x = key_logit(L.key[i]);
-                const uint32_t b = L.place[i] >> 10;
-                if (b >= bin_m0 && b <= bin_m1 && above_min_p(R, x, q.min_p)) { above++; am += weight_of(R, table, x); }
+            auto near = [&](uint32_t b, float x) { return b >= bin_m0 && b <= bin_m1 && above_min_p(R, x, q.min_p); };
+            if (is_few) {
+                if (lane_id() < F.n && near(F.bin, entry_logit(F.entry))) { above = 1; am = F.w; }
+                above = (uint32_t)__popcll(__ballot(above));
+                am = lane_u64(wave_scan_u64(am), 63);
+            } else {
+                for (uint32_t i = tid; i < L.n_list; i += kSmpThreads) {
+                    const float x = key_logit(L.key[i]);
+                    if (near(L.place[i] >> 10, x)) { above++; am += weight_of(R, table, x); }
+                }
+                above = wg_sum<uint32_t>(above, L.red_i);
+                am = wg_sum<uint64_t>(am, L.red);
             }
-            above = wg_sum<uint32_t>(above, L.red_i) + (bin_m0 ? L.upto[bin_m0 - 1] : 0);
-            am = wg_sum<uint64_t>(am, L.red) + mass_in_front(bin_m0);
+            above += bin_m0 ? L.upto[bin_m0 - 1] : 0;
+            am += mass_in_front(bin_m0);
             if (q.min_p > 1.f) { above = 1; am = kTopWeight; }
             if (above < kept) { kept = above; mass = am; }
         }
@@ -952,7 +1007,21 @@ __device__ __forceinline__ bool fast_row(const SampleArgs &a, FastLds &L, const 
             __syncthreads();
             bin = L.found[5];
         }
-        const End e = end_in_bin(L, R, table, vocab, bin, stage == 0 ? (uint32_t)q.top_k : 0, want, stage == 2);
+        const uint32_t count = stage == 0 ? (uint32_t)q.top_k : 0;
+        const uint32_t in_bin = L.upto[bin] - (bin ? L.upto[bin - 1] : 0);
+        if (!is_few && in_bin <= 64) {
+            if (tid == 0) L.n_few = 0;
+            __syncthreads();
+            for (uint32_t i = tid; i < L.n_list; i += kSmpThreads)
+                if (L.place[i] >> 10 == bin) L.few[atomicAdd(&L.n_few, 1u)] = (uint64_t)L.key[i] << 32 | ~L.id[i];
+            __syncthreads();
+            F = Few{0, 0, bin, (int)in_bin};
+            if (lane_id() < F.n) {
+                F.entry = L.few[lane_id()];
+                F.w = weight_of(R, table, entry_logit(F.entry));
+            }
+        }
+        const End e = in_bin <= 64 ? end_among_few(L, F, bin, count, want) : end_in_bin(L, R, table, vocab, bin, count, want, stage == 2);
         if (!e.ok) return false;
         if (stage == 2) {
             *out = Drawn{~(uint32_t)e.entry, kept, log_share(R, entry_logit(e.entry), mass)};
@@ -970,7 +1039,6 @@ __global__ __launch_bounds__(kSmpThreads) void sample_row_kernel(SampleArgs a)
     __shared__ RowLds lds;
     __shared__ double table[1024];
     FastLds &L = lds.f;
-    fill_powers(table);                                      // (the first barrier is in front of its first use)
     const int tid = (int)threadIdx.x, r = (int)blockIdx.x, vocab = a.S.vocab;
     const etc_serving_sample_io &io = a.io;
     const void *row = row_of<F32>(a, r);
@@ -987,8 +1055,12 @@ __global__ __launch_bounds__(kSmpThreads) void sample_row_kernel(SampleArgs a)
         if (io.kept_out) *as_global(io.kept_out + r) = (int32_t)kept;
     };
     RowStats st;
-    if constexpr (WHOLE) st = row_stats<F32, kSmpThreads>(row, 0, vocab, lds.stats);
-    else st = join_stats(a, r);
+    if constexpr (WHOLE) {
+        st = row_stats<F32, kSmpThreads>(row, 0, vocab, lds.stats, [&]() { fill_powers(table); });
+    } else {
+        fill_powers(table);                                  // (a barrier is in front of its first use)
+        st = join_stats(a, r);
+    }
     if (st.live == 0) return answer(-1, -INFINITY, 0);
     if (!(q.T > 0.f)) return answer((int32_t)st.first, 0.f, 1);
     const RowScale R = scale_of(st, q.T);
