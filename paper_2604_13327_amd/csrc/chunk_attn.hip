@@ -21,6 +21,7 @@ constexpr int kCaWaves = 8, kCaThreads = kCaWaves * 64;
 constexpr int kCaRows = 32 * kCaWaves;      // rows of a block
 constexpr int kCaKeys = 64;                 // keys of a tile
 constexpr int kCaMinTiles = 2;              // of a piece, where keys are cut
+constexpr int kCaWholeTiles = 5;            // items of no more are not cut: three sequences of 5 tiles 10.4 us, 10.5 to 11.2 in pieces; of 16 21.5, 14.6 in pieces
 constexpr int kCaNarrowRows = 64, kCaNarrowKeys = 128;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -56,20 +57,26 @@ __device__ __forceinline__ int last_not_above(ETC_AS_LDS const int *indptr, int 
 // kCaTries that is estimated to end first; every workgroup computes this by itself from the lengths, one sequence to a thread.  A
 // sequence's long blocks come first, and workgroups take pieces forwards and backwards in turn, so that their sums come out about
 // equal: a chunk of 4096 (512 pieces of 1 to 64 tiles) takes 146 us, 188 where every workgroup takes piece w + 256 after piece w, 164
-// from a queue of pieces.  KV heads are the fastest index of a piece: neighbouring workgroups, on different dies, take different heads,
-// and a die's L2 sees the keys of one or two.
+// from a queue of pieces.  Where there are more pieces than workgroups, sequences of at most kCaNarrowRows rows (narrow ones) go by
+// length, and their pieces are spread among the others': the former are bound by memory, the latter by LDS and matrix units, and those
+// at the same time are faster than one after the other.  (64 single tokens: 158 us, 170 as they come; 32 of them with a prompt of 1000: 59 and
+// 64; 30 with two prompts 65, 66 as they come and 83 with all narrow ones in front.)  KV heads are the fastest index of a piece:
+// neighbouring workgroups, on different dies, take different heads, and a die's L2 sees the keys of one or two.
 constexpr int kCaTries = kCaWaves;          // a wavefront estimates one
+constexpr int kCaClasses = 8;               // of sequences: narrow ones by length, then the others
 
 struct Seq { int q0, n, kv; };             // first row, new tokens, cached ones
 
 struct CaLds {
     int q0[kServingMaxSeqs], n[kServingMaxSeqs], kv[kServingMaxSeqs];      // n == 0: nothing to do
     int split[kServingMaxSeqs];             // pieces of the longest item
-    int first[kServingMaxSeqs + 1];         // prefix sum: pieces of the sequences
+    uint16_t order[kServingMaxSeqs];        // the sequences in the order of their pieces
+    int first[kServingMaxSeqs + 1];         // prefix sum, in that order: pieces of the sequences
     int slot[kServingMaxSeqs + 1];          // prefix sum: those that leave a partial result
     float wave_f[kCaWaves];
-    int wave_i[2][kCaWaves];
+    int wave_i[kCaClasses / 2][kCaWaves];
     int limit;                              // tiles of a piece
+    int narrow;                             // pieces of narrow sequences, which are in front (0: in any order)
     int odd, last;
 };
 
@@ -90,7 +97,7 @@ __device__ __forceinline__ int cut(const ServingDev &S, const etc_serving_attent
 {
     const int tid = (int)threadIdx.x, wave = __builtin_amdgcn_readfirstlane(wave_id()), lane = lane_id(), grp = S.nq / S.nkv, grid = (int)gridDim.x;
     float work = 0.f;                                    // tiles, all items
-    int tokens = 0;                                      // at most 2^30
+    int tokens = 0, most = 0;                            // at most 2^30; tiles of an item
     for (int b = tid; b < io.n_seqs; b += kCaThreads) {
         const int q0 = gld_i32(io.q_indptr + b), q1 = gld_i32(io.q_indptr + b + 1), kv = gld_i32(io.kv_len + b);
         int n = q1 - q0;
@@ -103,16 +110,18 @@ __device__ __forceinline__ int cut(const ServingDev &S, const etc_serving_attent
         L.n[b] = n;
         L.kv[b] = kv;
         tokens += n;
+        most = max(most, tiles_of(kv, n));
         if (n > 0) work += (float)S.nkv * blocks_of(n, grp) * 0.5f * (float)(tiles_of(kv, n) + tiles_of(kv, min(n, kCaRows / grp)));
     }
     work = wave_sum(work);
     tokens = wave_sum_i(tokens);
-    if (lane == 0) { L.wave_f[wave] = work; L.wave_i[0][wave] = tokens; }
+    most = wave_max_i(most);
+    if (lane == 0) { L.wave_f[wave] = work; L.wave_i[0][wave] = tokens; L.wave_i[1][wave] = most; }
     __syncthreads();
     work = 0.f;
     tokens = 0;
 #pragma unroll
-    for (int w = 0; w < kCaWaves; ++w) { work += L.wave_f[w]; tokens += L.wave_i[0][w]; }
+    for (int w = 0; w < kCaWaves; ++w) { work += L.wave_f[w]; tokens += L.wave_i[0][w]; most = max(most, L.wave_i[1][w]); }
     if (tokens > io.n_tokens) {                          // ranges that overlap: no call's lengths
         if (blockIdx.x == 0 && tid == 0) refuse(S.error, SRV_BAD_LENGTH, SRV_ATTENTION, io.n_seqs, tokens);
         return 0;
@@ -128,56 +137,112 @@ __device__ __forceinline__ int cut(const ServingDev &S, const etc_serving_attent
         const float f = w == 1 ? 4.f : w == 2 ? 3.f : w == 3 ? 2.f : w == 4 ? 1.5f : w == 5 ? 1.25f : w == 6 ? 1.1f : 1.f;
         return w == 0 ? 1 << 30 : max(kCaMinTiles, (int)fminf(ceilf(share * f), 1e9f));
     };
-    float pieces = 0.f, slots = 0.f;
-    int longest = 0, parts = 1;
-    bool whole = false;
-    const int per = limit_of(wave);
-    for (int b = lane; b < io.n_seqs; b += 64) {
-        const int n = L.n[b], tiles = tiles_of(L.kv[b], n);
-        if (n == 0) continue;
-        const int blocks = blocks_of(n, grp), s = div_up(tiles, per);
-        const float k = (float)S.nkv * blocks, some = 0.5f * (float)(s + div_up(tiles_of(L.kv[b], min(n, div_up(kCaRows, grp))), per));
-        pieces += k * some;
-        if (s > 1) { slots += k * s; whole |= n * grp > kCaNarrowRows; }
-        parts = max(parts, s);
-        longest = max(longest, div_up(tiles, s));
-    }
-    pieces = wave_sum(pieces);
-    slots = wave_sum(slots);
-    longest = wave_max_i(longest);
-    parts = wave_max_i(parts);
-    float ends = fmaxf((float)longest + 1.f, ceilf(pieces / (float)grid) * ((work + pieces) / fmaxf(pieces, 1.f))) + 0.5f * (float)parts + (__any(whole) ? 9.f : 0.f);
-    if (wave > 0 && slots > (float)S.attn_slots) ends = INFINITY;
-    __syncthreads();
-    if (lane == 0) L.wave_f[wave] = ends;
-    __syncthreads();
-    int best = 0;
-    float best_ends = L.wave_f[0];
-#pragma unroll
-    for (int w = 1; w < kCaTries; ++w)
-        if (L.wave_f[w] < best_ends) { best = w; best_ends = L.wave_f[w]; }
-    const int limit = limit_of(best);
-    int done = 0, done_slots = 0;
-    for (int b0 = 0; b0 < io.n_seqs; b0 += kCaThreads) {
-        const int b = b0 + tid;
-        int k = 0, sl = 0;
-        if (b < io.n_seqs && L.n[b] > 0) {
-            const int s = div_up(tiles_of(L.kv[b], L.n[b]), limit);
-            L.split[b] = s;
-            k = S.nkv * blocks_of(L.n[b], grp) * s;      // all together at most 2^20 tokens * 1024 heads / 256 rows + 2^20, and attn_slots
-            sl = s > 1 ? k : 0;
+    int best = 0, longest_piece = most;
+    if (most > kCaWholeTiles) {
+        float pieces = 0.f, slots = 0.f;
+        int longest = 0, parts = 1;
+        bool whole = false;
+        const int per = limit_of(wave);
+        for (int b = lane; b < io.n_seqs; b += 64) {
+            const int n = L.n[b], tiles = tiles_of(L.kv[b], n);
+            if (n == 0) continue;
+            const int blocks = blocks_of(n, grp), s = div_up(tiles, per);
+            const float k = (float)S.nkv * blocks, some = 0.5f * (float)(s + div_up(tiles_of(L.kv[b], min(n, div_up(kCaRows, grp))), per));
+            pieces += k * some;
+            if (s > 1) { slots += k * s; whole |= n * grp > kCaNarrowRows; }
+            parts = max(parts, s);
+            longest = max(longest, div_up(tiles, s));
         }
-        int sum = wave_scan_i(k), sum_sl = wave_scan_i(sl);
-        if (lane == 63) { L.wave_i[0][wave] = sum; L.wave_i[1][wave] = sum_sl; }
+        pieces = wave_sum(pieces);
+        slots = wave_sum(slots);
+        longest = wave_max_i(longest);
+        parts = wave_max_i(parts);
+        float ends = fmaxf((float)longest + 1.f, ceilf(pieces / (float)grid) * ((work + pieces) / fmaxf(pieces, 1.f))) + 0.5f * (float)parts + (__any(whole) ? 9.f : 0.f);
+        if (wave > 0 && slots > (float)S.attn_slots) ends = INFINITY;
         __syncthreads();
-        for (int w = 0; w < wave; ++w) { sum += L.wave_i[0][w]; sum_sl += L.wave_i[1][w]; }
-        if (b < io.n_seqs) { L.first[b + 1] = done + sum; L.slot[b + 1] = done_slots + sum_sl; }
-        for (int w = 0; w < kCaWaves; ++w) { done += L.wave_i[0][w]; done_slots += L.wave_i[1][w]; }
-        if (b0 + kCaThreads < io.n_seqs) __syncthreads();
+        if (lane == 0) { L.wave_f[wave] = ends; L.wave_i[0][wave] = longest; }
+        __syncthreads();
+        float best_ends = L.wave_f[0];
+#pragma unroll
+        for (int w = 1; w < kCaTries; ++w)
+            if (L.wave_f[w] < best_ends) { best = w; best_ends = L.wave_f[w]; }
+        longest_piece = L.wave_i[0][best];
     }
-    if (tid == 0) { L.first[0] = L.slot[0] = 0; L.limit = limit; }
+    const int limit = limit_of(best);
+    if (tid == 0) { L.first[0] = L.slot[0] = 0; L.limit = limit; L.narrow = 0; }
+    auto count = [&](auto as_they_come) {                // the prefix sums; the number of pieces
+        int done = 0, done_slots = 0;
+        for (int i0 = 0; i0 < io.n_seqs; i0 += kCaThreads) {
+            const int i = i0 + tid;
+            int k = 0, sl = 0;
+            __syncthreads();
+            if (i < io.n_seqs) {
+                int b = i, parts;
+                if (as_they_come) {
+                    parts = max(1, div_up(tiles_of(L.kv[i], L.n[i]), limit));
+                    L.order[i] = (uint16_t)i;
+                    L.split[i] = parts;
+                } else {
+                    b = L.order[i];
+                    parts = L.split[b];
+                }
+                k = S.nkv * blocks_of(L.n[b], grp) * parts;      // all together at most 2^20 tokens * 1024 heads / 256 rows + 2^20, and attn_slots
+                sl = parts > 1 ? k : 0;
+            }
+            int sum = wave_scan_i(k), sum_sl = wave_scan_i(sl);
+            if (lane == 63) { L.wave_i[0][wave] = sum; L.wave_i[1][wave] = sum_sl; }
+            __syncthreads();
+            for (int w = 0; w < wave; ++w) { sum += L.wave_i[0][w]; sum_sl += L.wave_i[1][w]; }
+            if (i < io.n_seqs) { L.first[i + 1] = done + sum; L.slot[i + 1] = done_slots + sum_sl; }
+            for (int w = 0; w < kCaWaves; ++w) { done += L.wave_i[0][w]; done_slots += L.wave_i[1][w]; }
+        }
+        return done;
+    };
+    int n_pieces = count(std::true_type());
+    if (n_pieces > grid && io.n_seqs > 1) {
+        // Ranks: classes by length in sevenths of the longest piece, within a class as they come.  Two classes' counts to a word.
+        int before[2][kCaClasses / 2], total[kCaClasses / 2] = {}, cls[2];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const int b = c * kCaThreads + tid, rows = b < io.n_seqs ? L.n[b] * grp : 0;
+            const int len = rows > 0 ? div_up(tiles_of(L.kv[b], L.n[b]), L.split[b]) : 0;
+            cls[c] = rows > kCaNarrowRows ? kCaClasses - 1 : min(kCaClasses - 2, (int)((float)((kCaClasses - 1) * (longest_piece - len)) / (float)longest_piece));
+            if (c * kCaThreads >= io.n_seqs) break;
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < kCaClasses / 2; ++j) {
+                const int mine = b < io.n_seqs && cls[c] >> 1 == j ? 1 << (cls[c] & 1) * 16 : 0;
+                before[c][j] = wave_scan_i(mine);
+                if (lane == 63) L.wave_i[j][wave] = before[c][j];
+                before[c][j] += total[j] - mine;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < kCaClasses / 2; ++j)
+                for (int w = 0; w < kCaWaves; ++w) {
+                    if (w < wave) before[c][j] += L.wave_i[j][w];
+                    total[j] += L.wave_i[j][w];
+                }
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const int b = c * kCaThreads + tid;
+            if (b >= io.n_seqs) break;
+            int rank = 0;
+#pragma unroll
+            for (int j = 0; j < kCaClasses; ++j) {
+                const int shift = (j & 1) * 16;
+                if (j < cls[c]) rank += (total[j >> 1] >> shift) & 0xFFFF;
+                else if (j == cls[c]) rank += (before[c][j >> 1] >> shift) & 0xFFFF;
+            }
+            L.order[rank] = (uint16_t)b;
+        }
+        n_pieces = count(std::false_type());
+        __syncthreads();
+        if (tid == 0) L.narrow = L.first[io.n_seqs - (total[kCaClasses / 2 - 1] >> 16)];
+    }
     __syncthreads();
-    return done;
+    return n_pieces;
 }
 
 // Partial results of a slot, wavefront by wavefront: [16-byte piece of a lane][lane] of the output, then m and l of 32 rows.
@@ -366,25 +431,27 @@ struct Tiles {
 };
 
 struct Piece {
-    int b, local, kvh, part, split, parts;  // part `part` of an item that has `parts` of them; of a sequence whose longest items have `split`
+    int b, kvh, part, parts;                // part `part` of an item that has `parts` of them
+    int slot0;                              // slot of part 0 (part j: j * nkv behind it)
     int tile0, tile1;                       // of the piece: [tile0, tile1)
     int n_keys;                             // that the last row of the block sees
     int grp, rows, r0;                      // query heads per KV head; rows of (sequence, KV head); first one of the block
     Seq seq;
 };
 
-__device__ __forceinline__ Piece piece_of(const ServingDev &S, const etc_serving_attention_io &io, ETC_AS_LDS const CaLds &L, int b, int local)
+__device__ __forceinline__ Piece piece_of(const ServingDev &S, const etc_serving_attention_io &io, ETC_AS_LDS const CaLds &L, int p)
 {
+    const int i = __builtin_amdgcn_readfirstlane(last_not_above(L.first, io.n_seqs, p)), local = p - __builtin_amdgcn_readfirstlane(L.first[i]);
     Piece P;
-    P.b = b;
-    P.local = local;
-    P.seq = wave_uniform(Seq{L.q0[b], L.n[b], L.kv[b]});
-    P.split = __builtin_amdgcn_readfirstlane(L.split[b]);
+    P.b = __builtin_amdgcn_readfirstlane((int)L.order[i]);
+    P.seq = wave_uniform(Seq{L.q0[P.b], L.n[P.b], L.kv[P.b]});
+    const int split = __builtin_amdgcn_readfirstlane(L.split[P.b]);
     P.kvh = local % S.nkv;
-    P.part = local / S.nkv % P.split;
+    P.part = local / S.nkv % split;
+    P.slot0 = __builtin_amdgcn_readfirstlane(L.slot[i]) + local - P.part * S.nkv;
     P.grp = S.nq / S.nkv;
     P.rows = P.seq.n * P.grp;
-    P.r0 = (blocks_of(P.seq.n, P.grp) - 1 - local / S.nkv / P.split) * kCaRows;      // long blocks first
+    P.r0 = (blocks_of(P.seq.n, P.grp) - 1 - local / S.nkv / split) * kCaRows;      // long blocks first
     P.n_keys = P.seq.kv + min(P.r0 + kCaRows - 1, P.rows - 1) / P.grp + 1;
     const int tiles = (P.n_keys - 1) / kCaKeys + 1;
     P.parts = div_up(tiles, __builtin_amdgcn_readfirstlane(L.limit));      // of a block shorter than its sequence's last one maybe fewer than `split`
@@ -510,12 +577,12 @@ struct Join {
 
 // Behind a part's partial result: who arrives last at the item joins its parts, in the order of the keys.
 template <int D>
-__device__ __forceinline__ void join_parts(const ServingDev &S, const etc_serving_attention_io &io, ETC_AS_LDS CaLds &L, const Piece &P, int slot0, int tid, int wave, int lane)
+__device__ __forceinline__ void join_parts(const ServingDev &S, const etc_serving_attention_io &io, ETC_AS_LDS CaLds &L, const Piece &P, int tid, int wave, int lane)
 {
     const int half = lane >> 5, col = lane & 31;
     wg_release();
     if (tid == 0) {
-        int32_t *ctr = S.attn_arrive + slot0;
+        int32_t *ctr = S.attn_arrive + P.slot0;
         const int last = __hip_atomic_fetch_add(as_global(ctr), 1, __ATOMIC_RELAXED, ETC_SCOPE) + 1 == P.parts;
         if (last) st_i32(ctr, 0);
         L.last = last;
@@ -531,7 +598,7 @@ __device__ __forceinline__ void join_parts(const ServingDev &S, const etc_servin
             uint64_t ml[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const float *src = partial<D>(S, slot0 + min(j0 + u, P.parts - 1) * S.nkv, rw);
+                const float *src = partial<D>(S, P.slot0 + min(j0 + u, P.parts - 1) * S.nkv, rw);
                 ov[u] = __builtin_bit_cast(f32x4, buf_ld_16B(buf_of(src), (uint32_t)((pc * 64 + lane) * 16), 0));
                 ml[u] = ld_u64(src + kCaPartO<D> + col * 2);
             }
@@ -663,9 +730,8 @@ __device__ __forceinline__ void wide_piece(const ServingDev &S, const etc_servin
                 put_out<D>(S, io, P, row, dt * 4 + q, half, f32x4{o[dt][4 * q] * inv, o[dt][4 * q + 1] * inv, o[dt][4 * q + 2] * inv, o[dt][4 * q + 3] * inv});
         return;
     }
-    const int slot0 = __builtin_amdgcn_readfirstlane(L.slot[P.b]) + P.local - P.part * S.nkv;
     if (wave_live) {
-        const __amdgpu_buffer_rsrc_t d_b = buf_of(partial<D>(S, slot0 + P.part * S.nkv, wave));
+        const __amdgpu_buffer_rsrc_t d_b = buf_of(partial<D>(S, P.slot0 + P.part * S.nkv, wave));
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -674,7 +740,7 @@ __device__ __forceinline__ void wide_piece(const ServingDev &S, const etc_servin
                            __builtin_bit_cast(u32x4, f32x4{o[dt][4 * q], o[dt][4 * q + 1], o[dt][4 * q + 2], o[dt][4 * q + 3]}));
         if (half == 0) buf_st_8B(d_b, (uint32_t)(kCaPartO<D> * 4 + col * 8), u32x2{__float_as_uint(m), __float_as_uint(l)});
     }
-    join_parts<D>(S, io, L, P, slot0, tid, wave, lane);
+    join_parts<D>(S, io, L, P, tid, wave, lane);
 }
 
 // A block of at most 64 rows is bound by the rows of the cache: all wavefronts work on the same keys' arrival, four to 128 keys (32 each)
@@ -787,7 +853,6 @@ __device__ __forceinline__ void narrow_piece(const ServingDev &S, const etc_serv
             *reinterpret_cast<ETC_AS_LDS f32x4 *>(mine_at + ((dt * 4 + q) * 64 + lane) * 16) = f32x4{o[dt][4 * q], o[dt][4 * q + 1], o[dt][4 * q + 2], o[dt][4 * q + 3]};
     if (half == 0) *reinterpret_cast<ETC_AS_LDS f32x2_t *>(ml_at + (wave * 32 + col) * 8) = f32x2_t{m, l};
     __syncthreads();
-    const int slot0 = __builtin_amdgcn_readfirstlane(L.slot[P.b]) + P.local - P.part * S.nkv;
     for (int cc = wave; cc < div_up(P.rows, 32) * (D / 8); cc += kCaWaves) {
         const int jr = cc / (D / 8), pc = cc % (D / 8);
         Join J;
@@ -799,12 +864,12 @@ __device__ __forceinline__ void narrow_piece(const ServingDev &S, const etc_serv
         if (P.parts == 1) {
             put_out<D>(S, io, P, jr * 32 + col, pc, half, J.result());
         } else {
-            const __amdgpu_buffer_rsrc_t d_b = buf_of(partial<D>(S, slot0 + P.part * S.nkv, jr));
+            const __amdgpu_buffer_rsrc_t d_b = buf_of(partial<D>(S, P.slot0 + P.part * S.nkv, jr));
             buf_st_16B(d_b, (uint32_t)((pc * 64 + lane) * 16), __builtin_bit_cast(u32x4, J.o));
             if (pc == 0 && half == 0) buf_st_8B(d_b, (uint32_t)(kCaPartO<D> * 4 + col * 8), u32x2{__float_as_uint(J.m), __float_as_uint(J.l)});
         }
     }
-    if (P.parts > 1) join_parts<D>(S, io, L, P, slot0, tid, wave, lane);
+    if (P.parts > 1) join_parts<D>(S, io, L, P, tid, wave, lane);
 }
 
 template <int D>
@@ -815,12 +880,22 @@ __global__ __launch_bounds__(kCaThreads) void chunk_attention_kernel(ServingDev 
     ETC_AS_LDS CaLds &L = *as_lds(&s_cut);
     ETC_AS_LDS Tiles<D> &B = *as_lds(&s_tiles);
     const int n_pieces = cut(S, io, L), grid = (int)gridDim.x;
-    // In every other round of the launch in reverse, by groups of kXcds workgroups, so that piece p stays with die p % kXcds.
+    if (n_pieces == 0) return;
+    const int narrow = __builtin_amdgcn_readfirstlane(L.narrow);
+    // In groups of kXcds, so that piece p stays with die p % kXcds: narrow pieces' groups spread evenly among the others', and in every
+    // other round of the launch the workgroups' groups in reverse.
+    const int gn = div_up(narrow, kXcds), groups = gn + div_up(n_pieces - narrow, kXcds);
     const int w = (int)blockIdx.x, all = grid & ~(kXcds - 1), back = w < all ? all - kXcds - (w & ~(kXcds - 1)) + (w & (kXcds - 1)) : w;
-    for (int round = 0; round * grid + ((round & 1) ? back : w) < n_pieces; ++round) {
-        const int p = round * grid + ((round & 1) ? back : w);
-        const int b = __builtin_amdgcn_readfirstlane(last_not_above(L.first, io.n_seqs, p));
-        const Piece P = piece_of(S, io, L, b, p - __builtin_amdgcn_readfirstlane(L.first[b]));
+    for (int round = 0; round * grid < groups * kXcds; ++round) {
+        int p = round * grid + ((round & 1) ? back : w), end = n_pieces;
+        if (narrow > 0 && narrow < n_pieces) {
+            const int g = p / kXcds, g0 = (int)((int64_t)g * gn / groups);
+            const bool of_narrow = (int64_t)(g + 1) * gn / groups > g0;
+            p = (of_narrow ? g0 * kXcds : narrow + (g - g0) * kXcds) + p % kXcds;
+            if (of_narrow) end = narrow;
+        }
+        if (p >= end) continue;
+        const Piece P = piece_of(S, io, L, p);
         if (P.tile0 < P.tile1) {
             if (P.rows <= kCaNarrowRows) narrow_piece<D>(S, io, L, B, P);
             else wide_piece<D>(S, io, L, B, P);

@@ -231,6 +231,14 @@ def test_attention_most_sequences(etc):
     _attention(etc, ref.shape(4, 2, 64, page=8), rng.integers(0, 300, 1024).tolist(), new)
 
 
+def test_attention_few_and_many_rows_together(etc):
+    """More pieces than workgroups, of sequences of a few tokens and of prompts: in another order than the sequences'."""
+    rng = np.random.default_rng(3)
+    _attention(etc, ref.shape(8, 2, 64, page=8), rng.integers(0, 200, 700).tolist(), rng.choice([0, 1, 1, 2, 40], 700).tolist(), pad=2)
+    _attention(etc, ref.shape(8, 8, 64), rng.integers(10, 3000, 40).tolist(), [1] * 9 + [150] + [3] * 20 + [300, 0] + [1] * 8)
+    _attention(etc, ref.shape(4, 4, 128), rng.integers(0, 400, 70).tolist(), [80 + i for i in range(70)])
+
+
 @pytest.mark.parametrize("new", [1, 70])
 def test_attention_more_pages_than_a_window(etc, new):
     """Pages of one token, and as many sequences as workgroups take without cutting their keys: page ids come 1024 at a time."""
