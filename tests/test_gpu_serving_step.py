@@ -268,3 +268,35 @@ def test_two_handles_at_once(etc):
     for sv in svs:
         assert sv.read_error()[0] == 0
         sv.close()
+
+
+@pytest.mark.parametrize("vocab", [16383, 40001])
+def test_captured_sampling_of_long_rows(etc, vocab):
+    """One launch and three: replays with other logits and settings equal the eager calls of another handle."""
+    s, n = ref.shape(vocab=vocab), 5
+    g = torch.Generator(device="cuda").manual_seed(vocab)
+    svs = [etc.Serving(s, max_seqs=n, max_tokens=1, max_kv_len=1) for _ in range(2)]
+    x, u = torch.zeros(n, vocab, device="cuda"), torch.zeros(n, device="cuda")
+    top_k, top_p = i32([0, 40, 1, 3000, 0]), torch.tensor([1.0, 0.9, 0.5, 0.99, 0.8], device="cuda")
+    outs = [(i32([-5] * n), torch.zeros(n, device="cuda"), i32([-5] * n)) for _ in svs]
+
+    def call(i):
+        svs[i].sample(x, u, outs[i][0], top_k=top_k, top_p=top_p, logprob_out=outs[i][1], kept_out=outs[i][2])
+
+    call(0)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(0)
+    for step in range(4):
+        x.copy_(torch.randn(n, vocab, device="cuda", generator=g) * (0.5 + step))
+        u.copy_(torch.rand(n, device="cuda", generator=g))
+        top_k.copy_(top_k.roll(1))
+        graph.replay()
+        call(1)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(*outs)), step
+        assert int(outs[0][0].min()) >= 0
+    for sv in svs:
+        assert sv.read_error()[0] == 0
+        sv.close()
