@@ -21,7 +21,7 @@ constexpr int kCaWaves = 8, kCaThreads = kCaWaves * 64;
 constexpr int kCaRows = 32 * kCaWaves;      // rows of a block
 constexpr int kCaKeys = 64;                 // keys of a tile
 constexpr int kCaMinTiles = 2;              // of a piece, where keys are cut
-constexpr int kCaWholeTiles = 5;            // items of no more are not cut: three sequences of 5 tiles 10.4 us, 10.5 to 11.2 in pieces; of 16 21.5, 14.6 in pieces
+constexpr int kCaWholeTiles = 5;            // items of no more are not cut, nor a cut estimated: three sequences of 5 tiles 9.5 us, 10.5 to 11.2 in pieces; of 16 21.5, 14.6 in pieces
 constexpr int kCaNarrowRows = 64, kCaNarrowKeys = 128;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -59,8 +59,8 @@ __device__ __forceinline__ int last_not_above(ETC_AS_LDS const int *indptr, int 
 // equal: a chunk of 4096 (512 pieces of 1 to 64 tiles) takes 146 us, 188 where every workgroup takes piece w + 256 after piece w, 164
 // from a queue of pieces.  Where there are more pieces than workgroups, sequences of at most kCaNarrowRows rows (narrow ones) go by
 // length, and their pieces are spread among the others': the former are bound by memory, the latter by LDS and matrix units, and those
-// at the same time are faster than one after the other.  (64 single tokens: 158 us, 170 as they come; 32 of them with a prompt of 1000: 59 and
-// 64; 30 with two prompts 65, 66 as they come and 83 with all narrow ones in front.)  KV heads are the fastest index of a piece:
+// at the same time are faster than one after the other.  (64 single tokens take 7 % less than as they come, 32 of them with a prompt of
+// 1000 9 %, 30 with two prompts 2 %, and those 25 % more with all narrow ones in front.)  KV heads are the fastest index of a piece:
 // neighbouring workgroups, on different dies, take different heads, and a die's L2 sees the keys of one or two.
 constexpr int kCaTries = kCaWaves;          // a wavefront estimates one
 constexpr int kCaClasses = 8;               // of sequences: narrow ones by length, then the others
@@ -412,13 +412,15 @@ __device__ __forceinline__ bool any_odd(u32x4 v)          // an exponent of all 
 // Rows go from memory to LDS without a stop in registers: 64 lanes, 16 bytes each, to 1 KB of LDS from `to` on (the same for the
 // whole wavefront).  The compiler would have every LDS read wait for all such loads in flight; here their order is the
 // program's own: arrived(n) waits until at most n of this wavefront's are on their way, a barrier then covers everyone's.
-__device__ __forceinline__ void fetch_1k(const char *from, uint32_t to)
+template <bool ONCE> __device__ __forceinline__ void fetch_1k(const char *from, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory");
+    if (ONCE) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" : : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory");
+    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory");
 }
-__device__ __forceinline__ void fetch_1k(const char *base, uint32_t lane_off, uint32_t to)      // base the same for the wavefront
+template <bool ONCE> __device__ __forceinline__ void fetch_1k(const char *base, uint32_t lane_off, uint32_t to)      // base the same for the wavefront
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(lane_off), "s"(base) : "memory");
+    if (ONCE) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" : : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(lane_off), "s"(base) : "memory");
+    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(lane_off), "s"(base) : "memory");
 }
 template <int N> __device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(%0)" : : "i"(N) : "memory"); }
 
@@ -487,7 +489,10 @@ struct PageWindow {
 // are that key's again (their scores are masked).
 // Where the rows of a load lie in one page (pages of RPL tokens and more) its address is a scalar and a constant of the lane: no vector
 // instruction at all.  (With addresses per lane, and their page ids read from LDS on the spot, the fetches cost the long prompt 16 %.)
-template <int D, int KEYS>
+// ONCE: no other workgroup of the launch reads these rows, and the next call that does comes behind all other layers' caches, so they leave
+// no copy in the caches on their way: 64 single tokens over 2000 to 4000 keys 146 us, 159 else; 16 sequences of 5 tokens 53 and 56 us
+// with caches turned over between calls (but 52 and 46 where all 197 MB stay in the memory-side cache from call to call).
+template <int D, int KEYS, bool ONCE>
 struct Fetch {
     static constexpr int CH = D / 8, RPL = 64 / CH, LOADS = KEYS / RPL / kCaWaves;
     const etc_serving_attention_io &io;
@@ -524,16 +529,16 @@ struct Fetch {
             for (int u = 0; u < LOADS; ++u) {
                 const int r = row_of(u);
                 const uint64_t off = (uint32_t)__builtin_amdgcn_readfirstlane(id[u]) * page_bytes + (uint64_t)(uint32_t)((key0 + (r & ~63)) & pmask) * row_bytes;
-                fetch_1k((const char *)io.k_pages + off, k_off[u], kb + r * D * 2);
-                fetch_1k((const char *)io.v_pages + off, v_off[u], vb + r * D * 2);
+                fetch_1k<ONCE>((const char *)io.k_pages + off, k_off[u], kb + r * D * 2);
+                fetch_1k<ONCE>((const char *)io.v_pages + off, v_off[u], vb + r * D * 2);
             }
         } else {
 #pragma unroll 1
             for (int u = 0; u < LOADS; ++u) {
                 const int r = row_of(u), key = min(key0 + r + lrow, last_key);
                 const uint64_t off = (uint32_t)B.ids[(key >> psh) - first_page] * page_bytes + (uint64_t)((uint32_t)(key & pmask)) * row_bytes + head_off;
-                fetch_1k((const char *)io.k_pages + (off + (uint32_t)((c ^ k_swap<D>(r + lrow)) * 16)), kb + r * D * 2);
-                fetch_1k((const char *)io.v_pages + (off + (uint32_t)((c ^ v_swap<D>(r + lrow)) * 16)), vb + r * D * 2);
+                fetch_1k<ONCE>((const char *)io.k_pages + (off + (uint32_t)((c ^ k_swap<D>(r + lrow)) * 16)), kb + r * D * 2);
+                fetch_1k<ONCE>((const char *)io.v_pages + (off + (uint32_t)((c ^ v_swap<D>(r + lrow)) * 16)), vb + r * D * 2);
             }
         }
     }
@@ -613,7 +618,7 @@ __device__ __forceinline__ void join_parts(const ServingDev &S, const etc_servin
 // A block of more than 64 rows: 32 of them to a wavefront, all wavefronts over the same tiles of 64 keys, in ring slot t % 3: while
 // tile t is being read, t + 1 has arrived or is about to, and the rows of t + 2 are on their way.
 // Measured: 4001 tokens behind 30000 keys, 64 heads of 128 on 8 (4.2 TFLOP): 3.9 ms, 1.08 PFLOP/s, nine tenths of the rate of a large
-// library product on this chip; matrix units busy 46 % of the cycles, no bank conflicts, memory idle (0.46 GB).  The bound is reading K and
+// library product on this chip; matrix units busy 48 % of the cycles, no bank conflicts, memory idle (1 GB).  The bound is reading K and
 // V from LDS, 32 KB by each of 8 wavefronts, 2048 of a tile's 4000 cycles, with the softmax of the same wavefronts in between; to delay
 // half of the wavefronts, to give them priorities, or to share tiles between early and late rows changed nothing.
 constexpr int kCaSlots = 3;
@@ -643,7 +648,7 @@ __device__ __forceinline__ void wide_piece(const ServingDev &S, const etc_servin
     const int wave_last = P.seq.kv + min((P.r0 + wave * 32 + 31) / P.grp, P.seq.n - 1);
     const bool wave_live = P.r0 + wave * 32 < P.rows;
     const uint32_t k_base = (uint32_t)(uintptr_t)&B.rows[0], v_base = k_base + kCaSlots * BUF;
-    Fetch<D, kCaKeys> G(S, io, B, P.kvh, P.n_keys - 1, wave, lane);
+    Fetch<D, kCaKeys, false> G(S, io, B, P.kvh, P.n_keys - 1, wave, lane);
 
     f32x16 o[DT];
 #pragma unroll
@@ -745,8 +750,9 @@ __device__ __forceinline__ void wide_piece(const ServingDev &S, const etc_servin
 
 // A block of at most 64 rows is bound by the rows of the cache: all wavefronts work on the same keys' arrival, four to 128 keys (32 each)
 // for the first 32 rows and four for the rest, and the keys' results are joined in LDS.  Two buffers of 128 keys: one on its
-// way, or both, at any time.  Measured: 16 sequences of 5 tokens behind 2000 to 4100 keys (197 MB): 46 us, 4.3 TB/s, of which about 8 us
-// are there for three short sequences too (launch, cut, page ids, rows and code that no cache holds yet, one after the other).
+// way, or both, at any time.  Measured: 16 sequences of 5 tokens behind 2000 to 4100 keys (197 MB): 53 us, 3.7 TB/s, of which about 8 us
+// are there for three short sequences too (launch, cut, page ids, rows and code that no cache holds yet, one after the other).  Many of them: 5.9 TB/s, and 3 % less time without any
+// computation.
 
 template <int D>
 __device__ __forceinline__ void narrow_piece(const ServingDev &S, const etc_serving_attention_io &io, ETC_AS_LDS CaLds &L, ETC_AS_LDS Tiles<D> &B, const Piece &P)
@@ -772,7 +778,7 @@ __device__ __forceinline__ void narrow_piece(const ServingDev &S, const etc_serv
     const int all_see = min(P.seq.kv + 1, key_end);      // keys in front of it are seen by all rows
     const bool live = rw * 32 < P.rows;
     const uint32_t base = (uint32_t)(uintptr_t)&B.rows[0];
-    Fetch<D, KEYS> G(S, io, B, P.kvh, key_end - 1, wave, lane);
+    Fetch<D, KEYS, true> G(S, io, B, P.kvh, key_end - 1, wave, lane);
     auto fetch = [&](int step) {
         const uint32_t to = base + (step & 1) * 2 * BUF;
         G.fetch(key0 + step * KEYS, W.first, to, to + BUF);
