@@ -373,8 +373,8 @@ etc_status etc_rowsum_launch_noalloc(const float *A, float *C, int32_t n, void *
  * the step etc_bind_step describes.  Sequences of one call are ragged and may be idle (n = 0).  RoPE, per-head norms, cache
  * layout and scale are those of the decoder.
  *
- * Lengths and tables are device memory: no call synchronises, allocates or copies, each is one or two kernel launches on
- * its stream and can be captured into a graph, whose replays then follow whatever the arrays hold.  A handle belongs to the
+ * Lengths and tables are device memory: no call synchronises, allocates or copies, each is one to three kernel launches
+ * on its stream and can be captured into a graph, whose replays then follow whatever the arrays hold.  A handle belongs to the
  * device that was current at create (a call with another current device is refused) and owns the workspace of its calls:
  * like a context it is not thread-safe and its calls go to one stream, or the caller orders them (two captured graphs that
  * may run at the same time need two handles).  Unlike a megakernel launch nothing here waits for other workgroups, so these

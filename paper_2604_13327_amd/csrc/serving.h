@@ -32,7 +32,12 @@ struct ServingDev {
     // sampling of long rows: statistics and bins of the slices
     void *smp_stats;
     uint64_t *smp_bins;
+    // and of the rows that several workgroups share: [row] tokens listed, [row] workgroups that have listed theirs (zero between launches),
+    // [row][kSampleList] the tokens
+    int32_t *smp_listed, *smp_done, *smp_list;
 };
+constexpr int kSampleList = 8192;
+constexpr int kSampleSharedRows = 128;
 constexpr int kAttnMaxSlots = 1024;
 int64_t attention_slot_bytes(int head_dim);
 int64_t sample_slices(int vocab, int max_rows);

@@ -254,12 +254,12 @@ hipError_t launch_serving_append(const ServingDev &S, const etc_serving_append_i
 // sample_row; short ones: sample_row does it all.  Rows with more tokens in the bins in question than the list holds (flat or with
 // many ties, in the wrong place) and rows with +inf take slow_row, which descends through the bits of the logits' keys instead.
 // Measured: one row of 1024 in 14 us (a quarter of it the first pass, over code that no cache holds yet), 16 rows of 128256 without
-// filters in 33 us (scan 4, bins 7, row 21), 64 in bf16 with all of them in 55 (7, 14, 33).  A third of sample_row is one compute unit's
-// look at a row of 128256, 30 bytes a cycle; the same by slices, with a hand-over, was 2 us less for 16 rows and 12 more for 64.
+// filters in 30 us (scan 4, bins 7, row 18), 64 in bf16 with all of them in 51 (7, 14, 30).  One compute unit looks through a row of 128256
+// at 30 bytes a cycle, half of sample_row's time: where there are units for it, several do (33 and 55 us with one to a row).
 constexpr int kSmpThreads = 1024;           // of sample_row
 constexpr int kSliceThreads = 512;
 constexpr int kSmpBins = 1024;              // a bin: 1 / 1024 of min(32 temperatures, the row's range); a weight below 2^-36 is 0
-constexpr int kSmpList = 8192;              // tokens
+constexpr int kSmpList = kSampleList;       // tokens
 constexpr int kSmpFew = 1024;               // compared one by one
 constexpr int kUnitBits = 35;
 constexpr uint64_t kTopWeight = 1ull << kUnitBits;
@@ -453,6 +453,7 @@ struct SampleArgs {
     ServingDev S;
     etc_serving_sample_io io;
     int slices, per_slice;   // of a row; tokens of one
+    int shares;              // workgroups of sample_row to a row
 };
 template <bool F32> __device__ __forceinline__ const void *row_of(const SampleArgs &a, int r)
 {
@@ -848,9 +849,11 @@ __device__ __forceinline__ End end_among_few(const FastLds &L, const Few &F, uin
     return End{(uint32_t)__builtin_amdgcn_readlane((int)c + 1, at), lane_u64(m + F.w, at), lane_u64(F.entry, at), true};
 }
 
-// The row by its bins.  False: more tokens are in question than the list holds.
+// The row by its bins.  Several workgroups (none of them waits): each does the sums for itself and looks through a share of the row, and
+// who lists its tokens last goes on alone.  TOO_MANY: more tokens are in question than the list holds.
+enum RowEnd { ROW_DRAWN, ROW_TOO_MANY, ROW_OF_ANOTHER };
 template <bool F32, bool WHOLE>
-__device__ __forceinline__ bool fast_row(const SampleArgs &a, FastLds &L, const void *row, const RowScale &R, const double *table, const Settings &q, int r, Drawn *out)
+__device__ __forceinline__ RowEnd fast_row(const SampleArgs &a, FastLds &L, const void *row, const RowScale &R, const double *table, const Settings &q, int r, Drawn *out)
 {
     const int tid = (int)threadIdx.x, vocab = a.S.vocab;
     // ---- the bins, one a thread, and their running sums
@@ -909,7 +912,7 @@ __device__ __forceinline__ bool fast_row(const SampleArgs &a, FastLds &L, const 
     const uint32_t p0 = L.found[1], p1 = L.found[2], d0 = L.found[3], d1 = L.found[4];
     // The tokens of the bins in question, by intervals of logits a hundredth of a bin wider, in fp32: their ids first, then all their
     // logits at once.  One interval from the first of the bins to the last where that holds few tokens (with filters the ends lie close
-    // together: 64 rows of 128256 with all filters: 55 us for 64, with what follows), else one for each end.
+    // together: 64 rows of 128256 with all filters: 55 us for 64, with what follows it and one workgroup to a row), else one for each end.
     const uint32_t b0[4] = {d0, p0, bin_k, bin_m0}, b1[4] = {d1, p1, bin_k, bin_m1};
     bool use[4] = {true, use_p, use_k, use_m};
     uint32_t first = d0, last = d1;
@@ -930,7 +933,8 @@ __device__ __forceinline__ bool fast_row(const SampleArgs &a, FastLds &L, const 
         }
     }
     auto inside = [&](float x, int i) { return __builtin_amdgcn_fmed3f(x, lo[i], hi[i]) == x; };      // NaN: no
-    for_tokens<F32, kSmpThreads, 4>(row, 0, vocab, [&](const u32x4 (&w)[4], int n, int id) {
+    const int per_share = WHOLE ? vocab : (vocab + a.shares - 1) / a.shares, i0 = WHOLE ? 0 : min(vocab, (int)blockIdx.y * per_share);
+    for_tokens<F32, kSmpThreads, 4>(row, i0, min(vocab, i0 + per_share), [&](const u32x4 (&w)[4], int n, int id) {
         constexpr int E = F32 ? 4 : 8, ALL = 4 * E;
         uint32_t hits = 0;                                   // the first element's is the highest of ALL bits
 #pragma unroll
@@ -955,7 +959,28 @@ __device__ __forceinline__ bool fast_row(const SampleArgs &a, FastLds &L, const 
         if (at < kSmpList) L.id[at] = (uint32_t)id;
     });
     __syncthreads();
-    if (L.n_list > kSmpList) return false;
+    if (!WHOLE && a.shares > 1) {
+        int32_t *list = a.S.smp_list + (size_t)r * kSmpList;
+        const uint32_t mine = L.n_list;
+        if (tid == 0) L.end_count = (uint32_t)__hip_atomic_fetch_add(as_global(a.S.smp_listed + r), (int)mine, __ATOMIC_RELAXED, ETC_SCOPE);
+        __syncthreads();
+        for (uint32_t i = tid; i < min(mine, (uint32_t)kSmpList) && L.end_count + i < kSmpList; i += kSmpThreads) st_i32(list + L.end_count + i, (int)L.id[i]);
+        wg_release();
+        if (tid == 0) {
+            const bool last = __hip_atomic_fetch_add(as_global(a.S.smp_done + r), 1, __ATOMIC_RELAXED, ETC_SCOPE) + 1 == a.shares;
+            if (last) {
+                L.n_list = (uint32_t)ld_i32(a.S.smp_listed + r);
+                st_i32(a.S.smp_listed + r, 0);
+                st_i32(a.S.smp_done + r, 0);
+            }
+            L.end_count = last;
+        }
+        __syncthreads();
+        if (!L.end_count) return ROW_OF_ANOTHER;
+        for (uint32_t i = tid; i < min(L.n_list, (uint32_t)kSmpList); i += kSmpThreads) L.id[i] = (uint32_t)ld_i32(list + i);
+        __syncthreads();
+    }
+    if (L.n_list > kSmpList) return ROW_TOO_MANY;
     const bool is_few = L.n_list <= 64;
     Few F{0, 0, 0, (int)L.n_list};
     if (is_few) {
@@ -1025,7 +1050,7 @@ __device__ __forceinline__ bool fast_row(const SampleArgs &a, FastLds &L, const 
             }
         }
         const End e = in_bin <= 64 ? end_among_few(L, F, bin, count, want) : end_in_bin(L, R, table, vocab, bin, count, want, stage == 2);
-        if (!e.ok) return false;
+        if (!e.ok) return ROW_TOO_MANY;
         if (stage == 2) {
             *out = Drawn{~(uint32_t)e.entry, kept, log_share(R, entry_logit(e.entry), mass)};
         } else {
@@ -1033,7 +1058,7 @@ __device__ __forceinline__ bool fast_row(const SampleArgs &a, FastLds &L, const 
             mass = e.mass;
         }
     }
-    return true;
+    return ROW_DRAWN;
 }
 
 template <bool F32, bool WHOLE>
@@ -1051,6 +1076,7 @@ __global__ __launch_bounds__(kSmpThreads) void sample_row_kernel(SampleArgs a)
     q.top_p = io.top_p ? *as_global(io.top_p + r) : 1.f;
     q.min_p = io.min_p ? *as_global(io.min_p + r) : 0.f;
     q.u = *as_global(io.u + r);
+    const bool first = blockIdx.y == 0;                      // of the row's workgroups: for what all of them know
     auto answer = [&](int32_t token, float logprob, uint32_t kept) {
         if (tid != 0) return;
         *as_global(io.token_out + r) = token;
@@ -1064,11 +1090,14 @@ __global__ __launch_bounds__(kSmpThreads) void sample_row_kernel(SampleArgs a)
         fill_powers(table);                                  // (a barrier is in front of its first use)
         st = join_stats(a, r);
     }
+    if (!first && (st.live == 0 || !(q.T > 0.f) || st.top == INFINITY)) return;
     if (st.live == 0) return answer(-1, -INFINITY, 0);
     if (!(q.T > 0.f)) return answer((int32_t)st.first, 0.f, 1);
     const RowScale R = scale_of(st, q.T);
     Drawn drawn;
-    if (R.top == INFINITY || !fast_row<F32, WHOLE>(a, L, row, R, table, q, r, &drawn)) {
+    const RowEnd end = R.top == INFINITY ? ROW_TOO_MANY : fast_row<F32, WHOLE>(a, L, row, R, table, q, r, &drawn);
+    if (end == ROW_OF_ANOTHER) return;
+    if (end == ROW_TOO_MANY) {
         __syncthreads();
         drawn = slow_row<F32>(lds.s, row, vocab, R, table, st.live, q);
     }
@@ -1084,6 +1113,14 @@ static int slices_of(int vocab, int rows)
     return s < least ? least : s;
 }
 
+// Workgroups of sample_row to a row: as many as there are compute units for (one fills one), with kBinTokens to look through at least.
+static int shares_of(int vocab, int rows)
+{
+    const int room = kSmpWgs / rows, most = vocab / kBinTokens;
+    static_assert(kSmpWgs / (kSampleSharedRows + 1) < 2, "rows that are shared have a list");
+    return room < 2 || most < 2 ? 1 : room < most ? room : most;
+}
+
 template <bool F32>
 static void launch_sample(const SampleArgs &a, hipStream_t s)
 {
@@ -1094,12 +1131,12 @@ static void launch_sample(const SampleArgs &a, hipStream_t s)
     const dim3 grid((unsigned)a.slices, (unsigned)a.io.n_rows);
     hipLaunchKernelGGL((sample_scan_kernel<F32>), grid, dim3(kSliceThreads), 0, s, a);
     hipLaunchKernelGGL((sample_bins_kernel<F32>), grid, dim3(kSliceThreads), 0, s, a);
-    hipLaunchKernelGGL((sample_row_kernel<F32, false>), dim3(a.io.n_rows), dim3(kSmpThreads), 0, s, a);
+    hipLaunchKernelGGL((sample_row_kernel<F32, false>), dim3((unsigned)a.io.n_rows, (unsigned)a.shares), dim3(kSmpThreads), 0, s, a);
 }
 
 hipError_t launch_serving_sample(const ServingDev &S, const etc_serving_sample_io &io, hipStream_t s)
 {
-    SampleArgs a{S, io, slices_of(S.vocab, io.n_rows), 0};
+    SampleArgs a{S, io, slices_of(S.vocab, io.n_rows), 0, shares_of(S.vocab, io.n_rows)};
     a.per_slice = (S.vocab + a.slices - 1) / a.slices;
     if (io.dtype == ETC_FP32) launch_sample<true>(a, s); else launch_sample<false>(a, s);
     return hipGetLastError();

@@ -82,7 +82,7 @@ int main()
         CHECK(bad([](M, L b) { b.max_kv_len = 0; }));
         CHECK(etc_serving_create(nullptr, &l, &s) == ETC_EINVAL && etc_serving_create(&m, nullptr, &s) == ETC_EINVAL);
         CHECK(etc_serving_create(&m, &l, nullptr) == ETC_EINVAL);
-        for (int k = 0; k < 6; ++k) {                     // no memory: everything is given back
+        for (int k = 0; k < 7; ++k) {                     // no memory: everything is given back
             g_fail_malloc = k;
             CHECK(etc_serving_create(&m, &l, &s) == ETC_ENOMEM && s == nullptr && g_allocs == 0 && etc_serving_last_error(nullptr)[0]);
             g_fail_malloc = -1;

@@ -418,6 +418,21 @@ def test_sample_a_slice_of_equal_logits(etc):
     _sample(etc, x, u, top_p=[0.5, 0.99999, 0.999, 1.0], top_k=[0, 0, 300000, 17000])
 
 
+@pytest.mark.parametrize("rows", [128, 129])
+def test_sample_rows_with_and_without_shares(etc, rows):
+    """Two workgroups to a row, and one; rows that need none, and flat ones whose tokens fill no list, among them."""
+    vocab = 33001
+    x = _logits(rows, rows, vocab, torch.bfloat16)
+    x[3], x[77], x[100] = -math.inf, 0.25, math.nan
+    x[5, 40:] = -math.inf
+    x[9, 30000] = math.inf
+    rng = np.random.default_rng(rows)
+    kw = dict(temperature=rng.choice([0.0, 0.5, 1.0, 2.0], rows), top_k=rng.choice([0, 1, 40, 20000], rows), top_p=rng.choice([1.0, 0.9, 0.2], rows),
+              min_p=rng.choice([0.0, 0.05], rows))
+    for _ in range(2):
+        assert _sample(etc, x, rng.random(rows, np.float32), **kw) < rows // 2
+
+
 def test_sample_banned_and_infinite(etc):
     vocab = 3001
     x = _logits(5, 10, vocab, torch.float32)
