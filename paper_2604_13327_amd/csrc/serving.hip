@@ -343,16 +343,16 @@ __device__ __forceinline__ void fill_powers(double *table)
 }
 __device__ __forceinline__ uint64_t weight_of(const RowScale &R, const double *table, float x)      // exp((x - top) / T) in units
 {
-    if (x == R.top) return kTopWeight;                       // +inf among them
-    const double t = ((double)R.top - (double)x) * R.steps;
-    if (!(t < 37.0 * 1024.0)) return 0;                      // below half a unit; next to +inf (all but which are banned)
-    const double fl = floor(t);
-    const int n = (int)fl;
-    const float r = (float)(t - fl) * (float)(0.69314718055994531 / 1024.0);
+    // No branches: a thread's tokens then go through side by side.  From 37 on 0 (below half a unit), and what is no number as well: next
+    // to +inf, where all finite ones are banned, and what is banned itself.
+    const double t = fmin(((double)R.top - (double)x) * R.steps, 37.0 * 1024.0);
+    const int n = (int)t;
+    const float r = (float)(t - (double)n) * (float)(0.69314718055994531 / 1024.0);
     const float s = -r + r * r * (0.5f - r * 0.16666667f);
     const double base = table[n & 1023];
     const double w = __builtin_ldexp(__builtin_fma(base, (double)s, base), -(n >> 10));
-    return (uint64_t)__double_as_longlong(w + 0x1p52) & ((1ull << 52) - 1);      // rounded to a whole number
+    const uint64_t whole = (uint64_t)__double_as_longlong(w + 0x1p52) & ((1ull << 52) - 1);      // rounded
+    return x == R.top ? kTopWeight : whole;                  // +inf among them
 }
 __device__ __forceinline__ uint32_t place_of(const RowScale &R, float x)      // bin << 10 | place within it; does not decrease with the distance from the top
 {
@@ -431,7 +431,9 @@ template <bool F32, int THREADS>
 __device__ __forceinline__ void fill_bins(const void *row, int i0, int i1, const RowScale &R, const double *table, unsigned long long *bins)
 {
     auto one = [&](float x, int) {
-        if (x > -INFINITY) atomicAdd(&bins[place_of(R, x) >> 10], (unsigned long long)(weight_of(R, table, x) | 1ull << kCountShift));
+        const uint64_t own = weight_of(R, table, x) | 1ull << kCountShift;
+        const uint32_t bin = place_of(R, x) >> 10;
+        if (x > -INFINITY) atomicAdd(&bins[bin], (unsigned long long)own);
     };
     // word by word, in a loop: written out for all, the code does not stay in the instruction cache
     for_tokens<F32, THREADS, 2>(row, i0, i1, [&](const u32x4 (&w)[2], int n, int) {
