@@ -258,16 +258,16 @@ def test_far_pages(etc):
     kv, new = [60, 3], [30, 80]
     slots = [int(table[b, p // 16]) * 16 + p % 16 for b in range(2) for p in range(kv[b], kv[b] + new[b])]
     pos = [p for b in range(2) for p in range(kv[b], kv[b] + new[b])]
-    qkv = randn(5, 110, 32 * 128).cuda()
+    rows = randn(5, 110, 32 * 128).cuda().split([16 * 128, 8 * 128, 8 * 128], 1)
     q, out = torch.zeros(110, 16, 128, dtype=torch.bfloat16, device="cuda"), torch.zeros(110, 16, 128, dtype=torch.bfloat16, device="cuda")
     sv = etc.Serving(s, max_seqs=2, max_tokens=110, max_kv_len=96)
-    sv.append(qkv[:, :2048], qkv[:, 2048:3072], qkv[:, 3072:], i32(pos), i32(slots), q, *pools)
+    sv.append(*rows, i32(pos), i32(slots), q, *pools)
     sv.attention(q, out, i32([0, 30, 110]), i32(kv), i32(table), *pools)
     torch.cuda.synchronize()
     assert sv.read_error() == (0, 0, 0, 0)
     sv.close()
     near = [p[-used:].cpu() for p in pools]
-    assert torch.equal(near[1].view(-1, 8, 128)[torch.as_tensor(slots) - (n_pages - used) * 16], qkv[:, 3072:].cpu().view(-1, 8, 128))
+    assert torch.equal(near[1].view(-1, 8, 128)[torch.as_tensor(slots) - (n_pages - used) * 16], rows[2].cpu().reshape(-1, 8, 128))
     want, size = ref.attention(s, q, *near, [0, 30, 110], kv, table - (n_pages - used))
     ref.check_attention(out, want, size)
     assert not any(bool(p[:-used].any()) for p in pools)
