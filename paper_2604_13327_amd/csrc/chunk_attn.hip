@@ -21,7 +21,9 @@ constexpr int kCaWaves = 8, kCaThreads = kCaWaves * 64;
 constexpr int kCaRows = 32 * kCaWaves;      // rows of a block
 constexpr int kCaKeys = 64;                 // keys of a tile
 constexpr int kCaMinTiles = 2;              // of a piece, where keys are cut
-constexpr int kCaWholeTiles = 5;            // items of no more are not cut, nor a cut estimated: three sequences of 5 tiles 9.5 us, 10.5 to 11.2 in pieces; of 16 21.5, 14.6 in pieces
+// Items of no more tiles are not cut, nor is a cut estimated: three sequences of 5 tiles 9.5 us, 10.5 to 11.2 in pieces (of 16 tiles 21.5,
+// 14.6 in pieces).
+constexpr int kCaWholeTiles = 5;
 constexpr int kCaNarrowRows = 64, kCaNarrowKeys = 128;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
