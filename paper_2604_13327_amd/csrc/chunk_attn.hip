@@ -25,6 +25,7 @@ constexpr int kCaMinTiles = 2;              // of a piece, where keys are cut
 // 14.6 in pieces).
 constexpr int kCaWholeTiles = 5;
 constexpr int kCaNarrowRows = 64, kCaNarrowKeys = 128;
+constexpr float kCaNoReference = -3e38f;     // of a row that has seen no key yet
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float partner_max(float x)      // with lane + 32
@@ -320,9 +321,10 @@ __device__ __forceinline__ void attend(f32x16 (&s)[KT], f32x16 (&o)[D / 32], flo
         for (int i = 0; i < 16; ++i) mt = fmaxf(mt, s[kt][i]);
     mt = partner_max(mt) * scale;
     // The reference follows the maximum only when that has grown by 2^8 (rows of a wavefront together): until then
-    // probabilities up to 2^8 lose nothing, and the running output need not be multiplied.
+    // probabilities up to 2^8 lose nothing, and the running output need not be multiplied.  A row's first reference multiplies nothing:
+    // the output is 0 until then but for infinities of this very tile (odd_values), which a factor of 0 would make NaN.
     if (__builtin_amdgcn_ballot_w64(mt > m + 8.f) != 0) {
-        const float nm = fmaxf(m, mt), sc = exp2_fast(m - nm);
+        const float nm = fmaxf(m, mt), sc = m > kCaNoReference ? exp2_fast(m - nm) : 1.f;
         m = nm;
         l *= sc;
 #pragma unroll
@@ -565,7 +567,7 @@ __device__ __forceinline__ float *partial(const ServingDev &S, int slot, int rw)
 
 // Running join of partial results (reference, sum, 4 elements of the output).
 struct Join {
-    float m = -3e38f, l = 0.f;
+    float m = kCaNoReference, l = 0.f;
     f32x4 o{0.f, 0.f, 0.f, 0.f};
     __device__ __forceinline__ void add(float mj, float lj, f32x4 oj)
     {
@@ -655,7 +657,7 @@ __device__ __forceinline__ void wide_piece(const ServingDev &S, const etc_servin
     f32x16 o[DT];
 #pragma unroll
     for (int i = 0; i < DT; ++i) o[i] = f32x16{};
-    float m = -3e38f, l = 0.f;                           // reference of the row's exponentials; sum over this lane's keys
+    float m = kCaNoReference, l = 0.f;                           // reference of the row's exponentials; sum over this lane's keys
     const float scale = 1.44269504088896f / sqrtf((float)D);      // scores and reference count in powers of two
     const Fragments<D> F(lane);
     f32x16 s[2];
@@ -791,7 +793,7 @@ __device__ __forceinline__ void narrow_piece(const ServingDev &S, const etc_serv
     f32x16 o[DT];
 #pragma unroll
     for (int i = 0; i < DT; ++i) o[i] = f32x16{};
-    float m = -3e38f, l = 0.f;
+    float m = kCaNoReference, l = 0.f;
     const float scale = 1.44269504088896f / sqrtf((float)D);
     const Fragments<D> F(lane);
     f32x16 s[1];
