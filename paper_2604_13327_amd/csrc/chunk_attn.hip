@@ -287,13 +287,24 @@ __device__ __forceinline__ void scores(f32x16 (&s)[KT], const Fragments<D> &F, u
 {
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) s[kt] = f32x16{};
+    bf16x8 a[2][KT];                                     // K's fragments a step ahead of their products
+    auto k_frag = [&](int ks, int kt) {
+        return *reinterpret_cast<ETC_AS_LDS const bf16x8 *>(reinterpret_cast<ETC_AS_LDS const char *>(F.k[ks] + base) + kt * 32 * D * 2);
+    };
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks)
+    for (int kt = 0; kt < KT; ++kt) a[0][kt] = k_frag(0, kt);
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt) {
-            const bf16x8 a = *reinterpret_cast<ETC_AS_LDS const bf16x8 *>(reinterpret_cast<ETC_AS_LDS const char *>(F.k[ks] + base) + kt * 32 * D * 2);
-            s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[ks], s[kt], 0, 0, 0);
+    for (int ks = 0; ks < D / 16; ++ks) {
+        if (ks + 1 < D / 16) {
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt) a[(ks + 1) & 1][kt] = k_frag(ks + 1, kt);
         }
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[ks & 1][kt], qf[ks], s[kt], 0, 0, 0);
+        // In this order: with all 256 registers taken the compiler reads one of two tiles' fragments behind the other's product (3 to 5 % of
+        // a long prompt).
+        if (KT > 1) __builtin_amdgcn_sched_barrier(0);
+    }
 }
 
 // Softmax of a tile's scores and O^T += V^T . P^T.  l is this lane's sum, over half of the keys.
@@ -324,7 +335,7 @@ __device__ __forceinline__ void attend(f32x16 (&s)[KT], f32x16 (&o)[D / 32], flo
     // probabilities up to 2^8 lose nothing, and the running output need not be multiplied.  A row's first reference multiplies nothing:
     // the output is 0 until then but for infinities of this very tile (odd_values), which a factor of 0 would make NaN.
     if (__builtin_amdgcn_ballot_w64(mt > m + 8.f) != 0) {
-        const float nm = fmaxf(m, mt), sc = m > kCaNoReference ? exp2_fast(m - nm) : 1.f;
+        const float nm = fmaxf(m, mt), sc = MASKED && m == kCaNoReference ? 1.f : exp2_fast(m - nm);
         m = nm;
         l *= sc;
 #pragma unroll
