@@ -410,7 +410,10 @@ etc_status etc_serving_read_error(etc_serving *s, int32_t word[4]);
  * q_indptr[b] + i: its position is kv_len[b] + i, its slot (page id) * page_size + position mod page_size.
  * All or nothing: *status = 0, or the number of pages that free_pages lacks, or -1 (a length out of range, more tokens than
  * n_tokens, more pages than a row of block_table or page_ids holds).  Other than 0 nothing is taken: block_table stays,
- * *free_count_out = *free_count, total_len = kv_len, all slots are -1, q_indptr and page_indptr are 0, page_ids stays. */
+ * *free_count_out = *free_count, total_len = kv_len, all slots are -1, q_indptr and page_indptr are 0, page_ids stays.
+ * How many pages the pool has is not known here: ids are handed on, and what lies outside the pool is refused where it is used. An id
+ * that new tokens need and whose slots are no int32 (below 0, above (2^31 - 1) / page_size) is reported (status stays 0); its tokens get
+ * slot 2^31 - 1, which lies in no pool. */
 typedef struct {
     int32_t n_seqs, n_tokens;       /* sequences; rows of slots and positions (rows behind the last token: slot -1, position 0) */
     const int32_t *kv_len;          /* [n_seqs] */

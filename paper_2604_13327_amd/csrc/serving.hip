@@ -91,7 +91,13 @@ __global__ __launch_bounds__(kTabThreads) void serving_tables_kernel(ServingDev 
         if (status == 0 && t < n_tok) {
             const int b = seq_of(s_tok, n, t);
             pos = s_kv[b] + (t - s_tok[b]);
-            slot = (page_id(b, pos >> psh, pages_held(b)) << psh) + (pos & pmask);
+            const int id = page_id(b, pos >> psh, pages_held(b));
+            if ((unsigned)id <= (unsigned)(INT32_MAX >> psh)) {
+                slot = (id << psh) + (pos & pmask);
+            } else {                                     // its slots do not fit: one that lies in no pool
+                refuse(S.error, SRV_BAD_PAGE, SRV_TABLES, b, id);
+                slot = INT32_MAX;
+            }
         }
         *as_global(io.slots + t) = slot;
         *as_global(io.positions + t) = pos;

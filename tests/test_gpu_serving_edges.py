@@ -59,3 +59,62 @@ def test_attention_infinities_of_both_signs(etc, kv, new):
     """+inf in one element, -inf in another; where both meet in one, NaN from the later token on."""
     a, b = kv[0] + 1, kv[0] + new[0] // 2
     _attend_to(etc, ref.shape(8, 2, 128), kv, new, [(0, a, 0, math.inf), (0, a, 1, -math.inf), (0, b, 1, math.inf), (0, b, 3, -math.inf), (0, b + 2, 4, math.nan)])
+
+
+# ---- tables: page ids of no pool --------------------------------------------------------------------------------------
+PAGE, N_PAGES, KV, NEW = 16, 8, [20, 5, 0], [3, 30, 18]
+
+
+@pytest.mark.parametrize("where", ["table", "free"])
+@pytest.mark.parametrize("bad", [-1, -(1 << 31), 1 << 27, 1 << 28, (1 << 28) + 1, 1 << 30, (1 << 31) - 1])
+def test_tables_hand_on_no_slot_of_a_page_id_out_of_range(etc, where, bad):
+    """An id below 0 or of more tokens than 31 bits count: `id * page` in 32 bits is a slot of another page, or a negative one that
+    stands for padding.  Its tokens get a slot that append refuses, and tables reports it; everything else is as ever."""
+    s = ref.shape(4, 2, 64, page=PAGE)
+    sv = etc.Serving(s, max_seqs=3, max_tokens=60, max_kv_len=64)
+    table, free = np.full((3, 4), -7, np.int32), [7, 6, 5, 4, 3]      # taken from the end: 3, 4 (sequence 1), 5, 6 (2)
+    table[0, :2], table[1, 0] = [0, 1], 2
+    if where == "table":
+        table[0, 1], seq = bad, 0                         # positions 20 .. 22 lie in it
+    else:
+        free[3], seq = bad, 1                             # the second page of sequence 1's two, positions 32 .. 34
+    rows = 55                                             # 51 tokens and padding
+    e = lambda n: torch.full((n,), 12345, dtype=torch.int32, device="cuda")        # noqa: E731
+    o = {"q_indptr": e(4), "slots": e(rows), "positions": e(rows), "status": e(1), "total_len": e(3)}
+    t, count = i32(table), i32([len(free)])
+    sv.tables(i32(KV), i32(NEW), t, i32(free), count, **o)
+    assert sv.read_error() == (3, 1, seq, bad)
+    want = ref.tables(KV, NEW, table, free, PAGE, rows)
+    slots = np.array([x if 0 <= x < 1 << 31 else (1 << 31) - 1 for x in want["slots"][:51]] + [-1] * 4)
+    held = {"table": slice(0, 3), "free": slice(3 + 27, 3 + 30)}[where]      # the rows of the bad page's tokens
+    slots[held] = (1 << 31) - 1
+    assert np.array_equal(o["slots"].cpu().numpy(), slots)
+    for name in ("q_indptr", "positions", "status", "total_len"):
+        assert np.array_equal(o[name].cpu().numpy(), np.asarray(want[name])), name
+    assert np.array_equal(t.cpu().numpy(), want["block_table"]) and int(count) == 1
+
+    pools = [randn(i, N_PAGES, PAGE, 2, 64).cuda() for i in (1, 2)]
+    before = [p.clone() for p in pools]
+    q, k, v, out = randn(3, rows, 256).cuda(), randn(4, rows, 128).cuda(), randn(5, rows, 128).cuda(), torch.full((rows, 4, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    sv.append(q, k, v, o["positions"], o["slots"], out, *pools)
+    word = sv.read_error()
+    assert word[:2] == (1, 2) and held.start <= word[2] < held.stop and word[3] == (1 << 31) - 1
+    written = torch.zeros(N_PAGES * PAGE, dtype=torch.bool)
+    written[[int(x) for x in slots if 0 <= x < N_PAGES * PAGE]] = True
+    for p, b in zip(pools, before):
+        same = (p == b).view(N_PAGES * PAGE, -1).all(1).cpu()
+        assert torch.equal(same, ~written)
+    good = [r for r, x in enumerate(slots) if 0 <= x < N_PAGES * PAGE]
+    assert torch.equal(pools[1].view(-1, 128)[torch.as_tensor(slots[good]).cuda()], v[good])
+    assert bool((out[held] == 7.0).all()) and sv.read_error() == (0, 0, 0, 0)
+    sv.close()
+
+
+def test_tables_page_ids_to_the_end_of_their_range(etc):
+    """Pages of one token and of 16: the last id whose slots fit 31 bits."""
+    for page, last in ((1, (1 << 31) - 2), (16, (1 << 27) - 1)):
+        sv = etc.Serving(ref.shape(page=page), max_seqs=1, max_tokens=1, max_kv_len=16)
+        o = {n: i32([5] * k) for n, k in (("q_indptr", 2), ("slots", 1), ("positions", 1), ("status", 1))}
+        sv.tables(i32([0]), i32([1]), i32([[0]]), i32([last]), i32([1]), **o)
+        assert int(o["slots"]) == last * page and int(o["status"]) == 0 and sv.read_error() == (0, 0, 0, 0)
+        sv.close()
