@@ -401,7 +401,8 @@ typedef struct {
 etc_status etc_serving_create(const etc_model_desc *model, const etc_serving_limits *limits, etc_serving **out);
 void etc_serving_destroy(etc_serving *s);                   /* synchronises */
 const char *etc_serving_last_error(const etc_serving *s);   /* s may be NULL: error of this thread's last failed create */
-/* Synchronises; word (host) = code (0: none), operator (1 tables .. 4 sample), index, value of what a kernel refused. */
+/* Synchronises the handle's device, whichever is current; word (host) = code (0: none), operator (1 tables .. 4 sample), index, value of
+ * what a kernel refused. */
 etc_status etc_serving_read_error(etc_serving *s, int32_t word[4]);
 
 /* Page tables and slot maps of one step.  Sequence b holds ceil(kv_len[b] / page_size) pages, the first entries of row b of

@@ -190,7 +190,12 @@ etc_status etc_serving_create(const etc_model_desc *m, const etc_serving_limits 
 etc_status etc_serving_read_error(etc_serving *s, int32_t word[4])
 {
     if (!s || !word) return fail(s, ETC_EINVAL, "NULL argument");
-    SRV_TRY(s, hipDeviceSynchronize());
+    int dev = -1;
+    SRV_TRY(s, hipGetDevice(&dev));
+    if (dev != s->device) SRV_TRY(s, hipSetDevice(s->device));      // whose launches the word is about
+    const hipError_t synchronized = hipDeviceSynchronize();
+    if (dev != s->device) SRV_TRY(s, hipSetDevice(dev));
+    SRV_TRY(s, synchronized);
     return report_refusals(s, word);
 }
 

@@ -1,0 +1,26 @@
+"""Handles of the serving operators, on the CPU over a stub runtime (tests/serving_handles.cpp)."""
+import os
+import shutil
+import subprocess
+
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+CSRC = os.path.join(HERE, "..", "paper_2604_13327_amd", "csrc")
+HIP = "/opt/rocm/include"
+
+pytestmark = pytest.mark.skipif(shutil.which("g++") is None or not os.path.isdir(HIP), reason="no compiler or HIP headers")
+
+
+@pytest.fixture(scope="module")
+def program(tmp_path_factory):
+    exe = tmp_path_factory.mktemp("serving") / "serving_handles"
+    subprocess.check_call(["g++", "-O1", "-std=c++17", "-D__HIP_PLATFORM_AMD__", "-fsanitize=undefined", "-fno-sanitize-recover=all",
+                           "-I", CSRC, "-I", HIP, "-o", str(exe), os.path.join(HERE, "serving_handles.cpp")])
+    return str(exe)
+
+
+@pytest.mark.parametrize("which", ["read_error"])
+def test_handles(program, which):
+    out = subprocess.run([program, which], capture_output=True, text=True, timeout=60)
+    assert out.returncode == 0, out.stdout + out.stderr
