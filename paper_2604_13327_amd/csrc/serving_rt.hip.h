@@ -5,13 +5,15 @@
 
 namespace etc {
 
-// Reports something a kernel found in device memory and did not use (pinned host memory; the last report stays, code last).
+// Reports something a kernel found in device memory and did not use (pinned host memory; the last report stays).  Words 2 and 3 in one
+// store, then words 0 and 1, by the first of the lanes that refuse: of refusals at the same time, index and value are one's own.
 __device__ __forceinline__ void refuse(int32_t *error, int code, int op, int index, int value)
 {
-    __hip_atomic_store(as_global(error + 1), op, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
-    __hip_atomic_store(as_global(error + 2), index, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
-    __hip_atomic_store(as_global(error + 3), value, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
-    __hip_atomic_store(as_global(error), code, __ATOMIC_RELEASE, __HIP_MEMORY_SCOPE_SYSTEM);
+    if (lane_id() != __builtin_amdgcn_readfirstlane(lane_id())) return;
+    auto pair = [](int a, int b) { return (uint64_t)(uint32_t)b << 32 | (uint32_t)a; };
+    uint64_t *word = reinterpret_cast<uint64_t *>(error);
+    __hip_atomic_store(as_global(word + 1), pair(index, value), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+    __hip_atomic_store(as_global(word), pair(code, op), __ATOMIC_RELEASE, __HIP_MEMORY_SCOPE_SYSTEM);
 }
 
 typedef __attribute__((ext_vector_type(2))) float f32x2_t;

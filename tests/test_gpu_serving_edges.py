@@ -118,3 +118,19 @@ def test_tables_page_ids_to_the_end_of_their_range(etc):
         sv.tables(i32([0]), i32([1]), i32([[0]]), i32([last]), i32([1]), **o)
         assert int(o["slots"]) == last * page and int(o["status"]) == 0 and sv.read_error() == (0, 0, 0, 0)
         sv.close()
+
+
+# ---- reports ----------------------------------------------------------------------------------------------------------
+def test_a_report_is_of_one_refusal(etc):
+    """Many rows refused at once, by many wavefronts: index and value belong together."""
+    s, n = ref.shape(4, 2, 64), 8192
+    sv = etc.Serving(s, max_seqs=1, max_tokens=n, max_kv_len=100)
+    q, k, v = (torch.zeros(n, w, dtype=torch.bfloat16, device="cuda") for w in (256, 128, 128))
+    out, pools = torch.zeros(n, 4, 64, dtype=torch.bfloat16, device="cuda"), [torch.zeros(2, 16, 2, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    positions = i32(np.zeros(n))
+    for trial in range(20):
+        base = 1000 + 10000 * trial
+        sv.append(q, k, v, positions, i32(base + np.arange(n)), out, *pools)
+        word = sv.read_error()
+        assert word[:2] == (1, 2) and word[3] == base + word[2], word
+    sv.close()
