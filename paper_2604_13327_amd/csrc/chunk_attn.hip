@@ -427,16 +427,24 @@ __device__ __forceinline__ bool any_odd(u32x4 v)          // an exponent of all 
 // Rows go from memory to LDS without a stop in registers: 64 lanes, 16 bytes each, to 1 KB of LDS from `to` on (the same for the
 // whole wavefront).  The compiler would have every LDS read wait for all such loads in flight; here their order is the
 // program's own: arrived(n) waits until at most n of this wavefront's are on their way, a barrier then covers everyone's.
+// The place goes by m0, which an asm statement cannot name among what it overwrites (it is reserved): it is put back.
+#define ETC_FETCH_1K(address, ...)                                                                                                     \
+    do {                                                                                                                               \
+        int m0_;                                                                                                                       \
+        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 " address "\n\ts_mov_b32 m0, %0"        \
+                     : "=&s"(m0_) : "s"(__builtin_amdgcn_readfirstlane(to)), __VA_ARGS__ : "memory");                                  \
+    } while (0)
 template <bool ONCE> __device__ __forceinline__ void fetch_1k(const char *from, uint32_t to)
 {
-    if (ONCE) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" : : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory");
-    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory");
+    if (ONCE) ETC_FETCH_1K("%2, off nt", "v"(from));
+    else ETC_FETCH_1K("%2, off", "v"(from));
 }
 template <bool ONCE> __device__ __forceinline__ void fetch_1k(const char *base, uint32_t lane_off, uint32_t to)      // base the same for the wavefront
 {
-    if (ONCE) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" : : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(lane_off), "s"(base) : "memory");
-    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(lane_off), "s"(base) : "memory");
+    if (ONCE) ETC_FETCH_1K("%2, %3 nt", "v"(lane_off), "s"(base));
+    else ETC_FETCH_1K("%2, %3", "v"(lane_off), "s"(base));
 }
+#undef ETC_FETCH_1K
 template <int N> __device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(%0)" : : "i"(N) : "memory"); }
 
 // LDS of a piece: rows of K and V, and the ids of its pages, a window of them at a time.
