@@ -396,8 +396,9 @@ typedef struct {
 } etc_serving_limits;
 
 /* Of `model` n_q_heads, n_kv_heads (any ratio up to 64), head_dim (64 or 128), page_size (a power of two), rms_eps,
- * rope_theta, qk_norm and vocab (0: no sampling; <= 2^20) are read.  Allocates all workspace.  A model the kernels have no
- * form for: ETC_EINVAL. */
+ * rope_theta, qk_norm and vocab (0: no sampling; <= 2^20) are read.  Allocates all workspace, by the limits: for attention 133 KB
+ * (heads of 128; half for 64) a partial result, at most 1024 of those and none where max_kv_len <= 384; for rows of more than 16383
+ * logits 4 MB and 8 KB a slice, max(256, max_seqs * ceil(vocab / 16383)) of those.  A model the kernels have no form for: ETC_EINVAL. */
 etc_status etc_serving_create(const etc_model_desc *model, const etc_serving_limits *limits, etc_serving **out);
 void etc_serving_destroy(etc_serving *s);                   /* synchronises */
 const char *etc_serving_last_error(const etc_serving *s);   /* s may be NULL: error of this thread's last failed create */

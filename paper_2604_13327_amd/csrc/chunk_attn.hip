@@ -18,17 +18,14 @@ typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((ext_vector_type(2))) short s16x2;
 
 constexpr int kCaWaves = 8, kCaThreads = kCaWaves * 64;
-constexpr int kCaRows = 32 * kCaWaves;      // rows of a block
-constexpr int kCaKeys = 64;                 // keys of a tile
-constexpr int kCaMinTiles = 2;              // of a piece, where keys are cut
-// Items of no more tiles are not cut, nor is a cut estimated.  Whole and as the estimate has it, in us, calls back to back:
+static_assert(kCaRows == 32 * kCaWaves, "32 rows to a wavefront");
+// Items of no more than kCaWholeTiles are not cut, nor is a cut estimated.  Whole and as the estimate has it, in us, calls back to back:
 //   tiles of the longest                          5           6           7           9          10          12          14
 //   3 single tokens, 4 heads of 64 on 2        9.9  11.4   9.9  11.5  10.8  11.4  11.6  12.4  11.8  12.0  12.7  12.4  13.6  12.8
 //   3 single tokens, 32 heads of 128 on 8     12.7  14.0  12.7  14.0  14.4  14.1  15.8  15.2  15.9  15.1  17.5  15.3  19.1  16.5
 //   1 single token, 64 heads of 128 on 8      12.6  14.0  12.0  13.4  14.2  14.1  15.7  15.1  15.1  14.4  16.6  15.3  18.3  16.2
 // With caches turned over between calls: at 6 tiles 13.0 14.5, 17.2 17.8, 16.6 17.0, at 7 tiles 13.9 15.1, 18.9 17.7, 18.9 17.4.  Eight
 // prompts of 20 to 40 tokens, which are estimated and then not cut, lose 1.2 us by the estimate.
-constexpr int kCaWholeTiles = 6;
 constexpr int kCaNarrowRows = 64, kCaNarrowKeys = 128;
 constexpr float kCaNoReference = -3e38f;     // of a row that has seen no key yet
 

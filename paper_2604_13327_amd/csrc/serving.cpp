@@ -156,9 +156,11 @@ etc_status etc_serving_create(const etc_model_desc *m, const etc_serving_limits 
         memset(s->h_error, 0, 4 * sizeof(int32_t));
         SRV_TRY(s, hipHostGetDevicePointer((void **)&D.error, s->h_error, 0));
         SRV_TRY(s, owned_alloc(s, &D.arrive, 2));
-        D.attn_slots = kAttnMaxSlots;
-        SRV_TRY(s, owned_alloc(s, &D.attn_arrive, (size_t)kAttnMaxSlots));
-        SRV_TRY(s, owned_alloc(s, (char **)&D.attn_part, (size_t)kAttnMaxSlots * attention_slot_bytes(m->head_dim), false));
+        D.attn_slots = attention_slots(m->n_q_heads, m->n_kv_heads, *l);
+        if (D.attn_slots > 0) {
+            SRV_TRY(s, owned_alloc(s, &D.attn_arrive, (size_t)D.attn_slots));
+            SRV_TRY(s, owned_alloc(s, (char **)&D.attn_part, (size_t)D.attn_slots * attention_slot_bytes(m->head_dim), false));
+        }
         if (m->vocab > 0) {
             const size_t n = (size_t)sample_slices(m->vocab, l->max_seqs);
             if (n > 0) {

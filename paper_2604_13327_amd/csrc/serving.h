@@ -28,7 +28,7 @@ struct ServingDev {
     // attention: partial results of items whose keys are cut, a slot each, and per item how many have arrived (zero between launches)
     float *attn_part;
     int32_t *attn_arrive;
-    int attn_slots;
+    int attn_slots;              // no cut takes more
     // sampling of long rows: statistics and bins of the slices
     void *smp_stats;
     uint64_t *smp_bins;
@@ -39,6 +39,18 @@ struct ServingDev {
 constexpr int kSampleList = 8192;
 constexpr int kSampleSharedRows = 128;
 constexpr int kAttnMaxSlots = 1024;
+constexpr int kCaRows = 256;                // of attention: rows of a block
+constexpr int kCaKeys = 64;                 // keys of a tile
+constexpr int kCaMinTiles = 2;              // of a piece, where keys are cut
+constexpr int kCaWholeTiles = 6;            // of an item that is not cut (chunk_attn.hip says why)
+// Slots a handle can need: an item's keys are cut into pieces of kCaMinTiles at least, a sequence's rows into blocks.
+inline int attention_slots(int nq, int nkv, const etc_serving_limits &l)
+{
+    const int64_t tiles = ((int64_t)l.max_kv_len + kCaKeys - 1) / kCaKeys, seqs = l.max_seqs < l.max_tokens ? l.max_seqs : l.max_tokens;
+    if (tiles <= kCaWholeTiles) return 0;
+    const int64_t items = ((int64_t)l.max_tokens * (nq / nkv) / kCaRows + seqs) * nkv, slots = items * ((tiles + kCaMinTiles - 1) / kCaMinTiles);
+    return slots < kAttnMaxSlots ? (int)slots : kAttnMaxSlots;
+}
 int64_t attention_slot_bytes(int head_dim);
 int64_t sample_slices(int vocab, int max_rows);
 int64_t sample_stat_bytes();

@@ -62,10 +62,36 @@ static int read_error_waits_for_the_handles_device()
     return 0;
 }
 
+// Partial results of cut keys: a handle's limits say how many can ever be needed, none where the longest sequence is too short to be cut.
+static int memory_follows_the_limits()
+{
+    etc_model_desc m = model();
+    auto bytes = [&](int seqs, int tokens, int kv) -> size_t {
+        const etc_serving_limits l{seqs, tokens, kv};
+        etc_serving *s = nullptr;
+        g_bytes = 0;
+        if (etc_serving_create(&m, &l, &s) != ETC_OK) return (size_t)-1;
+        const size_t n = g_bytes;
+        etc_serving_destroy(s);
+        return n;
+    };
+    const size_t slot = (size_t)etc::attention_slot_bytes(128), all = 1024 * slot;
+    m.vocab = 0;
+    CHECK(bytes(64, 64, 1) < 16384);                      // a handle that only samples, or appends
+    CHECK(bytes(64, 64, 6 * 64) < 16384);                 // 6 tiles are never cut
+    CHECK(bytes(1, 1, 7 * 64) >= 8 * 4 * slot && bytes(1, 1, 7 * 64) < 8 * 4 * slot + 16384);      // 8 heads, 4 parts of 2 tiles at most
+    CHECK(bytes(1, 8, 1000) < 8 * 9 * slot);
+    CHECK(bytes(64, 4096, 1 << 20) >= all && bytes(64, 4096, 1 << 20) < all + 16384);
+    CHECK(bytes(1024, 1 << 20, 1 << 30) >= all && bytes(1024, 1 << 20, 1 << 30) < all + 16384);
+    CHECK(bytes(1, 1, 1 << 30) >= all);
+    return 0;
+}
+
 int main(int argc, char **argv)
 {
     const char *which = argc > 1 ? argv[1] : "";
     if (!strcmp(which, "read_error")) return read_error_waits_for_the_handles_device();
+    if (!strcmp(which, "memory")) return memory_follows_the_limits();
     printf("which?\n");
     return 2;
 }

@@ -61,6 +61,26 @@ def test_attention_infinities_of_both_signs(etc, kv, new):
     _attend_to(etc, ref.shape(8, 2, 128), kv, new, [(0, a, 0, math.inf), (0, a, 1, -math.inf), (0, b, 1, math.inf), (0, b, 3, -math.inf), (0, b + 2, 4, math.nan)])
 
 
+@pytest.mark.parametrize("nq,nkv,d", [(4, 2, 64), (64, 8, 128), (8, 8, 128)])
+@pytest.mark.parametrize("kv,new", [([0], [1]), ([383], [1]), ([384], [1]), ([5000], [1]), ([900], [60]), ([2000, 1500, 10], [1, 3, 1]), ([700] * 40, [1] * 40)])
+def test_attention_of_a_handle_with_tight_limits(etc, nq, nkv, d, kv, new):
+    """The workspace follows the limits; the way keys are cut, and so every bit, is that of a handle with room for everything."""
+    s = ref.shape(nq, nkv, d)
+    total = [a + b for a, b in zip(kv, new)]
+    table, n_pages = ref.paged(total, 16, 3)
+    q, k, v = randn(1, sum(new), nq, d).cuda(), randn(2, n_pages, 16, nkv, d).cuda(), randn(3, n_pages, 16, nkv, d).cuda()
+    outs = []
+    for limits in ((len(kv), sum(new), max(total)), (1024, 1 << 16, 1 << 20)):
+        sv = etc.Serving(s, *limits)
+        out = torch.zeros_like(q)
+        for _ in range(2):
+            sv.attention(q, out, i32(np.concatenate(([0], np.cumsum(new)))), i32(kv), i32(table), k, v)
+        assert sv.read_error() == (0, 0, 0, 0)
+        sv.close()
+        outs.append(out)
+    assert torch.equal(*outs)
+
+
 # ---- tables: page ids of no pool --------------------------------------------------------------------------------------
 PAGE, N_PAGES, KV, NEW = 16, 8, [20, 5, 0], [3, 30, 18]
 

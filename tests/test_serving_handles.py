@@ -20,7 +20,7 @@ def program(tmp_path_factory):
     return str(exe)
 
 
-@pytest.mark.parametrize("which", ["read_error"])
+@pytest.mark.parametrize("which", ["read_error", "memory"])
 def test_handles(program, which):
     out = subprocess.run([program, which], capture_output=True, text=True, timeout=60)
     assert out.returncode == 0, out.stdout + out.stderr
