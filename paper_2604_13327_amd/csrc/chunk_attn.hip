@@ -311,11 +311,18 @@ __device__ __forceinline__ void scores(f32x16 (&s)[KT], const Fragments<D> &F, u
 
 // Softmax of a tile's scores and O^T += V^T . P^T.  l is this lane's sum, over half of the keys.
 // MASKED: keys behind `limit` do not count; their rows of V hold numbers (odd_values has seen to that).
+// The second product takes bf16.  Blocks of many rows (KT 2) round probabilities to it: half a unit of each, 2^-8 of the sum of p |v| at
+// most and, where that sum is much larger than the result, more than the result's own rounding; l sums what was rounded, so that equal
+// values come out as they are.  A second part there is exact to 2^-15 and costs 38 % (4001 tokens behind 30000 keys 3849 -> 5304 us).
+// Blocks of few rows (KT 1), which wait for memory, take both parts, for up to 1 % (64 single tokens over 2000 to 4000 keys 145.7 -> 146.5
+// us, 16 sequences of 5 tokens 52.1 -> 52.4, three short ones 9.7 -> 10.1).  The upper part there is below the probability, so that the
+// rest is positive too: an infinity of V times either part has one sign.
 template <int D, int KT, bool MASKED>
 __device__ __forceinline__ void attend(f32x16 (&s)[KT], f32x16 (&o)[D / 32], float &m, float &l, const Fragments<D> &F, uint32_t base,
                                        int half, float scale, int k0, int limit)
 {
     constexpr int DT = D / 32;
+    constexpr bool SPLIT = KT == 1;
     if constexpr (MASKED) {
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
@@ -344,26 +351,36 @@ __device__ __forceinline__ void attend(f32x16 (&s)[KT], f32x16 (&o)[D / 32], flo
         for (int dt = 0; dt < DT; ++dt) o[dt] *= sc;
     }
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt) {
-        uint32_t p[8];
-#pragma unroll
-        for (int i = 0; i < 16; i += 2) {
-            const float a = exp2_fast(__builtin_fmaf(s[kt][i], scale, -m)), b = exp2_fast(__builtin_fmaf(s[kt][i + 1], scale, -m));
-            p[i >> 1] = to_bf16x2(a, b);                 // half a unit of bf16 of a probability: below the rounding of the output
-            l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(s16x2, p[i >> 1]), __builtin_bit_cast(s16x2, 0x3F803F80u), l, false);
-        }
+    for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int step = kt * 2 + h;
-            const bf16x8 pb = __builtin_bit_cast(bf16x8, u32x4{p[4 * h], p[4 * h + 1], p[4 * h + 2], p[4 * h + 3]});
+            u32x4 p, rest;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float a = exp2_fast(__builtin_fmaf(s[kt][8 * h + 2 * i], scale, -m)), b = exp2_fast(__builtin_fmaf(s[kt][8 * h + 2 * i + 1], scale, -m));
+                if constexpr (SPLIT) {
+                    const uint32_t ah = __builtin_elementwise_sub_sat(__float_as_uint(a), 1u), bh = __builtin_elementwise_sub_sat(__float_as_uint(b), 1u);
+                    p[i] = __builtin_amdgcn_perm(bh, ah, 0x07060302u);
+                    rest[i] = to_bf16x2(a - __uint_as_float(ah & 0xFFFF0000u), b - __uint_as_float(bh & 0xFFFF0000u));
+                    l += a + b;
+                } else {
+                    const uint32_t both = to_bf16x2(a, b);
+                    p[i] = both;
+                    l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(s16x2, both), __builtin_bit_cast(s16x2, 0x3F803F80u), l, false);
+                }
+            }
             if (step + 1 < 2 * KT) {
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) w[(step + 1) & 1][dt] = F.v_frag(base, step + 1, dt);
             }
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w[step & 1][dt]), pb, o[dt], 0, 0, 0);
+            for (int dt = 0; dt < DT; ++dt) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w[step & 1][dt]), __builtin_bit_cast(bf16x8, p), o[dt], 0, 0, 0);
+            if constexpr (SPLIT) {                           // behind all of the first parts': none waits for the one in front of it
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w[step & 1][dt]), __builtin_bit_cast(bf16x8, rest), o[dt], 0, 0, 0);
+            }
         }
-    }
 }
 
 // Values of V that are no numbers, in a tile that some rows see a part of: the probability 0 of what a row does not see would make a
@@ -495,6 +512,7 @@ struct PageWindow {
     int first, end;                         // first page; first key that is not covered
     __device__ __forceinline__ void load(const ServingDev &S, const etc_serving_attention_io &io, ETC_AS_LDS Tiles<D> &B, int b, int key, int key_end, int tid)
     {
+        asm volatile("" : "+v"(tid));                    // addresses of this load: none of them waits in registers for the next window
         first = key >> S.page_shift;
         const int last = (key_end - 1) >> S.page_shift, n = min(last - first + 1, kCaIds);
         end = last - first < kCaIds ? key_end : (int)(((int64_t)(first + kCaIds)) << S.page_shift);

@@ -48,7 +48,7 @@ def _attend_to(etc, s, kv, new, odd, seed=0):
 @pytest.mark.parametrize("nq,nkv,d", [(8, 2, 128), (4, 2, 64), (8, 8, 64)])
 @pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
 @pytest.mark.parametrize("kv,new,pos", [([0], [1], 0), ([0], [9], 3), ([0], [130], 3), ([40], [2], 40), ([40], [100], 41), ([127], [1], 127),
-                                        ([128], [1], 128), ([64], [70], 70), ([5000], [3], 5001), ([5000], [90], 5030), ([5000], [90], 17)])
+                                        ([128], [1], 128), ([64], [70], 70), ([5000], [3], 5001), ([5000], [90], 5030), ([5000], [90], 17), ([5000], [3], 17)])
 def test_attention_infinities_a_row_sees(etc, nq, nkv, d, value, kv, new, pos):
     """In tiles seen whole, in tiles some rows see a part of, and in the first tile of a row or of a piece of its keys."""
     _attend_to(etc, ref.shape(nq, nkv, d), kv, new, [(0, pos, 2, value)])
@@ -59,6 +59,47 @@ def test_attention_infinities_of_both_signs(etc, kv, new):
     """+inf in one element, -inf in another; where both meet in one, NaN from the later token on."""
     a, b = kv[0] + 1, kv[0] + new[0] // 2
     _attend_to(etc, ref.shape(8, 2, 128), kv, new, [(0, a, 0, math.inf), (0, a, 1, -math.inf), (0, b, 1, math.inf), (0, b, 3, -math.inf), (0, b + 2, 4, math.nan)])
+
+
+@pytest.mark.parametrize("nq,nkv,d", [(8, 2, 128), (4, 2, 64)])
+@pytest.mark.parametrize("kv,new", [([300], [1]), ([2000, 10], [5, 1]), ([900], [70])])
+def test_attention_infinities_of_every_key(etc, nq, nkv, d, kv, new):
+    """Every probability times an infinity, those of a single bf16 part among them (the largest score's is 1)."""
+    every = [(b, pos, e, value) for b in range(len(kv)) for pos in range(kv[b] + new[b]) for e, value in ((0, math.inf), (1, -math.inf))]
+    _attend_to(etc, ref.shape(nq, nkv, d), kv, new, every)
+
+
+def _cancelling(etc, s, kv, new, seed):
+    """Values of both signs that nearly cancel: (what came out, the 64-bit form, the sum of p |v|)."""
+    table, n_pages = ref.paged([a + b for a, b in zip(kv, new)], s.page, seed)
+    q_indptr = np.concatenate(([0], np.cumsum(new))).astype(np.int32)
+    q, k, v = randn(seed, int(q_indptr[-1]), s.nq, s.d), randn(seed + 1, n_pages, s.page, s.nkv, s.d), randn(seed + 2, n_pages, s.page, s.nkv, s.d)
+    v = (1000.0 * v.sign() + v.float()).bfloat16()
+    out = torch.zeros(q.shape, dtype=torch.bfloat16, device="cuda")
+    sv = etc.Serving(s, max_seqs=len(kv), max_tokens=int(q_indptr[-1]), max_kv_len=max(a + b for a, b in zip(kv, new)))
+    sv.attention(q.cuda(), out, i32(q_indptr), i32(kv), i32(table), k.cuda(), v.cuda())
+    torch.cuda.synchronize()
+    sv.close()
+    want, size = ref.attention(s, q, k, v, q_indptr, kv, table)
+    return out.double().cpu(), want, size
+
+
+# Rounding of the result (2^-8 of it), and of scores, exponentials and sums (2^-12 of the sum of p |v|, tests/serving_ref.py)
+@pytest.mark.parametrize("nq,nkv,d,kv,new", [(8, 2, 128, [1], [1]), (8, 2, 128, [300, 40], [5, 1]), (4, 2, 64, [700], [32]), (64, 8, 128, [6000, 90], [1, 8])])
+def test_attention_of_few_rows_keeps_its_probabilities(etc, nq, nkv, d, kv, new):
+    """At most 64 rows (tokens times heads to a KV head): a probability is two bf16 parts, exact to 2^-15 (the upper part leaves less than
+    2^-7 of it, the rest is rounded by 2^-8 of that)."""
+    got, want, size = _cancelling(etc, ref.shape(nq, nkv, d), kv, new, 11)
+    err, bound = (got - want).abs(), 2.0 ** -8 * want.abs() + (2.0 ** -12 + 2.0 ** -15) * size
+    assert bool((err <= bound).all()), f"worst error / bound {float((err / bound).max()):.3f}"
+
+
+@pytest.mark.parametrize("nq,nkv,d,kv,new", [(8, 2, 128, [300, 0], [17, 100]), (4, 2, 64, [700], [33]), (64, 8, 128, [6000, 90], [9, 40])])
+def test_attention_of_many_rows_rounds_its_probabilities(etc, nq, nkv, d, kv, new):
+    """More: half a unit of bf16 each, 2^-8 of the sum of p |v| at most, whatever cancels; and again in the sum they are divided by."""
+    got, want, size = _cancelling(etc, ref.shape(nq, nkv, d), kv, new, 12)
+    err, bound = (got - want).abs(), 2.0 ** -8 * (2 * want.abs() + size) + 2.0 ** -12 * size
+    assert bool((err <= bound).all()), f"worst error / bound {float((err / bound).max()):.3f}"
 
 
 @pytest.mark.parametrize("nq,nkv,d", [(4, 2, 64), (64, 8, 128), (8, 8, 128)])
