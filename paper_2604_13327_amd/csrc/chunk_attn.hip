@@ -532,9 +532,12 @@ struct PageWindow {
 // are that key's again (their scores are masked).
 // Where the rows of a load lie in one page (pages of RPL tokens and more) its address is a scalar and a constant of the lane: no vector
 // instruction at all.  (With addresses per lane, and their page ids read from LDS on the spot, the fetches cost the long prompt 16 %.)
-// ONCE: no other workgroup of the launch reads these rows, and the next call that does comes behind all other layers' caches, so they leave
-// no copy in the caches on their way: 64 single tokens over 2000 to 4000 keys 146 us, 159 else; 16 sequences of 5 tokens 53 and 56 us
-// with caches turned over between calls (but 52 and 46 where all 197 MB stay in the memory-side cache from call to call).
+// ONCE, for the blocks of few rows: most rows are read by one workgroup of the launch, and by the next call only behind all other layers'
+// caches, so they leave no copy in the caches on their way.  In us, with ONCE and without, caches turned over between calls / calls back to
+// back: 64 single tokens over 2000 to 4000 keys 152 226 / 146 159, 16 sequences of 5 tokens 57 92 / 52 47, a mixed step 85 103 / 76 66, 16 single
+// tokens over 500 to 1000 keys 26 34 / 22 22, one over 30000 45 69 / 41 39: it loses only where a call finds in the memory-side cache (256 MB) what
+// the call before it read, as a model of one layer would.  Sequences that share pages read rows more than once: 64 tokens with all of 4000
+// keys in common 117 113 / 101 99, with a quarter in common 144 196 / 134 138.
 template <int D, int KEYS, bool ONCE>
 struct Fetch {
     static constexpr int CH = D / 8, RPL = 64 / CH, LOADS = KEYS / RPL / kCaWaves;
