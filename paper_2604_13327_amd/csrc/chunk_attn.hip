@@ -61,7 +61,7 @@ __device__ __forceinline__ int last_not_above(ETC_AS_LDS const int *indptr, int 
 // An item is (sequence, block of rows, KV head).  Its keys are cut into pieces of at most L tiles, about equal ones, with the L out of
 // kCaTries that is estimated to end first; every workgroup computes this by itself from the lengths, one sequence to a thread.  A
 // sequence's long blocks come first, and workgroups take pieces forwards and backwards in turn, so that their sums come out about
-// equal: a chunk of 4096 (512 pieces of 1 to 64 tiles) takes 146 us, 188 where every workgroup takes piece w + 256 after piece w, 164
+// equal: a chunk of 4096 (32 heads of 128 on 8, 512 pieces of 1 to 64 tiles) takes 145 us, 188 where every workgroup takes piece w + 256 after piece w, 164
 // from a queue of pieces.  Where there are more pieces than workgroups, sequences of at most kCaNarrowRows rows (narrow ones) go by
 // length, and their pieces are spread among the others': the former are bound by memory, the latter by LDS and matrix units, and those
 // at the same time are faster than one after the other.  (64 single tokens take 7 % less than as they come, 32 of them with a prompt of
@@ -663,7 +663,7 @@ __device__ __forceinline__ void join_parts(const ServingDev &S, const etc_servin
 
 // A block of more than 64 rows: 32 of them to a wavefront, all wavefronts over the same tiles of 64 keys, in ring slot t % 3: while
 // tile t is being read, t + 1 has arrived or is about to, and the rows of t + 2 are on their way.
-// Measured: 4001 tokens behind 30000 keys, 64 heads of 128 on 8 (4.2 TFLOP): 3.9 ms, 1.08 PFLOP/s, nine tenths of the rate of a large
+// Measured: 4001 tokens behind 30000 keys, 64 heads of 128 on 8 (4.2 TFLOP): 3.8 to 3.9 ms, 1.08 to 1.10 PFLOP/s, nine tenths of the rate of a large
 // library product on this chip; matrix units busy 48 % of the cycles, no bank conflicts, memory idle (1 GB).  The bound is reading K and
 // V from LDS, 32 KB by each of 8 wavefronts, 2048 of a tile's 4000 cycles, with the softmax of the same wavefronts in between; to delay
 // half of the wavefronts, to give them priorities, or to share tiles between early and late rows changed nothing.
@@ -796,10 +796,9 @@ __device__ __forceinline__ void wide_piece(const ServingDev &S, const etc_servin
 
 // A block of at most 64 rows is bound by the rows of the cache: all wavefronts work on the same keys' arrival, four to 128 keys (32 each)
 // for the first 32 rows and four for the rest, and the keys' results are joined in LDS.  Two buffers of 128 keys: one on its
-// way, or both, at any time.  Measured: 16 sequences of 5 tokens behind 2000 to 4100 keys (197 MB): 53 us, 3.7 TB/s, of which about 8 us
-// are there for three short sequences too (launch, cut, page ids, rows and code that no cache holds yet, one after the other).  Many of them: 5.9 TB/s, and 3 % less time without any
-// computation.
-
+// way, or both, at any time.  Measured: 16 sequences of 5 tokens behind 2000 to 4100 keys, 32 heads of 128 on 8 (197 MB): 52 us, 3.8 TB/s, of
+// which about 8 us are there for three short sequences too (launch, cut, page ids, rows and code that no cache holds yet, one after the
+// other); 64 single tokens behind 2000 to 4000 keys (786 MB) 146 us, 5.4 TB/s, behind 16000 to 32000 (6.28 GB) 1040 us, 6.0 TB/s.
 template <int D>
 __device__ __forceinline__ void narrow_piece(const ServingDev &S, const etc_serving_attention_io &io, ETC_AS_LDS CaLds &L, ETC_AS_LDS Tiles<D> &B, const Piece &P)
 {

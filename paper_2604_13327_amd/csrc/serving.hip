@@ -9,7 +9,7 @@ namespace etc {
 // every token row finds its sequence by a search in LDS.  A workgroup computes all sums itself (at most 1024 sequences), so
 // that one launch is enough.  Inputs that outputs may alias (lengths, free count) are written by the workgroup that is the
 // last to have read them.
-// Measured: 3 sequences in 3.8 us, hardly more than an empty launch; 200 with 32397 new tokens in 6.4: a chain of loads, sums, searches.
+// Measured: 3 sequences in 3.8 us, hardly more than an empty launch; 200 with 32397 new tokens in 6.5: a chain of loads, sums, searches.
 constexpr int kTabThreads = 1024;
 
 struct TabSums { int tokens, pages, fresh; };
@@ -145,7 +145,7 @@ hipError_t launch_serving_tables(const ServingDev &S, const etc_serving_tables_i
 // elements is D / 16 neighbouring lanes (its sum of squares: 2 or 3 lane exchanges).  Bound by memory: every row is read and written once.
 // A workgroup takes enough tokens to have work for all threads; their (cos, sin) tables are computed once, in LDS.
 // Measured: 8192 tokens of 64 + 2 * 8 heads of 128, bf16 with norms (336 MB): 59 us, 5.7 TB/s (a large copy: 4.8); 1000 tokens of 32 + 2 * 8
-// heads, fp32 (37 MB): 6.2 us, 5.9 TB/s.
+// heads, fp32 (37 MB): 6.3 us, 5.9 TB/s.
 constexpr int kAppThreads = 256;
 constexpr int kAppMaxTokens = 16;
 
@@ -257,10 +257,12 @@ hipError_t launch_serving_append(const ServingDev &S, const etc_serving_append_i
 // to a list in LDS, where the same is done once more within a bin, and the handful left is compared one by one.
 // Weights are whole numbers of 2^-35 of the largest and summed as such: sums are exact, so no result depends on an order of additions.
 // Long rows: sample_scan (largest and smallest logit) and sample_bins over slices of the rows, as many as fill the chip, then
-// sample_row; short ones: sample_row does it all.  Rows with more tokens in the bins in question than the list holds (flat or with
-// many ties, in the wrong place) and rows with +inf take slow_row, which descends through the bits of the logits' keys instead.
+// sample_row; short ones: sample_row does it all.  Rows with more tokens in the bins in question than the list holds and rows with +inf
+// take slow_row, which descends through the bits of the logits' keys instead.  The former are flat, or have many ties in the wrong
+// place, or a low temperature and a top_k whose last token lies behind all that have weight, in the last bin, with most of the row.
 // Measured: one row of 1024 in 14 us (a quarter of it the first pass, over code that no cache holds yet), 16 rows of 128256 without
-// filters in 30 us (scan 4, bins 7, row 18), 64 in bf16 with all of them in 51 (7, 14, 30).  One compute unit looks through a row of 128256
+// filters in 30 us (scan 4, bins 8, row 18), 64 in bf16 with all of them in 50 (7, 14, 30).  By slow_row 64 in bf16 with a top_k of 50 at a
+// temperature of 0.1 in 327 us (38 at 1); one of 1024, whose last bin fits the list and is compared one by one, in 101 (13 at 1).  One compute unit looks through a row of 128256
 // at 30 bytes a cycle, half of sample_row's time: where there are units for it, several do (33 and 55 us with one to a row).
 constexpr int kSmpThreads = 1024;           // of sample_row
 constexpr int kSliceThreads = 512;
@@ -920,7 +922,7 @@ __device__ __forceinline__ RowEnd fast_row(const SampleArgs &a, FastLds &L, cons
     const uint32_t p0 = L.found[1], p1 = L.found[2], d0 = L.found[3], d1 = L.found[4];
     // The tokens of the bins in question, by intervals of logits a hundredth of a bin wider, in fp32: their ids first, then all their
     // logits at once.  One interval from the first of the bins to the last where that holds few tokens (with filters the ends lie close
-    // together: 64 rows of 128256 with all filters: 55 us for 64, with what follows it and one workgroup to a row), else one for each end.
+    // together: 64 rows of 128256 with all filters took 55 us so, 64 before, with what follows it and one workgroup to a row), else one for each end.
     const uint32_t b0[4] = {d0, p0, bin_k, bin_m0}, b1[4] = {d1, p1, bin_k, bin_m1};
     bool use[4] = {true, use_p, use_k, use_m};
     uint32_t first = d0, last = d1;
