@@ -145,12 +145,9 @@ def load_library(path: str):
     L.etc_destroy.restype = None
     L.etc_destroy.argtypes = [C.c_void_p]
     L.etc_plan_free.restype = None
-    L.etc_serving_last_error.restype = C.c_char_p
-    L.etc_serving_last_error.argtypes = [C.c_void_p]
-    L.etc_serving_destroy.restype = None
-    L.etc_serving_destroy.argtypes = [C.c_void_p]
+    serving = hasattr(L, "etc_serving_create")     # not in libraries generated for a graph before there were serving operators
     for name in EXPORTS:
-        if name not in ("etc_last_error", "etc_destroy", "etc_plan_free", "etc_serving_last_error", "etc_serving_destroy"):
+        if name not in ("etc_last_error", "etc_destroy", "etc_plan_free") and (serving or not name.startswith("etc_serving_")):
             getattr(L, name).restype = C.c_int
     L.etc_create.argtypes = [C.POINTER(ModelDesc), C.POINTER(TileDesc), C.POINTER(SchedDesc), C.POINTER(C.c_void_p)]
     L.etc_bind_layer_weights.argtypes = [C.c_void_p, C.c_int32, C.POINTER(LayerWeights)]
@@ -180,12 +177,17 @@ def load_library(path: str):
     L.etc_plan_free.argtypes = [C.POINTER(PlanView)]
     L.etc_rowsum_launch_noalloc.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]
     L.etc_graph_user_fn_count.argtypes = [C.POINTER(C.c_int32)]
-    L.etc_serving_create.argtypes = [C.POINTER(ModelDesc), C.POINTER(ServingLimits), C.POINTER(C.c_void_p)]
-    L.etc_serving_read_error.argtypes = [C.c_void_p, C.POINTER(C.c_int32)]
-    L.etc_serving_tables.argtypes = [C.c_void_p, C.POINTER(ServingTablesIo), C.c_void_p]
-    L.etc_serving_append.argtypes = [C.c_void_p, C.POINTER(ServingAppendIo), C.c_void_p]
-    L.etc_serving_attention.argtypes = [C.c_void_p, C.POINTER(ServingAttentionIo), C.c_void_p]
-    L.etc_serving_sample.argtypes = [C.c_void_p, C.POINTER(ServingSampleIo), C.c_void_p]
+    if serving:
+        L.etc_serving_last_error.restype = C.c_char_p
+        L.etc_serving_last_error.argtypes = [C.c_void_p]
+        L.etc_serving_destroy.restype = None
+        L.etc_serving_destroy.argtypes = [C.c_void_p]
+        L.etc_serving_create.argtypes = [C.POINTER(ModelDesc), C.POINTER(ServingLimits), C.POINTER(C.c_void_p)]
+        L.etc_serving_read_error.argtypes = [C.c_void_p, C.POINTER(C.c_int32)]
+        L.etc_serving_tables.argtypes = [C.c_void_p, C.POINTER(ServingTablesIo), C.c_void_p]
+        L.etc_serving_append.argtypes = [C.c_void_p, C.POINTER(ServingAppendIo), C.c_void_p]
+        L.etc_serving_attention.argtypes = [C.c_void_p, C.POINTER(ServingAttentionIo), C.c_void_p]
+        L.etc_serving_sample.argtypes = [C.c_void_p, C.POINTER(ServingSampleIo), C.c_void_p]
     return L
 
 

@@ -24,3 +24,13 @@ def program(tmp_path_factory):
 def test_handles(program, which):
     out = subprocess.run([program, which], capture_output=True, text=True, timeout=60)
     assert out.returncode == 0, out.stdout + out.stderr
+
+
+def test_library_without_serving_operators_loads(tmp_path):
+    """One that the front end generated for a graph before the serving operators were there."""
+    from paper_2604_13327_amd import binding
+    src, so = tmp_path / "old.c", tmp_path / "old.so"
+    src.write_text("".join(f"int {name}(void) {{ return 0; }}\n" for name in binding.EXPORTS if not name.startswith("etc_serving_")))
+    subprocess.check_call(["gcc", "-shared", "-fPIC", "-o", str(so), str(src)])
+    L = binding.load_library(str(so))
+    assert L.etc_graph_user_fn_count.argtypes and not hasattr(L, "etc_serving_create")
