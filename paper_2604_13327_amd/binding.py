@@ -543,7 +543,9 @@ class Serving:
     def tables(self, kv_len, new_len, block_table, free_pages, free_count, *, q_indptr, slots, positions, status,
                free_count_out=None, total_len=None, page_indptr=None, page_ids=None, stream=None):
         """Grows block_table [seqs, pages] (in place) for new_len tokens per sequence and maps every new token to its slot and
-        position; int32 tensors.  free_count_out: free_count unless given."""
+        position; int32 tensors.  free_count_out: free_count unless given.  page_indptr and page_ids: both or neither."""
+        if (page_indptr is None) != (page_ids is None):
+            raise ValueError("page_indptr and page_ids go together")
         i32, dev, n, rows = self._i32, self._device, kv_len.shape[0], slots.shape[0]
         cols, free, ids = block_table.shape[-1], free_pages.shape[0], 0 if page_ids is None else page_ids.shape[0]
         table, stride = _rows(block_table, "block_table", i32, (n, cols), dev)

@@ -34,3 +34,15 @@ def test_library_without_serving_operators_loads(tmp_path):
     subprocess.check_call(["gcc", "-shared", "-fPIC", "-o", str(so), str(src)])
     L = binding.load_library(str(so))
     assert L.etc_graph_user_fn_count.argtypes and not hasattr(L, "etc_serving_create")
+
+
+def test_page_arrays_go_together():
+    """One without the other: refused by the call (on the device it is a status of -1 for every step that holds a page)."""
+    import torch
+    from paper_2604_13327_amd.binding import Serving
+    sv = object.__new__(Serving)                          # the check comes in front of any use of the handle
+    sv._h, sv._device, sv._i32 = None, 0, (torch.int32,)
+    t = torch.zeros(2, dtype=torch.int32)
+    for kw in ({"page_indptr": t}, {"page_ids": t}):
+        with pytest.raises(ValueError, match="page_indptr and page_ids"):
+            sv.tables(t, t, t.view(2, 1), t, t[:1], q_indptr=t, slots=t, positions=t, status=t[:1], **kw)
