@@ -457,7 +457,7 @@ typedef struct {
 etc_status etc_serving_append(etc_serving *s, const etc_serving_append_io *io, void *hip_stream);
 
 /* Attention of the new tokens over the paged cache, which holds their own keys and values already: the query at position p
- * of a sequence sees its keys 0 .. p.  out = softmax(q . k / sqrt(head_dim)) . v, fp32 sums and softmax statistics, rounded once.
+ * of a sequence sees its keys 0 .. p.  out = softmax(q . k / sqrt(head_dim)) . v, sums and softmax statistics in fp32.
  * The probabilities of a sequence with more than 64 rows in the call (new tokens * n_q_heads / n_kv_heads) are rounded to bf16, half a
  * unit of each (2^-8 of the sum of p |v| at most); of others they keep 15 bits.
  * What lies in the pool outside a row's keys (later tokens of the chunk, slots behind the last token, pages of others) does

@@ -61,8 +61,8 @@ __device__ __forceinline__ int last_not_above(ETC_AS_LDS const int *indptr, int 
 // An item is (sequence, block of rows, KV head).  Its keys are cut into pieces of at most L tiles, about equal ones, with the L out of
 // kCaTries that is estimated to end first; every workgroup computes this by itself from the lengths, one sequence to a thread.  A
 // sequence's long blocks come first, and workgroups take pieces forwards and backwards in turn, so that their sums come out about
-// equal: a chunk of 4096 (32 heads of 128 on 8, 512 pieces of 1 to 64 tiles) takes 145 us, 188 where every workgroup takes piece w + 256 after piece w, 164
-// from a queue of pieces.  Where there are more pieces than workgroups, sequences of at most kCaNarrowRows rows (narrow ones) go by
+// equal: a chunk of 4096 (32 heads of 128 on 8, 512 pieces of 1 to 64 tiles) takes 145 us, 188 where every workgroup takes piece w + 256
+// after piece w, 164 from a queue of pieces.  Where there are more pieces than workgroups, sequences of at most kCaNarrowRows rows (narrow ones) go by
 // length, and their pieces are spread among the others': the former are bound by memory, the latter by LDS and matrix units, and those
 // at the same time are faster than one after the other.  (64 single tokens take 7 % less than as they come, 32 of them with a prompt of
 // 1000 9 %, 30 with two prompts 2 %, and those 25 % more with all narrow ones in front.)  KV heads are the fastest index of a piece:
@@ -316,7 +316,8 @@ __device__ __forceinline__ void scores(f32x16 (&s)[KT], const Fragments<D> &F, u
 // values come out as they are.  A second part there is exact to 2^-15 and costs 38 % (4001 tokens behind 30000 keys 3849 -> 5304 us).
 // Blocks of few rows (KT 1), which wait for memory, take both parts, for up to 1 % (64 single tokens over 2000 to 4000 keys 145.7 -> 146.5
 // us, 16 sequences of 5 tokens 52.1 -> 52.4, three short ones 9.7 -> 10.1).  The upper part there is below the probability, so that the
-// rest is positive too: an infinity of V times either part has one sign.
+// rest is positive too: an infinity of V times either part has one sign (with probabilities above 2^-103; the rest of smaller ones can
+// be less than a bf16 holds).
 template <int D, int KT, bool MASKED>
 __device__ __forceinline__ void attend(f32x16 (&s)[KT], f32x16 (&o)[D / 32], float &m, float &l, const Fragments<D> &F, uint32_t base,
                                        int half, float scale, int k0, int limit)
@@ -699,7 +700,7 @@ __device__ __forceinline__ void wide_piece(const ServingDev &S, const etc_servin
     f32x16 o[DT];
 #pragma unroll
     for (int i = 0; i < DT; ++i) o[i] = f32x16{};
-    float m = kCaNoReference, l = 0.f;                           // reference of the row's exponentials; sum over this lane's keys
+    float m = kCaNoReference, l = 0.f;                   // reference of the row's exponentials; sum over this lane's keys
     const float scale = 1.44269504088896f / sqrtf((float)D);      // scores and reference count in powers of two
     const Fragments<D> F(lane);
     f32x16 s[2];

@@ -262,8 +262,9 @@ hipError_t launch_serving_append(const ServingDev &S, const etc_serving_append_i
 // place, or a low temperature and a top_k whose last token lies behind all that have weight, in the last bin, with most of the row.
 // Measured: one row of 1024 in 14 us (a quarter of it the first pass, over code that no cache holds yet), 16 rows of 128256 without
 // filters in 30 us (scan 4, bins 8, row 18), 64 in bf16 with all of them in 50 (7, 14, 30).  By slow_row 64 in bf16 with a top_k of 50 at a
-// temperature of 0.1 in 327 us (38 at 1); one of 1024, whose last bin fits the list and is compared one by one, in 101 (13 at 1).  One compute unit looks through a row of 128256
-// at 30 bytes a cycle, half of sample_row's time: where there are units for it, several do (33 and 55 us with one to a row).
+// temperature of 0.1 in 327 us (38 at 1); one of 1024, whose last bin fits the list and is compared one by one, in 101 (13 at 1).
+// One compute unit looks through a row of 128256 at 30 bytes a cycle, half of sample_row's time: where there are units for it, several do
+// (33 and 55 us with one to a row).
 constexpr int kSmpThreads = 1024;           // of sample_row
 constexpr int kSliceThreads = 512;
 constexpr int kSmpBins = 1024;              // a bin: 1 / 1024 of min(32 temperatures, the row's range); a weight below 2^-36 is 0

@@ -69,6 +69,31 @@ def test_attention_infinities_of_every_key(etc, nq, nkv, d, kv, new):
     _attend_to(etc, ref.shape(nq, nkv, d), kv, new, every)
 
 
+@pytest.mark.parametrize("gap", [20.0, 45.0, 65.0])
+@pytest.mark.parametrize("new", [1, 3, 90])
+def test_attention_infinities_of_small_probability(etc, gap, new):
+    """Probabilities down to e^-65 (2^-94), in a tile seen whole and in the last one; what a row does not see leaves no trace."""
+    s, kv = ref.shape(4, 2, 64), 300
+    table, n_pages = ref.paged([kv + new], 16, 1)
+    q, k, v = torch.zeros(new, 4, 64), torch.zeros(n_pages, 16, 2, 64), randn(2, n_pages, 16, 2, 64)
+    q[:, :, 0], q[:, :, 1] = gap / 2, 1.0
+    at = lambda pos: (int(table[0, pos // 16]), pos % 16)        # noqa: E731
+    k[at(7)][:, 0] = 16.0                                 # scores 0 but for this one's, q . k / sqrt(64) = gap
+    k[..., 1] = (randn(3, n_pages, 16, 2) * 4).float()    # and the others' about 0, so that probabilities are of all kinds
+    for pos, e, value in ((40, 0, math.inf), (90, 1, -math.inf), (kv, 2, math.inf), (kv + new - 1, 3, -math.inf), (120, 4, 3.3e38), (kv + new - 1, 5, -3.3e38)):
+        v[at(pos)][:, e] = value
+    q, k = q.bfloat16(), k.bfloat16()
+    out = torch.zeros(q.shape, dtype=torch.bfloat16, device="cuda")
+    sv = etc.Serving(s, max_seqs=1, max_tokens=new, max_kv_len=kv + new)
+    sv.attention(q.cuda(), out, i32([0, new]), i32([kv]), i32(table), k.cuda(), v.cuda())
+    torch.cuda.synchronize()
+    sv.close()
+    want, size = ref.attention(s, q, k, v, [0, new], [kv], table)
+    _same_kinds(out, want)
+    ref.check_attention(out[..., :4], want[..., :4], size[..., :4])
+    ref.check_attention(out[..., 6:], want[..., 6:], size[..., 6:])
+
+
 def _cancelling(etc, s, kv, new, seed):
     """Values of both signs that nearly cancel: (what came out, the 64-bit form, the sum of p |v|)."""
     table, n_pages = ref.paged([a + b for a, b in zip(kv, new)], s.page, seed)
