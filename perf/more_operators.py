@@ -2,8 +2,8 @@
 tokens to a paged cache of e4m3 codes with a power of two for each page and KV head, attention of a chunk over that cache, and log
 probabilities of given tokens with entropy and the likeliest alternatives.
 
-A step of a server that keeps its cache in 8 bits calls, per layer, `append_f8` (rows of the QKV projection in; queries, codes and
-scales out) and `attention_f8`; a request that asks for log probabilities has `score` over its rows of logits.  A case is one call
+A step of a server that keeps its cache in 8 bits calls, per layer, `append_codes` (rows of the QKV projection in; queries, codes and
+scales out) and `attention_codes`; a request that asks for log probabilities has `score` over its rows of logits.  A case is one call
 of one of them.  `run` makes the framework's calls where `own` is true and computes the plain form otherwise.
 """
 from __future__ import annotations
@@ -248,7 +248,7 @@ def _run_append(i):
     nq, nkv, d, norm, theta, eps = HEADS[i.case["shape"]]
     q, k, v = i.qkv[:, :nq * d], i.qkv[:, nq * d:(nq + nkv) * d], i.qkv[:, (nq + nkv) * d:]
     if own:
-        i.serving.append_f8(q, k, v, i.positions, i.slots, i.q_out, i.k, i.v, i.ks, i.vs, gq=i.gq, gk=i.gk)
+        i.serving.append_codes(q, k, v, i.positions, i.slots, i.q_out, i.k, i.v, i.ks, i.vs, gq=i.gq, gk=i.gk)
         return {"q": i.q_out, "k": i.k, "v": i.v, "k_scale": i.ks, "v_scale": i.vs}
     rows = i.slots.shape[0]
     q, k, v = (t.float().reshape(rows, -1, d) for t in (q, k, v))
@@ -288,7 +288,7 @@ def _values(codes, scale, pages):
 
 def _run_attention(i):
     if own:
-        i.serving.attention_f8(i.q, i.out, i.q_indptr, i.kv_len, i.table, i.k, i.v, i.ks, i.vs)
+        i.serving.attention_codes(i.q, i.out, i.q_indptr, i.kv_len, i.table, i.k, i.v, i.ks, i.vs)
         return i.out
     nq = i.q.shape[1]
     few = i.case["few"]
