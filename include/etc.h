@@ -402,8 +402,8 @@ typedef struct {
 etc_status etc_serving_create(const etc_model_desc *model, const etc_serving_limits *limits, etc_serving **out);
 void etc_serving_destroy(etc_serving *s);                   /* synchronises */
 const char *etc_serving_last_error(const etc_serving *s);   /* s may be NULL: error of this thread's last failed create */
-/* Synchronises the handle's device, whichever is current; word (host) = code (0: none), operator (1 tables .. 4 sample), index, value of
- * what a kernel refused. */
+/* Synchronises the handle's device, whichever is current; word (host) = code (0: none), operator (1 tables .. 4 sample, 5 append_codes,
+ * 6 attention_codes, 7 score), index, value of what a kernel refused. */
 etc_status etc_serving_read_error(etc_serving *s, int32_t word[4]);
 
 /* Page tables and slot maps of one step.  Sequence b holds ceil(kv_len[b] / page_size) pages, the first entries of row b of
@@ -500,6 +500,54 @@ typedef struct {
     int32_t *kept_out;              /* [n_rows] number of tokens kept (greedy: 1), or NULL */
 } etc_serving_sample_io;
 etc_status etc_serving_sample(etc_serving *s, const etc_serving_sample_io *io, void *hip_stream);
+
+/* ---- a cache of 8 bits -----------------------------------------------------------------------------------------------
+ * Pools of 8-bit codes (e4m3: 4 significant bits, exponents from 2^-6, largest 448, no infinities) in the layout of the bf16 ones, half
+ * their bytes, and a scale for the tokens of a page and KV head: one byte b, the power of two 2^(b - 127) (e8m0).  A value is its code
+ * times its scale, exactly; a bf16 holds it too.  The decoder's step (etc_launch) reads bf16 pools only. */
+
+/* etc_serving_append to such pools: norms, RoPE and q_out as there, keys (fp32, behind the rotation) and values rounded once, to codes.
+ * The rows of a call that lie in one page stand one after the other, each one's slot the next, as etc_serving_tables gives them (rows that are
+ * left out may stand between them); a page may occur in one such run of a call.  For each page and KV head, of K and of V: x the run's values, E(x) the smallest whole number >= -40
+ * with max |x| <= 448 * 2^E.  A run that begins a page sets the scale to 2^E(x), whatever the page held.  Behind tokens that the page
+ * holds already the scale stays, or grows to 2^E(x) where that is larger, and the tokens in front of the run are rounded again to codes of
+ * it (which changes those only that become less than 2^-6).  Codes are rounded to nearest even; infinities and NaN become NaN, and do not
+ * count in max |x|.  Codes behind the run's last token stay as they are; their tokens are nobody's. */
+typedef struct {
+    etc_serving_append_io append;   /* k_pages, v_pages: codes [n_pages][page_size][n_kv_heads][head_dim] */
+    void *k_scale, *v_scale;        /* bytes [n_pages][n_kv_heads] */
+} etc_serving_append_codes_io;
+etc_status etc_serving_append_codes(etc_serving *s, const etc_serving_append_codes_io *io, void *hip_stream);
+
+/* etc_serving_attention over such pools.  The scores are products of q and the values that the codes stand for: q goes through the
+ * matrix units as two codes of 4 bits each, at scales of its row, exact to 2^-21 of the row's largest element.  The rest as there: sums
+ * and softmax statistics in fp32, probabilities rounded to bf16 for sequences of more than 64 rows in the call and of 15 bits for others,
+ * nothing outside a row's keys reaches it, NaN codes included.  Scale bytes 27 to 227 are supported (append writes 87 to 247 for values
+ * up to 2^128, and none above 227 for values up to 2^108). */
+typedef struct {
+    etc_serving_attention_io attention;      /* k_pages, v_pages: codes, as in etc_serving_append_codes */
+    const void *k_scale, *v_scale;
+} etc_serving_attention_codes_io;
+etc_status etc_serving_attention_codes(etc_serving *s, const etc_serving_attention_codes_io *io, void *hip_stream);
+
+/* Log-probabilities (natural, at temperature 1) of given tokens, the entropy of each row and its likeliest tokens.  p_i = exp(x_i) / sum
+ * exp(x); NaN and -inf logits are banned (p = 0), and next to +inf all finite ones (those that are +inf share alike).  Entropy is
+ * -sum p ln p.  The likeliest are the first n_top in the order larger logit first, equal logits by lower id, without the banned ones;
+ * where fewer are left the places behind them hold token -1, log-probability -inf.  A row with nothing left: log-probability -inf, entropy
+ * 0.  A row whose token is negative is left out, its outputs stay as they were; one whose token is vocab or more as well, and is reported.
+ * exp in fp32, sums in fp32 within a thread and in fp64 across threads, in an order that does not depend on the run. */
+typedef struct {
+    int32_t n_rows, dtype;          /* up to max_tokens; etc_dtype of logits */
+    const void *logits;             /* [n_rows][vocab], rows row_stride elements apart; any alignment of the type */
+    int64_t row_stride;
+    const int32_t *tokens;          /* [n_rows], or NULL: no given tokens, and no row left out */
+    float *logprob_out;             /* [n_rows], with tokens; else NULL */
+    float *entropy_out;             /* [n_rows], or NULL */
+    int32_t n_top;                  /* 0 .. 64 */
+    int32_t *top_ids;               /* [n_rows][n_top], or NULL with n_top = 0 */
+    float *top_logprobs;            /* [n_rows][n_top], or NULL */
+} etc_serving_score_io;
+etc_status etc_serving_score(etc_serving *s, const etc_serving_score_io *io, void *hip_stream);
 
 /* ---- host-only inspection of the scheduling transformation (no device needed) ---------------
  * Instantiates the decoder's event-tensor graph for one sampled batch size exactly as etc_create

@@ -28,7 +28,7 @@ EXPORTS = ["etc_create", "etc_destroy", "etc_last_error", "etc_bind_layer_weight
            "etc_graph_bind_buffer", "etc_graph_bind_shape", "etc_graph_launch", "etc_plan_build", "etc_plan_free",
            "etc_rowsum_launch_noalloc", "etc_graph_user_fn_count", "etc_serving_create", "etc_serving_destroy",
            "etc_serving_last_error", "etc_serving_read_error", "etc_serving_tables", "etc_serving_append",
-           "etc_serving_attention", "etc_serving_sample"]
+           "etc_serving_attention", "etc_serving_sample", "etc_serving_append_codes", "etc_serving_attention_codes", "etc_serving_score"]
 ROWSUM_NOALLOC_MAX_N = 2048
 
 
@@ -118,6 +118,20 @@ class ServingSampleIo(C.Structure):
                 ("token_out", C.c_void_p), ("logprob_out", C.c_void_p), ("kept_out", C.c_void_p)]
 
 
+class ServingAppendCodesIo(C.Structure):
+    _fields_ = [("append", ServingAppendIo), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+
+
+class ServingAttentionCodesIo(C.Structure):
+    _fields_ = [("attention", ServingAttentionIo), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+
+
+class ServingScoreIo(C.Structure):
+    _fields_ = [("n_rows", C.c_int32), ("dtype", C.c_int32), ("logits", C.c_void_p), ("row_stride", C.c_int64), ("tokens", C.c_void_p),
+                ("logprob_out", C.c_void_p), ("entropy_out", C.c_void_p), ("n_top", C.c_int32), ("top_ids", C.c_void_p),
+                ("top_logprobs", C.c_void_p)]
+
+
 TASK_DTYPE = np.dtype([("fn", "u1"), ("layer", "u1"), ("flags", "<u2"), ("c0", "<i4"), ("c1", "<i4"), ("c2", "<i4"),
                        ("wait0", "<i4"), ("wait1", "<i4"), ("notify0", "<i4"), ("id", "<i4")])
 
@@ -147,7 +161,7 @@ def load_library(path: str):
     L.etc_plan_free.restype = None
     serving = hasattr(L, "etc_serving_create")     # not in libraries generated for a graph before there were serving operators
     for name in EXPORTS:
-        if name not in ("etc_last_error", "etc_destroy", "etc_plan_free") and (serving or not name.startswith("etc_serving_")):
+        if name not in ("etc_last_error", "etc_destroy", "etc_plan_free") and (not name.startswith("etc_serving_") or hasattr(L, name)):
             getattr(L, name).restype = C.c_int
     L.etc_create.argtypes = [C.POINTER(ModelDesc), C.POINTER(TileDesc), C.POINTER(SchedDesc), C.POINTER(C.c_void_p)]
     L.etc_bind_layer_weights.argtypes = [C.c_void_p, C.c_int32, C.POINTER(LayerWeights)]
@@ -188,6 +202,10 @@ def load_library(path: str):
         L.etc_serving_append.argtypes = [C.c_void_p, C.POINTER(ServingAppendIo), C.c_void_p]
         L.etc_serving_attention.argtypes = [C.c_void_p, C.POINTER(ServingAttentionIo), C.c_void_p]
         L.etc_serving_sample.argtypes = [C.c_void_p, C.POINTER(ServingSampleIo), C.c_void_p]
+    if hasattr(L, "etc_serving_score"):            # the same for the cache of 8 bits and the scores
+        L.etc_serving_append_codes.argtypes = [C.c_void_p, C.POINTER(ServingAppendCodesIo), C.c_void_p]
+        L.etc_serving_attention_codes.argtypes = [C.c_void_p, C.POINTER(ServingAttentionCodesIo), C.c_void_p]
+        L.etc_serving_score.argtypes = [C.c_void_p, C.POINTER(ServingScoreIo), C.c_void_p]
     return L
 
 
@@ -515,6 +533,7 @@ class Serving:
         self._i32, self._f32, self._bf16 = (torch.int32,), (torch.float32,), (torch.bfloat16,)
         self._float = (torch.bfloat16, torch.float32)
         self._code = {torch.bfloat16: 0, torch.float32: 1}
+        self._f8, self._e8 = (torch.float8_e4m3fn,), (torch.float8_e8m0fnu, torch.uint8)
 
     def _call(self, fn, io, stream):
         st = fn(self._h, C.byref(io), self._stream(self._device) if stream is None else stream.cuda_stream)
@@ -559,38 +578,58 @@ class Serving:
             None if page_ids is None else _tensor(page_ids, "page_ids", i32, (ids,), dev), ids, _tensor(status, "status", i32, (1,), dev))
         self._call(self._L.etc_serving_tables, io, stream)
 
-    def _pool(self, k_pages, v_pages):
-        s, pages = self.shape, k_pages.shape[0]
+    def _pool(self, k_pages, v_pages, kind=None):
+        s, pages, kind = self.shape, k_pages.shape[0], self._bf16 if kind is None else kind
         shape = (pages, s.page, s.nkv, s.d)
-        return _tensor(k_pages, "k_pages", self._bf16, shape, self._device), _tensor(v_pages, "v_pages", self._bf16, shape, self._device), pages
+        return _tensor(k_pages, "k_pages", kind, shape, self._device), _tensor(v_pages, "v_pages", kind, shape, self._device), pages
 
     def append(self, q, k, v, positions, slots, q_out, k_pages, v_pages, gq=None, gk=None, stream=None):
         """Per-head norms (qk_norm models), RoPE and KV append of the rows of a QKV projection: q [tokens, nq * d], k and v
         [tokens, nkv * d], bf16 or fp32, rows may be parts of wider ones; q_out bf16 [tokens, nq, d]; pools of one layer."""
+        io = self._append_io(q, k, v, positions, slots, q_out, self._pool(k_pages, v_pages), gq, gk)
+        self._call(self._L.etc_serving_append, io, stream)
+
+    def _append_io(self, q, k, v, positions, slots, q_out, pool, gq, gk):
         s, n, dev, kind = self.shape, q.shape[0], self._device, (q.dtype,)
         if q.dtype not in self._float:
             raise ValueError(f"q, k and v must be bf16 or fp32, not {q.dtype}")
-        kp, vp, pages = self._pool(k_pages, v_pages)
         qp, qs = _rows(q, "q", kind, (n, s.nq * s.d), dev)
         kk, ks = _rows(k, "k", kind, (n, s.nkv * s.d), dev)
         vv, vs = _rows(v, "v", kind, (n, s.nkv * s.d), dev)
-        io = ServingAppendIo(
+        return ServingAppendIo(
             n, self._code[q.dtype], qp, kk, vv, qs, ks, vs, _tensor(positions, "positions", self._i32, (n,), dev),
             _tensor(slots, "slots", self._i32, (n,), dev), None if gq is None else _tensor(gq, "gq", self._bf16, (s.d,), dev),
             None if gk is None else _tensor(gk, "gk", self._bf16, (s.d,), dev), _tensor(q_out, "q_out", self._bf16, (n, s.nq, s.d), dev),
-            kp, vp, pages)
-        self._call(self._L.etc_serving_append, io, stream)
+            *pool)
 
     def attention(self, q, out, q_indptr, kv_len, block_table, k_pages, v_pages, stream=None):
         """Attention of the new tokens q [tokens, nq, d] (bf16) of every sequence over its pages, the new tokens' own keys
         among them; out like q.  q_indptr [seqs + 1], kv_len [seqs] (tokens in front of the new ones), block_table [seqs, pages]."""
+        self._call(self._L.etc_serving_attention, self._attention_io(q, out, q_indptr, kv_len, block_table, self._pool(k_pages, v_pages)), stream)
+
+    def _attention_io(self, q, out, q_indptr, kv_len, block_table, pool):
         s, n, rows, dev, cols = self.shape, kv_len.shape[0], q.shape[0], self._device, block_table.shape[-1]
-        kp, vp, pages = self._pool(k_pages, v_pages)
         table, stride = _rows(block_table, "block_table", self._i32, (n, cols), dev)
-        io = ServingAttentionIo(
+        return ServingAttentionIo(
             n, rows, _tensor(q, "q", self._bf16, (rows, s.nq, s.d), dev), _tensor(out, "out", self._bf16, (rows, s.nq, s.d), dev),
-            _tensor(q_indptr, "q_indptr", self._i32, (n + 1,), dev), _tensor(kv_len, "kv_len", self._i32, (n,), dev), table, stride, cols, kp, vp, pages)
-        self._call(self._L.etc_serving_attention, io, stream)
+            _tensor(q_indptr, "q_indptr", self._i32, (n + 1,), dev), _tensor(kv_len, "kv_len", self._i32, (n,), dev), table, stride, cols, *pool)
+
+    def _scales(self, k_scale, v_scale, pages):
+        shape = (pages, self.shape.nkv)
+        return _tensor(k_scale, "k_scale", self._e8, shape, self._device), _tensor(v_scale, "v_scale", self._e8, shape, self._device)
+
+    def append_codes(self, q, k, v, positions, slots, q_out, k_pages, v_pages, k_scale, v_scale, gq=None, gk=None, stream=None):
+        """append() to pools of 8 bits: k_pages and v_pages float8_e4m3fn [pages, page, nkv, d], k_scale and v_scale float8_e8m0fnu (or
+        their bytes) [pages, nkv].  The rows of a page stand one after the other with rising slots, as tables() gives them."""
+        pool = self._pool(k_pages, v_pages, self._f8)
+        io = ServingAppendCodesIo(self._append_io(q, k, v, positions, slots, q_out, pool, gq, gk), *self._scales(k_scale, v_scale, pool[2]))
+        self._call(self._L.etc_serving_append_codes, io, stream)
+
+    def attention_codes(self, q, out, q_indptr, kv_len, block_table, k_pages, v_pages, k_scale, v_scale, stream=None):
+        """attention() over pools of 8 bits, as append_codes() fills them."""
+        pool = self._pool(k_pages, v_pages, self._f8)
+        io = ServingAttentionCodesIo(self._attention_io(q, out, q_indptr, kv_len, block_table, pool), *self._scales(k_scale, v_scale, pool[2]))
+        self._call(self._L.etc_serving_attention_codes, io, stream)
 
     def sample(self, logits, u, token_out, temperature=None, top_k=None, top_p=None, min_p=None, logprob_out=None, kept_out=None,
                stream=None):
@@ -604,3 +643,17 @@ class Serving:
             opt(top_k, "top_k", self._i32), opt(top_p, "top_p", f32), opt(min_p, "min_p", f32),
             _tensor(token_out, "token_out", self._i32, (n,), dev), opt(logprob_out, "logprob_out", f32), opt(kept_out, "kept_out", self._i32))
         self._call(self._L.etc_serving_sample, io, stream)
+
+    def score(self, logits, tokens=None, logprob_out=None, entropy_out=None, top_ids=None, top_logprobs=None, stream=None):
+        """Log-probabilities of given tokens [rows] (int32; a negative one leaves its row out) under logits [rows, vocab] (fp32 or bf16, rows
+        may be parts of wider ones), the rows' entropy [rows], and their likeliest tokens with log-probabilities [rows, up to 64]: what is
+        given is written.  At most max_tokens rows."""
+        n, dev, f32 = logits.shape[0], self._device, self._f32
+        top = 0 if top_ids is None else top_ids.shape[-1]
+        opt = lambda t, name, kind, shape: None if t is None else _tensor(t, name, kind, shape, dev)      # noqa: E731
+        rows, stride = _rows(logits, "logits", self._float, (n, int(self.shape.vocab)), dev)
+        io = ServingScoreIo(
+            n, self._code[logits.dtype], rows, stride, opt(tokens, "tokens", self._i32, (n,)), opt(logprob_out, "logprob_out", f32, (n,)),
+            opt(entropy_out, "entropy_out", f32, (n,)), top, opt(top_ids, "top_ids", self._i32, (n, top)),
+            opt(top_logprobs, "top_logprobs", f32, (n, top)))
+        self._call(self._L.etc_serving_score, io, stream)

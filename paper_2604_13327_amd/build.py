@@ -7,9 +7,10 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libetc.so")
-SOURCES = ["api.cpp", "graph.cpp", "megakernel.hip", "serving.cpp", "serving.hip", "chunk_attn.hip"]
+SOURCES = ["api.cpp", "graph.cpp", "megakernel.hip", "serving.cpp", "serving.hip", "chunk_attn.hip",
+           "serving_codes.cpp", "append_codes.hip", "chunk_attn_codes.hip", "score.hip"]
 HEADERS = ["etc_types.h", "arm_args.h", "graph.h", "device_rt.hip.h", "task_gemm.hip.h", "task_attn.hip.h", "task_moe.hip.h",
-           "serving.h", "serving_rt.hip.h"]
+           "serving.h", "serving_handle.h", "serving_rt.hip.h", "chunk_attn_rt.hip.h", "codes_rt.hip.h"]
 
 
 def needs_build() -> bool:

@@ -1,0 +1,408 @@
+// Attention of a chunk of new tokens over a paged cache of 8 bits (include/etc.h, etc_serving_attention_codes).
+//
+// Rows, blocks, pieces and softmax are those of the attention over bf16 (chunk_attn.hip).  The first product takes the codes as they
+// are: K's rows with the scale of their page, and q in two codes of 4 bits, q = hi + lo, each with a scale of its row, by two 32 x 32 x
+// 64 instructions with scales, which take as long as the bf16 ones and read half as much.  The second product is that of bf16: V's codes
+// are converted, with their page's scale, on their way to LDS.
+#ifndef ETC_GENERIC_ONLY
+#include "chunk_attn_rt.hip.h"
+#include "codes_rt.hip.h"
+
+namespace etc {
+
+typedef __attribute__((ext_vector_type(8))) int i32x8;
+
+constexpr int kCa8Keys = 32;                // of a wavefront's step in a narrow piece
+
+__device__ __forceinline__ i32x8 join_codes(u32x4 a, u32x4 b)
+{
+    return i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
+}
+
+// A row of q, this lane's half of it: elements half * D / 2 + 0 .. D / 2 - 1.  A scale takes the row's largest element to 224 .. 448: hi has
+// 4 bits of each element, lo, of scale 2^-4, 4 more of them, down to 2^-13 of a code's unit.  Infinities and NaN are NaN.
+template <int D>
+struct QCodes {
+    i32x8 hi[D / 64], lo[D / 64];
+    int hi_scale, lo_scale;
+    __device__ __forceinline__ void load(const uint16_t *row, int half)
+    {
+        u32x4 w[D / 16];
+        float most = 0.f;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+            w[i] = gld_16B(row + half * (D / 2) + i * 8);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) most = fmaxf(most, fmaxf(fabsf(finite_or_nan(bf16_lo(w[i][j]))), fabsf(finite_or_nan(bf16_hi(w[i][j])))));
+        }
+        hi_scale = scale_byte(partner_max(most), 20);
+        lo_scale = hi_scale - 4;
+        const float inv = one_over_scale(hi_scale);
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const float a = finite_or_nan(bf16_lo(w[i][2 * j])) * inv, b = finite_or_nan(bf16_hi(w[i][2 * j])) * inv;
+                const float c = finite_or_nan(bf16_lo(w[i][2 * j + 1])) * inv, d = finite_or_nan(bf16_hi(w[i][2 * j + 1])) * inv;
+                const uint32_t h = to_f8x4(a, b, c, d);
+                const f32x4 back = from_f8x4(h);
+                hi[i / 4][(i & 3) * 2 + j] = (int)h;
+                lo[i / 4][(i & 3) * 2 + j] = (int)to_f8x4((a - back[0]) * 16.f, (b - back[1]) * 16.f, (c - back[2]) * 16.f, (d - back[3]) * 16.f);
+            }
+    }
+};
+
+// S^T = K . Q^T over 32 keys: the lane's part of a key's row, as of q's, and the byte of the key's scale.
+template <int D>
+__device__ __forceinline__ f32x16 scores_of(const u32x4 (&k)[D / 32], int k_scale, const QCodes<D> &Q)
+{
+    f32x16 s{};
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) {
+        const i32x8 a = join_codes(k[2 * j], k[2 * j + 1]);
+        s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, Q.hi[j], s, 0, 0, 0, k_scale, 0, Q.hi_scale);
+        s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, Q.lo[j], s, 0, 0, 0, k_scale, 0, Q.lo_scale);
+    }
+    return s;
+}
+
+__device__ __forceinline__ bool any_nan_code(u32x4 w)
+{
+    uint32_t nan = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) nan |= (w[i] & 0x7F7F7F7Fu) + 0x01010101u;
+    return (nan & 0x80808080u) != 0;
+}
+
+struct Pool8 { const uint8_t *k, *v, *k_scale, *v_scale; };
+
+template <int D>
+struct Tiles8 {
+    uint16_t rows[512 * D];                 // 128 KB for heads of 128
+    int ids[kCaIds];
+    int k_scale[2][kCaKeys];
+};
+
+// Where the rows of a (sequence, KV head) lie: offset of a key's row in the pools, and of its scale.
+struct Rows8 {
+    int psh, pmask, nkv, kvh;
+    uint32_t row_bytes, head_off;
+    __device__ __forceinline__ Rows8(const ServingDev &S, int kvh_, int D) : psh(S.page_shift), pmask((1 << S.page_shift) - 1), nkv(S.nkv), kvh(kvh_), row_bytes((uint32_t)(S.nkv * D)), head_off((uint32_t)(kvh_ * D)) {}
+    template <int N> __device__ __forceinline__ int page(ETC_AS_LDS const int (&ids)[N], int key, int first) const { return ids[(key >> psh) - first]; }
+    __device__ __forceinline__ uint64_t at(int id, int key) const { return ((uint64_t)(uint32_t)id * row_bytes << psh) + (uint32_t)(key & pmask) * (uint64_t)row_bytes + head_off; }
+    __device__ __forceinline__ uint64_t scale_at(int id) const { return (uint64_t)(uint32_t)id * (uint32_t)nkv + (uint32_t)kvh; }
+};
+
+// ---- a block of more than 64 rows ------------------------------------------------------------------------------------------
+// 32 rows to a wavefront, all wavefronts over the same tiles of 64 keys, in two buffers of LDS: while tile t is being read, t + 1 is on its way
+// through registers, 16 bytes of K and of V to a thread.
+template <int D>
+__device__ __forceinline__ void wide_piece_codes(const ServingDev &S, const etc_serving_attention_io &io, const Pool8 &pool, ETC_AS_LDS CaLds &L, ETC_AS_LDS Tiles8<D> &B, const Piece &P)
+{
+    constexpr int DT = D / 32, PPR = D / 16;             // tiles of the output; pieces (of 16 codes) of a row
+    constexpr uint32_t KBUF = kCaKeys * D, VBUF = kCaKeys * D * 2;
+    static_assert(2 * (KBUF + VBUF) <= 512 * D * 2, "LDS");
+    int tid = (int)threadIdx.x;
+    asm volatile("" : "+v"(tid));                        // of this piece: what is computed from it does not stay in registers across pieces
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, half = lane >> 5, col = lane & 31;
+    const int tile0 = P.tile0, n_tiles = P.tile1, key_end = min(n_tiles * kCaKeys, P.n_keys);
+    PageWindow W{io.block_table + (int64_t)P.b * io.table_stride, 0, 0};
+    W.load<SRV_ATTENTION_CODES>(S, io, B.ids, P.b, tile0 * kCaKeys, key_end, tid);
+
+    const int row = P.r0 + wave * 32 + col, rr = min(row, P.rows - 1), t = rr / P.grp, head = P.kvh * P.grp + (rr - t * P.grp);
+    QCodes<D> Q;
+    Q.load((const uint16_t *)io.q + ((int64_t)(P.seq.q0 + t) * S.nq + head) * D, half);
+    const int limit = P.seq.kv + t;                      // last key this row sees
+    const int first_masked = (P.seq.kv + P.r0 / P.grp + 1) / kCaKeys;      // tiles in front of it are seen whole by all rows of the block
+    const int wave_last = P.seq.kv + min((P.r0 + wave * 32 + 31) / P.grp, P.seq.n - 1);
+    const bool wave_live = P.r0 + wave * 32 < P.rows;
+    const uint32_t k_base = (uint32_t)(uintptr_t)&B.rows[0], v_base = k_base + 2 * KBUF;
+
+    // what this thread brings: row lr of a tile, codes 16 lp .. 16 lp + 15
+    const Rows8 R(S, P.kvh, D);
+    const int lr = tid / PPR, lp = tid % PPR;
+    const bool brings = lr < kCaKeys;
+    u32x4 k_in, v_in;
+    uint32_t ks_in = 0, vs_in = 0;
+    auto load = [&](int tile) {
+        if (!brings) return;
+        const int key = min(tile * kCaKeys + lr, P.n_keys - 1), id = R.page(B.ids, key, W.first);
+        const uint64_t at = R.at(id, key) + lp * 16;
+        k_in = gld_16B(pool.k + at);
+        v_in = gld_16B(pool.v + at);
+        ks_in = *as_global(pool.k_scale + R.scale_at(id));
+        vs_in = *as_global(pool.v_scale + R.scale_at(id));
+    };
+    auto k_swap8 = [](int r) { return D == 128 ? (r >> 1) & 7 : (r >> 2) & 3; };
+    auto put = [&](uint32_t buf) {
+        if (!brings) return;
+        *reinterpret_cast<ETC_AS_LDS u32x4 *>(k_base + buf * KBUF + lr * D + (lp ^ k_swap8(lr)) * 16) = k_in;
+        if (lp == 0) B.k_scale[buf][lr] = (int)ks_in;
+        const uint32_t to = v_base + buf * VBUF + lr * D * 2;
+        const float f = scale_of(vs_in);
+        *reinterpret_cast<ETC_AS_LDS u32x4 *>(to + ((2 * lp) ^ v_swap<D>(lr)) * 16) = f8_to_bf16x8(v_in[0], v_in[1], f);
+        *reinterpret_cast<ETC_AS_LDS u32x4 *>(to + ((2 * lp + 1) ^ v_swap<D>(lr)) * 16) = f8_to_bf16x8(v_in[2], v_in[3], f);
+    };
+
+    f32x16 o[DT];
+#pragma unroll
+    for (int i = 0; i < DT; ++i) o[i] = f32x16{};
+    float m = kCaNoReference, l = 0.f;                   // reference of the row's exponentials; sum over this lane's keys
+    const float scale = 1.44269504088896f / sqrtf((float)D);      // scores and reference count in powers of two
+    const Fragments<D> F(lane);
+    uint32_t k_at[D / 32];                               // of this lane's pieces of K's rows
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) k_at[i] = k_base + col * D + ((half * (D / 32) + i) ^ k_swap8(col)) * 16;
+    f32x16 s[2];
+    auto scores = [&](uint32_t buf) {
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+            u32x4 k[D / 32];
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) k[i] = *reinterpret_cast<ETC_AS_LDS const u32x4 *>(k_at[i] + buf * KBUF + kt * 32 * D);
+            s[kt] = scores_of<D>(k, B.k_scale[buf][kt * 32 + col], Q);
+        }
+    };
+    auto covered = [&](int tile) { return min((tile + 1) * kCaKeys, key_end) <= W.end; };
+    auto ahead = [&](int tile) {                         // the next tile to the other buffer, the one behind it on its way
+        if (tile + 1 < n_tiles) put((tile + 1 - tile0) & 1);
+        if (tile + 2 < n_tiles) {
+            if (!covered(tile + 2)) {
+                __syncthreads();
+                W.load<SRV_ATTENTION_CODES>(S, io, B.ids, P.b, (tile + 2) * kCaKeys, key_end, tid);
+                __syncthreads();
+            }
+            load(tile + 2);
+        }
+    };
+
+    if (tid == 0) L.odd = -1;
+    __syncthreads();
+    load(tile0);
+    put(0);
+    if (tile0 + 1 < n_tiles) {
+        if (!covered(tile0 + 1)) {
+            __syncthreads();
+            W.load<SRV_ATTENTION_CODES>(S, io, B.ids, P.b, (tile0 + 1) * kCaKeys, key_end, tid);
+            __syncthreads();
+        }
+        load(tile0 + 1);
+    }
+    __syncthreads();
+    int tile = tile0;
+    const int n_seen = min(first_masked, n_tiles);
+    for (; tile < n_seen; ++tile) {
+        const uint32_t buf = (tile - tile0) & 1;
+        if (wave_live) scores(buf);
+        ahead(tile);
+        if (wave_live) attend<D, 2, false>(s, o, m, l, F, v_base + buf * VBUF, half, scale, 0, 0);
+        __syncthreads();
+    }
+    for (; tile < n_tiles; ++tile) {
+        const uint32_t buf = (tile - tile0) & 1, v_tile = v_base + buf * VBUF;
+        constexpr int N = D / 64;
+        u32x4 mine[N];
+        uint32_t mine_at[N];
+        bool odd = false;                                // values that are no numbers, in any row of the tile
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            mine_at[u] = v_tile + (u * kCaThreads + tid) * 16;
+            mine[u] = *reinterpret_cast<ETC_AS_LDS const u32x4 *>(mine_at[u]);
+            odd |= any_odd(mine[u]);
+        }
+        if (odd) L.odd = tile;
+        __syncthreads();
+        const bool live = wave_live && tile * kCaKeys <= wave_last;
+        if (__builtin_expect(L.odd == tile, 0)) odd_values<D, kCaKeys, N>(mine, mine_at, o, F, v_tile, half, tile * kCaKeys, limit, live);
+        if (live) scores(buf);
+        ahead(tile);
+        if (live) attend<D, 2, true>(s, o, m, l, F, v_tile, half, scale, tile * kCaKeys, limit);
+        __syncthreads();
+    }
+    l = partner_sum(l);
+    if (P.parts == 1) {
+        if (!wave_live) return;
+        const float inv = 1.0f / l;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                put_out<D>(S, io, P, row, dt * 4 + q, half, f32x4{o[dt][4 * q] * inv, o[dt][4 * q + 1] * inv, o[dt][4 * q + 2] * inv, o[dt][4 * q + 3] * inv});
+        return;
+    }
+    if (wave_live) {
+        const __amdgpu_buffer_rsrc_t d_b = buf_of(partial<D>(S, P.slot0 + P.part * S.nkv, wave));
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                buf_st_16B(d_b, (uint32_t)(((dt * 4 + q) * 64 + lane) * 16),
+                           __builtin_bit_cast(u32x4, f32x4{o[dt][4 * q], o[dt][4 * q + 1], o[dt][4 * q + 2], o[dt][4 * q + 3]}));
+        if (half == 0) buf_st_8B(d_b, (uint32_t)(kCaPartO<D> * 4 + col * 8), u32x2{__float_as_uint(m), __float_as_uint(l)});
+    }
+    join_parts<D>(S, io, L, P, tid, wave, lane);
+}
+
+// ---- a block of at most 64 rows --------------------------------------------------------------------------------------------
+// Bound by the rows of the cache.  Every wavefront goes through keys of its own, 32 at a time, every eighth such step (every fourth of more
+// than 32 rows, which two wavefronts share), without a barrier: K's codes from memory to registers in the order the first product wants
+// them, V's to registers and, converted, to the wavefront's own part of LDS, where the second product reads them transposed.  Two steps are on
+// their way at any time, 16 KB.  The wavefronts' results are joined in LDS.
+template <int D>
+struct Step8 {
+    u32x4 k[D / 32], v[D / 32];
+    uint32_t k_scale, v_scale[D / 32];
+};
+
+template <int D>
+__device__ __forceinline__ void narrow_piece_codes(const ServingDev &S, const etc_serving_attention_io &io, const Pool8 &pool, ETC_AS_LDS CaLds &L, ETC_AS_LDS Tiles8<D> &B, const Piece &P)
+{
+    constexpr int DT = D / 32, PPR = D / 16, RPL = 64 / PPR, LOADS = kCa8Keys / RPL;      // pieces of a row, rows of a load of V, loads
+    static_assert(LOADS == D / 32, "a step's V");
+    int tid = (int)threadIdx.x;
+    asm volatile("" : "+v"(tid));
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, half = lane >> 5, col = lane & 31;
+    const int groups = P.rows <= 32 ? kCaWaves : kCaWaves / 2, rw = wave / groups, kg = wave % groups;      // wavefronts to 32 rows
+    const int key0 = P.tile0 * kCaKeys, key_end = min(P.tile1 * kCaKeys, P.n_keys), n_steps = div_up(key_end - key0, kCa8Keys);
+    PageWindow W{io.block_table + (int64_t)P.b * io.table_stride, 0, 0};
+    W.load<SRV_ATTENTION_CODES>(S, io, B.ids, P.b, key0, key_end, tid);
+
+    const int row = rw * 32 + col, rr = min(row, P.rows - 1), t = rr / P.grp, head = P.kvh * P.grp + (rr - t * P.grp);
+    QCodes<D> Q;
+    Q.load((const uint16_t *)io.q + ((int64_t)(P.seq.q0 + t) * S.nq + head) * D, half);
+    const int limit = min(P.seq.kv + t, key_end - 1);    // last key this row sees in this piece
+    const int all_see = min(P.seq.kv + 1, key_end);      // keys in front of it are seen by all rows
+    const uint32_t base = (uint32_t)(uintptr_t)&B.rows[0], v_buf = base + wave * (kCa8Keys * D * 2);
+
+    const Rows8 R(S, P.kvh, D);
+    auto load = [&](Step8<D> &T, int step) {
+        const int k0 = key0 + step * kCa8Keys;
+        {
+            const int key = min(k0 + col, key_end - 1), id = R.page(B.ids, key, W.first);
+            const uint8_t *const at = pool.k + R.at(id, key) + half * (D / 2);
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) T.k[i] = gld_16B(at + i * 16);
+            T.k_scale = *as_global(pool.k_scale + R.scale_at(id));
+        }
+#pragma unroll
+        for (int u = 0; u < LOADS; ++u) {
+            const int key = min(k0 + u * RPL + lane / PPR, key_end - 1), id = R.page(B.ids, key, W.first);
+            T.v[u] = gld_16B(pool.v + R.at(id, key) + lane % PPR * 16);
+            T.v_scale[u] = *as_global(pool.v_scale + R.scale_at(id));
+        }
+    };
+    f32x16 o[DT];
+#pragma unroll
+    for (int i = 0; i < DT; ++i) o[i] = f32x16{};
+    float m = kCaNoReference, l = 0.f;
+    const float scale = 1.44269504088896f / sqrtf((float)D);
+    const Fragments<D> F(lane);
+    f32x16 s[1];
+    auto work = [&](Step8<D> &T, int step, int end) {
+        const int k0 = key0 + step * kCa8Keys;
+        uint32_t at[2 * LOADS];
+        bool odd = false;
+        in_order();
+#pragma unroll
+        for (int u = 0; u < LOADS; ++u) {
+            const int r = u * RPL + lane / PPR, p = lane % PPR;
+            at[2 * u] = v_buf + r * D * 2 + ((2 * p) ^ v_swap<D>(r)) * 16;
+            at[2 * u + 1] = v_buf + r * D * 2 + ((2 * p + 1) ^ v_swap<D>(r)) * 16;
+            const float f = scale_of(T.v_scale[u]);
+            *reinterpret_cast<ETC_AS_LDS u32x4 *>(at[2 * u]) = f8_to_bf16x8(T.v[u][0], T.v[u][1], f);
+            *reinterpret_cast<ETC_AS_LDS u32x4 *>(at[2 * u + 1]) = f8_to_bf16x8(T.v[u][2], T.v[u][3], f);
+            odd |= any_nan_code(T.v[u]);
+        }
+        in_order();
+        s[0] = scores_of<D>(T.k, (int)T.k_scale, Q);
+        const bool masked = k0 + kCa8Keys > all_see;
+        const bool any = masked && __builtin_amdgcn_ballot_w64(odd) != 0;
+        if (step + 2 * groups < end) load(T, step + 2 * groups);
+        if (!masked) {
+            attend<D, 1, false>(s, o, m, l, F, v_buf, half, scale, 0, 0);
+        } else {
+            if (__builtin_expect(any, 0)) {
+                u32x4 mine[2 * LOADS];
+#pragma unroll
+                for (int u = 0; u < 2 * LOADS; ++u) mine[u] = *reinterpret_cast<ETC_AS_LDS const u32x4 *>(at[u]);
+                odd_values<D, kCa8Keys, 2 * LOADS, true>(mine, at, o, F, v_buf, half, k0, limit, true);
+            }
+            attend<D, 1, true>(s, o, m, l, F, v_buf, half, scale, k0, limit);
+        }
+    };
+    __syncthreads();
+    for (int begin = 0; begin < n_steps;) {              // a window of page ids
+        const int end = W.end < key_end ? (W.end - key0) / kCa8Keys : n_steps;
+        Step8<D> T[2];
+        int step = begin + kg;
+        if (step < end) load(T[0], step);
+        if (step + groups < end) load(T[1], step + groups);
+        for (; step < end; step += 2 * groups) {
+            work(T[0], step, end);
+            if (step + groups < end) work(T[1], step + groups, end);
+        }
+        begin = end;
+        if (begin < n_steps) {
+            __syncthreads();
+            W.load<SRV_ATTENTION_CODES>(S, io, B.ids, P.b, key0 + begin * kCa8Keys, key_end, tid);
+            __syncthreads();
+        }
+    }
+
+    // ---- the wavefronts of a row, in the order of their steps: output pieces of a lane as in a partial result, then m and l
+    l = partner_sum(l);
+    const uint32_t mine_at = base + wave * (kCaPartO<D> * 4), ml_at = (uint32_t)(uintptr_t)&B.ids[0];
+    static_assert(kCaWaves * kCaPartO<D> * 4 <= 512 * D * 2, "LDS");
+    __syncthreads();                                     // everyone's V has been read, and the page ids
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            *reinterpret_cast<ETC_AS_LDS f32x4 *>(mine_at + ((dt * 4 + q) * 64 + lane) * 16) = f32x4{o[dt][4 * q], o[dt][4 * q + 1], o[dt][4 * q + 2], o[dt][4 * q + 3]};
+    if (half == 0) *reinterpret_cast<ETC_AS_LDS f32x2_t *>(ml_at + (wave * 32 + col) * 8) = f32x2_t{m, l};
+    __syncthreads();
+    for (int cc = wave; cc < div_up(P.rows, 32) * (D / 8); cc += kCaWaves) {
+        const int jr = cc / (D / 8), pc = cc % (D / 8);
+        Join J;
+        for (int g = 0; g < groups; ++g) {
+            const f32x2_t ml = *reinterpret_cast<ETC_AS_LDS const f32x2_t *>(ml_at + ((jr * groups + g) * 32 + col) * 8);
+            J.add(ml[0], ml[1], *reinterpret_cast<ETC_AS_LDS const f32x4 *>(base + (jr * groups + g) * (kCaPartO<D> * 4) + (pc * 64 + lane) * 16));
+        }
+        if (P.parts == 1) {
+            put_out<D>(S, io, P, jr * 32 + col, pc, half, J.result());
+        } else {
+            const __amdgpu_buffer_rsrc_t d_b = buf_of(partial<D>(S, P.slot0 + P.part * S.nkv, jr));
+            buf_st_16B(d_b, (uint32_t)((pc * 64 + lane) * 16), __builtin_bit_cast(u32x4, J.o));
+            if (pc == 0 && half == 0) buf_st_8B(d_b, (uint32_t)(kCaPartO<D> * 4 + col * 8), u32x2{__float_as_uint(J.m), __float_as_uint(J.l)});
+        }
+    }
+    if (P.parts > 1) join_parts<D>(S, io, L, P, tid, wave, lane);
+}
+
+template <int D>
+__global__ __launch_bounds__(kCaThreads) void chunk_attention_codes_kernel(ServingDev S, etc_serving_attention_codes_io io8)
+{
+    __shared__ CaLds s_cut;
+    __shared__ __attribute__((aligned(16))) Tiles8<D> s_tiles;
+    ETC_AS_LDS CaLds &L = *as_lds(&s_cut);
+    ETC_AS_LDS Tiles8<D> &B = *as_lds(&s_tiles);
+    const etc_serving_attention_io &io = io8.attention;
+    const Pool8 pool{(const uint8_t *)io.k_pages, (const uint8_t *)io.v_pages, (const uint8_t *)io8.k_scale, (const uint8_t *)io8.v_scale};
+    const int n_pieces = cut<SRV_ATTENTION_CODES>(S, io, L);
+    if (n_pieces == 0) return;
+    for_pieces(S, io, L, n_pieces, [&](const Piece &P) {
+        if (P.rows <= kCaNarrowRows) narrow_piece_codes<D>(S, io, pool, L, B, P);
+        else wide_piece_codes<D>(S, io, pool, L, B, P);
+    });
+}
+
+hipError_t launch_serving_attention_codes(const ServingDev &S, const etc_serving_attention_codes_io &io, hipStream_t s)
+{
+    const dim3 grid(attention_grid(S, io.attention)), block(kCaThreads);
+    if (S.d == 128) hipLaunchKernelGGL((chunk_attention_codes_kernel<128>), grid, block, 0, s, S, io);
+    else hipLaunchKernelGGL((chunk_attention_codes_kernel<64>), grid, block, 0, s, S, io);
+    return hipGetLastError();
+}
+
+}  // namespace etc
+#endif  // ETC_GENERIC_ONLY

@@ -13,8 +13,8 @@ constexpr int kServingMaxKv = 1 << 30;
 constexpr int kServingMaxVocab = 1 << 20;
 
 // Operators in the error word, and what they refuse.
-enum ServingOp { SRV_TABLES = 1, SRV_APPEND = 2, SRV_ATTENTION = 3, SRV_SAMPLE = 4 };
-enum ServingError { SRV_BAD_SLOT = 1, SRV_BAD_LENGTH = 2, SRV_BAD_PAGE = 3 };
+enum ServingOp { SRV_TABLES = 1, SRV_APPEND = 2, SRV_ATTENTION = 3, SRV_SAMPLE = 4, SRV_APPEND_CODES = 5, SRV_ATTENTION_CODES = 6, SRV_SCORE = 7 };
+enum ServingError { SRV_BAD_SLOT = 1, SRV_BAD_LENGTH = 2, SRV_BAD_PAGE = 3, SRV_BAD_TOKEN = 4 };
 
 // A handle's part in every launch.
 struct ServingDev {
@@ -36,6 +36,7 @@ struct ServingDev {
     // [row][kSampleList] the tokens
     int32_t *smp_listed, *smp_done, *smp_list;
 };
+constexpr int kScoreTop = 64;                // likeliest tokens of a row, at most
 constexpr int kSampleList = 8192;
 constexpr int kSampleSharedRows = 128;
 constexpr int kAttnMaxSlots = 1024;
@@ -60,5 +61,8 @@ hipError_t launch_serving_tables(const ServingDev &S, const etc_serving_tables_i
 hipError_t launch_serving_append(const ServingDev &S, const etc_serving_append_io &io, hipStream_t s);
 hipError_t launch_serving_attention(const ServingDev &S, const etc_serving_attention_io &io, hipStream_t s);
 hipError_t launch_serving_sample(const ServingDev &S, const etc_serving_sample_io &io, hipStream_t s);
+hipError_t launch_serving_append_codes(const ServingDev &S, const etc_serving_append_codes_io &io, hipStream_t s);
+hipError_t launch_serving_attention_codes(const ServingDev &S, const etc_serving_attention_codes_io &io, hipStream_t s);
+hipError_t launch_serving_score(const ServingDev &S, const etc_serving_score_io &io, hipStream_t s);
 
 }  // namespace etc

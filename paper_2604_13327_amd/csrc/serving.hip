@@ -149,15 +149,6 @@ hipError_t launch_serving_tables(const ServingDev &S, const etc_serving_tables_i
 constexpr int kAppThreads = 256;
 constexpr int kAppMaxTokens = 16;
 
-template <int D>
-__device__ __forceinline__ float head_sum(float v)          // over D / 16 lanes
-{
-    v += dpp_f32<0xB1>(v);
-    v += dpp_f32<0x4E>(v);
-    if (D == 128) v += dpp_f32<0x141>(v);
-    return v;
-}
-
 template <int D, bool F32>
 __global__ __launch_bounds__(kAppThreads) void serving_append_kernel(ServingDev S, etc_serving_append_io io, int tokens_per_wg)
 {

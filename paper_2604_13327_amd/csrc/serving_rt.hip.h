@@ -16,6 +16,9 @@ __device__ __forceinline__ void refuse(int32_t *error, int code, int op, int ind
     __hip_atomic_store(as_global(word), pair(code, op), __ATOMIC_RELEASE, __HIP_MEMORY_SCOPE_SYSTEM);
 }
 
+// Between LDS writes of a wavefront and reads of other lanes of the same one: the LDS keeps their order, the compiler shall.
+__device__ __forceinline__ void in_order() { asm volatile("" ::: "memory"); }
+
 typedef __attribute__((ext_vector_type(2))) float f32x2_t;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
 // Two values to bf16, round to nearest even (NaN stays NaN).
@@ -35,6 +38,16 @@ __device__ __forceinline__ int wave_scan_i(int v)
     v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
     v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);      // row_bcast 15 into rows 1 and 3
     v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);      // row_bcast 31 into rows 2 and 3
+    return v;
+}
+
+// Sum of a head whose elements lie in D / 16 neighbouring lanes.
+template <int D>
+__device__ __forceinline__ float head_sum(float v)
+{
+    v += dpp_f32<0xB1>(v);
+    v += dpp_f32<0x4E>(v);
+    if (D == 128) v += dpp_f32<0x141>(v);
     return v;
 }
 

@@ -1,0 +1,157 @@
+"""Log-probabilities of given tokens, entropy and likeliest tokens on the GPU, against their plain 64-bit form on the CPU."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import codes_ref as codes
+import serving_ref as ref
+from serving_ref import i32, randn
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def etc():
+    import paper_2604_13327_amd
+    return paper_2604_13327_amd
+
+
+def _run(etc, x, tokens, top, entropy=True, tops=True, max_seqs=None, stride=0, offset=0, serving=None):
+    """x [rows, vocab] on the CPU; rows `stride` elements longer in memory, the first one `offset` elements behind an aligned place."""
+    rows, vocab = x.shape
+    wide = torch.full((rows * (vocab + stride) + offset + 8,), 9.0, dtype=x.dtype, device="cuda")      # larger than most: not to be read
+    view = wide[offset:offset + rows * (vocab + stride)].view(rows, vocab + stride)[:, :vocab]
+    view.copy_(x)
+    sv = serving or etc.Serving(ref.shape(vocab=vocab), max_seqs=min(1024, max_seqs or rows), max_tokens=rows, max_kv_len=1)
+    out = {"logprob": torch.full((rows,), 55.0, device="cuda"), "entropy": torch.full((rows,), 55.0, device="cuda"),
+           "ids": torch.full((rows, top), 55, dtype=torch.int32, device="cuda"), "tops": torch.full((rows, top), 55.0, device="cuda")}
+    sv.score(view, None if tokens is None else i32(tokens), None if tokens is None else out["logprob"], out["entropy"] if entropy else None,
+             out["ids"] if top else None, out["tops"] if top and tops else None)
+    torch.cuda.synchronize()
+    if serving is None:
+        assert sv.read_error() == (0, 0, 0, 0)
+        sv.close()
+    return {k: v.cpu().numpy() for k, v in out.items()}
+
+
+def _check(x, tokens, top, got, rows=None):
+    """A thread adds at most 32 weights and then at most 16 such sums (longer rows than 2^17: 2^(-24) for each 8192 more), all positive: 48
+    roundings of 2^-24; a weight has an exponent rounded at up to 2^5 (2^-19) and an instruction's unit (2^-23): the sum is within 2^-17,
+    and so is its logarithm; the result is rounded once.  The sum of p ln p likewise, relative to the sum of p |ln p|, counted from a
+    reference within 6 of the largest."""
+    for r in range(x.shape[0]) if rows is None else rows:
+        if tokens is not None and tokens[r] < 0:
+            assert got["logprob"][r] == 55.0 and got["entropy"][r] == 55.0 and (got["ids"][r] == 55).all() and (got["tops"][r] == 55.0).all()
+            continue
+        lp, entropy, ids, tops = codes.score(x[r].double().numpy(), None if tokens is None else int(tokens[r]), top)
+        close = lambda a, b, tol: a == b or abs(a - b) <= tol      # noqa: E731
+        if tokens is not None:
+            assert close(got["logprob"][r], lp, 2.0 ** -17 + 2.0 ** -23 * abs(lp)), (r, got["logprob"][r], lp)
+        if got["entropy"][r] != 55.0:
+            assert close(got["entropy"][r], entropy, 2.0 ** -17 * (8 + entropy)), (r, got["entropy"][r], entropy)
+        assert np.array_equal(got["ids"][r], ids), (r, got["ids"][r], ids)
+        assert all(close(a, b, 2.0 ** -17 + 2.0 ** -23 * abs(b)) for a, b in zip(got["tops"][r], tops)), (r, got["tops"][r], tops)
+
+
+def _logits(seed, rows, vocab, dtype=torch.float32):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(rows, vocab, generator=g) * 2.5
+    return x.scatter_add(1, torch.randint(0, vocab, (rows, 8), generator=g), 6 + 2 * torch.randn(rows, 8, generator=g)).to(dtype)
+
+
+def _tokens(seed, rows, vocab):
+    return np.random.default_rng(seed).integers(0, vocab, rows)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,vocab,top", [(1, 1, 1), (3, 2, 5), (2, 7, 64), (5, 63, 20), (1, 1000, 5), (4, 1024, 64), (2, 16383, 20), (2, 16384, 20),
+                                            (1, 50257, 64), (17, 128256, 20), (300, 1111, 3), (257, 20001, 1), (130, 20001, 7), (2, 1 << 20, 33)])
+def test_score(etc, dtype, rows, vocab, top):
+    x, tokens = _logits(rows + vocab, rows, vocab, dtype), _tokens(vocab, rows, vocab)
+    _check(x, tokens, top, _run(etc, x, tokens, top), rows=range(0, rows, max(1, rows // 20)))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocab,stride,offset", [(1001, 0, 1), (1001, 7, 3), (20003, 1, 5), (5, 3, 1), (9, 0, 7)])
+def test_score_alignment(etc, dtype, vocab, stride, offset):
+    x, tokens = _logits(vocab, 6, vocab, dtype), _tokens(1, 6, vocab)
+    _check(x, tokens, 12, _run(etc, x, tokens, 12, stride=stride, offset=offset))
+
+
+@pytest.mark.parametrize("vocab", [500, 30000])
+@pytest.mark.parametrize("top", [1, 20, 64])
+def test_score_shapes_of_rows(etc, vocab, top):
+    """Rows that keep a list busy: rising, falling, flat, few different values, all banned but some, far from zero, steep."""
+    n = torch.arange(vocab).float()
+    g = torch.Generator().manual_seed(vocab)
+    few = torch.full((vocab,), -math.inf)
+    few[torch.randint(0, vocab, (9,), generator=g)] = 1.5
+    end = torch.full((vocab,), -math.inf)
+    end[-1] = -3e38
+    x = torch.stack((n / vocab, -n / vocab, torch.zeros(vocab), torch.randint(0, 3, (vocab,), generator=g).float(), few, torch.randn(vocab, generator=g) + 1e4,
+                     torch.randn(vocab, generator=g) - 3e4, torch.randn(vocab, generator=g) * 1000, n, end, torch.full((vocab,), -0.0) + (n % 2) * 0.0,
+                     torch.randn(vocab, generator=g) * 1e-3))
+    for y in (x, x.bfloat16()):
+        tokens = _tokens(2, y.shape[0], vocab)
+        _check(y, tokens, top, _run(etc, y, tokens, top))
+
+
+@pytest.mark.parametrize("vocab", [300, 40000])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_score_no_numbers(etc, vocab, dtype):
+    x = _logits(5, 12, vocab, dtype)
+    lowest = torch.finfo(dtype).min
+    x[0, ::3], x[1, :] = math.nan, -math.inf
+    x[2, :] = math.nan
+    x[3, 7], x[3, vocab - 1] = math.inf, math.inf
+    x[4, 11] = math.inf
+    x[5, :] = lowest
+    x[6, 1:] = lowest
+    x[7, :] = lowest
+    x[7, 5] = -torch.finfo(dtype).max / 2
+    x[8, 9] = torch.finfo(dtype).max
+    x[9, :], x[9, 3] = -math.inf, -2.0
+    x[10, :vocab // 2] = -math.inf
+    x[11, 5], x[11, 6] = torch.finfo(dtype).max, math.nan
+    x.view(torch.int32 if dtype == torch.float32 else torch.int16)[0, 1] = 0x7F800001 if dtype == torch.float32 else 0x7F81      # a signalling NaN
+    for tokens in (np.full(12, 7), np.array([0, 1, 2, 3, 11, 5, 0, 5, 9, 3, 0, 6])):
+        _check(x, tokens, 9, _run(etc, x, tokens, 9))
+
+
+def test_score_what_is_asked_for(etc):
+    x, tokens = _logits(1, 5, 2000), np.array([3, -1, 5, -7, 1999])
+    _check(x, tokens, 6, _run(etc, x, tokens, 6))
+    _check(x, tokens, 0, _run(etc, x, tokens, 0))
+    _check(x, None, 6, _run(etc, x, None, 6))
+    got = _run(etc, x, None, 6, entropy=False, tops=False)
+    assert (got["entropy"] == 55.0).all() and (got["tops"] == 55.0).all() and np.array_equal(got["ids"], _run(etc, x, None, 6)["ids"])
+    sv = etc.Serving(ref.shape(vocab=2000), max_seqs=1, max_tokens=5, max_kv_len=1)
+    tokens[2] = 2000
+    got = _run(etc, x, tokens, 6, serving=sv)
+    assert sv.read_error() == (4, 7, 2, 2000)
+    tokens[2] = -1
+    _check(x, tokens, 6, got)
+    sv.close()
+
+
+def test_score_after_and_before_sample(etc):
+    """Sampling and scores share a handle's workspace: long rows of both in turn, twice the same."""
+    vocab, rows = 60000, 7
+    x, tokens = _logits(8, rows, vocab), _tokens(9, rows, vocab)
+    sv = etc.Serving(ref.shape(vocab=vocab), max_seqs=rows, max_tokens=rows, max_kv_len=1)
+    dev, u = x.cuda(), torch.full((rows,), 0.37, device="cuda")
+    first = None
+    for _ in range(3):
+        token, lp = torch.zeros(rows, dtype=torch.int32, device="cuda"), torch.zeros(rows, device="cuda")
+        sv.sample(dev, u, token, logprob_out=lp)
+        got = _run(etc, x, tokens, 11, serving=sv)
+        _check(x, tokens, 11, got)
+        again = {"token": token.cpu().numpy(), "lp": lp.cpu().numpy(), **got}
+        first = first or again
+        assert all(np.array_equal(first[k], again[k]) for k in first)
+        drawn = _run(etc, x, token.cpu().numpy(), 0, serving=sv)["logprob"]
+        assert np.allclose(drawn, again["lp"], atol=2.0 ** -16)          # without filters both are the same share
+    assert sv.read_error() == (0, 0, 0, 0)
+    sv.close()
