@@ -77,13 +77,6 @@ __device__ __forceinline__ void rotate_head(float (&a)[8], float (&b)[8], ETC_AS
     }
 }
 
-__device__ __forceinline__ float wave_max_f(float v)
-{
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-    return v;
-}
-
 // Blocks [0, kv_groups * kv_wgs): runs that begin in rows [g * rows_per_wg, ..), heads 4 h .. of K or V.  Blocks behind: queries.
 template <int D, bool F32>
 __global__ __launch_bounds__(kAp8Threads) void serving_append_codes_kernel(ServingDev S, etc_serving_append_codes_io io8, int rows_per_wg, int kv_groups, int kv_wgs, int q_tokens)

@@ -37,29 +37,6 @@ __device__ __forceinline__ void scores(f32x16 (&s)[KT], const Fragments<D> &F, u
     }
 }
 
-// Rows go from memory to LDS without a stop in registers: 64 lanes, 16 bytes each, to 1 KB of LDS from `to` on (the same for the
-// whole wavefront).  The compiler would have every LDS read wait for all such loads in flight; here their order is the
-// program's own: arrived(n) waits until at most n of this wavefront's are on their way, a barrier then covers everyone's.
-// The place goes by m0, which an asm statement cannot name among what it overwrites (it is reserved): it is put back.
-#define ETC_FETCH_1K(address, ...)                                                                                                     \
-    do {                                                                                                                               \
-        int m0_;                                                                                                                       \
-        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 " address "\n\ts_mov_b32 m0, %0"        \
-                     : "=&s"(m0_) : "s"(__builtin_amdgcn_readfirstlane(to)), __VA_ARGS__ : "memory");                                  \
-    } while (0)
-template <bool ONCE> __device__ __forceinline__ void fetch_1k(const char *from, uint32_t to)
-{
-    if (ONCE) ETC_FETCH_1K("%2, off nt", "v"(from));
-    else ETC_FETCH_1K("%2, off", "v"(from));
-}
-template <bool ONCE> __device__ __forceinline__ void fetch_1k(const char *base, uint32_t lane_off, uint32_t to)      // base the same for the wavefront
-{
-    if (ONCE) ETC_FETCH_1K("%2, %3 nt", "v"(lane_off), "s"(base));
-    else ETC_FETCH_1K("%2, %3", "v"(lane_off), "s"(base));
-}
-#undef ETC_FETCH_1K
-template <int N> __device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(%0)" : : "i"(N) : "memory"); }
-
 // LDS of a piece: rows of K and V, and the ids of its pages, a window of them at a time.
 template <int D>
 struct Tiles {
@@ -149,7 +126,7 @@ __device__ __forceinline__ void wide_piece(const ServingDev &S, const etc_servin
     asm volatile("" : "+v"(tid));                        // of this piece: what is computed from it does not stay in registers across pieces
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, half = lane >> 5, col = lane & 31;
     const int tile0 = P.tile0, n_tiles = P.tile1, key_end = min(n_tiles * kCaKeys, P.n_keys);
-    PageWindow W{io.block_table + (int64_t)P.b * io.table_stride, 0, 0};
+    PageWindow<> W{io.block_table + (int64_t)P.b * io.table_stride, 0, 0};
     W.load<SRV_ATTENTION>(S, io, B.ids, P.b, tile0 * kCaKeys, key_end, tid);
 
     // this lane's row: query fragments (right operand: 8 consecutive elements of step ks at ks * 16 + half * 8)
@@ -280,7 +257,7 @@ __device__ __forceinline__ void narrow_piece(const ServingDev &S, const etc_serv
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, half = lane >> 5, col = lane & 31;
     const int rw = wave >> 2, kg = wave & 3;             // rows 32 rw + 0 .. 31, keys 32 kg + 0 .. 31 of a step
     const int key0 = P.tile0 * kCaKeys, key_end = min(P.tile1 * kCaKeys, P.n_keys), n_steps = div_up(key_end - key0, KEYS);
-    PageWindow W{io.block_table + (int64_t)P.b * io.table_stride, 0, 0};
+    PageWindow<> W{io.block_table + (int64_t)P.b * io.table_stride, 0, 0};
     W.load<SRV_ATTENTION>(S, io, B.ids, P.b, key0, key_end, tid);
 
     const int row = rw * 32 + col, rr = min(row, P.rows - 1), t = rr / P.grp, head = P.kvh * P.grp + (rr - t * P.grp);

@@ -12,7 +12,11 @@ namespace etc {
 
 typedef __attribute__((ext_vector_type(8))) int i32x8;
 
+typedef __attribute__((ext_vector_type(2))) int i32x2;
+
 constexpr int kCa8Keys = 32;                // of a wavefront's step in a narrow piece
+
+__device__ __forceinline__ void read_from_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }      // what was asked for is in registers
 
 __device__ __forceinline__ i32x8 join_codes(u32x4 a, u32x4 b)
 {
@@ -66,21 +70,16 @@ __device__ __forceinline__ f32x16 scores_of(const u32x4 (&k)[D / 32], int k_scal
     return s;
 }
 
-__device__ __forceinline__ bool any_nan_code(u32x4 w)
-{
-    uint32_t nan = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) nan |= (w[i] & 0x7F7F7F7Fu) + 0x01010101u;
-    return (nan & 0x80808080u) != 0;
-}
-
 struct Pool8 { const uint8_t *k, *v, *k_scale, *v_scale; };
 
+constexpr int kCa8Ids = kCaThreads;         // page ids in LDS, with their scales: one to a thread
 template <int D>
 struct Tiles8 {
     uint16_t rows[512 * D];                 // 128 KB for heads of 128
-    int ids[kCaIds];
-    int k_scale[2][kCaKeys];
+    int ids[kCa8Ids];
+    uint8_t k_byte[kCa8Ids], v_byte[kCa8Ids];      // narrow pieces: scales of the pages
+    float v_scale[kCaWaves][kCa8Keys];      // of a wavefront's keys
+    int k_scale[2][kCaKeys];                // wide pieces: of a tile's keys
 };
 
 // Where the rows of a (sequence, KV head) lie: offset of a key's row in the pools, and of its scale.
@@ -106,7 +105,7 @@ __device__ __forceinline__ void wide_piece_codes(const ServingDev &S, const etc_
     asm volatile("" : "+v"(tid));                        // of this piece: what is computed from it does not stay in registers across pieces
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, half = lane >> 5, col = lane & 31;
     const int tile0 = P.tile0, n_tiles = P.tile1, key_end = min(n_tiles * kCaKeys, P.n_keys);
-    PageWindow W{io.block_table + (int64_t)P.b * io.table_stride, 0, 0};
+    PageWindow<kCa8Ids> W{io.block_table + (int64_t)P.b * io.table_stride, 0, 0};
     W.load<SRV_ATTENTION_CODES>(S, io, B.ids, P.b, tile0 * kCaKeys, key_end, tid);
 
     const int row = P.r0 + wave * 32 + col, rr = min(row, P.rows - 1), t = rr / P.grp, head = P.kvh * P.grp + (rr - t * P.grp);
@@ -140,8 +139,8 @@ __device__ __forceinline__ void wide_piece_codes(const ServingDev &S, const etc_
         if (lp == 0) B.k_scale[buf][lr] = (int)ks_in;
         const uint32_t to = v_base + buf * VBUF + lr * D * 2;
         const float f = scale_of(vs_in);
-        *reinterpret_cast<ETC_AS_LDS u32x4 *>(to + ((2 * lp) ^ v_swap<D>(lr)) * 16) = f8_to_bf16x8(v_in[0], v_in[1], f);
-        *reinterpret_cast<ETC_AS_LDS u32x4 *>(to + ((2 * lp + 1) ^ v_swap<D>(lr)) * 16) = f8_to_bf16x8(v_in[2], v_in[3], f);
+        *reinterpret_cast<ETC_AS_LDS u32x4 *>(to + ((2 * lp) ^ v_swap<D>(lr)) * 16) = codes_to_bf16x8(v_in[0], v_in[1], f);
+        *reinterpret_cast<ETC_AS_LDS u32x4 *>(to + ((2 * lp + 1) ^ v_swap<D>(lr)) * 16) = codes_to_bf16x8(v_in[2], v_in[3], f);
     };
 
     f32x16 o[DT];
@@ -245,26 +244,122 @@ __device__ __forceinline__ void wide_piece_codes(const ServingDev &S, const etc_
 
 // ---- a block of at most 64 rows --------------------------------------------------------------------------------------------
 // Bound by the rows of the cache.  Every wavefront goes through keys of its own, 32 at a time, every eighth such step (every fourth of more
-// than 32 rows, which two wavefronts share), without a barrier: K's codes from memory to registers in the order the first product wants
-// them, V's to registers and, converted, to the wavefront's own part of LDS, where the second product reads them transposed.  Two steps are on
-// their way at any time, 16 KB.  The wavefronts' results are joined in LDS.
+// than 32 rows, which two wavefronts share), without a barrier: codes go to its own part of LDS, two steps of them on their way or at hand, and from
+// there to registers as they are, K's as rows, V's transposed, so that a step's place is free for the one behind the next while it is worked on.
+// V's codes become bf16 without their scales, which the probabilities take (keys of one instruction may lie in several pages).
+// The wavefronts' results are joined in LDS.
+
+// NaN codes of V, among keys that some rows do not see: 1 in a byte of each; 0 in their place; as bf16, 1 where there is one.
+__device__ __forceinline__ uint32_t nan_mask(uint32_t w) { return (((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) >> 7; }
+__device__ __forceinline__ uint32_t without_nan(uint32_t w) { return w & ~(nan_mask(w) * 0xFFu); }
+__device__ __forceinline__ u32x4 nan_counts(u32x2 w)
+{
+    auto pair = [](uint32_t m, int at) { return ((m >> at & 1u) | (m >> (at + 8) & 1u) << 16) * 0x3F80u; };
+    const uint32_t m = nan_mask(w[0]), n = nan_mask(w[1]);
+    return u32x4{pair(m, 0), pair(m, 16), pair(n, 0), pair(n, 16)};
+}
+
+// A wavefront's steps on their way to LDS: 32 rows of K, behind them 32 of V, D bytes each; a row's 16-byte pieces change places with the row
+// so that 16 rows of a piece lie in different banks.
 template <int D>
-struct Step8 {
-    u32x4 k[D / 32], v[D / 32];
-    uint32_t k_scale, v_scale[D / 32];
+struct Ring8 {
+    static constexpr int PPR = D / 16, RPL = 64 / PPR, LOADS = kCa8Keys / RPL;      // pieces of a row, rows of a load, loads of K (and of V)
+    static constexpr uint32_t HALF = kCa8Keys * D, STEP = 2 * HALF;
+    static __device__ __forceinline__ int swap(int row) { return D == 128 ? (row >> 1) & 7 : (row >> 2) & 3; }
+    const Pool8 &pool;
+    ETC_AS_LDS const int (&ids)[kCa8Ids];
+    const Rows8 &R;
+    uint32_t base;                          // of the wavefront's part of LDS
+    int lane, key0, last_key;
+    uint32_t off[2];                        // of the lane, from the page's row of a load's first key on: loads with an even number, and odd ones
+    __device__ __forceinline__ Ring8(const Pool8 &pool_, ETC_AS_LDS const int (&ids_)[kCa8Ids], const Rows8 &R_, uint32_t base_, int lane_, int key0_, int last)
+        : pool(pool_), ids(ids_), R(R_), base(base_), lane(lane_), key0(key0_), last_key(last)
+    {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) off[u] = (lane / PPR) * R.row_bytes + R.head_off + ((lane % PPR) ^ swap(u * RPL + lane / PPR)) * 16;
+    }
+    __device__ __forceinline__ void fetch(int step, int buf, int first_page)
+    {
+        const int k0 = key0 + step * kCa8Keys;
+        const uint32_t to = base + buf * STEP;
+        if (R.pmask + 1 >= RPL && k0 + kCa8Keys - 1 <= last_key) {      // a load's rows lie in one page: scalar addresses
+            int id[LOADS];
+#pragma unroll
+            for (int u = 0; u < LOADS; ++u) id[u] = R.page(ids, k0 + u * RPL, first_page);
+#pragma unroll
+            for (int u = 0; u < LOADS; ++u) {
+                const uint64_t at = ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane(id[u]) * R.row_bytes << R.psh) + (uint64_t)((uint32_t)((k0 + u * RPL) & R.pmask) * (uint64_t)R.row_bytes);
+                fetch_1k<true>((const char *)pool.k + at, off[u & 1], to + u * 1024);
+                fetch_1k<true>((const char *)pool.v + at, off[u & 1], to + HALF + u * 1024);
+            }
+        } else {
+#pragma unroll 1
+            for (int u = 0; u < LOADS; ++u) {
+                const int r = u * RPL + lane / PPR, key = min(k0 + r, last_key);
+                const uint64_t at = R.at(R.page(ids, key, first_page), key) + ((lane % PPR) ^ swap(r)) * 16;
+                fetch_1k<true>((const char *)pool.k + at, to + u * 1024);
+                fetch_1k<true>((const char *)pool.v + at, to + HALF + u * 1024);
+            }
+        }
+    }
 };
+
+// Softmax of a step's scores and O^T += V^T . P^T, as attend() of few rows: both parts of a probability.  v: V's codes, [16 keys][32 elements], a
+// lane's 8 keys of an element in the order the scores have them; by: the scales of the lane's 16 keys.
+template <int D, bool MASKED>
+__device__ __forceinline__ void attend_codes(f32x16 &s, f32x16 (&o)[D / 32], float &m, float &l, const u32x2 (&v)[2][D / 32], const f32x4 (&by)[4], int half, float scale, int k0, int limit)
+{
+    constexpr int DT = D / 32;
+    if constexpr (MASKED) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (k0 + 8 * (i >> 2) + 4 * half + (i & 3) > limit) s[i] = -INFINITY;
+    }
+    float mt = s[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mt = fmaxf(mt, s[i]);
+    mt = partner_max(mt) * scale;
+    if (__builtin_amdgcn_ballot_w64(mt > m + 8.f) != 0) {
+        const float nm = fmaxf(m, mt), sc = MASKED && m == kCaNoReference ? 1.f : exp2_fast(m - nm);      // (NaN that are in o already stay)
+        m = nm;
+        l *= sc;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[dt] *= sc;
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        u32x4 p, rest;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float a = exp2_fast(__builtin_fmaf(s[8 * h + 2 * i], scale, -m)), b = exp2_fast(__builtin_fmaf(s[8 * h + 2 * i + 1], scale, -m));
+            l += a + b;
+            a *= by[2 * h + (i >> 1)][(i & 1) * 2];
+            b *= by[2 * h + (i >> 1)][(i & 1) * 2 + 1];
+            const uint32_t ah = __float_as_uint(a), bh = __float_as_uint(b);      // the upper part below the probability; codes hold no infinities, so 0 may be one
+            p[i] = __builtin_amdgcn_perm(bh, ah, 0x07060302u);
+            rest[i] = to_bf16x2(a - __uint_as_float(ah & 0xFFFF0000u), b - __uint_as_float(bh & 0xFFFF0000u));
+        }
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+            const bf16x8 w = __builtin_bit_cast(bf16x8, codes_to_bf16x8(v[h][dt][0], v[h][dt][1], 1.f));
+            o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, __builtin_bit_cast(bf16x8, p), o[dt], 0, 0, 0);
+            o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, __builtin_bit_cast(bf16x8, rest), o[dt], 0, 0, 0);
+        }
+    }
+}
 
 template <int D>
 __device__ __forceinline__ void narrow_piece_codes(const ServingDev &S, const etc_serving_attention_io &io, const Pool8 &pool, ETC_AS_LDS CaLds &L, ETC_AS_LDS Tiles8<D> &B, const Piece &P)
 {
-    constexpr int DT = D / 32, PPR = D / 16, RPL = 64 / PPR, LOADS = kCa8Keys / RPL;      // pieces of a row, rows of a load of V, loads
-    static_assert(LOADS == D / 32, "a step's V");
+    constexpr int DT = D / 32;
+    typedef Ring8<D> Ring;
+    static_assert(kCaWaves * 2 * Ring::STEP <= 512 * D * 2, "LDS");
     int tid = (int)threadIdx.x;
     asm volatile("" : "+v"(tid));
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, half = lane >> 5, col = lane & 31;
     const int groups = P.rows <= 32 ? kCaWaves : kCaWaves / 2, rw = wave / groups, kg = wave % groups;      // wavefronts to 32 rows
     const int key0 = P.tile0 * kCaKeys, key_end = min(P.tile1 * kCaKeys, P.n_keys), n_steps = div_up(key_end - key0, kCa8Keys);
-    PageWindow W{io.block_table + (int64_t)P.b * io.table_stride, 0, 0};
+    PageWindow<kCa8Ids> W{io.block_table + (int64_t)P.b * io.table_stride, 0, 0};
     W.load<SRV_ATTENTION_CODES>(S, io, B.ids, P.b, key0, key_end, tid);
 
     const int row = rw * 32 + col, rr = min(row, P.rows - 1), t = rr / P.grp, head = P.kvh * P.grp + (rr - t * P.grp);
@@ -272,79 +367,112 @@ __device__ __forceinline__ void narrow_piece_codes(const ServingDev &S, const et
     Q.load((const uint16_t *)io.q + ((int64_t)(P.seq.q0 + t) * S.nq + head) * D, half);
     const int limit = min(P.seq.kv + t, key_end - 1);    // last key this row sees in this piece
     const int all_see = min(P.seq.kv + 1, key_end);      // keys in front of it are seen by all rows
-    const uint32_t base = (uint32_t)(uintptr_t)&B.rows[0], v_buf = base + wave * (kCa8Keys * D * 2);
+    const uint32_t base = (uint32_t)(uintptr_t)&B.rows[0], mine = base + wave * 2 * Ring::STEP;
 
     const Rows8 R(S, P.kvh, D);
-    auto load = [&](Step8<D> &T, int step) {
-        const int k0 = key0 + step * kCa8Keys;
-        {
-            const int key = min(k0 + col, key_end - 1), id = R.page(B.ids, key, W.first);
-            const uint8_t *const at = pool.k + R.at(id, key) + half * (D / 2);
+    Ring G(pool, B.ids, R, mine, lane, key0, key_end - 1);
+    uint32_t k_at[DT], v_at[DT];                         // LDS addresses of this lane's pieces of a step that starts at 0
+    const int v_row = 4 * half + ((lane & 7) >> 1) + (lane & 8), v_piece = (lane >> 4) & 1;      // 8 rows to 16 lanes, 8 codes each: rows 4 half .. and 8 + 4 half ..
 #pragma unroll
-            for (int i = 0; i < D / 32; ++i) T.k[i] = gld_16B(at + i * 16);
-            T.k_scale = *as_global(pool.k_scale + R.scale_at(id));
-        }
-#pragma unroll
-        for (int u = 0; u < LOADS; ++u) {
-            const int key = min(k0 + u * RPL + lane / PPR, key_end - 1), id = R.page(B.ids, key, W.first);
-            T.v[u] = gld_16B(pool.v + R.at(id, key) + lane % PPR * 16);
-            T.v_scale[u] = *as_global(pool.v_scale + R.scale_at(id));
-        }
-    };
+    for (int i = 0; i < DT; ++i) {
+        k_at[i] = mine + col * D + ((half * DT + i) ^ Ring::swap(col)) * 16;
+        v_at[i] = mine + Ring::HALF + v_row * D + ((i * 2 + v_piece) ^ Ring::swap(v_row)) * 16 + (lane & 1) * 8;
+    }
     f32x16 o[DT];
 #pragma unroll
     for (int i = 0; i < DT; ++i) o[i] = f32x16{};
     float m = kCaNoReference, l = 0.f;
     const float scale = 1.44269504088896f / sqrtf((float)D);
-    const Fragments<D> F(lane);
-    f32x16 s[1];
-    auto work = [&](Step8<D> &T, int step, int end) {
-        const int k0 = key0 + step * kCa8Keys;
-        uint32_t at[2 * LOADS];
-        bool odd = false;
-        in_order();
-#pragma unroll
-        for (int u = 0; u < LOADS; ++u) {
-            const int r = u * RPL + lane / PPR, p = lane % PPR;
-            at[2 * u] = v_buf + r * D * 2 + ((2 * p) ^ v_swap<D>(r)) * 16;
-            at[2 * u + 1] = v_buf + r * D * 2 + ((2 * p + 1) ^ v_swap<D>(r)) * 16;
-            const float f = scale_of(T.v_scale[u]);
-            *reinterpret_cast<ETC_AS_LDS u32x4 *>(at[2 * u]) = f8_to_bf16x8(T.v[u][0], T.v[u][1], f);
-            *reinterpret_cast<ETC_AS_LDS u32x4 *>(at[2 * u + 1]) = f8_to_bf16x8(T.v[u][2], T.v[u][3], f);
-            odd |= any_nan_code(T.v[u]);
-        }
-        in_order();
-        s[0] = scores_of<D>(T.k, (int)T.k_scale, Q);
-        const bool masked = k0 + kCa8Keys > all_see;
-        const bool any = masked && __builtin_amdgcn_ballot_w64(odd) != 0;
-        if (step + 2 * groups < end) load(T, step + 2 * groups);
-        if (!masked) {
-            attend<D, 1, false>(s, o, m, l, F, v_buf, half, scale, 0, 0);
-        } else {
-            if (__builtin_expect(any, 0)) {
-                u32x4 mine[2 * LOADS];
-#pragma unroll
-                for (int u = 0; u < 2 * LOADS; ++u) mine[u] = *reinterpret_cast<ETC_AS_LDS const u32x4 *>(at[u]);
-                odd_values<D, kCa8Keys, 2 * LOADS, true>(mine, at, o, F, v_buf, half, k0, limit, true);
-            }
-            attend<D, 1, true>(s, o, m, l, F, v_buf, half, scale, k0, limit);
-        }
+    auto v_codes = [&](int buf, int h, int i) {
+        return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(reinterpret_cast<ETC_AS_LDS i32x2 *>(v_at[i] + buf * Ring::STEP + h * 16 * D)));
     };
+    // NaN codes of V in a step that some rows see a part of: the probability 0 of what a row does not see would make a NaN of them.  Counted by a
+    // product over the keys a row sees, which goes to the output; the step then holds zeros in their place.
+    auto without_nans = [&](int k0, int buf) {
+        auto piece = [&](int u) { return reinterpret_cast<ETC_AS_LDS u32x4 *>(mine + buf * Ring::STEP + Ring::HALF + (u * 64 + lane) * 16); };
+        uint32_t nan = 0;
+#pragma unroll
+        for (int u = 0; u < Ring::LOADS; ++u) {
+            const u32x4 w = *piece(u);
+            nan |= nan_mask(w[0]) | nan_mask(w[1]) | nan_mask(w[2]) | nan_mask(w[3]);
+        }
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(nan != 0) == 0, 1)) return;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+            f32x16 n{};
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+                u32x4 seen;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int key = k0 + h * 16 + 4 * half + (j >> 1) * 8 + (j & 1) * 2;
+                    seen[j] = (key <= limit ? 0x3F80u : 0u) | (key + 1 <= limit ? 0x3F800000u : 0u);
+                }
+                n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, nan_counts(v_codes(buf, h, i))), __builtin_bit_cast(bf16x8, seen), n, 0, 0, 0);
+            }
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                if (n[j] > 0.f) o[i][j] = __uint_as_float(0x7FC00000u);
+                __builtin_amdgcn_sched_barrier(0);       // one condition at a time: all at once fill the scalar registers
+            }
+        }
+        read_from_lds();
+#pragma unroll
+        for (int u = 0; u < Ring::LOADS; ++u) {
+            u32x4 w = *piece(u);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = without_nan(w[j]);
+            *piece(u) = w;
+        }
+        in_order();
+    };
+    auto work = [&](auto with_mask, int step, int end, int buf) {
+        constexpr bool MASKED = decltype(with_mask)::value;
+        const int k0 = key0 + step * kCa8Keys;
+        if (step + groups < end) arrived<2 * Ring::LOADS>(); else arrived<0>();
+        if constexpr (MASKED) without_nans(k0, buf);
+        u32x4 k[DT];
+        u32x2 v[2][DT];
+#pragma unroll
+        for (int i = 0; i < DT; ++i) k[i] = *reinterpret_cast<ETC_AS_LDS const u32x4 *>(k_at[i] + buf * Ring::STEP);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < DT; ++i)
+                v[h][i] = v_codes(buf, h, i);
+        const int page = (min(k0 + col, key_end - 1) >> R.psh) - W.first, k_scale = B.k_byte[page];
+        if (half == 0) B.v_scale[wave][col] = scale_of(B.v_byte[page]);
+        in_order();
+        f32x4 by[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) by[j] = *reinterpret_cast<ETC_AS_LDS const f32x4 *>(&B.v_scale[wave][8 * j + 4 * half]);
+        read_from_lds();                                 // the step's place is free
+        if (step + 2 * groups < end) G.fetch(step + 2 * groups, buf, W.first);
+        f32x16 s = scores_of<D>(k, k_scale, Q);
+        attend_codes<D, MASKED>(s, o, m, l, v, by, half, scale, k0, limit);
+    };
+    drain_vmem();                                        // nothing but rows on their way from here on
     __syncthreads();
     for (int begin = 0; begin < n_steps;) {              // a window of page ids
         const int end = W.end < key_end ? (W.end - key0) / kCa8Keys : n_steps;
-        Step8<D> T[2];
-        int step = begin + kg;
-        if (step < end) load(T[0], step);
-        if (step + groups < end) load(T[1], step + groups);
-        for (; step < end; step += 2 * groups) {
-            work(T[0], step, end);
-            if (step + groups < end) work(T[1], step + groups, end);
+        int step = begin + kg, buf = 0;
+        if (step < end) G.fetch(step, 0, W.first);
+        if (step + groups < end) G.fetch(step + groups, 1, W.first);
+        if (tid <= ((min(W.end, key_end) - 1) >> R.psh) - W.first) {      // the pages' scales, behind the first rows
+            const uint64_t at = R.scale_at(B.ids[tid]);
+            const uint8_t a = *as_global(pool.k_scale + at), b = *as_global(pool.v_scale + at);
+            B.k_byte[tid] = a;
+            B.v_byte[tid] = b;
         }
+        __syncthreads();
+        const int seen = min(end, (all_see - key0) / kCa8Keys);      // steps that all rows see whole, then the others
+        for (; step < seen; step += groups, buf ^= 1) work(std::false_type(), step, end, buf);
+        for (; step < end; step += groups, buf ^= 1) work(std::true_type(), step, end, buf);
         begin = end;
         if (begin < n_steps) {
             __syncthreads();
             W.load<SRV_ATTENTION_CODES>(S, io, B.ids, P.b, key0 + begin * kCa8Keys, key_end, tid);
+            drain_vmem();
             __syncthreads();
         }
     }
@@ -352,8 +480,8 @@ __device__ __forceinline__ void narrow_piece_codes(const ServingDev &S, const et
     // ---- the wavefronts of a row, in the order of their steps: output pieces of a lane as in a partial result, then m and l
     l = partner_sum(l);
     const uint32_t mine_at = base + wave * (kCaPartO<D> * 4), ml_at = (uint32_t)(uintptr_t)&B.ids[0];
-    static_assert(kCaWaves * kCaPartO<D> * 4 <= 512 * D * 2, "LDS");
-    __syncthreads();                                     // everyone's V has been read, and the page ids
+    static_assert(kCaWaves * kCaPartO<D> * 4 <= 512 * D * 2 && kCaWaves * 32 * 8 <= kCa8Ids * 4, "LDS");
+    __syncthreads();                                     // everyone's rows have been read, and the page ids
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll

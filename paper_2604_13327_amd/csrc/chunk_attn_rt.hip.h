@@ -356,12 +356,10 @@ __device__ __forceinline__ void attend(f32x16 (&s)[KT], f32x16 (&o)[D / 32], flo
 // Values of V that are no numbers, in a tile that some rows see a part of: the probability 0 of what a row does not see would make a
 // NaN of them.  They are counted by kind, in a product over the keys each row sees (+inf as 1, -inf as 2^8, NaN as 2^16, at most 64 of
 // each: exact), which goes to the output as infinities and NaN; the tile then holds zeros in their place.  `mine` are the pieces of the tile this
-// thread looks after, at the LDS addresses at[]; the wavefront's rows see the KEYS keys from k0 on, at `base`.  For the whole workgroup,
-// or (ALONE) for a wavefront that has the tile to itself.
-template <int D, int KEYS, int N, bool ALONE = false>
+// thread looks after, at the LDS addresses at[]; the wavefront's rows see the KEYS keys from k0 on, at `base`.  For the whole workgroup.
+template <int D, int KEYS, int N>
 __device__ __forceinline__ void odd_values(const u32x4 (&mine)[N], const uint32_t (&at)[N], f32x16 (&o)[D / 32], const Fragments<D> &F, uint32_t base, int half, int k0, int limit, bool live)
 {
-    auto meet = [] { if constexpr (ALONE) in_order(); else __syncthreads(); };
 #pragma unroll
     for (int u = 0; u < N; ++u) {
         u32x4 kind;
@@ -369,7 +367,7 @@ __device__ __forceinline__ void odd_values(const u32x4 (&mine)[N], const uint32_
         for (int i = 0; i < 4; ++i) kind[i] = odd_kind(mine[u][i] & 0xFFFFu) | odd_kind(mine[u][i] >> 16) << 16;
         *reinterpret_cast<ETC_AS_LDS u32x4 *>(at[u]) = kind;
     }
-    meet();
+    __syncthreads();
     if (live) {
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt) {
@@ -395,7 +393,7 @@ __device__ __forceinline__ void odd_values(const u32x4 (&mine)[N], const uint32_
             }                                                // the lanes of eleven vector registers of the whole kernel with them (10 % of a long prompt)
         }
     }
-    meet();
+    __syncthreads();
 #pragma unroll
     for (int u = 0; u < N; ++u) {
         u32x4 w = mine[u];
@@ -404,7 +402,7 @@ __device__ __forceinline__ void odd_values(const u32x4 (&mine)[N], const uint32_
             w[i] &= ((w[i] & 0x7F80u) == 0x7F80u ? 0u : 0xFFFFu) | ((w[i] & 0x7F800000u) == 0x7F800000u ? 0u : 0xFFFF0000u);
         *reinterpret_cast<ETC_AS_LDS u32x4 *>(at[u]) = w;
     }
-    meet();
+    __syncthreads();
 }
 
 __device__ __forceinline__ bool any_odd(u32x4 v)          // an exponent of all ones among 8 values
@@ -414,6 +412,29 @@ __device__ __forceinline__ bool any_odd(u32x4 v)          // an exponent of all 
     for (int i = 0; i < 4; ++i) odd |= (v[i] & 0x7F80u) == 0x7F80u || (v[i] & 0x7F800000u) == 0x7F800000u;
     return odd;
 }
+
+// Rows go from memory to LDS without a stop in registers: 64 lanes, 16 bytes each, to 1 KB of LDS from `to` on (the same for the
+// whole wavefront).  The compiler would have every LDS read wait for all such loads in flight; here their order is the
+// program's own: arrived(n) waits until at most n of this wavefront's are on their way, a barrier then covers everyone's.
+// The place goes by m0, which an asm statement cannot name among what it overwrites (it is reserved): it is put back.
+#define ETC_FETCH_1K(address, ...)                                                                                                     \
+    do {                                                                                                                               \
+        int m0_;                                                                                                                       \
+        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 " address "\n\ts_mov_b32 m0, %0"        \
+                     : "=&s"(m0_) : "s"(__builtin_amdgcn_readfirstlane(to)), __VA_ARGS__ : "memory");                                  \
+    } while (0)
+template <bool ONCE> __device__ __forceinline__ void fetch_1k(const char *from, uint32_t to)
+{
+    if (ONCE) ETC_FETCH_1K("%2, off nt", "v"(from));
+    else ETC_FETCH_1K("%2, off", "v"(from));
+}
+template <bool ONCE> __device__ __forceinline__ void fetch_1k(const char *base, uint32_t lane_off, uint32_t to)      // base the same for the wavefront
+{
+    if (ONCE) ETC_FETCH_1K("%2, %3 nt", "v"(lane_off), "s"(base));
+    else ETC_FETCH_1K("%2, %3", "v"(lane_off), "s"(base));
+}
+#undef ETC_FETCH_1K
+template <int N> __device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(%0)" : : "i"(N) : "memory"); }
 
 constexpr int kCaIds = 1024;                // page ids in LDS, a window of them at a time
 
@@ -449,15 +470,16 @@ __device__ __forceinline__ Piece piece_of(const ServingDev &S, const etc_serving
 }
 
 // The ids of a piece's pages for the keys [key, ., .): a window, valid in front of key `end`.  Between barriers.
+template <int N = kCaIds>
 struct PageWindow {
     const int32_t *table;
     int first, end;                         // first page; first key that is not covered
-    template <int OP> __device__ __forceinline__ void load(const ServingDev &S, const etc_serving_attention_io &io, ETC_AS_LDS int (&ids)[kCaIds], int b, int key, int key_end, int tid)
+    template <int OP> __device__ __forceinline__ void load(const ServingDev &S, const etc_serving_attention_io &io, ETC_AS_LDS int (&ids)[N], int b, int key, int key_end, int tid)
     {
         asm volatile("" : "+v"(tid));                    // addresses of this load: none of them waits in registers for the next window
         first = key >> S.page_shift;
-        const int last = (key_end - 1) >> S.page_shift, n = min(last - first + 1, kCaIds);
-        end = last - first < kCaIds ? key_end : (int)(((int64_t)(first + kCaIds)) << S.page_shift);
+        const int last = (key_end - 1) >> S.page_shift, n = min(last - first + 1, N);
+        end = last - first < N ? key_end : (int)(((int64_t)(first + N)) << S.page_shift);
         for (int i = tid; i < n; i += kCaThreads) {
             int id = gld_i32(table + first + i);
             if ((uint32_t)id >= (uint64_t)io.n_pages) {

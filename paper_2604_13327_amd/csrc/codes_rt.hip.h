@@ -24,7 +24,7 @@ __device__ __forceinline__ int scale_byte(float most, int least)
 }
 __device__ __forceinline__ float one_over_scale(int byte) { return __uint_as_float((uint32_t)(254 - byte) << 23); }
 // Eight codes as bf16, times a power of two: exact.
-__device__ __forceinline__ u32x4 f8_to_bf16x8(uint32_t a, uint32_t b, float scale)
+__device__ __forceinline__ u32x4 codes_to_bf16x8(uint32_t a, uint32_t b, float scale)
 {
     return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true)),
                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true))};

@@ -2,37 +2,41 @@
 //
 // One pass over a row.  A thread keeps a reference r, l = sum 2^y and t = sum 2^y y of its logits, y = (x - r) / ln 2; the reference follows
 // the largest logit only when that has grown by kScoreLag, so that almost no sum is scaled again.  Then ln sum exp x = r + ln l, and the
-// entropy is ln l - t ln 2 / l.  The likeliest tokens are found on the way, wavefront by wavefront: a list in LDS takes what is above a
-// threshold, and is cut to its first n_top, the last of which is the new threshold, where it is full.  The first threshold is the n_top-th
-// largest of the 64 lanes' first maxima.  Everything but the sums is a comparison, so nothing depends on how rows are cut.
+// entropy is ln l - t ln 2 / l.  The likeliest tokens are found on the way, wavefront by wavefront: vectors with something above a
+// threshold wait in LDS until there is one for every lane, what is above it in them goes to a list, and a full list is cut to its first n_top,
+// which raises the threshold.  The first threshold is what the first maxima of n_top lanes reach.  What is found does not depend on how rows are cut.
 // Few rows are cut into slices; the workgroup that arrives last at a row joins them.
 #ifndef ETC_GENERIC_ONLY
+#include <type_traits>
+
 #include "serving_rt.hip.h"
 
 namespace etc {
 
-constexpr int kScoreThreads = 256, kScoreWaves = kScoreThreads / 64;
+constexpr int kScoreWaves = 4, kScoreThreads = kScoreWaves * 64;
 constexpr int kScoreLoads = 4;              // of 16 bytes, of a thread, at once
 constexpr int kScoreList = 128;             // entries of a wavefront: kScoreTop and one from every lane
-constexpr int kScoreAll = 2048;             // entries of a row's slices together
+constexpr int kScoreSlices = 32;            // of a row, at most
+constexpr int kIdBits = 20;
+static_assert(kServingMaxVocab <= 1 << kIdBits, "ids");
 constexpr float kScoreLag = 6.f;
 constexpr float kScoreHuge = 1e38f;         // references from here on leave no room for their multiple by 1 / ln 2
 constexpr float kLog2E = 1.44269504088896f;
 constexpr double kPerLog2E = 1.0 / (double)kLog2E;      // of that very number: what it is off by scales all logits, not their differences
-constexpr int kScoreRows = 2 * kSampleSharedRows;       // rows that are cut: each has a counter
+constexpr int kScoreParts = 1024;           // slices of a launch, at most
 constexpr int kScoreMinSlice = 4096;
-static_assert(kScoreTop <= 64 && kScoreList >= kScoreTop + 64 && kScoreAll >= kScoreWaves * kScoreTop, "lists");
+static_assert(kScoreTop <= 64 && kScoreList >= kScoreTop + 64, "lists");
 
-struct ScorePart { float ref, sum, moment; int count; uint64_t top[kScoreTop]; };      // of a slice; top sorted
-
-__device__ __forceinline__ uint32_t score_key(float x)       // larger for the larger logit; x is not -0
+// An entry of a list: larger for the larger logit (not -0), then for the lower id; never 0.
+__device__ __forceinline__ uint32_t score_key(float x)
 {
     const uint32_t u = __float_as_uint(x);
     return u ^ ((u >> 31) ? 0xFFFFFFFFu : 0x80000000u);
 }
 __device__ __forceinline__ float score_logit(uint32_t k) { return __uint_as_float(k ^ ((k >> 31) ? 0x80000000u : 0xFFFFFFFFu)); }
+__device__ __forceinline__ uint64_t score_entry(float x, int id) { return (uint64_t)score_key(x + 0.f) << 32 | (uint32_t)~id; }
 
-// Largest logit of a threshold's that is below all that it lets pass.
+// A logit that is below all that a threshold lets pass, and not below others.
 __device__ __forceinline__ float below(uint64_t threshold)
 {
     uint32_t k = (uint32_t)(threshold >> 32);
@@ -41,70 +45,151 @@ __device__ __forceinline__ float below(uint64_t threshold)
     return score_logit(k);
 }
 
+__device__ __forceinline__ uint32_t wave_max_u(uint32_t v)
+{
+    auto with = [&](int w) { v = max(v, (uint32_t)w); };
+    with(dpp_i32<0xB1>((int)v));
+    with(dpp_i32<0x4E>((int)v));
+    with(dpp_i32<0x141>((int)v));
+    with(dpp_i32<0x140>((int)v));
+    auto row = [&](int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); };
+    return max(max(row(0), row(16)), max(row(32), row(48)));
+}
+
+// A number that the `top` largest of a wavefront's entries, N to a lane, reach, and no more than 64 do (0 where there are no more): bit by
+// bit, by counting, the logit's bits first.
+template <int N>
+__device__ __forceinline__ uint64_t threshold_of(const uint64_t (&x)[N], int top)
+{
+    auto reach = [&](auto at_least) {
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) n += __builtin_popcountll(__builtin_amdgcn_ballot_w64(at_least(x[i])));
+        return n;
+    };
+    if (reach([](uint64_t e) { return e != 0; }) <= 64) return 0;
+    uint32_t most = 0, least = 0xFFFFFFFFu;              // of the logits' bits: those that they have in common are the threshold's
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        most = max(most, (uint32_t)(x[i] >> 32));
+        least = min(least, x[i] != 0 ? (uint32_t)(x[i] >> 32) : 0xFFFFFFFFu);
+    }
+    most = wave_max_u(most);
+    least = ~wave_max_u(~least);
+    uint32_t hi = most;
+    if (most != least) {
+        int b = 31 - __builtin_clz(most ^ least);
+        hi = most >> b >> 1 << b << 1;
+        for (; b >= 0; --b) {
+            const uint32_t c = hi | 1u << b;
+            const int n = reach([&](uint64_t e) { return (uint32_t)(e >> 32) >= c; });
+            if (n < top) continue;
+            hi = c;
+            if (n <= 64) return (uint64_t)hi << 32;
+        }
+    }
+    uint64_t t = (uint64_t)hi << 32 | 0xFFFFFFFFu << kIdBits;      // of equal logits the lower ids
+    for (int b = kIdBits - 1; b >= 0; --b) {
+        const uint64_t c = t | 1u << b;
+        const int n = reach([&](uint64_t e) { return e >= c; });
+        if (n < top) continue;
+        t = c;
+        if (n <= 64) break;
+    }
+    return t;
+}
+// Those that reach a threshold, in turn to put(i, entry): how many.
+template <int N, class Put>
+__device__ __forceinline__ int keep(const uint64_t (&x)[N], uint64_t threshold, Put put)
+{
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const bool stays = x[i] != 0 && x[i] >= threshold;
+        const uint64_t mask = __builtin_amdgcn_ballot_w64(stays);
+        if (stays) put(n + __builtin_popcountll(mask & ((1ull << lane_id()) - 1)), x[i]);
+        n += __builtin_popcountll(mask);
+    }
+    return n;
+}
+
 template <bool F32> struct Vec {
     static constexpr int E = F32 ? 4 : 8;
     static __device__ __forceinline__ float at(u32x4 w, int e) { return F32 ? __uint_as_float(w[e & 3]) : (e & 1) ? bf16_hi(w[e >> 1]) : bf16_lo(w[e >> 1]); }
 };
 constexpr uint32_t kAllNan = 0xFFFFFFFFu;                    // as a fp32 or as two bf16
 
+struct Pending { u32x4 w[kScoreList]; int id[kScoreList]; };      // vectors with something in them, and their first token
+
 struct TopList {
     ETC_AS_LDS uint64_t *list;                           // [kScoreList] of this wavefront
-    int top, count;                                      // the same for the wavefront
-    uint64_t threshold;                                  // entries above it are taken
+    ETC_AS_LDS Pending *pending;
+    int top, count, n_pending;                           // the same for the wavefront
+    uint64_t threshold;                                  // entries from it on are taken
     float under;
 
-    __device__ __forceinline__ void cut()                // to the first `top`, sorted
+    __device__ __forceinline__ void set(uint64_t t)
+    {
+        threshold = t;
+        under = below(t);
+    }
+    __device__ __forceinline__ void cut()                // to 64 at most, the first `top` among them
     {
         const int lane = lane_id();
         in_order();
-        const uint64_t a = lane < count ? list[lane] : 0, b = lane + 64 < count ? list[lane + 64] : 0;
-        int ra = 0, rb = 0;
-        for (int j = 0; j < count; ++j) {
-            const uint64_t e = list[j];
-            ra += e > a;
-            rb += e > b;
-        }
+        const uint64_t x[2] = {lane < count ? list[lane] : 0, lane + 64 < count ? list[lane + 64] : 0};
         in_order();
-        if (lane < count && ra < top) list[ra] = a;
-        if (lane + 64 < count && rb < top) list[rb] = b;
+        const uint64_t t = threshold_of<2>(x, top);
+        if (t == 0) return;
+        count = keep<2>(x, t, [&](int i, uint64_t e) { list[i] = e; });
         in_order();
-        count = min(count, top);
+        set(t);
     }
-    __device__ __forceinline__ void raise()
+    // What at least `n` lanes' maxima reach.  Sixteen bits of it do.
+    static __device__ __forceinline__ uint64_t reached(float most, int n)
     {
-        if (count < top) return;
-        const uint64_t last = list[top - 1];
-        threshold = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(last >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)last);
-        under = below(threshold);
+        const uint32_t key = score_key(most > -INFINITY ? most + 0.f : -INFINITY) >> 16;
+        uint32_t t = 0;
+        for (int b = 15; b >= 0; --b)
+            if (__builtin_popcountll(__builtin_amdgcn_ballot_w64(key >= (t | 1u << b))) >= n) t |= 1u << b;
+        return (uint64_t)t << 48;
     }
-    // Of the first maxima, one from each lane: at least `top` logits are no smaller than the threshold's.
-    __device__ __forceinline__ void begin(float most)
+    // The vectors that wait, a vector to a lane.
+    template <bool F32> __device__ __forceinline__ void settle()
     {
-        list[lane_id()] = (uint64_t)score_key(most > -INFINITY ? most + 0.f : -INFINITY) << 32 | (uint32_t)lane_id();
-        count = 64;
-        cut();
-        raise();
-        threshold &= 0xFFFFFFFF00000000ull;
-        under = below(threshold);
-        count = 0;
-    }
-    template <bool F32> __device__ __forceinline__ void take(u32x4 w, int id)
-    {
+        in_order();
+        for (int at = 0; at < n_pending; at += 64) {
+            const bool mine = at + lane_id() < n_pending;
+            const u32x4 w = pending->w[mine ? at + lane_id() : at];
+            const int id = pending->id[mine ? at + lane_id() : at];
 #pragma unroll
-        for (int e = 0; e < Vec<F32>::E; ++e) {
-            const float x = Vec<F32>::at(w, e);
-            const uint64_t entry = (uint64_t)score_key(x + 0.f) << 32 | (uint32_t)~(id + e);
-            uint64_t takes = __builtin_amdgcn_ballot_w64(x > under && entry > threshold);
-            if (takes == 0) continue;
-            if (count + __builtin_popcountll(takes) > kScoreList) {
-                cut();
-                raise();
-                takes = __builtin_amdgcn_ballot_w64(x > under && entry > threshold);
+            for (int e = 0; e < Vec<F32>::E; ++e) {
+                const float x = Vec<F32>::at(w, e);
+                const uint64_t entry = score_entry(x, id + e);
+                uint64_t takes = __builtin_amdgcn_ballot_w64(mine && x > under && entry >= threshold);
+                if (takes == 0) continue;
+                if (count + __builtin_popcountll(takes) > kScoreList) {
+                    cut();
+                    takes = __builtin_amdgcn_ballot_w64(mine && x > under && entry >= threshold);
+                }
+                if ((takes >> lane_id()) & 1) list[count + __builtin_popcountll(takes & ((1ull << lane_id()) - 1))] = entry;
+                count += __builtin_popcountll(takes);
             }
-            if ((takes >> lane_id()) & 1) list[count + __builtin_popcountll(takes & ((1ull << lane_id()) - 1))] = entry;
-            in_order();
-            count += __builtin_popcountll(takes);
         }
+        n_pending = 0;
+        in_order();
+    }
+    template <bool F32> __device__ __forceinline__ void take(u32x4 w, float most, int id)
+    {
+        const uint64_t takes = __builtin_amdgcn_ballot_w64(most > under);
+        if (takes == 0) return;
+        if ((takes >> lane_id()) & 1) {
+            const int at = n_pending + __builtin_popcountll(takes & ((1ull << lane_id()) - 1));
+            pending->w[at] = w;
+            pending->id[at] = id;
+        }
+        n_pending += __builtin_popcountll(takes);
+        if (n_pending >= 64) settle<F32>();
     }
 };
 
@@ -117,38 +202,34 @@ __device__ __forceinline__ float in_log2(float ref)          // rounded, whereve
 // By how many powers of two sums from `ref` are smaller when they count from `most`, as -300 .. 0.
 __device__ __forceinline__ float log2_between(float ref, float most) { return fmaxf(in_log2(ref) - in_log2(most), -300.f); }
 
-__device__ __forceinline__ double exp2_between(float ref, float most)      // factor of sums from ref where they are to count from most
+// Of a wavefront's sums one.
+__device__ __forceinline__ Sums wave_total(Sums s)
 {
-    if (fabsf(most) >= kScoreHuge) return ref == most ? 1.0 : 0.0;      // numbers of this size differ by far more than exp can tell, or not at all
-    return exp2((double)log2_between(ref, most));
+    const float ref = wave_max_f(s.ref);
+    float l = 0.f, t = 0.f;
+    if (s.ref == ref) {
+        l = s.l;
+        t = s.t;
+    } else if (s.ref > -INFINITY && fabsf(ref) < kScoreHuge) {      // (numbers of that size differ by far more than an exponential can tell)
+        const float by = log2_between(s.ref, ref), f = __builtin_amdgcn_exp2f(by);
+        l = f * s.l;
+        t = f * __builtin_fmaf(s.l, by, s.t);
+    }
+    return Sums{ref, wave_sum(l), wave_sum(t)};
 }
 
-// Sum, over n parts of ref, l, t, by all threads of a wavefront alike.
-struct Total { float ref; double l, t; };
-template <class At>
-__device__ __forceinline__ Total total_of(int n, At at)
-{
-    Total T{-INFINITY, 0.0, 0.0};
-    for (int i = 0; i < n; ++i) T.ref = fmaxf(T.ref, at(i).ref);
-    if (T.ref == -INFINITY) return T;
-    for (int i = 0; i < n; ++i) {
-        const Sums s = at(i);
-        if (s.ref == -INFINITY) continue;
-        const double f = exp2_between(s.ref, T.ref);
-        T.l += f * s.l;
-        if (fabsf(T.ref) < kScoreHuge) T.t += f * ((double)s.t + (double)s.l * (double)log2_between(s.ref, T.ref));
-    }
-    return T;
-}
+// What a slice leaves: its sums and its largest logit, and the entries it found, 64 (0: none).
+__device__ __forceinline__ float *slice_sums(const ServingDev &S, int64_t slice) { return reinterpret_cast<float *>(S.smp_bins) + slice * 4; }
+__device__ __forceinline__ uint64_t *slice_entries(const ServingDev &S, int64_t slice) { return S.smp_bins + (size_t)kScoreParts * 2 + slice * 64; }
 
 template <bool F32>
 __global__ __launch_bounds__(kScoreThreads) void serving_score_kernel(ServingDev S, etc_serving_score_io io, int slices, int per_slice)
 {
-    constexpr int E = Vec<F32>::E, SIZE = F32 ? 4 : 2, U = kScoreLoads;
-    __shared__ uint64_t s_list[kScoreAll];
-    __shared__ Sums s_sums[kScoreAll / 16];
-    __shared__ int s_count[kScoreAll / 16];
-    __shared__ int s_last;
+    constexpr int E = Vec<F32>::E, SIZE = F32 ? 4 : 2, U = kScoreLoads, WAVES = kScoreWaves, THREADS = kScoreThreads;
+    __shared__ uint64_t s_list[WAVES * kScoreList], s_found[64], s_begin[WAVES];
+    __shared__ Pending s_pending[WAVES];
+    __shared__ Sums s_sums[WAVES];
+    __shared__ int s_count[WAVES], s_last;
     const int tid = (int)threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id());
     const int row = (int)blockIdx.x / slices, slice = (int)blockIdx.x - row * slices, top = io.n_top;
     int token = 0;
@@ -166,11 +247,11 @@ __global__ __launch_bounds__(kScoreThreads) void serving_score_kernel(ServingDev
     const int a0 = min(i1, i0 + (int)((16 - ((uintptr_t)from & 15)) & 15) / SIZE), nv = (i1 - a0) / E, t0 = a0 + nv * E;
     const char *const body = logits + (int64_t)a0 * SIZE;
 
-    TopList list{as_lds(s_list) + wave * kScoreList, top, 0, 0, -INFINITY};
+    TopList list{as_lds(s_list) + wave * kScoreList, as_lds(s_pending) + wave, top, 0, 0, 0, -INFINITY};
     Sums s{-INFINITY, 0.f, 0.f};
     float from_ref = INFINITY;                           // -in_log2(s.ref)
     bool first = true;
-    auto feed = [&](const u32x4 (&w)[U], int id) {       // vector u: tokens id + u * kScoreThreads * E ..; out of range: NaN
+    auto feed = [&](const u32x4 (&w)[U], int id) {       // vector u: tokens id + u * THREADS * E ..; out of range: NaN
         float most[U], all = -INFINITY;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -201,26 +282,33 @@ __global__ __launch_bounds__(kScoreThreads) void serving_score_kernel(ServingDev
         s.l += l;
         s.t += t;
         if (top == 0) return;
-        if (first) list.begin(all);
-        first = false;
+        if (first) {                                     // the wavefronts' lanes together: `top` of them reach the least of this
+            const uint64_t t = TopList::reached(all, (top + WAVES - 1) / WAVES);
+            if (lane == 0) s_begin[wave] = t;
+            __syncthreads();
+            uint64_t least = s_begin[0];
+#pragma unroll
+            for (int i = 1; i < WAVES; ++i) least = min(least, s_begin[i]);
+            list.set(least);
+            first = false;
+        }
         if (__builtin_amdgcn_ballot_w64(all > list.under) == 0) return;
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (__builtin_amdgcn_ballot_w64(most[u] > list.under) != 0) list.take<F32>(w[u], id + u * kScoreThreads * E);
+        for (int u = 0; u < U; ++u) list.take<F32>(w[u], most[u], id + u * THREADS * E);
     };
     u32x4 w[U], behind[U];
     auto load = [&](u32x4 (&to)[U], int v0) {
         if (v0 >= nv) return;                            // the same for the workgroup
 #pragma unroll
-        for (int u = 0; u < U; ++u) to[u] = gld_16B(body + (int64_t)min(v0 + u * kScoreThreads + tid, nv - 1) * 16);
+        for (int u = 0; u < U; ++u) to[u] = gld_16B(body + (int64_t)min(v0 + u * THREADS + tid, nv - 1) * 16);
     };
     load(w, 0);
-    for (int v0 = 0; v0 < nv; v0 += kScoreThreads * U) {
-        load(behind, v0 + kScoreThreads * U);
-        if (v0 + kScoreThreads * U > nv) {
+    for (int v0 = 0; v0 < nv; v0 += THREADS * U) {
+        load(behind, v0 + THREADS * U);
+        if (v0 + THREADS * U > nv) {
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                if (v0 + u * kScoreThreads + tid >= nv) w[u] = u32x4{kAllNan, kAllNan, kAllNan, kAllNan};
+                if (v0 + u * THREADS + tid >= nv) w[u] = u32x4{kAllNan, kAllNan, kAllNan, kAllNan};
         }
         feed(w, a0 + (v0 + tid) * E);
 #pragma unroll
@@ -235,123 +323,113 @@ __global__ __launch_bounds__(kScoreThreads) void serving_score_kernel(ServingDev
         feed(w, id);
     }
 
-    // ---- the workgroup's: sums by thread 0 .. in the order of the threads, lists by rank
-    auto reduce = [&](Sums v) {                          // of a wavefront, in every lane; the order is that of the lanes' distances
-        float ref = v.ref;
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) ref = fmaxf(ref, __shfl_xor(ref, o, 64));
-        double l = 0.0, t = 0.0;
-        if (v.ref > -INFINITY) {
-            const double f = exp2_between(v.ref, ref);
-            l = f * v.l;
-            if (fabsf(ref) < kScoreHuge) t = f * ((double)v.t + (double)v.l * (double)log2_between(v.ref, ref));
-        }
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) { l += __shfl_xor(l, o, 64); t += __shfl_xor(t, o, 64); }
-        return Sums{ref, (float)l, (float)t};
-    };
-    const Sums mine = reduce(s);
-    if (lane == 0) s_sums[wave] = mine;
-    if (top > 0) list.cut();
-    if (lane == 0) s_count[wave] = list.count;
+    // ---- the workgroup's: by one wavefront
+    const Sums mine = wave_total(s);
+    if (top > 0) {
+        list.settle<F32>();
+        if (list.count > 64) list.cut();
+    }
+    if (lane == 0) {
+        s_sums[wave] = mine;
+        s_count[wave] = list.count;
+    }
     __syncthreads();
-    Total T = total_of(kScoreWaves, [&](int i) { return s_sums[i]; });
+    Sums T = wave_total(lane < WAVES ? s_sums[lane] : Sums{-INFINITY, 0.f, 0.f});
     if (T.ref != -INFINITY && fabsf(T.ref) >= kScoreHuge) {      // how many there are of the largest: nothing else has weight
         int n = 0;
-        for (int i = i0 + tid; i < i1; i += kScoreThreads)
+        for (int i = i0 + tid; i < i1; i += THREADS)
             n += (F32 ? *as_global((const float *)logits + i) : bf16_bits_to_f32(gld_u16((const uint16_t *)logits + i))) == T.ref;
         n = wave_sum_i(n);
         __syncthreads();
         if (lane == 0) s_sums[wave].l = (float)n;
         __syncthreads();
-        T.l = T.t = 0.0;
-        for (int i = 0; i < kScoreWaves; ++i) T.l += (double)s_sums[i].l;
+        T.l = wave_sum(lane < WAVES ? s_sums[lane].l : 0.f);
+        T.t = 0.f;
     }
-    // entry i of n lists of up to `stride` entries each: how many are in front of it in all
-    auto rank_of = [&](uint64_t entry, int lists, int stride) {
-        int r = 0;
-        for (int k = 0; k < lists; ++k) {
-            const int n = s_count[k];
-            for (int j = 0; j < n; ++j) r += s_list[k * stride + j] > entry;
+    // The first `top` of the wavefronts' lists, and others up to 64.
+    auto select = [&](auto put) {
+        uint64_t x[WAVES];
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) x[i] = lane < s_count[i] ? s_list[i * kScoreList + lane] : 0;
+        return keep<WAVES>(x, threshold_of<WAVES>(x, top), put);
+    };
+    if (slices > 1) {                                    // to memory; the last to arrive joins the row's
+        const int64_t at = (int64_t)row * slices + slice;
+        if (wave == 0) {
+            float *const to = slice_sums(S, at);
+            float largest = -INFINITY;
+            if (top > 0) {
+                uint64_t *const entries = slice_entries(S, at);
+                uint32_t key = 0;
+                const int n = select([&](int i, uint64_t e) { st_u64(entries + i, e); key = max(key, (uint32_t)(e >> 32)); });
+                if (lane >= n) st_u64(entries + lane, 0);
+                if (n > 0) largest = score_logit(wave_max_u(key));
+            }
+            if (lane < 4) st_f32(to + lane, lane == 0 ? T.ref : lane == 1 ? T.l : lane == 2 ? T.t : largest);
         }
-        return r;
-    };
-    int n_top = 0;
-    for (int i = 0; i < kScoreWaves; ++i) n_top += s_count[i];
-    n_top = min(n_top, top);
-    uint64_t entry = 0;
-    int rank = kScoreTop;
-    if (top > 0 && lane < s_count[wave]) {
-        entry = list.list[lane];
-        rank = rank_of(entry, kScoreWaves, kScoreList);
-    }
-    auto finish = [&](const Total &T) {                  // (by one thread)
-        if (io.entropy_out) *as_global(io.entropy_out + row) = T.ref == -INFINITY ? 0.f : (float)fmax(log(T.l) - T.t / T.l * 0.6931471805599453, 0.0);
-    };
-    auto logprob = [&](float x, const Total &T) {        // of a logit
-        if (!(x > -INFINITY)) return -INFINITY;
-        if (fabsf(T.ref) >= kScoreHuge) return x == T.ref ? (float)-log(T.l) : (float)((double)x - (double)T.ref);
-        return (float)((double)x - ((double)in_log2(T.ref) * kPerLog2E + log(T.l)));
-    };
-    auto write_row = [&](const Total &T) {
-        if (tid == 0) finish(T);
-        if (tid == 64 && io.logprob_out) {
-            const float x = F32 ? *as_global((const float *)logits + token) : bf16_bits_to_f32(gld_u16((const uint16_t *)logits + token));
-            *as_global(io.logprob_out + row) = T.ref == -INFINITY ? -INFINITY : logprob(x, T);
+        wg_release();
+        if (tid == 0) {
+            int32_t *const arrived = S.score_arrived + row;
+            s_last = __hip_atomic_fetch_add(as_global(arrived), 1, __ATOMIC_RELAXED, ETC_SCOPE) + 1 == slices;
+            if (s_last) st_i32(arrived, 0);
         }
-    };
-    auto write_top = [&](uint64_t e, int r, const Total &T) {
-        const int64_t at = (int64_t)row * top + r;
-        *as_global(io.top_ids + at) = (int)~(uint32_t)e;
-        if (io.top_logprobs) *as_global(io.top_logprobs + at) = logprob(score_logit((uint32_t)(e >> 32)), T);
-    };
-    auto write_none = [&](int have) {
-        for (int r = have + tid; r < top; r += kScoreThreads) {
-            *as_global(io.top_ids + (int64_t)row * top + r) = -1;
-            if (io.top_logprobs) *as_global(io.top_logprobs + (int64_t)row * top + r) = -INFINITY;
+        __syncthreads();
+        if (!s_last) return;
+        Sums part{-INFINITY, 0.f, 0.f};
+        float largest = -INFINITY;
+        if (lane < slices) {
+            const float *const from = slice_sums(S, (int64_t)row * slices + lane);
+            part = Sums{ld_f32(from), ld_f32(from + 1), ld_f32(from + 2)};
+            largest = ld_f32(from + 3);
         }
+        if (top > 0) {                                   // a wavefront every fourth slice
+            constexpr int N = kScoreSlices / WAVES;
+            const uint64_t *const from = slice_entries(S, (int64_t)row * slices);
+            uint64_t x[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int k = i * WAVES + wave;
+                x[i] = k < slices ? ld_u64(from + k * 64 + lane) : 0;
+            }
+            uint64_t t = slices >= top ? TopList::reached(largest, top) : 0;      // `top` slices' largest do
+            int n = 0;
+#pragma unroll
+            for (int i = 0; i < N; ++i) n += __builtin_popcountll(__builtin_amdgcn_ballot_w64(x[i] != 0 && x[i] >= t));
+            if (n > 64) t = threshold_of<N>(x, top);
+            n = keep<N>(x, t, [&](int i, uint64_t e) { list.list[i] = e; });
+            if (lane == 0) s_count[wave] = n;
+        }
+        T = wave_total(part);
+        __syncthreads();
+    }
+    // ---- the row's outputs
+    const double log_l = T.ref == -INFINITY ? 0.0 : log((double)T.l);
+    auto logprob = [&](float x) {                        // of a logit
+        if (!(x > -INFINITY) || T.ref == -INFINITY) return -INFINITY;
+        if (fabsf(T.ref) >= kScoreHuge) return x == T.ref ? (float)-log_l : (float)((double)x - (double)T.ref);
+        return (float)((double)x - ((double)in_log2(T.ref) * kPerLog2E + log_l));
     };
-    if (slices == 1) {
-        write_row(T);
-        if (rank < top) write_top(entry, rank, T);
-        write_none(n_top);
-        return;
+    if (wave == WAVES - 1 && lane == 0) {
+        if (io.entropy_out) *as_global(io.entropy_out + row) = T.ref == -INFINITY ? 0.f : (float)fmax(log_l - (double)(T.t / T.l) * 0.6931471805599453, 0.0);
+        if (io.logprob_out)
+            *as_global(io.logprob_out + row) = logprob(F32 ? *as_global((const float *)logits + token) : bf16_bits_to_f32(gld_u16((const uint16_t *)logits + token)));
     }
-    // ---- a slice's: to memory; the last to arrive joins the row's
-    ScorePart *const parts = reinterpret_cast<ScorePart *>(S.smp_bins) + (size_t)row * slices;
-    if (tid == 0) {
-        st_f32(&parts[slice].ref, T.ref);
-        st_f32(&parts[slice].sum, (float)T.l);
-        st_f32(&parts[slice].moment, (float)T.t);
-        st_i32(&parts[slice].count, n_top);
+    if (wave != 0 || top == 0) return;
+    in_order();
+    ETC_AS_LDS uint64_t *const found = as_lds(s_found);
+    const int n = select([&](int i, uint64_t e) { found[i] = e; });
+    in_order();
+    const uint64_t entry = lane < n ? found[lane] : 0;
+    int rank = 0;
+    for (int i = 0; i < n; ++i) {
+        const uint64_t e = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(entry >> 32), i) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)entry, i);
+        rank += e > entry;
     }
-    if (rank < top) __hip_atomic_store(as_global(&parts[slice].top[rank]), entry, __ATOMIC_RELAXED, ETC_SCOPE);
-    wg_release();
-    if (tid == 0) {
-        int32_t *const arrived = S.smp_listed + row;
-        s_last = __hip_atomic_fetch_add(as_global(arrived), 1, __ATOMIC_RELAXED, ETC_SCOPE) + 1 == slices;
-        if (s_last) st_i32(arrived, 0);
-    }
-    __syncthreads();
-    if (!s_last) return;
-    for (int i = tid; i < slices; i += kScoreThreads) {
-        s_sums[i] = Sums{ld_f32(&parts[i].ref), ld_f32(&parts[i].sum), ld_f32(&parts[i].moment)};
-        s_count[i] = ld_i32(&parts[i].count);
-    }
-    __syncthreads();
-    for (int i = tid; i < slices * top; i += kScoreThreads)
-        if (i % top < s_count[i / top]) s_list[i] = ld_u64(&parts[i / top].top[i % top]);
-    __syncthreads();
-    T = total_of(slices, [&](int i) { return s_sums[i]; });
-    write_row(T);
-    int have = 0;
-    for (int i = 0; i < slices; ++i) have += s_count[i];
-    for (int i = tid; i < slices * top; i += kScoreThreads) {
-        if (i % top >= s_count[i / top]) continue;
-        const int r = rank_of(s_list[i], slices, top);
-        if (r < top) write_top(s_list[i], r, T);
-    }
-    write_none(min(have, top));
+    if (lane >= n) rank = lane;
+    if (rank >= top) return;
+    const int64_t at = (int64_t)row * top + rank;
+    *as_global(io.top_ids + at) = lane < n ? (int)~(uint32_t)entry : -1;
+    if (io.top_logprobs) *as_global(io.top_logprobs + at) = lane < n ? logprob(score_logit((uint32_t)(entry >> 32))) : -INFINITY;
 }
 
 hipError_t launch_serving_score(const ServingDev &S, const etc_serving_score_io &io, hipStream_t s)
@@ -360,9 +438,10 @@ hipError_t launch_serving_score(const ServingDev &S, const etc_serving_score_io 
     int slices = 1;
     if (S.smp_bins && io.n_rows <= kScoreRows) {
         slices = (2 * S.n_cus + io.n_rows - 1) / io.n_rows;
-        const int most = (S.vocab + kScoreMinSlice - 1) / kScoreMinSlice, entries = kScoreAll / (io.n_top > 16 ? io.n_top : 16);
+        const int most = (S.vocab + kScoreMinSlice - 1) / kScoreMinSlice;
         if (slices > most) slices = most;
-        if (slices > entries) slices = entries;
+        if (slices > kScoreSlices) slices = kScoreSlices;
+        if (slices > kScoreParts / io.n_rows) slices = kScoreParts / io.n_rows;
     }
     const int per_slice = ((S.vocab + slices - 1) / slices + 7) & ~7;
     slices = (S.vocab + per_slice - 1) / per_slice;

@@ -41,6 +41,17 @@ __device__ __forceinline__ int wave_scan_i(int v)
     return v;
 }
 
+// Largest over the wavefront, the same value in every lane.
+__device__ __forceinline__ float wave_max_f(float v)
+{
+    v = fmaxf(v, dpp_f32<0xB1>(v));
+    v = fmaxf(v, dpp_f32<0x4E>(v));
+    v = fmaxf(v, dpp_f32<0x141>(v));
+    v = fmaxf(v, dpp_f32<0x140>(v));
+    auto row = [&](int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); };
+    return fmaxf(fmaxf(row(0), row(16)), fmaxf(row(32), row(48)));
+}
+
 // Sum of a head whose elements lie in D / 16 neighbouring lanes.
 template <int D>
 __device__ __forceinline__ float head_sum(float v)

@@ -38,7 +38,7 @@ def _run(etc, x, tokens, top, entropy=True, tops=True, max_seqs=None, stride=0, 
 
 def _check(x, tokens, top, got, rows=None):
     """A thread adds at most 32 weights and then at most 16 such sums (longer rows than 2^17: 2^(-24) for each 8192 more), all positive: 48
-    roundings of 2^-24; a weight has an exponent rounded at up to 2^5 (2^-19) and an instruction's unit (2^-23): the sum is within 2^-17,
+    roundings of 2^-24, and at most 18 more across a wavefront, wavefronts and slices; a weight has an exponent rounded at up to 2^5 (2^-19) and an instruction's unit (2^-23): the sum is within 2^-17,
     and so is its logarithm; the result is rounded once.  The sum of p ln p likewise, relative to the sum of p |ln p|, counted from a
     reference within 6 of the largest."""
     for r in range(x.shape[0]) if rows is None else rows:
