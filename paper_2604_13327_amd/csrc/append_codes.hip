@@ -10,19 +10,28 @@ namespace etc {
 
 constexpr int kAp8Threads = 256, kAp8Waves = kAp8Threads / 64;
 constexpr int kAp8Rows = 16;                // of the angles in LDS, and of a run in registers
+constexpr int kAp8Heads = 2;                // queries of a lane at once
 constexpr int kAp8LowByte = 127 - 40;       // of a scale
 constexpr int kAp8HighByte = 127 + 120;     // of 2^128 / 448
 
 template <int D>
 struct Angles { float c[kAp8Rows][D / 2], s[kAp8Rows][D / 2]; };
 
-// Sine and cosine of the rows r0 .. r0 + n - 1.  The angle in fp64, reduced to half a turn: positions run into the millions.
-template <int D>
-__device__ __forceinline__ void fill_angles(ETC_AS_LDS Angles<D> &A, const ServingDev &S, const int32_t *positions, int r0, int n)
+// Sine and cosine of n rows (at most kAp8Rows), whose positions are position(row); a thread has one frequency.  The angle in fp64, reduced to half
+// a turn: positions run into the millions.
+template <int D, class Position>
+__device__ __forceinline__ void fill_angles(ETC_AS_LDS Angles<D> &A, double freq, int n, Position position)
 {
-    for (int i = (int)threadIdx.x; i < n * (D / 2); i += kAp8Threads) {
-        const int t = i / (D / 2), e = i - t * (D / 2);
-        const double turns = (double)gld_i32(positions + r0 + t) * *as_global(S.inv_freq + e) * 0.15915494309189535;
+    constexpr int AT_ONCE = kAp8Threads / (D / 2), TIMES = kAp8Rows / AT_ONCE;
+    const int t0 = (int)threadIdx.x / (D / 2), e = (int)threadIdx.x % (D / 2);
+    int p[TIMES];
+#pragma unroll
+    for (int k = 0; k < TIMES; ++k) p[k] = position(min(t0 + k * AT_ONCE, n - 1));
+#pragma unroll
+    for (int k = 0; k < TIMES; ++k) {
+        const int t = t0 + k * AT_ONCE;
+        if (t >= n) break;
+        const double turns = (double)p[k] * freq * 0.15915494309189535;
         float sn, cs;
         sincospif((float)(2.0 * (turns - rint(turns))), &sn, &cs);
         A.c[t][e] = cs;
@@ -77,35 +86,49 @@ __device__ __forceinline__ void rotate_head(float (&a)[8], float (&b)[8], ETC_AS
     }
 }
 
-// Blocks [0, kv_groups * kv_wgs): runs that begin in rows [g * rows_per_wg, ..), heads 4 h .. of K or V.  Blocks behind: queries.
+// Blocks [0, kv_blocks): runs that begin in rows [g * rows_per_wg, ..), heads 4 h .. of K or V.  Blocks behind: queries.
 template <int D, bool F32>
-__global__ __launch_bounds__(kAp8Threads) void serving_append_codes_kernel(ServingDev S, etc_serving_append_codes_io io8, int rows_per_wg, int kv_groups, int kv_wgs, int q_tokens)
+__global__ __launch_bounds__(kAp8Threads) void serving_append_codes_kernel(ServingDev S, etc_serving_append_codes_io io8, int rows_per_wg, int kv_wgs, int kv_blocks, int q_tokens)
 {
     constexpr int LPH = D / 16, RPI = 64 / LPH, ITERS = kAp8Rows / RPI;     // lanes to a row, rows at once, times
+    constexpr int RPP = kAp8Threads / LPH;               // heads of a workgroup at once
     __shared__ Angles<D> s_angles;
     ETC_AS_LDS Angles<D> &A = *as_lds(&s_angles);
     const etc_serving_append_io &io = io8.append;
     const int tid = (int)threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id());
     const int psh = S.page_shift, pmask = (1 << psh) - 1, n_slots = (int)(io.n_pages << psh), c = (lane % LPH) * 8;
 
-    if ((int)blockIdx.x >= kv_groups * kv_wgs) {         // queries
-        const int t0 = ((int)blockIdx.x - kv_groups * kv_wgs) * q_tokens, nt = min(q_tokens, io.n_tokens - t0);
-        fill_angles<D>(A, S, io.positions, t0, nt);
-        __syncthreads();
-        for (int r = tid / LPH; r < nt * S.nq; r += kAp8Threads / LPH) {
-            const int t = r / S.nq, h = r - t * S.nq, row = t0 + t;
-            const int slot = gld_i32(io.slots + row);
-            if (slot < 0 || slot >= n_slots) continue;   // the same for all lanes of a head
-            float a[8], b[8];
-            load_head<D, F32>(a, b, io.q, (int64_t)row * io.q_stride + h * D + c);
-            if (S.qk_norm) norm_head<D>(a, b, io.gq, c, S.eps);
-            rotate_head<D>(a, b, A, t, c);
-            uint16_t *dst = (uint16_t *)io.q_out + ((int64_t)row * S.nq + h) * D + c;
-            u32x4 x, y;
+    if ((int)blockIdx.x >= kv_blocks) {                  // queries
+        const int t0 = ((int)blockIdx.x - kv_blocks) * q_tokens, nt = min(q_tokens, io.n_tokens - t0);
+        const double freq = *as_global(S.inv_freq + tid % (D / 2));
+        bool there = false;
+        for (int r0 = tid / LPH; r0 < (nt * S.nq + RPP - 1) / RPP * RPP; r0 += RPP * kAp8Heads) {
+            float a[kAp8Heads][8], b[kAp8Heads][8];      // asked for in front of the angles
+            int slot[kAp8Heads];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { x[i] = to_bf16x2(a[2 * i], a[2 * i + 1]); y[i] = to_bf16x2(b[2 * i], b[2 * i + 1]); }
-            *as_global(reinterpret_cast<u32x4 *>(dst)) = x;
-            *as_global(reinterpret_cast<u32x4 *>(dst + D / 2)) = y;
+            for (int u = 0; u < kAp8Heads; ++u) {
+                const int r = min(r0 + u * RPP, nt * S.nq - 1), t = r / S.nq, h = r - t * S.nq;
+                slot[u] = r0 + u * RPP < nt * S.nq ? gld_i32(io.slots + t0 + t) : -1;
+                load_head<D, F32>(a[u], b[u], io.q, (int64_t)(t0 + t) * io.q_stride + h * D + c);
+            }
+            if (!there) {
+                fill_angles<D>(A, freq, nt, [&](int t) { return gld_i32(io.positions + t0 + t); });
+                __syncthreads();
+                there = true;
+            }
+#pragma unroll
+            for (int u = 0; u < kAp8Heads; ++u) {
+                if (slot[u] < 0 || slot[u] >= n_slots) continue;      // the same for all lanes of a head
+                const int r = r0 + u * RPP, t = r / S.nq, h = r - t * S.nq;
+                if (S.qk_norm) norm_head<D>(a[u], b[u], io.gq, c, S.eps);
+                rotate_head<D>(a[u], b[u], A, t, c);
+                uint16_t *dst = (uint16_t *)io.q_out + ((int64_t)(t0 + t) * S.nq + h) * D + c;
+                u32x4 x, y;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { x[i] = to_bf16x2(a[u][2 * i], a[u][2 * i + 1]); y[i] = to_bf16x2(b[u][2 * i], b[u][2 * i + 1]); }
+                *as_global(reinterpret_cast<u32x4 *>(dst)) = x;
+                *as_global(reinterpret_cast<u32x4 *>(dst + D / 2)) = y;
+            }
         }
         return;
     }
@@ -128,31 +151,47 @@ __global__ __launch_bounds__(kAp8Threads) void serving_append_codes_kernel(Servi
         return -1;
     };
     auto slot_at = [&](int row) { return __builtin_amdgcn_readfirstlane(gld_i32(io.slots + row)); };
-    for (int r = row0; r < row1; ++r) {                  // (everything up to the head's part is the same for the workgroup)
-        const int slot = slot_at(r), off = slot & pmask;
-        if (slot < 0) continue;
-        if (slot >= n_slots) {
-            if (part == 0 && tid == 0) refuse(S.error, SRV_BAD_SLOT, SRV_APPEND_CODES, r, slot);
-            continue;
+    // The slots of the rows, of 32 in front of them and of those behind, a row to a lane: mostly that tells all.  (Everything up to the
+    // head's part is the same for the workgroup.)
+    const int w0 = row0 - 32, at_lane = w0 + lane;
+    const int slots = at_lane >= 0 && at_lane < io.n_tokens ? gld_i32(io.slots + min(max(at_lane, 0), io.n_tokens - 1)) : -1;
+    const bool asked = lane >= 32 && at_lane < row1, live = (uint32_t)slots < (uint32_t)n_slots;
+    if (asked && slots >= n_slots && part == 0 && wave == 0) refuse(S.error, SRV_BAD_SLOT, SRV_APPEND_CODES, at_lane, slots);
+    const uint64_t lives = __builtin_amdgcn_ballot_w64(live), in_front = lives & ((1ull << lane) - 1);
+    const int before_me = __shfl(slots, in_front != 0 ? 63 - __builtin_clzll(in_front) : 0, 64);
+    const bool goes_on = (slots & pmask) != 0 && in_front != 0 && before_me == slots - 1;      // an earlier row's run
+    uint64_t begins = __builtin_amdgcn_ballot_w64(asked && live && !goes_on);
+    if (begins == 0) return;                             // (most workgroups of a prompt: in front of loads that all of them would ask for at once)
+    double freq = 0.0;
+    int positions = 0;
+    if (!is_v) {
+        freq = *as_global(S.inv_freq + tid % (D / 2));
+        positions = gld_i32(io.positions + min(max(at_lane, 0), io.n_tokens - 1));
+    }
+    for (; begins != 0; begins &= begins - 1) {
+        const int j = __builtin_ctzll(begins), r = w0 + j, slot = __builtin_amdgcn_readlane(slots, j), off = slot & pmask;
+        if (off != 0 && (lives & ((1ull << j) - 1)) == 0 && w0 > 0) {
+            const int before = live_from(w0 - 1, -1);
+            if (before >= 0 && slot_at(before) == slot - 1) continue;
         }
-        if (off != 0 && r > 0) {
-            const int before = live_from(r - 1, -1);
-            if (before >= 0 && slot_at(before) == slot - 1) continue;      // of an earlier row's run
-        }
+        // its rows, if they stand side by side within the lanes and are no more than kAp8Rows: else 0
+        const int n = __builtin_ctzll(~(__builtin_amdgcn_ballot_w64(lane >= j && slots == slot + (lane - j) && off + (lane - j) <= pmask) >> j));
+        const uint64_t behind = j + n < 64 ? lives >> (j + n) << (j + n) : 0;
+        const bool whole = n <= kAp8Rows && (off + n > pmask || (behind != 0 ? __builtin_amdgcn_readlane(slots, __builtin_ctzll(behind)) != slot + n : w0 + 64 >= io.n_tokens));
         const int64_t page = slot >> psh;
         float a[ITERS][8], b[ITERS][8];
         // Rows row .. of the run, nr of them, up to kAp8Rows (those behind are the last one again): the values that are to be stored, in a and b.
         auto values = [&](int row, int nr) {
-            if (!is_v) {
-                __syncthreads();                         // who reads the angles of the rows before
-                fill_angles<D>(A, S, io.positions, row, nr);
-            }
             if (mine) {
 #pragma unroll
                 for (int u = 0; u < ITERS; ++u)
                     load_head<D, F32>(a[u], b[u], src, (int64_t)(row + min(u * RPI + lane / LPH, nr - 1)) * stride + h * D + c);
             }
-            if (!is_v) __syncthreads();
+            if (!is_v) {
+                __syncthreads();                         // who reads the angles of the rows before
+                fill_angles<D>(A, freq, nr, [&](int t) { return whole ? __shfl(positions, j + t, 64) : gld_i32(io.positions + row + t); });
+                __syncthreads();
+            }
             if (!mine) return;
 #pragma unroll
             for (int u = 0; u < ITERS; ++u) {
@@ -164,67 +203,65 @@ __global__ __launch_bounds__(kAp8Threads) void serving_append_codes_kernel(Servi
                 for (int i = 0; i < 8; ++i) { a[u][i] = finite_or_nan(a[u][i]); b[u][i] = finite_or_nan(b[u][i]); }
             }
         };
-        // The run, up to kAp8Rows rows without one left out between them at a time: f(first row, its slot, rows).  Returns how often.
-        auto for_run = [&](auto f) {
-            int row = r, at = slot, times = 0;
-            for (;;) {
-                const bool goes_on = lane < kAp8Rows && (at & pmask) + lane <= pmask && row + lane < io.n_tokens && gld_i32(io.slots + min(row + lane, io.n_tokens - 1)) == at + lane;
-                const int nr = (int)__builtin_ctzll(~__builtin_amdgcn_ballot_w64(goes_on));      // at least 1
-                f(row, at, nr);
-                ++times;
-                at += nr;
-                if ((at & pmask) == 0 || row + nr >= io.n_tokens) return times;
-                row = live_from(row + nr, 1);
-                if (row < 0 || slot_at(row) != at) return times;
-            }
-        };
-        float most = 0.f;
-        const int times = for_run([&](int row, int, int nr) {
-            values(row, nr);
-            if (!mine) return;
-#pragma unroll
-            for (int u = 0; u < ITERS; ++u)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) most = fmaxf(most, fmaxf(fabsf(a[u][i]), fabsf(b[u][i])));
-        });
-        int byte = scale_byte(wave_max_f(most), kAp8LowByte);
-        if (mine) {
-            uint8_t *const scale = scales + page * S.nkv + h;
-            if (off > 0) {
-                const int before = __builtin_amdgcn_readfirstlane((int)*as_global(scale));
-                if (byte > before) {                     // the tokens in front, in the new scale
-                    const float f = __uint_as_float((uint32_t)max(127 + before - byte, 0) << 23);
-                    for (int64_t i = lane; i < (int64_t)off * (D / 8); i += 64) {
-                        uint8_t *const at = codes + ((page << psh) + i / (D / 8)) * S.nkv * D + h * D + i % (D / 8) * 8;
-                        u32x2 w = *as_global(reinterpret_cast<u32x2 *>(at));
-#pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const f32x4 x = from_f8x4(w[j]);
-                            w[j] = to_f8x4(x[0] * f, x[1] * f, x[2] * f, x[3] * f);
-                        }
-                        *as_global(reinterpret_cast<u32x2 *>(at)) = w;
-                    }
-                } else {
-                    byte = min(before, kAp8HighByte);
+        uint8_t *const scale = scales + page * S.nkv + h;
+        const int before = mine && off > 0 ? (int)*as_global(scale) : 0;
+        float most = 0.f, inv = 0.f;
+        bool once = true;                                // the run's values are in a and b
+        // Up to kAp8Rows rows of the run without one left out between them at a time, for the largest value, then to be stored.
+#pragma unroll 1
+        for (int pass = 0; pass < 2; ++pass) {
+            for (int row = r, at = slot;;) {
+                int nr = n;
+                if (!whole) {
+                    const bool on = lane < kAp8Rows && (at & pmask) + lane <= pmask && row + lane < io.n_tokens && gld_i32(io.slots + min(row + lane, io.n_tokens - 1)) == at + lane;
+                    nr = (int)__builtin_ctzll(~__builtin_amdgcn_ballot_w64(on));      // at least 1
                 }
+                if (pass == 0 || !once) values(row, nr);
+                if (mine && pass == 0) {
+#pragma unroll
+                    for (int u = 0; u < ITERS; ++u)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) most = fmaxf(most, fmaxf(fabsf(a[u][i]), fabsf(b[u][i])));
+                } else if (mine) {
+#pragma unroll
+                    for (int u = 0; u < ITERS; ++u) {
+                        const int i = u * RPI + lane / LPH;
+                        if (i >= nr) continue;
+                        uint8_t *const dst = codes + ((int64_t)at + i) * S.nkv * D + h * D + c;
+                        const float *x = a[u], *y = b[u];
+                        *as_global(reinterpret_cast<u32x2 *>(dst)) = u32x2{to_f8x4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv), to_f8x4(x[4] * inv, x[5] * inv, x[6] * inv, x[7] * inv)};
+                        *as_global(reinterpret_cast<u32x2 *>(dst + D / 2)) = u32x2{to_f8x4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv), to_f8x4(y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv)};
+                    }
+                }
+                at += nr;
+                if (whole || (at & pmask) == 0 || row + nr >= io.n_tokens) break;
+                row = live_from(row + nr, 1);
+                if (row < 0 || slot_at(row) != at) break;
+                once = false;
+            }
+            if (pass != 0 || !mine) continue;
+            int byte = scale_byte(wave_max_f(most), kAp8LowByte);
+            if (off > 0 && byte > before) {              // the tokens in front, in the new scale
+                const float f = __uint_as_float((uint32_t)max(127 + before - byte, 0) << 23);
+                const int64_t pieces = (int64_t)off * (D / 8);
+                auto piece = [&](int64_t i) { return reinterpret_cast<u32x2 *>(codes + ((page << psh) + i / (D / 8)) * S.nkv * D + h * D + i % (D / 8) * 8); };
+                for (int64_t i0 = lane; i0 < pieces; i0 += 4 * 64) {
+                    u32x2 w[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) w[k] = *as_global(piece(i0 + k * 64 < pieces ? i0 + k * 64 : i0));
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const f32x4 x = from_f8x4(w[k][0]), y = from_f8x4(w[k][1]);
+                        w[k] = u32x2{to_f8x4(x[0] * f, x[1] * f, x[2] * f, x[3] * f), to_f8x4(y[0] * f, y[1] * f, y[2] * f, y[3] * f)};
+                        if (i0 + k * 64 < pieces) *as_global(piece(i0 + k * 64)) = w[k];
+                    }
+                }
+            } else if (off > 0) {
+                byte = min(before, kAp8HighByte);
             }
             if (lane == 0) *as_global(scale) = (uint8_t)byte;
+            inv = one_over_scale(byte);
         }
-        const float inv = one_over_scale(byte);
-        auto store = [&](int, int at, int nr) {
-            if (!mine) return;
-#pragma unroll
-            for (int u = 0; u < ITERS; ++u) {
-                const int i = u * RPI + lane / LPH;
-                if (i >= nr) continue;
-                uint8_t *const dst = codes + ((int64_t)at + i) * S.nkv * D + h * D + c;
-                const float *x = a[u], *y = b[u];
-                *as_global(reinterpret_cast<u32x2 *>(dst)) = u32x2{to_f8x4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv), to_f8x4(x[4] * inv, x[5] * inv, x[6] * inv, x[7] * inv)};
-                *as_global(reinterpret_cast<u32x2 *>(dst + D / 2)) = u32x2{to_f8x4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv), to_f8x4(y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv)};
-            }
-        };
-        if (times == 1) for_run(store);                  // the values are there still
-        else for_run([&](int row, int at, int nr) { values(row, nr); store(row, at, nr); });
     }
 }
 
@@ -233,18 +270,18 @@ hipError_t launch_serving_append_codes(const ServingDev &S, const etc_serving_ap
     const int n = io.append.n_tokens;
     int rows = 1;                                        // that a workgroup looks for runs in
     while (rows < kAp8Rows && rows * S.n_cus < n) rows *= 2;
-    int q_tokens = kAp8Threads / (S.nq * (S.d / 16));
+    int q_tokens = kAp8Heads * kAp8Threads / (S.nq * (S.d / 16));
     if (q_tokens < 1) q_tokens = 1;
     if (q_tokens > kAp8Rows) q_tokens = kAp8Rows;
-    const int kv_groups = (n + rows - 1) / rows, kv_wgs = 2 * ((S.nkv + kAp8Waves - 1) / kAp8Waves);
-    const dim3 grid((unsigned)kv_groups * kv_wgs + (unsigned)((n + q_tokens - 1) / q_tokens)), block(kAp8Threads);
+    const int kv_wgs = 2 * ((S.nkv + kAp8Waves - 1) / kAp8Waves), kv_blocks = (n + rows - 1) / rows * kv_wgs;
+    const dim3 grid((unsigned)(kv_blocks + (n + q_tokens - 1) / q_tokens)), block(kAp8Threads);
     const bool f32 = io.append.dtype == ETC_FP32;
     if (S.d == 128) {
-        if (f32) hipLaunchKernelGGL((serving_append_codes_kernel<128, true>), grid, block, 0, s, S, io, rows, kv_groups, kv_wgs, q_tokens);
-        else hipLaunchKernelGGL((serving_append_codes_kernel<128, false>), grid, block, 0, s, S, io, rows, kv_groups, kv_wgs, q_tokens);
+        if (f32) hipLaunchKernelGGL((serving_append_codes_kernel<128, true>), grid, block, 0, s, S, io, rows, kv_wgs, kv_blocks, q_tokens);
+        else hipLaunchKernelGGL((serving_append_codes_kernel<128, false>), grid, block, 0, s, S, io, rows, kv_wgs, kv_blocks, q_tokens);
     } else {
-        if (f32) hipLaunchKernelGGL((serving_append_codes_kernel<64, true>), grid, block, 0, s, S, io, rows, kv_groups, kv_wgs, q_tokens);
-        else hipLaunchKernelGGL((serving_append_codes_kernel<64, false>), grid, block, 0, s, S, io, rows, kv_groups, kv_wgs, q_tokens);
+        if (f32) hipLaunchKernelGGL((serving_append_codes_kernel<64, true>), grid, block, 0, s, S, io, rows, kv_wgs, kv_blocks, q_tokens);
+        else hipLaunchKernelGGL((serving_append_codes_kernel<64, false>), grid, block, 0, s, S, io, rows, kv_wgs, kv_blocks, q_tokens);
     }
     return hipGetLastError();
 }

@@ -243,8 +243,7 @@ __device__ __forceinline__ void wide_piece_codes(const ServingDev &S, const etc_
 }
 
 // ---- a block of at most 64 rows --------------------------------------------------------------------------------------------
-// Bound by the rows of the cache.  Every wavefront goes through keys of its own, 32 at a time, every eighth such step (every fourth of more
-// than 32 rows, which two wavefronts share), without a barrier: codes go to its own part of LDS, two steps of them on their way or at hand, and from
+// Bound by the rows of the cache.  Every wavefront goes through keys of its own, 32 at a time, every eighth such step, without a barrier: codes go to its own part of LDS, two steps of them on their way or at hand, and from
 // there to registers as they are, K's as rows, V's transposed, so that a step's place is free for the one behind the next while it is worked on.
 // V's codes become bf16 without their scales, which the probabilities take (keys of one instruction may lie in several pages).
 // The wavefronts' results are joined in LDS.
@@ -278,7 +277,7 @@ struct Ring8 {
 #pragma unroll
         for (int u = 0; u < 2; ++u) off[u] = (lane / PPR) * R.row_bytes + R.head_off + ((lane % PPR) ^ swap(u * RPL + lane / PPR)) * 16;
     }
-    __device__ __forceinline__ void fetch(int step, int buf, int first_page)
+    template <bool K, bool V> __device__ __forceinline__ void fetch(int step, int buf, int first_page)
     {
         const int k0 = key0 + step * kCa8Keys;
         const uint32_t to = base + buf * STEP;
@@ -289,16 +288,16 @@ struct Ring8 {
 #pragma unroll
             for (int u = 0; u < LOADS; ++u) {
                 const uint64_t at = ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane(id[u]) * R.row_bytes << R.psh) + (uint64_t)((uint32_t)((k0 + u * RPL) & R.pmask) * (uint64_t)R.row_bytes);
-                fetch_1k<true>((const char *)pool.k + at, off[u & 1], to + u * 1024);
-                fetch_1k<true>((const char *)pool.v + at, off[u & 1], to + HALF + u * 1024);
+                if (K) fetch_1k<true>((const char *)pool.k + at, off[u & 1], to + u * 1024);
+                if (V) fetch_1k<true>((const char *)pool.v + at, off[u & 1], to + HALF + u * 1024);
             }
         } else {
 #pragma unroll 1
             for (int u = 0; u < LOADS; ++u) {
                 const int r = u * RPL + lane / PPR, key = min(k0 + r, last_key);
                 const uint64_t at = R.at(R.page(ids, key, first_page), key) + ((lane % PPR) ^ swap(r)) * 16;
-                fetch_1k<true>((const char *)pool.k + at, to + u * 1024);
-                fetch_1k<true>((const char *)pool.v + at, to + HALF + u * 1024);
+                if (K) fetch_1k<true>((const char *)pool.k + at, to + u * 1024);
+                if (V) fetch_1k<true>((const char *)pool.v + at, to + HALF + u * 1024);
             }
         }
     }
@@ -348,16 +347,19 @@ __device__ __forceinline__ void attend_codes(f32x16 &s, f32x16 (&o)[D / 32], flo
     }
 }
 
-template <int D>
+// SHARED: 33 to 64 rows.  Two wavefronts, of 32 rows each, go through the same keys; one fetches K, the other V, in a ring of four steps, and a barrier
+// in front of each step says that it is there for both (and that the one in front of it has been read).
+template <int D, bool SHARED>
 __device__ __forceinline__ void narrow_piece_codes(const ServingDev &S, const etc_serving_attention_io &io, const Pool8 &pool, ETC_AS_LDS CaLds &L, ETC_AS_LDS Tiles8<D> &B, const Piece &P)
 {
     constexpr int DT = D / 32;
     typedef Ring8<D> Ring;
-    static_assert(kCaWaves * 2 * Ring::STEP <= 512 * D * 2, "LDS");
+    constexpr int GROUPS = SHARED ? kCaWaves / 2 : kCaWaves, STEPS = 2 * kCaWaves / GROUPS;      // wavefronts to 32 rows; steps of a ring
+    static_assert(GROUPS * STEPS * Ring::STEP <= 512 * D * 2, "LDS");
     int tid = (int)threadIdx.x;
     asm volatile("" : "+v"(tid));
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, half = lane >> 5, col = lane & 31;
-    const int groups = P.rows <= 32 ? kCaWaves : kCaWaves / 2, rw = wave / groups, kg = wave % groups;      // wavefronts to 32 rows
+    const int rw = wave / GROUPS, kg = wave % GROUPS;
     const int key0 = P.tile0 * kCaKeys, key_end = min(P.tile1 * kCaKeys, P.n_keys), n_steps = div_up(key_end - key0, kCa8Keys);
     PageWindow<kCa8Ids> W{io.block_table + (int64_t)P.b * io.table_stride, 0, 0};
     W.load<SRV_ATTENTION_CODES>(S, io, B.ids, P.b, key0, key_end, tid);
@@ -367,7 +369,7 @@ __device__ __forceinline__ void narrow_piece_codes(const ServingDev &S, const et
     Q.load((const uint16_t *)io.q + ((int64_t)(P.seq.q0 + t) * S.nq + head) * D, half);
     const int limit = min(P.seq.kv + t, key_end - 1);    // last key this row sees in this piece
     const int all_see = min(P.seq.kv + 1, key_end);      // keys in front of it are seen by all rows
-    const uint32_t base = (uint32_t)(uintptr_t)&B.rows[0], mine = base + wave * 2 * Ring::STEP;
+    const uint32_t base = (uint32_t)(uintptr_t)&B.rows[0], mine = base + kg * STEPS * Ring::STEP;
 
     const Rows8 R(S, P.kvh, D);
     Ring G(pool, B.ids, R, mine, lane, key0, key_end - 1);
@@ -387,13 +389,12 @@ __device__ __forceinline__ void narrow_piece_codes(const ServingDev &S, const et
         return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(reinterpret_cast<ETC_AS_LDS i32x2 *>(v_at[i] + buf * Ring::STEP + h * 16 * D)));
     };
     // NaN codes of V in a step that some rows see a part of: the probability 0 of what a row does not see would make a NaN of them.  Counted by a
-    // product over the keys a row sees, which goes to the output; the step then holds zeros in their place.
-    auto without_nans = [&](int k0, int buf) {
-        auto piece = [&](int u) { return reinterpret_cast<ETC_AS_LDS u32x4 *>(mine + buf * Ring::STEP + Ring::HALF + (u * 64 + lane) * 16); };
+    // product over the keys a row sees, which goes to the output; the second product has zeros in their place.
+    auto count_nans = [&](int k0, int buf) {
         uint32_t nan = 0;
 #pragma unroll
         for (int u = 0; u < Ring::LOADS; ++u) {
-            const u32x4 w = *piece(u);
+            const u32x4 w = *reinterpret_cast<ETC_AS_LDS const u32x4 *>(mine + buf * Ring::STEP + Ring::HALF + (u * 64 + lane) * 16);
             nan |= nan_mask(w[0]) | nan_mask(w[1]) | nan_mask(w[2]) | nan_mask(w[3]);
         }
         if (__builtin_expect(__builtin_amdgcn_ballot_w64(nan != 0) == 0, 1)) return;
@@ -416,21 +417,17 @@ __device__ __forceinline__ void narrow_piece_codes(const ServingDev &S, const et
                 __builtin_amdgcn_sched_barrier(0);       // one condition at a time: all at once fill the scalar registers
             }
         }
-        read_from_lds();
-#pragma unroll
-        for (int u = 0; u < Ring::LOADS; ++u) {
-            u32x4 w = *piece(u);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = without_nan(w[j]);
-            *piece(u) = w;
-        }
-        in_order();
     };
-    auto work = [&](auto with_mask, int step, int end, int buf) {
+    auto fetch = [&](int step, int buf) {
+        if (!SHARED) G.template fetch<true, true>(step, buf, W.first);
+        else if (rw == 0) G.template fetch<true, false>(step, buf, W.first);
+        else G.template fetch<false, true>(step, buf, W.first);
+    };
+    // A step that is there; `ahead` sends one more on its way once its place is free.
+    auto work = [&](auto with_mask, int step, int buf, auto ahead) {
         constexpr bool MASKED = decltype(with_mask)::value;
         const int k0 = key0 + step * kCa8Keys;
-        if (step + groups < end) arrived<2 * Ring::LOADS>(); else arrived<0>();
-        if constexpr (MASKED) without_nans(k0, buf);
+        if constexpr (MASKED) count_nans(k0, buf);
         u32x4 k[DT];
         u32x2 v[2][DT];
 #pragma unroll
@@ -441,13 +438,19 @@ __device__ __forceinline__ void narrow_piece_codes(const ServingDev &S, const et
             for (int i = 0; i < DT; ++i)
                 v[h][i] = v_codes(buf, h, i);
         const int page = (min(k0 + col, key_end - 1) >> R.psh) - W.first, k_scale = B.k_byte[page];
-        if (half == 0) B.v_scale[wave][col] = scale_of(B.v_byte[page]);
+        if (half == 0) B.v_scale[wave][col] = scale_of(B.v_byte[page]);      // (each wavefront for itself)
         in_order();
         f32x4 by[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) by[j] = *reinterpret_cast<ETC_AS_LDS const f32x4 *>(&B.v_scale[wave][8 * j + 4 * half]);
         read_from_lds();                                 // the step's place is free
-        if (step + 2 * groups < end) G.fetch(step + 2 * groups, buf, W.first);
+        ahead();
+        if constexpr (MASKED) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < DT; ++i) v[h][i] = u32x2{without_nan(v[h][i][0]), without_nan(v[h][i][1])};
+        }
         f32x16 s = scores_of<D>(k, k_scale, Q);
         attend_codes<D, MASKED>(s, o, m, l, v, by, half, scale, k0, limit);
     };
@@ -455,9 +458,11 @@ __device__ __forceinline__ void narrow_piece_codes(const ServingDev &S, const et
     __syncthreads();
     for (int begin = 0; begin < n_steps;) {              // a window of page ids
         const int end = W.end < key_end ? (W.end - key0) / kCa8Keys : n_steps;
+        const int seen = min(end, (all_see - key0) / kCa8Keys);      // steps that all rows see whole
         int step = begin + kg, buf = 0;
-        if (step < end) G.fetch(step, 0, W.first);
-        if (step + groups < end) G.fetch(step + groups, 1, W.first);
+#pragma unroll
+        for (int a = 0; a < (SHARED ? STEPS - 1 : STEPS); ++a)
+            if (step + a * GROUPS < end) fetch(step + a * GROUPS, a);
         if (tid <= ((min(W.end, key_end) - 1) >> R.psh) - W.first) {      // the pages' scales, behind the first rows
             const uint64_t at = R.scale_at(B.ids[tid]);
             const uint8_t a = *as_global(pool.k_scale + at), b = *as_global(pool.v_scale + at);
@@ -465,9 +470,31 @@ __device__ __forceinline__ void narrow_piece_codes(const ServingDev &S, const et
             B.v_byte[tid] = b;
         }
         __syncthreads();
-        const int seen = min(end, (all_see - key0) / kCa8Keys);      // steps that all rows see whole, then the others
-        for (; step < seen; step += groups, buf ^= 1) work(std::false_type(), step, end, buf);
-        for (; step < end; step += groups, buf ^= 1) work(std::true_type(), step, end, buf);
+        if constexpr (!SHARED) {
+            auto next = [&](auto with_mask) {
+                if (step + GROUPS < end) arrived<2 * Ring::LOADS>(); else arrived<0>();
+                work(with_mask, step, buf, [&] { if (step + STEPS * GROUPS < end) fetch(step + STEPS * GROUPS, buf); });
+                step += GROUPS;
+                buf ^= 1;
+            };
+            while (step < seen) next(std::false_type());
+            while (step < end) next(std::true_type());
+        } else {
+            int first = begin;                           // of a round of steps, for all wavefronts alike
+            auto next = [&](auto with_mask) {
+                if (step + 2 * GROUPS < end) arrived<2 * Ring::LOADS>();
+                else if (step + GROUPS < end) arrived<Ring::LOADS>();
+                else arrived<0>();
+                __syncthreads();
+                if (step + (STEPS - 1) * GROUPS < end) fetch(step + (STEPS - 1) * GROUPS, (buf + STEPS - 1) % STEPS);
+                if (step < end) work(with_mask, step, buf, [] {});
+                first += GROUPS;
+                step += GROUPS;
+                buf = (buf + 1) % STEPS;
+            };
+            while (first + GROUPS <= seen) next(std::false_type());
+            while (first < end) next(std::true_type());
+        }
         begin = end;
         if (begin < n_steps) {
             __syncthreads();
@@ -492,9 +519,9 @@ __device__ __forceinline__ void narrow_piece_codes(const ServingDev &S, const et
     for (int cc = wave; cc < div_up(P.rows, 32) * (D / 8); cc += kCaWaves) {
         const int jr = cc / (D / 8), pc = cc % (D / 8);
         Join J;
-        for (int g = 0; g < groups; ++g) {
-            const f32x2_t ml = *reinterpret_cast<ETC_AS_LDS const f32x2_t *>(ml_at + ((jr * groups + g) * 32 + col) * 8);
-            J.add(ml[0], ml[1], *reinterpret_cast<ETC_AS_LDS const f32x4 *>(base + (jr * groups + g) * (kCaPartO<D> * 4) + (pc * 64 + lane) * 16));
+        for (int g = 0; g < GROUPS; ++g) {
+            const f32x2_t ml = *reinterpret_cast<ETC_AS_LDS const f32x2_t *>(ml_at + ((jr * GROUPS + g) * 32 + col) * 8);
+            J.add(ml[0], ml[1], *reinterpret_cast<ETC_AS_LDS const f32x4 *>(base + (jr * GROUPS + g) * (kCaPartO<D> * 4) + (pc * 64 + lane) * 16));
         }
         if (P.parts == 1) {
             put_out<D>(S, io, P, jr * 32 + col, pc, half, J.result());
@@ -519,7 +546,8 @@ __global__ __launch_bounds__(kCaThreads) void chunk_attention_codes_kernel(Servi
     const int n_pieces = cut<SRV_ATTENTION_CODES>(S, io, L);
     if (n_pieces == 0) return;
     for_pieces(S, io, L, n_pieces, [&](const Piece &P) {
-        if (P.rows <= kCaNarrowRows) narrow_piece_codes<D>(S, io, pool, L, B, P);
+        if (P.rows <= 32) narrow_piece_codes<D, false>(S, io, pool, L, B, P);
+        else if (P.rows <= kCaNarrowRows) narrow_piece_codes<D, true>(S, io, pool, L, B, P);
         else wide_piece_codes<D>(S, io, pool, L, B, P);
     });
 }
