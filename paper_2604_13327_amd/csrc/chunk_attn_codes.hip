@@ -29,13 +29,20 @@ template <int D>
 struct QCodes {
     i32x8 hi[D / 64], lo[D / 64];
     int hi_scale, lo_scale;
-    __device__ __forceinline__ void load(const uint16_t *row, int half)
+    struct Asked { u32x4 w[D / 16]; };
+    static __device__ __forceinline__ Asked ask(const uint16_t *row, int half)
     {
-        u32x4 w[D / 16];
+        Asked a;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) a.w[i] = gld_16B(row + half * (D / 2) + i * 8);
+        return a;
+    }
+    __device__ __forceinline__ void set(const Asked &a)
+    {
+        const u32x4 (&w)[D / 16] = a.w;
         float most = 0.f;
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) {
-            w[i] = gld_16B(row + half * (D / 2) + i * 8);
 #pragma unroll
             for (int j = 0; j < 4; ++j) most = fmaxf(most, fmaxf(fabsf(finite_or_nan(bf16_lo(w[i][j]))), fabsf(finite_or_nan(bf16_hi(w[i][j])))));
         }
@@ -70,14 +77,25 @@ __device__ __forceinline__ f32x16 scores_of(const u32x4 (&k)[D / 32], int k_scal
     return s;
 }
 
+// Prices of a cut, in tiles of a whole block (1.7 us): 64 keys of a block of few rows are 16 KB, which a workgroup reads in less than half of that
+// time; what a piece costs besides its tiles, and where its keys are cut; what a call's last join takes.
+struct CodesPrices {
+    static constexpr bool OWN = true;
+    static __device__ __forceinline__ float factor(int w) { return w == 1 ? 4.f : w == 2 ? 2.f : w == 3 ? 1.5f : w == 4 ? 1.25f : w == 5 ? 1.1f : w == 6 ? 1.f : 0.85f; }
+    static __device__ __forceinline__ float tile(bool narrow) { return narrow ? 0.44f : 1.f; }
+    static __device__ __forceinline__ float piece(bool narrow) { return narrow ? 4.f : 8.f; }
+    static __device__ __forceinline__ float part(bool narrow) { return narrow ? 1.f : 3.f; }
+    static __device__ __forceinline__ float join(bool narrow, int parts) { return narrow ? 2.f + 0.3f * (float)parts : 5.f + 0.8f * (float)parts; }
+};
+
 struct Pool8 { const uint8_t *k, *v, *k_scale, *v_scale; };
 
-constexpr int kCa8Ids = kCaThreads;         // page ids in LDS, with their scales: one to a thread
+constexpr int kCa8Ids = 256;                // page ids in LDS, with their scales, a window of them at a time
 template <int D>
 struct Tiles8 {
     uint16_t rows[512 * D];                 // 128 KB for heads of 128
     int ids[kCa8Ids];
-    uint8_t k_byte[kCa8Ids], v_byte[kCa8Ids];      // narrow pieces: scales of the pages
+    int k_byte[kCa8Ids], v_byte[kCa8Ids];   // narrow pieces: scales of the pages
     float v_scale[kCaWaves][kCa8Keys];      // of a wavefront's keys
     int k_scale[2][kCaKeys];                // wide pieces: of a tile's keys
 };
@@ -105,12 +123,10 @@ __device__ __forceinline__ void wide_piece_codes(const ServingDev &S, const etc_
     asm volatile("" : "+v"(tid));                        // of this piece: what is computed from it does not stay in registers across pieces
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, half = lane >> 5, col = lane & 31;
     const int tile0 = P.tile0, n_tiles = P.tile1, key_end = min(n_tiles * kCaKeys, P.n_keys);
+    const int row = P.r0 + wave * 32 + col, rr = min(row, P.rows - 1), t = rr / P.grp, head = P.kvh * P.grp + (rr - t * P.grp);
+    typename QCodes<D>::Asked q = QCodes<D>::ask((const uint16_t *)io.q + ((int64_t)(P.seq.q0 + t) * S.nq + head) * D, half);      // with the page ids
     PageWindow<kCa8Ids> W{io.block_table + (int64_t)P.b * io.table_stride, 0, 0};
     W.load<SRV_ATTENTION_CODES>(S, io, B.ids, P.b, tile0 * kCaKeys, key_end, tid);
-
-    const int row = P.r0 + wave * 32 + col, rr = min(row, P.rows - 1), t = rr / P.grp, head = P.kvh * P.grp + (rr - t * P.grp);
-    QCodes<D> Q;
-    Q.load((const uint16_t *)io.q + ((int64_t)(P.seq.q0 + t) * S.nq + head) * D, half);
     const int limit = P.seq.kv + t;                      // last key this row sees
     const int first_masked = (P.seq.kv + P.r0 / P.grp + 1) / kCaKeys;      // tiles in front of it are seen whole by all rows of the block
     const int wave_last = P.seq.kv + min((P.r0 + wave * 32 + 31) / P.grp, P.seq.n - 1);
@@ -153,6 +169,7 @@ __device__ __forceinline__ void wide_piece_codes(const ServingDev &S, const etc_
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) k_at[i] = k_base + col * D + ((half * (D / 32) + i) ^ k_swap8(col)) * 16;
     f32x16 s[2];
+    QCodes<D> Q;
     auto scores = [&](uint32_t buf) {
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
@@ -178,6 +195,7 @@ __device__ __forceinline__ void wide_piece_codes(const ServingDev &S, const etc_
     if (tid == 0) L.odd = -1;
     __syncthreads();
     load(tile0);
+    Q.set(q);                                            // while the first rows are on their way
     put(0);
     if (tile0 + 1 < n_tiles) {
         if (!covered(tile0 + 1)) {
@@ -239,7 +257,7 @@ __device__ __forceinline__ void wide_piece_codes(const ServingDev &S, const etc_
                            __builtin_bit_cast(u32x4, f32x4{o[dt][4 * q], o[dt][4 * q + 1], o[dt][4 * q + 2], o[dt][4 * q + 3]}));
         if (half == 0) buf_st_8B(d_b, (uint32_t)(kCaPartO<D> * 4 + col * 8), u32x2{__float_as_uint(m), __float_as_uint(l)});
     }
-    join_parts<D>(S, io, L, P, tid, wave, lane);
+    join_parts<D, 4>(S, io, L, P, tid, wave, lane);
 }
 
 // ---- a block of at most 64 rows --------------------------------------------------------------------------------------------
@@ -361,12 +379,11 @@ __device__ __forceinline__ void narrow_piece_codes(const ServingDev &S, const et
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, half = lane >> 5, col = lane & 31;
     const int rw = wave / GROUPS, kg = wave % GROUPS;
     const int key0 = P.tile0 * kCaKeys, key_end = min(P.tile1 * kCaKeys, P.n_keys), n_steps = div_up(key_end - key0, kCa8Keys);
+    const int row = rw * 32 + col, rr = min(row, P.rows - 1), t = rr / P.grp, head = P.kvh * P.grp + (rr - t * P.grp);
+    typename QCodes<D>::Asked q = QCodes<D>::ask((const uint16_t *)io.q + ((int64_t)(P.seq.q0 + t) * S.nq + head) * D, half);      // with the page ids
     PageWindow<kCa8Ids> W{io.block_table + (int64_t)P.b * io.table_stride, 0, 0};
     W.load<SRV_ATTENTION_CODES>(S, io, B.ids, P.b, key0, key_end, tid);
-
-    const int row = rw * 32 + col, rr = min(row, P.rows - 1), t = rr / P.grp, head = P.kvh * P.grp + (rr - t * P.grp);
     QCodes<D> Q;
-    Q.load((const uint16_t *)io.q + ((int64_t)(P.seq.q0 + t) * S.nq + head) * D, half);
     const int limit = min(P.seq.kv + t, key_end - 1);    // last key this row sees in this piece
     const int all_see = min(P.seq.kv + 1, key_end);      // keys in front of it are seen by all rows
     const uint32_t base = (uint32_t)(uintptr_t)&B.rows[0], mine = base + kg * STEPS * Ring::STEP;
@@ -454,22 +471,29 @@ __device__ __forceinline__ void narrow_piece_codes(const ServingDev &S, const et
         f32x16 s = scores_of<D>(k, k_scale, Q);
         attend_codes<D, MASKED>(s, o, m, l, v, by, half, scale, k0, limit);
     };
-    drain_vmem();                                        // nothing but rows on their way from here on
-    __syncthreads();
-    for (int begin = 0; begin < n_steps;) {              // a window of page ids
-        const int end = W.end < key_end ? (W.end - key0) / kCa8Keys : n_steps;
-        const int seen = min(end, (all_see - key0) / kCa8Keys);      // steps that all rows see whole
-        int step = begin + kg, buf = 0;
-#pragma unroll
-        for (int a = 0; a < (SHARED ? STEPS - 1 : STEPS); ++a)
-            if (step + a * GROUPS < end) fetch(step + a * GROUPS, a);
-        if (tid <= ((min(W.end, key_end) - 1) >> R.psh) - W.first) {      // the pages' scales, behind the first rows
-            const uint64_t at = R.scale_at(B.ids[tid]);
-            const uint8_t a = *as_global(pool.k_scale + at), b = *as_global(pool.v_scale + at);
-            B.k_byte[tid] = a;
-            B.v_byte[tid] = b;
+    constexpr int FIRST = SHARED ? STEPS - 1 : STEPS, FIRST_LOADS = FIRST * (SHARED ? 1 : 2) * Ring::LOADS;      // steps that are sent on their way at once
+    int begin = 0, end = 0, step = 0;                    // a window of page ids: its steps; this wavefront's next one
+    auto open = [&] {
+        end = W.end < key_end ? (W.end - key0) / kCa8Keys : n_steps;
+        step = begin + kg;
+        if (wave < kCa8Ids / 64) {                       // the pages' scales, a page to a lane (behind the last one that one's again)
+            const uint64_t at = R.scale_at(B.ids[min(wave * 64 + lane, ((min(W.end, key_end) - 1) >> R.psh) - W.first)]);
+            fetch_bytes(pool.k_scale + at, (uint32_t)(uintptr_t)&B.k_byte[wave * 64]);
+            fetch_bytes(pool.v_scale + at, (uint32_t)(uintptr_t)&B.v_byte[wave * 64]);
         }
+#pragma unroll
+        for (int a = 0; a < FIRST; ++a)
+            if (step + a * GROUPS < end) fetch(step + a * GROUPS, a);
+    };
+    drain_vmem();                                        // nothing but rows (and scales) on their way from here on
+    __syncthreads();
+    open();
+    Q.set(q);
+    for (;;) {
+        if (step + (FIRST - 1) * GROUPS < end) arrived<FIRST_LOADS>(); else arrived<0>();      // the scales, in front of the rows
         __syncthreads();
+        const int seen = min(end, (all_see - key0) / kCa8Keys);      // steps that all rows see whole
+        int buf = 0;
         if constexpr (!SHARED) {
             auto next = [&](auto with_mask) {
                 if (step + GROUPS < end) arrived<2 * Ring::LOADS>(); else arrived<0>();
@@ -496,18 +520,18 @@ __device__ __forceinline__ void narrow_piece_codes(const ServingDev &S, const et
             while (first < end) next(std::true_type());
         }
         begin = end;
-        if (begin < n_steps) {
-            __syncthreads();
-            W.load<SRV_ATTENTION_CODES>(S, io, B.ids, P.b, key0 + begin * kCa8Keys, key_end, tid);
-            drain_vmem();
-            __syncthreads();
-        }
+        if (begin >= n_steps) break;
+        __syncthreads();
+        W.load<SRV_ATTENTION_CODES>(S, io, B.ids, P.b, key0 + begin * kCa8Keys, key_end, tid);
+        drain_vmem();
+        __syncthreads();
+        open();
     }
 
     // ---- the wavefronts of a row, in the order of their steps: output pieces of a lane as in a partial result, then m and l
     l = partner_sum(l);
-    const uint32_t mine_at = base + wave * (kCaPartO<D> * 4), ml_at = (uint32_t)(uintptr_t)&B.ids[0];
-    static_assert(kCaWaves * kCaPartO<D> * 4 <= 512 * D * 2 && kCaWaves * 32 * 8 <= kCa8Ids * 4, "LDS");
+    const uint32_t mine_at = base + wave * (kCaPartO<D> * 4), ml_at = (uint32_t)(uintptr_t)&B.ids[0];      // (and the scales behind them)
+    static_assert(kCaWaves * kCaPartO<D> * 4 <= 512 * D * 2 && kCaWaves * 32 * 8 <= 2 * kCa8Ids * 4, "LDS");
     __syncthreads();                                     // everyone's rows have been read, and the page ids
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
@@ -531,7 +555,7 @@ __device__ __forceinline__ void narrow_piece_codes(const ServingDev &S, const et
             if (pc == 0 && half == 0) buf_st_8B(d_b, (uint32_t)(kCaPartO<D> * 4 + col * 8), u32x2{__float_as_uint(J.m), __float_as_uint(J.l)});
         }
     }
-    if (P.parts > 1) join_parts<D>(S, io, L, P, tid, wave, lane);
+    if (P.parts > 1) join_parts<D, 4>(S, io, L, P, tid, wave, lane);
 }
 
 template <int D>
@@ -543,9 +567,9 @@ __global__ __launch_bounds__(kCaThreads) void chunk_attention_codes_kernel(Servi
     ETC_AS_LDS Tiles8<D> &B = *as_lds(&s_tiles);
     const etc_serving_attention_io &io = io8.attention;
     const Pool8 pool{(const uint8_t *)io.k_pages, (const uint8_t *)io.v_pages, (const uint8_t *)io8.k_scale, (const uint8_t *)io8.v_scale};
-    const int n_pieces = cut<SRV_ATTENTION_CODES>(S, io, L);
+    const int n_pieces = cut<SRV_ATTENTION_CODES, CodesPrices>(S, io, L);
     if (n_pieces == 0) return;
-    for_pieces(S, io, L, n_pieces, [&](const Piece &P) {
+    for_pieces<CodesPrices>(S, io, L, n_pieces, [&](const Piece &P) {
         if (P.rows <= 32) narrow_piece_codes<D, false>(S, io, pool, L, B, P);
         else if (P.rows <= kCaNarrowRows) narrow_piece_codes<D, true>(S, io, pool, L, B, P);
         else wide_piece_codes<D>(S, io, pool, L, B, P);

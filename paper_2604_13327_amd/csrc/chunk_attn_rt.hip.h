@@ -74,7 +74,7 @@ struct CaLds {
     int slot[kServingMaxSeqs + 1];          // prefix sum: those that leave a partial result
     float wave_f[kCaWaves];
     int wave_i[kCaClasses / 2][kCaWaves];
-    int limit;                              // tiles of a piece
+    int limit, narrow_limit;                // tiles of a piece; of one of a narrow sequence, where those have a price of their own
     int narrow;                             // pieces of narrow sequences, which are in front (0: in any order)
     int odd, last;
 };
@@ -91,8 +91,15 @@ __device__ __forceinline__ int wave_max_i(int v)
     return max(max(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16)), max(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
 }
 
+// What a cut is estimated with: candidates of a piece's length, in workgroups' shares, and (OWN) prices of what narrow and wide sequences ask for,
+// in wide tiles; without OWN those are as cut() has them.
+struct CutPrices {
+    static constexpr bool OWN = false;
+    static __device__ __forceinline__ float factor(int w) { return w == 1 ? 4.f : w == 2 ? 3.f : w == 3 ? 2.f : w == 4 ? 1.5f : w == 5 ? 1.25f : w == 6 ? 1.1f : 1.f; }
+};
+
 // Fills L and returns the number of pieces.
-template <int OP>
+template <int OP, class Prices = CutPrices>
 __device__ __forceinline__ int cut(const ServingDev &S, const etc_serving_attention_io &io, ETC_AS_LDS CaLds &L)
 {
     const int tid = (int)threadIdx.x, wave = __builtin_amdgcn_readfirstlane(wave_id()), lane = lane_id(), grp = S.nq / S.nkv, grid = (int)gridDim.x;
@@ -111,7 +118,11 @@ __device__ __forceinline__ int cut(const ServingDev &S, const etc_serving_attent
         L.kv[b] = kv;
         tokens += n;
         most = max(most, tiles_of(kv, n));
-        if (n > 0) work += (float)S.nkv * blocks_of(n, grp) * 0.5f * (float)(tiles_of(kv, n) + tiles_of(kv, min(n, kCaRows / grp)));
+        if (n > 0) {
+            float tiles = (float)S.nkv * blocks_of(n, grp) * 0.5f * (float)(tiles_of(kv, n) + tiles_of(kv, min(n, kCaRows / grp)));
+            if constexpr (Prices::OWN) tiles *= Prices::tile(n * grp <= kCaNarrowRows);
+            work += tiles;
+        }
     }
     work = wave_sum(work);
     tokens = wave_sum_i(tokens);
@@ -134,42 +145,84 @@ __device__ __forceinline__ int cut(const ServingDev &S, const etc_serving_attent
     // longest for one token of one sequence (18 and 58), 1.1 for a chunk of 512 behind 8000 keys (89 and 242).
     const float share = work / (float)grid;
     auto limit_of = [&](int w) {
-        const float f = w == 1 ? 4.f : w == 2 ? 3.f : w == 3 ? 2.f : w == 4 ? 1.5f : w == 5 ? 1.25f : w == 6 ? 1.1f : 1.f;
-        return w == 0 ? 1 << 30 : max(kCaMinTiles, (int)fminf(ceilf(share * f), 1e9f));
+        return w == 0 ? 1 << 30 : max(kCaMinTiles, (int)fminf(ceilf(share * Prices::factor(w)), 1e9f));
+    };
+    auto narrow_limit_of = [&](int w) {
+        if constexpr (Prices::OWN) return w == 0 ? 1 << 30 : max(kCaMinTiles, (int)fminf(ceilf(share * Prices::factor(w) * (1.f / Prices::tile(true))), 1e9f));
+        else return limit_of(w);
     };
     int best = 0, longest_piece = most;
+    int longest_narrow = 0;                              // (OWN; longest_piece is that of wide sequences then)
     if (most > kCaWholeTiles) {
         float pieces = 0.f, slots = 0.f;
         int longest = 0, parts = 1;
         bool whole = false;
+        float ends;
         const int per = limit_of(wave);
-        for (int b = lane; b < io.n_seqs; b += 64) {
-            const int n = L.n[b], tiles = tiles_of(L.kv[b], n);
-            if (n == 0) continue;
-            const int blocks = blocks_of(n, grp), s = div_up(tiles, per);
-            const float k = (float)S.nkv * blocks, some = 0.5f * (float)(s + div_up(tiles_of(L.kv[b], min(n, div_up(kCaRows, grp))), per));
-            pieces += k * some;
-            if (s > 1) { slots += k * s; whole |= n * grp > kCaNarrowRows; }
-            parts = max(parts, s);
-            longest = max(longest, div_up(tiles, s));
+        if constexpr (!Prices::OWN) {
+            for (int b = lane; b < io.n_seqs; b += 64) {
+                const int n = L.n[b], tiles = tiles_of(L.kv[b], n);
+                if (n == 0) continue;
+                const int blocks = blocks_of(n, grp), s = div_up(tiles, per);
+                const float k = (float)S.nkv * blocks, some = 0.5f * (float)(s + div_up(tiles_of(L.kv[b], min(n, div_up(kCaRows, grp))), per));
+                pieces += k * some;
+                if (s > 1) { slots += k * s; whole |= n * grp > kCaNarrowRows; }
+                parts = max(parts, s);
+                longest = max(longest, div_up(tiles, s));
+            }
+            pieces = wave_sum(pieces);
+            slots = wave_sum(slots);
+            longest = wave_max_i(longest);
+            parts = wave_max_i(parts);
+            ends = fmaxf((float)longest + 1.f, ceilf(pieces / (float)grid) * ((work + pieces) / fmaxf(pieces, 1.f))) + 0.5f * (float)parts + (__any(whole) ? 9.f : 0.f);
+        } else {
+            const int narrow_per = narrow_limit_of(wave);
+            int narrow_parts = 1;
+            float over = 0.f, longest_cost = 0.f;
+            for (int b = lane; b < io.n_seqs; b += 64) {
+                const int n = L.n[b], tiles = tiles_of(L.kv[b], n);
+                if (n == 0) continue;
+                const bool narrow = n * grp <= kCaNarrowRows;
+                const int blocks = blocks_of(n, grp), p = narrow ? narrow_per : per, s = div_up(tiles, p), len = div_up(tiles, s);
+                const float k = (float)S.nkv * blocks, some = k * 0.5f * (float)(s + div_up(tiles_of(L.kv[b], min(n, div_up(kCaRows, grp))), p));
+                const float each = Prices::piece(narrow) + (s > 1 ? Prices::part(narrow) : 0.f);
+                pieces += some;
+                over += some * each;
+                if (s > 1) slots += k * s;
+                if (narrow) { narrow_parts = max(narrow_parts, s); longest_narrow = max(longest_narrow, len); }
+                else { parts = max(parts, s); longest = max(longest, len); }
+                longest_cost = fmaxf(longest_cost, (float)len * Prices::tile(narrow) + each);
+            }
+            pieces = wave_sum(pieces);
+            slots = wave_sum(slots);
+            longest = wave_max_i(longest);
+            longest_narrow = wave_max_i(longest_narrow);
+            parts = wave_max_i(parts);
+            narrow_parts = wave_max_i(narrow_parts);
+            over = wave_sum(over);
+            longest_cost = wave_max_f(longest_cost);
+            ends = fmaxf(longest_cost, ceilf(pieces / (float)grid) * ((work + over) / fmaxf(pieces, 1.f))) +
+                   fmaxf(parts > 1 ? Prices::join(false, parts) : 0.f, narrow_parts > 1 ? Prices::join(true, narrow_parts) : 0.f);
         }
-        pieces = wave_sum(pieces);
-        slots = wave_sum(slots);
-        longest = wave_max_i(longest);
-        parts = wave_max_i(parts);
-        float ends = fmaxf((float)longest + 1.f, ceilf(pieces / (float)grid) * ((work + pieces) / fmaxf(pieces, 1.f))) + 0.5f * (float)parts + (__any(whole) ? 9.f : 0.f);
         if (wave > 0 && slots > (float)S.attn_slots) ends = INFINITY;
         __syncthreads();
-        if (lane == 0) { L.wave_f[wave] = ends; L.wave_i[0][wave] = longest; }
+        if (lane == 0) {
+            L.wave_f[wave] = ends;
+            L.wave_i[0][wave] = longest;
+            if (Prices::OWN) L.wave_i[1][wave] = longest_narrow;
+        }
         __syncthreads();
         float best_ends = L.wave_f[0];
 #pragma unroll
         for (int w = 1; w < kCaTries; ++w)
             if (L.wave_f[w] < best_ends) { best = w; best_ends = L.wave_f[w]; }
         longest_piece = L.wave_i[0][best];
+        if (Prices::OWN) longest_narrow = L.wave_i[1][best];
+    } else {
+        longest_narrow = most;
     }
-    const int limit = limit_of(best);
-    if (tid == 0) { L.first[0] = L.slot[0] = 0; L.limit = limit; L.narrow = 0; }
+    const int limit = limit_of(best), narrow_limit = narrow_limit_of(best);
+    if (tid == 0) { L.first[0] = L.slot[0] = 0; L.limit = limit; L.narrow_limit = narrow_limit; L.narrow = 0; }
     auto count = [&](auto as_they_come) {                // the prefix sums; the number of pieces
         int done = 0, done_slots = 0;
         for (int i0 = 0; i0 < io.n_seqs; i0 += kCaThreads) {
@@ -179,7 +232,7 @@ __device__ __forceinline__ int cut(const ServingDev &S, const etc_serving_attent
             if (i < io.n_seqs) {
                 int b = i, parts;
                 if (as_they_come) {
-                    parts = max(1, div_up(tiles_of(L.kv[i], L.n[i]), limit));
+                    parts = max(1, div_up(tiles_of(L.kv[i], L.n[i]), Prices::OWN && L.n[i] * grp <= kCaNarrowRows ? narrow_limit : limit));
                     L.order[i] = (uint16_t)i;
                     L.split[i] = parts;
                 } else {
@@ -206,7 +259,12 @@ __device__ __forceinline__ int cut(const ServingDev &S, const etc_serving_attent
         for (int c = 0; c < 2; ++c) {
             const int b = c * kCaThreads + tid, rows = b < io.n_seqs ? L.n[b] * grp : 0;
             const int len = rows > 0 ? div_up(tiles_of(L.kv[b], L.n[b]), L.split[b]) : 0;
-            cls[c] = rows > kCaNarrowRows ? kCaClasses - 1 : min(kCaClasses - 2, (int)((float)((kCaClasses - 1) * (longest_piece - len)) / (float)longest_piece));
+            if constexpr (Prices::OWN) {                 // half of the classes for each kind
+                const int most_of = rows > kCaNarrowRows ? longest_piece : longest_narrow;
+                cls[c] = (rows > kCaNarrowRows ? kCaClasses / 2 : 0) + max(0, min(kCaClasses / 2 - 1, (int)((float)(kCaClasses / 2 * (most_of - len)) / (float)max(most_of, 1))));
+            } else {
+                cls[c] = rows > kCaNarrowRows ? kCaClasses - 1 : min(kCaClasses - 2, (int)((float)((kCaClasses - 1) * (longest_piece - len)) / (float)longest_piece));
+            }
             if (c * kCaThreads >= io.n_seqs) break;
             __syncthreads();
 #pragma unroll
@@ -239,7 +297,13 @@ __device__ __forceinline__ int cut(const ServingDev &S, const etc_serving_attent
         }
         n_pieces = count(std::false_type());
         __syncthreads();
-        if (tid == 0) L.narrow = L.first[io.n_seqs - (total[kCaClasses / 2 - 1] >> 16)];
+        int wide = total[kCaClasses / 2 - 1] >> 16;      // sequences
+        if constexpr (Prices::OWN) {
+            wide = 0;
+#pragma unroll
+            for (int j = kCaClasses / 4; j < kCaClasses / 2; ++j) wide += (total[j] >> 16) + (total[j] & 0xFFFF);
+        }
+        if (tid == 0) L.narrow = L.first[io.n_seqs - wide];
     }
     __syncthreads();
     return n_pieces;
@@ -434,6 +498,12 @@ template <bool ONCE> __device__ __forceinline__ void fetch_1k(const char *base, 
     else ETC_FETCH_1K("%2, %3", "v"(lane_off), "s"(base));
 }
 #undef ETC_FETCH_1K
+// 64 lanes, a byte each, to 64 words of LDS from `to` on.
+__device__ __forceinline__ void fetch_bytes(const uint8_t *from, uint32_t to)
+{
+    int m0_;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_ubyte %2, off\n\ts_mov_b32 m0, %0" : "=&s"(m0_) : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory");
+}
 template <int N> __device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(%0)" : : "i"(N) : "memory"); }
 
 constexpr int kCaIds = 1024;                // page ids in LDS, a window of them at a time
@@ -447,6 +517,7 @@ struct Piece {
     Seq seq;
 };
 
+template <class Prices>
 __device__ __forceinline__ Piece piece_of(const ServingDev &S, const etc_serving_attention_io &io, ETC_AS_LDS const CaLds &L, int p)
 {
     const int i = __builtin_amdgcn_readfirstlane(last_not_above(L.first, io.n_seqs, p)), local = p - __builtin_amdgcn_readfirstlane(L.first[i]);
@@ -462,7 +533,7 @@ __device__ __forceinline__ Piece piece_of(const ServingDev &S, const etc_serving
     P.r0 = (blocks_of(P.seq.n, P.grp) - 1 - local / S.nkv / split) * kCaRows;      // long blocks first
     P.n_keys = P.seq.kv + min(P.r0 + kCaRows - 1, P.rows - 1) / P.grp + 1;
     const int tiles = (P.n_keys - 1) / kCaKeys + 1;
-    P.parts = div_up(tiles, __builtin_amdgcn_readfirstlane(L.limit));      // of a block shorter than its sequence's last one maybe fewer than `split`
+    P.parts = div_up(tiles, __builtin_amdgcn_readfirstlane(Prices::OWN && P.rows <= kCaNarrowRows ? L.narrow_limit : L.limit));      // of a block shorter than its sequence's last one maybe fewer than `split`
     const int each = tiles / P.parts, more = tiles - each * P.parts;      // the first `more` have one more
     P.tile0 = P.part * each + min(P.part, more);
     P.tile1 = P.part < P.parts ? P.tile0 + each + (P.part < more) : P.tile0;
@@ -527,8 +598,9 @@ struct Join {
     }
 };
 
-// Behind a part's partial result: who arrives last at the item joins its parts, in the order of the keys.
-template <int D>
+// Behind a part's partial result: who arrives last at the item joins its parts, in the order of the keys.  AT_ONCE: pieces of a row that a wavefront
+// asks for at once, of four parts, where an item has many rows (one piece of four parts, 4 KB, waits for memory most of the time).
+template <int D, int AT_ONCE = 1>
 __device__ __forceinline__ void join_parts(const ServingDev &S, const etc_serving_attention_io &io, ETC_AS_LDS CaLds &L, const Piece &P, int tid, int wave, int lane)
 {
     const int half = lane >> 5, col = lane & 31;
@@ -542,29 +614,40 @@ __device__ __forceinline__ void join_parts(const ServingDev &S, const etc_servin
     __syncthreads();
     if (!L.last) return;
     const int live = min(kCaWaves, div_up(P.rows - P.r0, 32));
-    for (int cc = wave; cc < live * (D / 8); cc += kCaWaves) {      // a wavefront per (32 rows, piece of them)
+    auto some = [&](auto pieces, int cc) {               // `pieces` pieces of 32 rows from piece cc on
+        constexpr int N = decltype(pieces)::value;
         const int rw = cc / (D / 8), pc = cc % (D / 8);
-        Join J;
+        Join J[N];
         for (int j0 = 0; j0 < P.parts; j0 += 4) {
-            f32x4 ov[4];
+            f32x4 ov[4][N];
             uint64_t ml[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const float *src = partial<D>(S, P.slot0 + min(j0 + u, P.parts - 1) * S.nkv, rw);
-                ov[u] = __builtin_bit_cast(f32x4, buf_ld_16B(buf_of(src), (uint32_t)((pc * 64 + lane) * 16), 0));
+#pragma unroll
+                for (int i = 0; i < N; ++i) ov[u][i] = __builtin_bit_cast(f32x4, buf_ld_16B(buf_of(src), (uint32_t)(((pc + i) * 64 + lane) * 16), 0));
                 ml[u] = ld_u64(src + kCaPartO<D> + col * 2);
             }
 #pragma unroll
             for (int u = 0; u < 4; ++u)
-                if (j0 + u < P.parts) J.add(__uint_as_float((uint32_t)ml[u]), __uint_as_float((uint32_t)(ml[u] >> 32)), ov[u]);
+                if (j0 + u < P.parts) {
+#pragma unroll
+                    for (int i = 0; i < N; ++i) J[i].add(__uint_as_float((uint32_t)ml[u]), __uint_as_float((uint32_t)(ml[u] >> 32)), ov[u][i]);
+                }
         }
-        put_out<D>(S, io, P, P.r0 + rw * 32 + col, pc, half, J.result());
+#pragma unroll
+        for (int i = 0; i < N; ++i) put_out<D>(S, io, P, P.r0 + rw * 32 + col, pc + i, half, J[i].result());
+    };
+    if (AT_ONCE > 1 && live > 2) {
+        for (int cc = wave * AT_ONCE; cc < live * (D / 8); cc += kCaWaves * AT_ONCE) some(std::integral_constant<int, AT_ONCE>(), cc);
+    } else {
+        for (int cc = wave; cc < live * (D / 8); cc += kCaWaves) some(std::integral_constant<int, 1>(), cc);      // a wavefront per (32 rows, piece of them)
     }
 }
 
 // The pieces of a workgroup, one after the other.  In groups of kXcds, so that piece p stays with die p % kXcds: narrow pieces' groups
 // spread evenly among the others', and in every other round of the launch the workgroups' groups in reverse.
-template <class F>
+template <class Prices = CutPrices, class F>
 __device__ __forceinline__ void for_pieces(const ServingDev &S, const etc_serving_attention_io &io, ETC_AS_LDS CaLds &L, int n_pieces, F f)
 {
     const int grid = (int)gridDim.x;
@@ -580,7 +663,7 @@ __device__ __forceinline__ void for_pieces(const ServingDev &S, const etc_servin
             if (of_narrow) end = narrow;
         }
         if (p >= end) continue;
-        const Piece P = piece_of(S, io, L, p);
+        const Piece P = piece_of<Prices>(S, io, L, p);
         if (P.tile0 < P.tile1) f(P);
         __syncthreads();
     }
