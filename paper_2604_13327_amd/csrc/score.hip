@@ -369,7 +369,7 @@ __global__ __launch_bounds__(kScoreThreads) void serving_score_kernel(ServingDev
         }
         wg_release();
         if (tid == 0) {
-            int32_t *const arrived = S.score_arrived + row;
+            int32_t *const arrived = S.score_arrived + row * kScoreApart;
             s_last = __hip_atomic_fetch_add(as_global(arrived), 1, __ATOMIC_RELAXED, ETC_SCOPE) + 1 == slices;
             if (s_last) st_i32(arrived, 0);
         }

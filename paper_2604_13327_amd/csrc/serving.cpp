@@ -94,7 +94,7 @@ etc_status etc_serving_create(const etc_model_desc *m, const etc_serving_limits 
             if (n > 0) {
                 SRV_TRY(s, owned_alloc(s, (char **)&D.smp_stats, n * (size_t)sample_stat_bytes(), false));
                 SRV_TRY(s, owned_alloc(s, (char **)&D.smp_bins, n * (size_t)sample_bins_bytes(), false));
-                SRV_TRY(s, owned_alloc(s, &D.smp_listed, (size_t)kSampleSharedRows * (2 + kSampleList) + kScoreRows));
+                SRV_TRY(s, owned_alloc(s, &D.smp_listed, (size_t)kSampleSharedRows * (2 + kSampleList) + (size_t)kScoreRows * kScoreApart));
                 D.smp_done = D.smp_listed + kSampleSharedRows;
                 D.smp_list = D.smp_done + kSampleSharedRows;
                 D.score_arrived = D.smp_list + (size_t)kSampleSharedRows * kSampleList;
