@@ -77,15 +77,17 @@ __device__ __forceinline__ f32x16 scores_of(const u32x4 (&k)[D / 32], int k_scal
     return s;
 }
 
-// Prices of a cut, in tiles of a whole block (1.7 us): 64 keys of a block of few rows are 16 KB, which a workgroup reads in less than half of that
-// time; what a piece costs besides its tiles, and where its keys are cut; what a call's last join takes.
+// Prices of a cut, in tiles of a whole block (1.5 to 1.8 us): 64 keys of a block of few rows are 16 KB, which a workgroup reads in less than half of
+// that time; what a piece costs besides its tiles, and where its keys are cut; what a call's last join takes; and what is left of a launch that takes
+// its pieces one after the other when the first workgroup finds none, of the longest piece and of the average one.
 struct CodesPrices {
     static constexpr bool OWN = true;
     static __device__ __forceinline__ float factor(int w) { return w == 1 ? 4.f : w == 2 ? 2.f : w == 3 ? 1.5f : w == 4 ? 1.25f : w == 5 ? 1.1f : w == 6 ? 1.f : 0.85f; }
     static __device__ __forceinline__ float tile(bool narrow) { return narrow ? 0.44f : 1.f; }
-    static __device__ __forceinline__ float piece(bool narrow) { return narrow ? 4.f : 8.f; }
-    static __device__ __forceinline__ float part(bool narrow) { return narrow ? 1.f : 3.f; }
-    static __device__ __forceinline__ float join(bool narrow, int parts) { return narrow ? 2.f + 0.3f * (float)parts : 5.f + 0.8f * (float)parts; }
+    static __device__ __forceinline__ float piece(bool narrow) { return narrow ? 4.6f : 8.1f; }
+    static __device__ __forceinline__ float part(bool narrow) { return narrow ? 1.4f : 2.5f; }
+    static __device__ __forceinline__ float join(bool narrow, int parts) { return narrow ? 0.6f + 0.44f * (float)parts : 1.6f + 1.15f * (float)parts; }
+    static __device__ __forceinline__ float left(float longest, float average) { return 0.25f * longest + 0.39f * average; }
 };
 
 struct Pool8 { const uint8_t *k, *v, *k_scale, *v_scale; };
@@ -549,7 +551,7 @@ __device__ __forceinline__ void narrow_piece_codes(const ServingDev &S, const et
         }
         if (P.parts == 1) {
             put_out<D>(S, io, P, jr * 32 + col, pc, half, J.result());
-        } else {
+        } else {                                         // (whole, also of few rows: their 64 bytes of each KB were slower to write)
             const __amdgpu_buffer_rsrc_t d_b = buf_of(partial<D>(S, P.slot0 + P.part * S.nkv, jr));
             buf_st_16B(d_b, (uint32_t)((pc * 64 + lane) * 16), __builtin_bit_cast(u32x4, J.o));
             if (pc == 0 && half == 0) buf_st_8B(d_b, (uint32_t)(kCaPartO<D> * 4 + col * 8), u32x2{__float_as_uint(J.m), __float_as_uint(J.l)});
@@ -558,10 +560,45 @@ __device__ __forceinline__ void narrow_piece_codes(const ServingDev &S, const et
     if (P.parts > 1) join_parts<D, 4>(S, io, L, P, tid, wave, lane);
 }
 
+// The pieces of a workgroup, one after the other, in groups of kXcds as for_pieces() has them, narrow pieces' groups evenly among the others'.  A
+// workgroup's first piece is its own; of the others each takes the die's next one when it has gone through its keys (a narrow piece takes 2 to 30 us, a
+// whole block's up to 45: dealt out in advance, 32 mixed sequences took 67 us, not 60, and 40 of heads of 8 to 4 262, not 184).
+template <class F>
+__device__ __forceinline__ void take_pieces(const ServingDev &S, const etc_serving_attention_io &io, ETC_AS_LDS CaLds &L, ETC_AS_LDS int *next, int n_pieces, F f)
+{
+    const int grid = (int)gridDim.x, dies = min(grid, kXcds), w = (int)blockIdx.x, die = w % dies;
+    const int narrow = __builtin_amdgcn_readfirstlane(L.narrow);
+    const int gn = div_up(narrow, kXcds), groups = gn + div_up(n_pieces - narrow, kXcds), all = groups * kXcds;
+    const bool asks = all > grid && threadIdx.x == 0;
+    for (int k = w / dies; k * dies + die < all;) {
+        int p = k * dies + die, end = n_pieces;
+        if (narrow > 0 && narrow < n_pieces) {
+            const int g = p / kXcds, g0 = (int)((int64_t)g * gn / groups);
+            const bool of_narrow = (int64_t)(g + 1) * gn / groups > g0;
+            p = (of_narrow ? g0 * kXcds : narrow + (g - g0) * kXcds) + p % kXcds;
+            if (of_narrow) end = narrow;
+        }
+        if (p < end) {
+            const Piece P = piece_of<CodesPrices>(S, io, L, p);
+            if (P.tile0 < P.tile1) f(P);
+        }
+        if (all <= grid) return;
+        if (asks) {
+            const int n = __hip_atomic_fetch_add(as_global(S.taken + die * kTakenApart), 1, __ATOMIC_RELAXED, ETC_SCOPE);
+            if (n == div_up(all - die, dies) - 1) st_i32(S.taken + die * kTakenApart, 0);      // the last: every piece of the die asks once
+            *next = div_up(grid - die, dies) + n;
+        }
+        __syncthreads();
+        k = __builtin_amdgcn_readfirstlane(*next);
+        __syncthreads();
+    }
+}
+
 template <int D>
 __global__ __launch_bounds__(kCaThreads) void chunk_attention_codes_kernel(ServingDev S, etc_serving_attention_codes_io io8)
 {
     __shared__ CaLds s_cut;
+    __shared__ int s_next;
     __shared__ __attribute__((aligned(16))) Tiles8<D> s_tiles;
     ETC_AS_LDS CaLds &L = *as_lds(&s_cut);
     ETC_AS_LDS Tiles8<D> &B = *as_lds(&s_tiles);
@@ -569,7 +606,7 @@ __global__ __launch_bounds__(kCaThreads) void chunk_attention_codes_kernel(Servi
     const Pool8 pool{(const uint8_t *)io.k_pages, (const uint8_t *)io.v_pages, (const uint8_t *)io8.k_scale, (const uint8_t *)io8.v_scale};
     const int n_pieces = cut<SRV_ATTENTION_CODES, CodesPrices>(S, io, L);
     if (n_pieces == 0) return;
-    for_pieces<CodesPrices>(S, io, L, n_pieces, [&](const Piece &P) {
+    take_pieces(S, io, L, as_lds(&s_next), n_pieces, [&](const Piece &P) {
         if (P.rows <= 32) narrow_piece_codes<D, false>(S, io, pool, L, B, P);
         else if (P.rows <= kCaNarrowRows) narrow_piece_codes<D, true>(S, io, pool, L, B, P);
         else wide_piece_codes<D>(S, io, pool, L, B, P);

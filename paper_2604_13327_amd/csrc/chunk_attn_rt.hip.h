@@ -201,7 +201,8 @@ __device__ __forceinline__ int cut(const ServingDev &S, const etc_serving_attent
             narrow_parts = wave_max_i(narrow_parts);
             over = wave_sum(over);
             longest_cost = wave_max_f(longest_cost);
-            ends = fmaxf(longest_cost, ceilf(pieces / (float)grid) * ((work + over) / fmaxf(pieces, 1.f))) +
+            const float all = work + over;
+            ends = fmaxf(longest_cost, pieces > (float)grid ? all * (1.f / (float)grid) + Prices::left(longest_cost, all / pieces) : 0.f) +
                    fmaxf(parts > 1 ? Prices::join(false, parts) : 0.f, narrow_parts > 1 ? Prices::join(true, narrow_parts) : 0.f);
         }
         if (wave > 0 && slots > (float)S.attn_slots) ends = INFINITY;
@@ -215,7 +216,7 @@ __device__ __forceinline__ int cut(const ServingDev &S, const etc_serving_attent
         float best_ends = L.wave_f[0];
 #pragma unroll
         for (int w = 1; w < kCaTries; ++w)
-            if (L.wave_f[w] < best_ends) { best = w; best_ends = L.wave_f[w]; }
+            if (L.wave_f[w] < best_ends || (Prices::OWN && best > 0 && L.wave_f[w] == best_ends)) { best = w; best_ends = L.wave_f[w]; }      // (OWN: of equals the shorter pieces)
         longest_piece = L.wave_i[0][best];
         if (Prices::OWN) longest_narrow = L.wave_i[1][best];
     } else {

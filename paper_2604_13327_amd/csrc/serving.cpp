@@ -83,7 +83,8 @@ etc_status etc_serving_create(const etc_model_desc *m, const etc_serving_limits 
         SRV_TRY(s, hipHostMalloc((void **)&s->h_error, 4 * sizeof(int32_t), hipHostMallocMapped));
         memset(s->h_error, 0, 4 * sizeof(int32_t));
         SRV_TRY(s, hipHostGetDevicePointer((void **)&D.error, s->h_error, 0));
-        SRV_TRY(s, owned_alloc(s, &D.arrive, 2));
+        SRV_TRY(s, owned_alloc(s, &D.arrive, (size_t)kTakenApart + 8 * kTakenApart));
+        D.taken = D.arrive + kTakenApart;
         D.attn_slots = attention_slots(m->n_q_heads, m->n_kv_heads, *l);
         if (D.attn_slots > 0) {
             SRV_TRY(s, owned_alloc(s, &D.attn_arrive, (size_t)D.attn_slots));

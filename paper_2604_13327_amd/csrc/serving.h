@@ -29,6 +29,7 @@ struct ServingDev {
     float *attn_part;
     int32_t *attn_arrive;
     int attn_slots;              // no cut takes more
+    int32_t *taken;              // [8 * kTakenApart] pieces that a die's workgroups have taken behind their first ones (zero between launches)
     // sampling of long rows: statistics and bins of the slices
     void *smp_stats;
     uint64_t *smp_bins;
@@ -37,6 +38,7 @@ struct ServingDev {
     int32_t *smp_listed, *smp_done, *smp_list;
     int32_t *score_arrived;      // [kScoreRows * kScoreApart] slices of a row that have arrived (zero between launches); a slice's results in smp_bins
 };
+constexpr int kTakenApart = 32;
 constexpr int kScoreTop = 64;                // likeliest tokens of a row, at most
 constexpr int kScoreRows = 512;            // rows that are cut
 constexpr int kScoreApart = 32;           // their counters stand a cache line apart: 512 arrivals at neighbours took 3 us longer
