@@ -253,6 +253,33 @@ def test_attention_many_sequences(etc, n_seqs):
     _attention(etc, ref.shape(4, 2, 64), kv, new)
 
 
+@pytest.mark.parametrize("nq,nkv,d", [(16, 8, 64), (9, 3, 128), (10, 5, 64)])
+def test_attention_calls_one_after_the_other(etc, nq, nkv, d):
+    """Calls of more pieces than workgroups, and of fewer, on one handle: what a workgroup takes next is counted from call to call."""
+    s, rng = ref.shape(nq, nkv, d), np.random.default_rng(nq)
+    some = lambda n, longest: [int(x) for x in rng.integers(1, longest, n)]      # noqa: E731
+    calls = []
+    for i, (kv, new) in enumerate((([*some(190, 150)], [1] * 190), (some(3, 200), [1, 2, 40]), ([0, 0, 90, *some(120, 300)], [700, 300, 201] + [1] * 120), ([1500] * 2, [400, 1]))):
+        table, n_pages = ref.paged([a + b for a, b in zip(kv, new)], s.page, i)
+        (k, ks), (v, vs) = codes.pools(i, n_pages, s.page, nkv, d), codes.pools(i + 9, n_pages, s.page, nkv, d)
+        indptr = np.concatenate(([0], np.cumsum(new)))
+        q = randn(i, int(indptr[-1]), nq, d)
+        want, size = ref.attention(s, q, codes.values(k, ks), codes.values(v, vs), indptr, kv, table)
+        calls.append(([q.cuda(), torch.empty(q.shape, dtype=q.dtype, device="cuda"), i32(indptr), i32(kv), i32(table), k.cuda(), v.cuda(), ks.cuda(), vs.cuda()], want, size))
+    sv = etc.Serving(s, max_seqs=190, max_tokens=1400, max_kv_len=2000)
+    first = {}
+    for turn in (0, 1, 2, 3, 0, 0, 2, 2, 1, 3, 2, 0, 3):
+        args, want, size = calls[turn]
+        args[1].fill_(7.0)
+        sv.attention_codes(*args)
+        if turn not in first:
+            first[turn] = args[1].clone()
+            ref.check_attention(args[1], want, size)
+        assert torch.equal(args[1], first[turn])
+    assert sv.read_error() == (0, 0, 0, 0)
+    sv.close()
+
+
 @pytest.mark.parametrize("d", [64, 128])
 def test_attention_queries_of_wide_range(etc, d):
     """Elements of a row over many powers of two; rows of zeros; rows so small or so large that their scale is."""
