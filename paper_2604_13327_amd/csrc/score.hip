@@ -250,7 +250,8 @@ __global__ __launch_bounds__(kScoreThreads) void serving_score_kernel(ServingDev
     TopList list{as_lds(s_list) + wave * kScoreList, as_lds(s_pending) + wave, top, 0, 0, 0, -INFINITY};
     Sums s{-INFINITY, 0.f, 0.f};
     float from_ref = INFINITY;                           // -in_log2(s.ref)
-    bool first = true;
+    float best = -INFINITY;                              // of what this lane has read
+    int fed = 0;
     auto feed = [&](const u32x4 (&w)[U], int id) {       // vector u: tokens id + u * THREADS * E ..; out of range: NaN
         float most[U], all = -INFINITY;
 #pragma unroll
@@ -282,16 +283,19 @@ __global__ __launch_bounds__(kScoreThreads) void serving_score_kernel(ServingDev
         s.l += l;
         s.t += t;
         if (top == 0) return;
-        if (first) {                                     // the wavefronts' lanes together: `top` of them reach the least of this
-            const uint64_t t = TopList::reached(all, (top + WAVES - 1) / WAVES);
+        // The wavefronts' lanes together: `top` of them reach the least of this.  Found again behind the second, fourth, eighth .. load (another
+        // wavefront's number may be an older one then, which holds as well): 512 rows of 128256 in bf16 with 5 alternatives, 35.8 us -> 32.3.
+        best = fmaxf(best, all);
+        if (fed != 1 && (fed & (fed - 1)) == 0) {
+            const uint64_t t = TopList::reached(best, (top + WAVES - 1) / WAVES);
             if (lane == 0) s_begin[wave] = t;
-            __syncthreads();
+            if (fed == 0) __syncthreads(); else in_order();
             uint64_t least = s_begin[0];
 #pragma unroll
             for (int i = 1; i < WAVES; ++i) least = min(least, s_begin[i]);
-            list.set(least);
-            first = false;
+            if (least > list.threshold) list.set(least);
         }
+        ++fed;
         if (__builtin_amdgcn_ballot_w64(all > list.under) == 0) return;
 #pragma unroll
         for (int u = 0; u < U; ++u) list.take<F32>(w[u], most[u], id + u * THREADS * E);
