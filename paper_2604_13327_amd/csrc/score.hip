@@ -23,7 +23,6 @@ constexpr float kScoreLag = 6.f;
 constexpr float kScoreHuge = 1e38f;         // references from here on leave no room for their multiple by 1 / ln 2
 constexpr float kLog2E = 1.44269504088896f;
 constexpr double kPerLog2E = 1.0 / (double)kLog2E;      // of that very number: what it is off by scales all logits, not their differences
-constexpr int kScoreParts = 1024;           // slices of a launch, at most
 constexpr int kScoreMinSlice = 4096;
 static_assert(kScoreTop <= 64 && kScoreList >= kScoreTop + 64, "lists");
 

@@ -38,10 +38,11 @@ struct ServingDev {
     int32_t *smp_listed, *smp_done, *smp_list;
     int32_t *score_arrived;      // [kScoreRows * kScoreApart] slices of a row that have arrived (zero between launches); a slice's results in smp_bins
 };
-constexpr int kTakenApart = 32;
+constexpr int kTakenApart = 32;              // counters stand a cache line apart: 512 arrivals at neighbours took 3 us longer
 constexpr int kScoreTop = 64;                // likeliest tokens of a row, at most
-constexpr int kScoreRows = 512;            // rows that are cut
-constexpr int kScoreApart = 32;           // their counters stand a cache line apart: 512 arrivals at neighbours took 3 us longer
+constexpr int kScoreRows = 512;              // rows that are cut
+constexpr int kScoreParts = 1024;            // slices of a launch, at most; a slice leaves 16 + 8 * kScoreTop bytes
+constexpr int kScoreApart = 32;
 constexpr int kSampleList = 8192;
 constexpr int kSampleSharedRows = 128;
 constexpr int kAttnMaxSlots = 1024;

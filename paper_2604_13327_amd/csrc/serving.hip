@@ -1144,7 +1144,8 @@ hipError_t launch_serving_sample(const ServingDev &S, const etc_serving_sample_i
     return hipGetLastError();
 }
 
-// Workspace of a handle: slices of a launch, all rows together.
+// Workspace of a handle: slices of a launch, all rows together (the bins' part holds the slices of the scores too).
+static_assert((int64_t)kSmpWgs * kSmpBins * 8 >= (int64_t)kScoreParts * (16 + 8 * kScoreTop), "scores");
 int64_t sample_slices(int vocab, int max_rows)
 {
     if (vocab <= kSmpWhole) return 0;
