@@ -93,13 +93,15 @@ struct CodesPrices {
 struct Pool8 { const uint8_t *k, *v, *k_scale, *v_scale; };
 
 constexpr int kCa8Ids = 256;                // page ids in LDS, with their scales, a window of them at a time
+constexpr int kCa8WideIds = 1024;           // of a whole block
+constexpr int kCa8Tiles = 3;                // of a whole block, in LDS
 template <int D>
 struct Tiles8 {
     uint16_t rows[512 * D];                 // 128 KB for heads of 128
     int ids[kCa8Ids];
     int k_byte[kCa8Ids], v_byte[kCa8Ids];   // narrow pieces: scales of the pages
     float v_scale[kCaWaves][kCa8Keys];      // of a wavefront's keys
-    int k_scale[2][kCaKeys];                // wide pieces: of a tile's keys
+    int k_scale[kCa8Tiles][kCaKeys];        // wide pieces: of a tile's keys
 };
 
 // Where the rows of a (sequence, KV head) lie: offset of a key's row in the pools, and of its scale.
@@ -113,27 +115,34 @@ struct Rows8 {
 };
 
 // ---- a block of more than 64 rows ------------------------------------------------------------------------------------------
-// 32 rows to a wavefront, all wavefronts over the same tiles of 64 keys, in two buffers of LDS: while tile t is being read, t + 1 is on its way
-// through registers, 16 bytes of K and of V to a thread.
+// 32 rows to a wavefront, all wavefronts over the same tiles of 64 keys, in three buffers of LDS: while tile t is being read, t + 1 comes to LDS
+// from registers, 16 bytes of K and of V to a thread, and t + 2 is on its way there.
+// Bound by the matrix units and the power they take: 4001 tokens behind 30000 keys, 64 heads of 128 on 8 (4.2 TFLOP), take 3.5 to 3.6 ms, 1.20
+// PFLOP/s where a large bf16 product of a library reaches 1.29; the units are busy for half of the cycles.  Tried and slower there: K's fragments
+// all asked for in front of their products (1 %), exponentials placed between the products by hand (5 %), the next tile to LDS in front of the
+// products (6 %), a higher wave priority for either half of a tile (1 to 3 %).
 template <int D>
 __device__ __forceinline__ void wide_piece_codes(const ServingDev &S, const etc_serving_attention_io &io, const Pool8 &pool, ETC_AS_LDS CaLds &L, ETC_AS_LDS Tiles8<D> &B, const Piece &P)
 {
     constexpr int DT = D / 32, PPR = D / 16;             // tiles of the output; pieces (of 16 codes) of a row
     constexpr uint32_t KBUF = kCaKeys * D, VBUF = kCaKeys * D * 2;
-    static_assert(2 * (KBUF + VBUF) <= 512 * D * 2, "LDS");
+    static_assert(kCa8Tiles * (KBUF + VBUF) + kCa8WideIds * 4 <= 512 * D * 2, "LDS");
+    static_assert(kCa8WideIds >= 2 * kCaKeys, "a window holds two tiles, whatever the pages");
     int tid = (int)threadIdx.x;
     asm volatile("" : "+v"(tid));                        // of this piece: what is computed from it does not stay in registers across pieces
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, half = lane >> 5, col = lane & 31;
     const int tile0 = P.tile0, n_tiles = P.tile1, key_end = min(n_tiles * kCaKeys, P.n_keys);
     const int row = P.r0 + wave * 32 + col, rr = min(row, P.rows - 1), t = rr / P.grp, head = P.kvh * P.grp + (rr - t * P.grp);
     typename QCodes<D>::Asked q = QCodes<D>::ask((const uint16_t *)io.q + ((int64_t)(P.seq.q0 + t) * S.nq + head) * D, half);      // with the page ids
-    PageWindow<kCa8Ids> W{io.block_table + (int64_t)P.b * io.table_stride, 0, 0};
-    W.load<SRV_ATTENTION_CODES>(S, io, B.ids, P.b, tile0 * kCaKeys, key_end, tid);
+    typedef int Ids[kCa8WideIds];
+    ETC_AS_LDS Ids &ids = *reinterpret_cast<ETC_AS_LDS Ids *>(&B.rows[kCa8Tiles * (KBUF + VBUF) / 2]);      // behind the tiles
+    PageWindow<kCa8WideIds> W{io.block_table + (int64_t)P.b * io.table_stride, 0, 0};
+    W.load<SRV_ATTENTION_CODES>(S, io, ids, P.b, tile0 * kCaKeys, key_end, tid);
     const int limit = P.seq.kv + t;                      // last key this row sees
     const int first_masked = (P.seq.kv + P.r0 / P.grp + 1) / kCaKeys;      // tiles in front of it are seen whole by all rows of the block
     const int wave_last = P.seq.kv + min((P.r0 + wave * 32 + 31) / P.grp, P.seq.n - 1);
     const bool wave_live = P.r0 + wave * 32 < P.rows;
-    const uint32_t k_base = (uint32_t)(uintptr_t)&B.rows[0], v_base = k_base + 2 * KBUF;
+    const uint32_t k_base = (uint32_t)(uintptr_t)&B.rows[0], v_base = k_base + kCa8Tiles * KBUF;
 
     // what this thread brings: row lr of a tile, codes 16 lp .. 16 lp + 15
     const Rows8 R(S, P.kvh, D);
@@ -143,7 +152,7 @@ __device__ __forceinline__ void wide_piece_codes(const ServingDev &S, const etc_
     uint32_t ks_in = 0, vs_in = 0;
     auto load = [&](int tile) {
         if (!brings) return;
-        const int key = min(tile * kCaKeys + lr, P.n_keys - 1), id = R.page(B.ids, key, W.first);
+        const int key = min(tile * kCaKeys + lr, P.n_keys - 1), id = R.page(ids, key, W.first);
         const uint64_t at = R.at(id, key) + lp * 16;
         k_in = gld_16B(pool.k + at);
         v_in = gld_16B(pool.v + at);
@@ -181,17 +190,18 @@ __device__ __forceinline__ void wide_piece_codes(const ServingDev &S, const etc_
             s[kt] = scores_of<D>(k, B.k_scale[buf][kt * 32 + col], Q);
         }
     };
-    auto covered = [&](int tile) { return min((tile + 1) * kCaKeys, key_end) <= W.end; };
-    auto ahead = [&](int tile) {                         // the next tile to the other buffer, the one behind it on its way
-        if (tile + 1 < n_tiles) put((tile + 1 - tile0) & 1);
-        if (tile + 2 < n_tiles) {
-            if (!covered(tile + 2)) {
-                __syncthreads();
-                W.load<SRV_ATTENTION_CODES>(S, io, B.ids, P.b, (tile + 2) * kCaKeys, key_end, tid);
-                __syncthreads();
-            }
-            load(tile + 2);
-        }
+    auto next = [](uint32_t buf) { return buf + 1 == kCa8Tiles ? 0 : buf + 1; };
+    auto ahead = [&](int tile, uint32_t buf) {           // the next tile to its buffer, the one behind it on its way
+        if (tile + 1 < n_tiles) put(next(buf));
+        if (tile + 2 < n_tiles) load(tile + 2);
+    };
+    int whole_tiles = 0;                                 // tiles whose pages, and those of the two behind them, are in LDS
+    auto opened = [&] { whole_tiles = W.end < key_end ? W.end / kCaKeys - 2 : n_tiles; };
+    auto window = [&](int tile) {                        // by all threads, none of them ahead
+        __syncthreads();
+        W.load<SRV_ATTENTION_CODES>(S, io, ids, P.b, (tile + 2) * kCaKeys, key_end, tid);
+        __syncthreads();
+        opened();
     };
 
     if (tid == 0) L.odd = -1;
@@ -199,26 +209,35 @@ __device__ __forceinline__ void wide_piece_codes(const ServingDev &S, const etc_
     load(tile0);
     Q.set(q);                                            // while the first rows are on their way
     put(0);
-    if (tile0 + 1 < n_tiles) {
-        if (!covered(tile0 + 1)) {
-            __syncthreads();
-            W.load<SRV_ATTENTION_CODES>(S, io, B.ids, P.b, (tile0 + 1) * kCaKeys, key_end, tid);
-            __syncthreads();
-        }
-        load(tile0 + 1);
-    }
+    if (tile0 + 1 < n_tiles) load(tile0 + 1);
+    opened();
     __syncthreads();
     int tile = tile0;
+    uint32_t buf = 0;
     const int n_seen = min(first_masked, n_tiles);
-    for (; tile < n_seen; ++tile) {
-        const uint32_t buf = (tile - tile0) & 1;
-        if (wave_live) scores(buf);
-        ahead(tile);
-        if (wave_live) attend<D, 2, false>(s, o, m, l, F, v_base + buf * VBUF, half, scale, 0, 0);
-        __syncthreads();
+    // Tiles that all rows see whole.  A SIMD has a wavefront of the upper and one of the lower half of the rows: the lower ones are half a tile late, so
+    // that one's products keep the matrix units busy while the other computes exponentials (7 % fewer cycles; 3605 -> 3490 us for 4001 tokens behind
+    // 30000 keys, 163 -> 153 for 1500 behind 4000, 32 heads of 128 on 4).
+    const bool late = wave >= kCaWaves / 2;
+    while (tile < n_seen) {
+        const int stop = min(n_seen, whole_tiles);
+        if (tile >= stop) {
+            window(tile);
+            continue;
+        }
+        if (late) __syncthreads();
+        for (; tile < stop; ++tile, buf = next(buf)) {
+            if (wave_live) scores(buf);
+            ahead(tile, buf);
+            __syncthreads();
+            if (wave_live) attend<D, 2, false>(s, o, m, l, F, v_base + buf * VBUF, half, scale, 0, 0);
+            __syncthreads();
+        }
+        if (!late) __syncthreads();
     }
-    for (; tile < n_tiles; ++tile) {
-        const uint32_t buf = (tile - tile0) & 1, v_tile = v_base + buf * VBUF;
+    for (; tile < n_tiles; ++tile, buf = next(buf)) {
+        if (tile >= whole_tiles) window(tile);
+        const uint32_t v_tile = v_base + buf * VBUF;
         constexpr int N = D / 64;
         u32x4 mine[N];
         uint32_t mine_at[N];
@@ -234,7 +253,7 @@ __device__ __forceinline__ void wide_piece_codes(const ServingDev &S, const etc_
         const bool live = wave_live && tile * kCaKeys <= wave_last;
         if (__builtin_expect(L.odd == tile, 0)) odd_values<D, kCaKeys, N>(mine, mine_at, o, F, v_tile, half, tile * kCaKeys, limit, live);
         if (live) scores(buf);
-        ahead(tile);
+        ahead(tile, buf);
         if (live) attend<D, 2, true>(s, o, m, l, F, v_tile, half, scale, tile * kCaKeys, limit);
         __syncthreads();
     }

@@ -237,6 +237,13 @@ def test_attention_pages(etc, page, d, kv, new):
     _attention(etc, ref.shape(4, 2, d, page=page), kv, new)
 
 
+@pytest.mark.parametrize("nq,nkv,d,n", [(64, 32, 64, 8), (32, 16, 128, 16)])
+def test_attention_whole_blocks_with_windows(etc, nq, nkv, d, n):
+    """Pages of one token, more of them in an uncut piece of a whole block than its window of page ids holds; NaN codes among what no row sees."""
+    kv, new = [1090 + 3 * b for b in range(n)], [129 - b for b in range(n)]
+    _attention(etc, ref.shape(nq, nkv, d, page=1), kv, new)
+
+
 @pytest.mark.parametrize("nq,nkv,d", [(8, 2, 128), (8, 2, 64)])
 def test_attention_long(etc, nq, nkv, d):
     """Keys in many pieces; sequences of few rows among prompts."""
