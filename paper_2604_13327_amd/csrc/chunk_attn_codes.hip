@@ -87,7 +87,7 @@ struct CodesPrices {
     static __device__ __forceinline__ float piece(bool narrow) { return narrow ? 4.6f : 8.1f; }
     static __device__ __forceinline__ float part(bool narrow) { return narrow ? 1.4f : 2.5f; }
     static __device__ __forceinline__ float join(bool narrow, int parts) { return narrow ? 0.6f + 0.44f * (float)parts : 1.6f + 1.15f * (float)parts; }
-    static __device__ __forceinline__ float left(float longest, float average) { return 0.25f * longest + 0.39f * average; }
+    static __device__ __forceinline__ float left(float longest, float average) { return 0.18f * longest + 0.39f * average; }
 };
 
 struct Pool8 { const uint8_t *k, *v, *k_scale, *v_scale; };
@@ -579,9 +579,10 @@ __device__ __forceinline__ void narrow_piece_codes(const ServingDev &S, const et
     if (P.parts > 1) join_parts<D, 4>(S, io, L, P, tid, wave, lane);
 }
 
-// The pieces of a workgroup, one after the other, in groups of kXcds as for_pieces() has them, narrow pieces' groups evenly among the others'.  A
-// workgroup's first piece is its own; of the others each takes the die's next one when it has gone through its keys (a narrow piece takes 2 to 30 us, a
-// whole block's up to 45: dealt out in advance, 32 mixed sequences took 67 us, not 60, and 40 of heads of 8 to 4 262, not 184).
+// The pieces of a workgroup, one after the other, in groups of kXcds so that piece p stays with die p % kXcds: whole blocks' first, which take up to
+// 45 us, then narrow ones (2 to 30).  A workgroup's first piece is its own; of the others each takes the die's next one when it has none.  Dealt out in
+// advance, narrow pieces among the others, 32 mixed sequences took 67 us, not 62, and 40 of heads of 8 to 4 262, not 156; taken in turn in that
+// order 65 and 171.
 template <class F>
 __device__ __forceinline__ void take_pieces(const ServingDev &S, const etc_serving_attention_io &io, ETC_AS_LDS CaLds &L, ETC_AS_LDS int *next, int n_pieces, F f)
 {
@@ -592,10 +593,13 @@ __device__ __forceinline__ void take_pieces(const ServingDev &S, const etc_servi
     for (int k = w / dies; k * dies + die < all;) {
         int p = k * dies + die, end = n_pieces;
         if (narrow > 0 && narrow < n_pieces) {
-            const int g = p / kXcds, g0 = (int)((int64_t)g * gn / groups);
-            const bool of_narrow = (int64_t)(g + 1) * gn / groups > g0;
-            p = (of_narrow ? g0 * kXcds : narrow + (g - g0) * kXcds) + p % kXcds;
-            if (of_narrow) end = narrow;
+            const int wide = (groups - gn) * kXcds;      // places
+            if (p < wide) {
+                p += narrow;
+            } else {
+                p -= wide;
+                end = narrow;
+            }
         }
         if (p < end) {
             const Piece P = piece_of<CodesPrices>(S, io, L, p);
