@@ -77,6 +77,8 @@ struct CaLds {
     int limit, narrow_limit;                // tiles of a piece; of one of a narrow sequence, where those have a price of their own
     int narrow;                             // pieces of narrow sequences, which are in front (0: in any order)
     int odd, last;
+    float try_f[kCaWaves];                  // candidates of a cut with prices of its own
+    int try_i[2][kCaWaves];
 };
 
 __device__ __forceinline__ int div_up(int a, int b) { return (a + b - 1) / b; }
@@ -206,24 +208,69 @@ __device__ __forceinline__ int cut(const ServingDev &S, const etc_serving_attent
                    fmaxf(parts > 1 ? Prices::join(false, parts) : 0.f, narrow_parts > 1 ? Prices::join(true, narrow_parts) : 0.f);
         }
         if (wave > 0 && slots > (float)S.attn_slots) ends = INFINITY;
-        __syncthreads();
-        if (lane == 0) {
-            L.wave_f[wave] = ends;
-            L.wave_i[0][wave] = longest;
-            if (Prices::OWN) L.wave_i[1][wave] = longest_narrow;
-        }
-        __syncthreads();
-        float best_ends = L.wave_f[0];
+        if constexpr (!Prices::OWN) {
+            __syncthreads();
+            if (lane == 0) { L.wave_f[wave] = ends; L.wave_i[0][wave] = longest; }
+            __syncthreads();
+            float best_ends = L.wave_f[0];
 #pragma unroll
-        for (int w = 1; w < kCaTries; ++w)
-            if (L.wave_f[w] < best_ends || (Prices::OWN && best > 0 && L.wave_f[w] == best_ends)) { best = w; best_ends = L.wave_f[w]; }      // (OWN: of equals the shorter pieces)
-        longest_piece = L.wave_i[0][best];
-        if (Prices::OWN) longest_narrow = L.wave_i[1][best];
+            for (int w = 1; w < kCaTries; ++w)
+                if (L.wave_f[w] < best_ends) { best = w; best_ends = L.wave_f[w]; }
+            longest_piece = L.wave_i[0][best];
+        } else {                                         // a candidate to a lane: no cut if that is best, of other equals the shorter pieces
+            if (lane == 0) { L.try_f[wave] = ends; L.try_i[0][wave] = longest; L.try_i[1][wave] = longest_narrow; }
+            __syncthreads();
+            const int w = min(lane, kCaTries - 1);
+            const float mine = L.try_f[w];
+            const int mine_longest = L.try_i[0][w], mine_narrow = L.try_i[1][w];
+            const uint32_t bests = (uint32_t)__builtin_amdgcn_ballot_w64(mine == -wave_max_f(-mine)) & ((1u << kCaTries) - 1);
+            best = (bests & 1) ? 0 : 31 - __builtin_clz(bests);
+            longest_piece = __builtin_amdgcn_readlane(mine_longest, best);
+            longest_narrow = __builtin_amdgcn_readlane(mine_narrow, best);
+        }
     } else {
         longest_narrow = most;
     }
     const int limit = limit_of(best), narrow_limit = narrow_limit_of(best);
     if (tid == 0) { L.first[0] = L.slot[0] = 0; L.limit = limit; L.narrow_limit = narrow_limit; L.narrow = 0; }
+    auto class_of = [](bool narrow, int most_of, int len) {      // (OWN: half of the classes for each kind)
+        return (narrow ? 0 : kCaClasses / 2) + max(0, min(kCaClasses / 2 - 1, (int)((float)(kCaClasses / 2 * (most_of - len)) / (float)max(most_of, 1))));
+    };
+    if constexpr (Prices::OWN) {
+        // Up to 64 sequences: what follows, by one wavefront in registers, a sequence to a lane (2 to 3 us of a call that has ranks).
+        if (io.n_seqs <= 64) {
+            if (wave == 0) {
+                const bool there = lane < io.n_seqs;
+                const int n = there ? L.n[lane] : 0, tiles = there ? tiles_of(L.kv[lane], n) : 0;
+                const bool narrow = n * grp <= kCaNarrowRows;
+                const int parts = max(1, div_up(tiles, narrow ? narrow_limit : limit)), k = S.nkv * blocks_of(n, grp) * parts;
+                int rank = lane, wide = 0;
+                if (wave_sum_i(k) > grid && io.n_seqs > 1) {
+                    const int cls = class_of(narrow, narrow ? longest_narrow : longest_piece, div_up(tiles, parts));
+                    const uint64_t in_front = (1ull << lane) - 1;
+                    int above = 0;
+#pragma unroll
+                    for (int j = 0; j < kCaClasses; ++j) {
+                        const uint64_t of_it = __builtin_amdgcn_ballot_w64(there && cls == j);
+                        if (cls == j) rank = above + __builtin_popcountll(of_it & in_front);
+                        above += __builtin_popcountll(of_it);
+                        if (j >= kCaClasses / 2) wide += __builtin_popcountll(of_it);
+                    }
+                }
+                if (there) {
+                    L.split[lane] = parts;
+                    L.order[rank] = (uint16_t)lane;
+                }
+                in_order();
+                const int b = there ? (int)L.order[lane] : lane, pieces = __shfl(k, b, 64), cut = __shfl(parts, b, 64) > 1 ? pieces : 0;
+                const int upto = wave_scan_i(pieces), slots_upto = wave_scan_i(cut);
+                if (there) { L.first[lane + 1] = upto; L.slot[lane + 1] = slots_upto; }
+                if (wide > 0 && lane == io.n_seqs - wide) L.narrow = upto - pieces;
+            }
+            __syncthreads();
+            return __builtin_amdgcn_readfirstlane(L.first[io.n_seqs]);
+        }
+    }
     auto count = [&](auto as_they_come) {                // the prefix sums; the number of pieces
         int done = 0, done_slots = 0;
         for (int i0 = 0; i0 < io.n_seqs; i0 += kCaThreads) {
@@ -260,9 +307,8 @@ __device__ __forceinline__ int cut(const ServingDev &S, const etc_serving_attent
         for (int c = 0; c < 2; ++c) {
             const int b = c * kCaThreads + tid, rows = b < io.n_seqs ? L.n[b] * grp : 0;
             const int len = rows > 0 ? div_up(tiles_of(L.kv[b], L.n[b]), L.split[b]) : 0;
-            if constexpr (Prices::OWN) {                 // half of the classes for each kind
-                const int most_of = rows > kCaNarrowRows ? longest_piece : longest_narrow;
-                cls[c] = (rows > kCaNarrowRows ? kCaClasses / 2 : 0) + max(0, min(kCaClasses / 2 - 1, (int)((float)(kCaClasses / 2 * (most_of - len)) / (float)max(most_of, 1))));
+            if constexpr (Prices::OWN) {
+                cls[c] = class_of(rows <= kCaNarrowRows, rows > kCaNarrowRows ? longest_piece : longest_narrow, len);
             } else {
                 cls[c] = rows > kCaNarrowRows ? kCaClasses - 1 : min(kCaClasses - 2, (int)((float)((kCaClasses - 1) * (longest_piece - len)) / (float)longest_piece));
             }
