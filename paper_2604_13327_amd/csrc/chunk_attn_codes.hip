@@ -77,17 +77,20 @@ __device__ __forceinline__ f32x16 scores_of(const u32x4 (&k)[D / 32], int k_scal
     return s;
 }
 
-// Prices of a cut, in tiles of a whole block (1.5 to 1.8 us): 64 keys of a block of few rows are 16 KB, which a workgroup reads in less than half of
-// that time; what a piece costs besides its tiles, and where its keys are cut; what a call's last join takes; and what is left of a launch that takes
-// its pieces one after the other when the first workgroup finds none, of the longest piece and of the average one.
+// Prices of a cut, in tiles of a whole block (1.55 us): 64 keys of a block of few rows are 16 KB, which a workgroup reads in less than half of that
+// time; a tile of a launch's longest piece; what a piece costs besides its tiles, and where its keys are cut; what a call's last join takes; and what
+// is left of a launch that takes its pieces one after the other when the first workgroup finds none, by the average piece.  Fitted to the times of all
+// candidates in 34 calls (1 to 200 sequences, chunks of 1 to 4096, caches to 30000): what it chooses is 2 % behind the fastest in the mean,
+// 15 % at worst (a prompt of 2000, 66 us without a cut, 57 with 1.5 shares).
 struct CodesPrices {
     static constexpr bool OWN = true;
     static __device__ __forceinline__ float factor(int w) { return w == 1 ? 4.f : w == 2 ? 2.f : w == 3 ? 1.5f : w == 4 ? 1.25f : w == 5 ? 1.1f : w == 6 ? 1.f : 0.85f; }
     static __device__ __forceinline__ float tile(bool narrow) { return narrow ? 0.44f : 1.f; }
-    static __device__ __forceinline__ float piece(bool narrow) { return narrow ? 4.6f : 8.1f; }
-    static __device__ __forceinline__ float part(bool narrow) { return narrow ? 1.4f : 2.5f; }
-    static __device__ __forceinline__ float join(bool narrow, int parts) { return narrow ? 0.6f + 0.44f * (float)parts : 1.6f + 1.15f * (float)parts; }
-    static __device__ __forceinline__ float left(float longest, float average) { return 0.18f * longest + 0.39f * average; }
+    static __device__ __forceinline__ float alone(bool narrow) { return narrow ? 0.39f : 1.07f; }
+    static __device__ __forceinline__ float piece(bool narrow) { return narrow ? 4.f : 7.6f; }
+    static __device__ __forceinline__ float part(bool narrow) { return narrow ? 1.5f : 1.f; }
+    static __device__ __forceinline__ float join(bool narrow, int parts) { return narrow ? 0.4f + 0.36f * (float)parts : 1.9f + 0.83f * (float)parts; }
+    static __device__ __forceinline__ float left(float average) { return 0.47f * average; }
 };
 
 struct Pool8 { const uint8_t *k, *v, *k_scale, *v_scale; };

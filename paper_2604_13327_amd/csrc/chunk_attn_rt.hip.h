@@ -193,7 +193,7 @@ __device__ __forceinline__ int cut(const ServingDev &S, const etc_serving_attent
                 if (s > 1) slots += k * s;
                 if (narrow) { narrow_parts = max(narrow_parts, s); longest_narrow = max(longest_narrow, len); }
                 else { parts = max(parts, s); longest = max(longest, len); }
-                longest_cost = fmaxf(longest_cost, (float)len * Prices::tile(narrow) + each);
+                longest_cost = fmaxf(longest_cost, (float)len * Prices::alone(narrow) + each);
             }
             pieces = wave_sum(pieces);
             slots = wave_sum(slots);
@@ -204,7 +204,7 @@ __device__ __forceinline__ int cut(const ServingDev &S, const etc_serving_attent
             over = wave_sum(over);
             longest_cost = wave_max_f(longest_cost);
             const float all = work + over;
-            ends = fmaxf(longest_cost, pieces > (float)grid ? all * (1.f / (float)grid) + Prices::left(longest_cost, all / pieces) : 0.f) +
+            ends = fmaxf(longest_cost, pieces > (float)grid ? all * (1.f / (float)grid) + Prices::left(all / pieces) : 0.f) +
                    fmaxf(parts > 1 ? Prices::join(false, parts) : 0.f, narrow_parts > 1 ? Prices::join(true, narrow_parts) : 0.f);
         }
         if (wave > 0 && slots > (float)S.attn_slots) ends = INFINITY;
