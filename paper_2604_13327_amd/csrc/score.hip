@@ -428,10 +428,12 @@ __global__ __launch_bounds__(kScoreThreads) void serving_score_kernel(ServingDev
     in_order();
     const uint64_t entry = lane < n ? found[lane] : 0;
     int rank = 0;
-    for (int i = 0; i < n; ++i) {
-        const uint64_t e = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(entry >> 32), i) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)entry, i);
-        rank += e > entry;
-    }
+    for (int i0 = 0; i0 < n; i0 += 8)
+#pragma unroll
+        for (int i = i0; i < i0 + 8; ++i) {              // (those behind the last are 0)
+            const uint64_t e = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(entry >> 32), i) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)entry, i);
+            rank += e > entry;
+        }
     if (lane >= n) rank = lane;
     if (rank >= top) return;
     const int64_t at = (int64_t)row * top + rank;
