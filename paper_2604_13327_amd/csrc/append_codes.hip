@@ -182,6 +182,8 @@ __global__ __launch_bounds__(kAp8Threads) void serving_append_codes_kernel(Servi
         const uint64_t behind = j + n < 64 ? lives >> (j + n) << (j + n) : 0;
         const bool whole = n <= kAp8Rows && (off + n > pmask || (behind != 0 ? __builtin_amdgcn_readlane(slots, __builtin_ctzll(behind)) != slot + n : w0 + 64 >= io.n_tokens));
         const int64_t page = slot >> psh;
+        uint8_t *const scale = scales + page * S.nkv + h;
+        int before = 0;                                  // the page's scale; asked for behind the rows, so that those do not wait for it
         float a[ITERS][8], b[ITERS][8];
         // Rows row .. of the run, nr of them, up to kAp8Rows (those behind are the last one again): the values that are to be stored, in a and b.
         auto values = [&](int row, int nr) {
@@ -189,6 +191,7 @@ __global__ __launch_bounds__(kAp8Threads) void serving_append_codes_kernel(Servi
 #pragma unroll
                 for (int u = 0; u < ITERS; ++u)
                     load_head<D, F32>(a[u], b[u], src, (int64_t)(row + min(u * RPI + lane / LPH, nr - 1)) * stride + h * D + c);
+                if (row == r) before = (int)*as_global(scale);
             }
             if (!is_v) {
                 __syncthreads();                         // who reads the angles of the rows before
@@ -206,8 +209,6 @@ __global__ __launch_bounds__(kAp8Threads) void serving_append_codes_kernel(Servi
                 for (int i = 0; i < 8; ++i) { a[u][i] = finite_or_nan(a[u][i]); b[u][i] = finite_or_nan(b[u][i]); }
             }
         };
-        uint8_t *const scale = scales + page * S.nkv + h;
-        const int before = mine && off > 0 ? (int)*as_global(scale) : 0;
         float most = 0.f, inv = 0.f;
         bool once = true;                                // the run's values are in a and b
         // Up to kAp8Rows rows of the run without one left out between them at a time, for the largest value, then to be stored.
