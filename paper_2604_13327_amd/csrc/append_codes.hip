@@ -2,11 +2,13 @@
 //
 // A page's tokens of one KV head share a scale, so their rows in the call, a run, are one wavefront's: it holds 16 elements of a row in
 // a lane, D / 16 neighbouring lanes to a row (8 of the first half and the 8 they are rotated with), 16 rows at once, finds the largest of all
-// by lane moves, and writes codes; longer runs are gone through twice.  Queries have no scale: they are rows as in serving_append_kernel, in workgroups of
+// by lane moves, and writes codes; longer runs are gone through twice.  Pages of more than 32 tokens are a workgroup's.  Queries have no scale: they are rows as in serving_append_kernel, in workgroups of
 // their own behind the others (in front of them, and of the runs' chains of loads, 66 us instead of 60 for the 7328 rows below).
 // Bound by memory: 7328 rows in bf16 of 64 + 2 * 8 heads of 128 take 60 us, 4.8 TB/s of the 285 MB that they read and write, a large copy's rate; 1000
 // rows of 32 + 2 * 8 heads 11 us (22.5 MB: 4.6), and three tokens 4.5: there a chain of slots, rows, angles and a largest value.
 #ifndef ETC_GENERIC_ONLY
+#include <type_traits>
+
 #include "codes_rt.hip.h"
 
 namespace etc {
@@ -17,15 +19,15 @@ constexpr int kAp8Heads = 2;                // queries of a lane at once
 constexpr int kAp8LowByte = 127 - 40;       // of a scale
 constexpr int kAp8HighByte = 127 + 120;     // of 2^128 / 448
 
-template <int D>
-struct Angles { float c[kAp8Rows][D / 2], s[kAp8Rows][D / 2]; };
+template <int D, int ROWS>
+struct Angles { float c[ROWS][D / 2], s[ROWS][D / 2]; };
 
-// Sine and cosine of n rows (at most kAp8Rows), whose positions are position(row); a thread has one frequency.  The angle in fp64, reduced to half
+// Sine and cosine of n rows (at most ROWS), whose positions are position(row); a thread has one frequency.  The angle in fp64, reduced to half
 // a turn: positions run into the millions.
-template <int D, class Position>
-__device__ __forceinline__ void fill_angles(ETC_AS_LDS Angles<D> &A, double freq, int n, Position position)
+template <int D, int ROWS, class Position>
+__device__ __forceinline__ void fill_angles(ETC_AS_LDS Angles<D, ROWS> &A, double freq, int n, Position position)
 {
-    constexpr int AT_ONCE = kAp8Threads / (D / 2), TIMES = kAp8Rows / AT_ONCE;
+    constexpr int AT_ONCE = kAp8Threads / (D / 2), TIMES = ROWS / AT_ONCE;
     const int t0 = (int)threadIdx.x / (D / 2), e = (int)threadIdx.x % (D / 2);
     int p[TIMES];
 #pragma unroll
@@ -78,8 +80,8 @@ __device__ __forceinline__ void norm_head(float (&a)[8], float (&b)[8], const vo
     }
 }
 
-template <int D>
-__device__ __forceinline__ void rotate_head(float (&a)[8], float (&b)[8], ETC_AS_LDS const Angles<D> &A, int t, int c)
+template <int D, int ROWS>
+__device__ __forceinline__ void rotate_head(float (&a)[8], float (&b)[8], ETC_AS_LDS const Angles<D, ROWS> &A, int t, int c)
 {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -89,14 +91,19 @@ __device__ __forceinline__ void rotate_head(float (&a)[8], float (&b)[8], ETC_AS
     }
 }
 
-// Blocks [0, kv_blocks): runs that begin in rows [g * rows_per_wg, ..), heads 4 h .. of K or V.  Blocks behind: queries.
-template <int D, bool F32>
+// Blocks [0, kv_blocks): runs that begin in rows [g * rows_per_wg, ..), of K or V, and SHARED: a head, whose runs the wavefronts share, 16 rows of
+// 64 each; else heads 4 h .., one to a wavefront.  Blocks behind: queries.
+// SHARED is for pages of more than 32 tokens: 8192 rows of a prompt, 32 + 2 * 8 heads of 128, not shared and shared, in us, by the page's tokens:
+// 16 34 and -, 32 55 and 69, 64 89 and 59, 128 162 and 85, 256 163 and 93, 1024 604 and 230 (and of smaller pages 4 45 and -, 1 107 and -).
+template <int D, bool F32, bool SHARED>
 __global__ __launch_bounds__(kAp8Threads) void serving_append_codes_kernel(ServingDev S, etc_serving_append_codes_io io8, int rows_per_wg, int kv_wgs, int kv_blocks, int q_tokens)
 {
     constexpr int LPH = D / 16, RPI = 64 / LPH, ITERS = kAp8Rows / RPI;     // lanes to a row, rows at once, times
     constexpr int RPP = kAp8Threads / LPH;               // heads of a workgroup at once
-    __shared__ Angles<D> s_angles;
-    ETC_AS_LDS Angles<D> &A = *as_lds(&s_angles);
+    constexpr int ROWS = SHARED ? kAp8Waves * kAp8Rows : kAp8Rows;          // of a run at once
+    __shared__ Angles<D, ROWS> s_angles;
+    __shared__ float s_most[kAp8Waves];
+    ETC_AS_LDS Angles<D, ROWS> &A = *as_lds(&s_angles);
     const etc_serving_append_io &io = io8.append;
     const int tid = (int)threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id());
     const int psh = S.page_shift, pmask = (1 << psh) - 1, n_slots = (int)(io.n_pages << psh), c = (lane % LPH) * 8;
@@ -115,7 +122,7 @@ __global__ __launch_bounds__(kAp8Threads) void serving_append_codes_kernel(Servi
                 load_head<D, F32>(a[u], b[u], io.q, (int64_t)(t0 + t) * io.q_stride + h * D + c);
             }
             if (!there) {
-                fill_angles<D>(A, freq, nt, [&](int t) { return gld_i32(io.positions + t0 + t); });
+                fill_angles(A, freq, nt, [&](int t) { return gld_i32(io.positions + t0 + t); });
                 __syncthreads();
                 there = true;
             }
@@ -124,7 +131,7 @@ __global__ __launch_bounds__(kAp8Threads) void serving_append_codes_kernel(Servi
                 if (slot[u] < 0 || slot[u] >= n_slots) continue;      // the same for all lanes of a head
                 const int r = r0 + u * RPP, t = r / S.nq, h = r - t * S.nq;
                 if (S.qk_norm) norm_head<D>(a[u], b[u], io.gq, c, S.eps);
-                rotate_head<D>(a[u], b[u], A, t, c);
+                rotate_head(a[u], b[u], A, t, c);
                 uint16_t *dst = (uint16_t *)io.q_out + ((int64_t)(t0 + t) * S.nq + h) * D + c;
                 u32x4 x, y;
 #pragma unroll
@@ -138,7 +145,8 @@ __global__ __launch_bounds__(kAp8Threads) void serving_append_codes_kernel(Servi
 
     const int part = (int)blockIdx.x % kv_wgs, group = (int)blockIdx.x / kv_wgs, head_groups = kv_wgs / 2;
     const bool is_v = part >= head_groups;
-    const int h = (is_v ? part - head_groups : part) * kAp8Waves + wave;
+    const int first = is_v ? part - head_groups : part, h = SHARED ? first : first * kAp8Waves + wave;
+    const int u0 = SHARED ? wave * kAp8Rows : 0;         // this wavefront's part of ROWS
     const bool mine = h < S.nkv;
     const void *src = is_v ? io.v : io.k;
     const int64_t stride = is_v ? io.v_stride : io.k_stride;
@@ -177,25 +185,25 @@ __global__ __launch_bounds__(kAp8Threads) void serving_append_codes_kernel(Servi
             const int before = live_from(w0 - 1, -1);
             if (before >= 0 && slot_at(before) == slot - 1) continue;
         }
-        // its rows, if they stand side by side within the lanes and are no more than kAp8Rows: else 0
+        // its rows, as far as they stand side by side within the lanes; whole: those are all, and no more than ROWS
         const int n = __builtin_ctzll(~(__builtin_amdgcn_ballot_w64(lane >= j && slots == slot + (lane - j) && off + (lane - j) <= pmask) >> j));
         const uint64_t behind = j + n < 64 ? lives >> (j + n) << (j + n) : 0;
-        const bool whole = n <= kAp8Rows && (off + n > pmask || (behind != 0 ? __builtin_amdgcn_readlane(slots, __builtin_ctzll(behind)) != slot + n : w0 + 64 >= io.n_tokens));
+        const bool whole = n <= ROWS && (off + n > pmask || (behind != 0 ? __builtin_amdgcn_readlane(slots, __builtin_ctzll(behind)) != slot + n : w0 + 64 >= io.n_tokens));
         const int64_t page = slot >> psh;
         uint8_t *const scale = scales + page * S.nkv + h;
         int before = 0;                                  // the page's scale; asked for behind the rows, so that those do not wait for it
         float a[ITERS][8], b[ITERS][8];
-        // Rows row .. of the run, nr of them, up to kAp8Rows (those behind are the last one again): the values that are to be stored, in a and b.
+        // Rows row .. of the run, nr of them, up to ROWS (those behind are the last one again): the values that are to be stored, in a and b.
         auto values = [&](int row, int nr) {
             if (mine) {
 #pragma unroll
                 for (int u = 0; u < ITERS; ++u)
-                    load_head<D, F32>(a[u], b[u], src, (int64_t)(row + min(u * RPI + lane / LPH, nr - 1)) * stride + h * D + c);
+                    load_head<D, F32>(a[u], b[u], src, (int64_t)(row + min(u0 + u * RPI + lane / LPH, nr - 1)) * stride + h * D + c);
                 if (row == r) before = (int)*as_global(scale);
             }
             if (!is_v) {
                 __syncthreads();                         // who reads the angles of the rows before
-                fill_angles<D>(A, freq, nr, [&](int t) { return whole ? __shfl(positions, j + t, 64) : gld_i32(io.positions + row + t); });
+                fill_angles(A, freq, nr, [&](int t) { return whole ? __shfl(positions, j + t, 64) : gld_i32(io.positions + row + t); });
                 __syncthreads();
             }
             if (!mine) return;
@@ -203,7 +211,7 @@ __global__ __launch_bounds__(kAp8Threads) void serving_append_codes_kernel(Servi
             for (int u = 0; u < ITERS; ++u) {
                 if (!is_v) {
                     if (S.qk_norm) norm_head<D>(a[u], b[u], io.gk, c, S.eps);
-                    rotate_head<D>(a[u], b[u], A, min(u * RPI + lane / LPH, nr - 1), c);
+                    rotate_head(a[u], b[u], A, min(u0 + u * RPI + lane / LPH, nr - 1), c);
                 }
 #pragma unroll
                 for (int i = 0; i < 8; ++i) { a[u][i] = finite_or_nan(a[u][i]); b[u][i] = finite_or_nan(b[u][i]); }
@@ -211,14 +219,15 @@ __global__ __launch_bounds__(kAp8Threads) void serving_append_codes_kernel(Servi
         };
         float most = 0.f, inv = 0.f;
         bool once = true;                                // the run's values are in a and b
-        // Up to kAp8Rows rows of the run without one left out between them at a time, for the largest value, then to be stored.
+        // Up to ROWS rows of the run without one left out between them at a time, for the largest value, then to be stored.
 #pragma unroll 1
         for (int pass = 0; pass < 2; ++pass) {
             for (int row = r, at = slot;;) {
                 int nr = n;
                 if (!whole) {
-                    const bool on = lane < kAp8Rows && (at & pmask) + lane <= pmask && row + lane < io.n_tokens && gld_i32(io.slots + min(row + lane, io.n_tokens - 1)) == at + lane;
-                    nr = (int)__builtin_ctzll(~__builtin_amdgcn_ballot_w64(on));      // at least 1
+                    const bool on = lane < ROWS && (at & pmask) + lane <= pmask && row + lane < io.n_tokens && gld_i32(io.slots + min(row + lane, io.n_tokens - 1)) == at + lane;
+                    const uint64_t off_it = ~__builtin_amdgcn_ballot_w64(on);
+                    nr = off_it != 0 ? (int)__builtin_ctzll(off_it) : 64;      // at least 1
                 }
                 if (pass == 0 || !once) values(row, nr);
                 if (mine && pass == 0) {
@@ -229,7 +238,7 @@ __global__ __launch_bounds__(kAp8Threads) void serving_append_codes_kernel(Servi
                 } else if (mine) {
 #pragma unroll
                     for (int u = 0; u < ITERS; ++u) {
-                        const int i = u * RPI + lane / LPH;
+                        const int i = u0 + u * RPI + lane / LPH;
                         if (i >= nr) continue;
                         uint8_t *const dst = codes + ((int64_t)at + i) * S.nkv * D + h * D + c;
                         const float *x = a[u], *y = b[u];
@@ -244,26 +253,36 @@ __global__ __launch_bounds__(kAp8Threads) void serving_append_codes_kernel(Servi
                 once = false;
             }
             if (pass != 0 || !mine) continue;
-            int byte = scale_byte(wave_max_f(most), kAp8LowByte);
+            most = wave_max_f(most);
+            if constexpr (SHARED) {
+                if (lane == 0) s_most[wave] = most;
+                asm volatile("" ::"v"(before));          // it is here: another wavefront writes the page's scale behind the barrier
+                __syncthreads();
+#pragma unroll
+                for (int w = 0; w < kAp8Waves; ++w) most = fmaxf(most, s_most[w]);
+                __syncthreads();
+            }
+            int byte = scale_byte(most, kAp8LowByte);
             if (off > 0 && byte > before) {              // the tokens in front, in the new scale
                 const float f = __uint_as_float((uint32_t)max(127 + before - byte, 0) << 23);
                 const int64_t pieces = (int64_t)off * (D / 8);
                 auto piece = [&](int64_t i) { return reinterpret_cast<u32x2 *>(codes + ((page << psh) + i / (D / 8)) * S.nkv * D + h * D + i % (D / 8) * 8); };
-                for (int64_t i0 = lane; i0 < pieces; i0 += 4 * 64) {
+                constexpr int N = SHARED ? kAp8Threads : 64;
+                for (int64_t i0 = SHARED ? tid : lane; i0 < pieces; i0 += 4 * N) {
                     u32x2 w[4];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) w[k] = *as_global(piece(i0 + k * 64 < pieces ? i0 + k * 64 : i0));
+                    for (int k = 0; k < 4; ++k) w[k] = *as_global(piece(i0 + k * N < pieces ? i0 + k * N : i0));
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const f32x4 x = from_f8x4(w[k][0]), y = from_f8x4(w[k][1]);
                         w[k] = u32x2{to_f8x4(x[0] * f, x[1] * f, x[2] * f, x[3] * f), to_f8x4(y[0] * f, y[1] * f, y[2] * f, y[3] * f)};
-                        if (i0 + k * 64 < pieces) *as_global(piece(i0 + k * 64)) = w[k];
+                        if (i0 + k * N < pieces) *as_global(piece(i0 + k * N)) = w[k];
                     }
                 }
             } else if (off > 0) {
                 byte = min(before, kAp8HighByte);
             }
-            if (lane == 0) *as_global(scale) = (uint8_t)byte;
+            if (SHARED ? tid == 0 : lane == 0) *as_global(scale) = (uint8_t)byte;
             inv = one_over_scale(byte);
         }
     }
@@ -277,16 +296,15 @@ hipError_t launch_serving_append_codes(const ServingDev &S, const etc_serving_ap
     int q_tokens = kAp8Heads * kAp8Threads / (S.nq * (S.d / 16));
     if (q_tokens < 1) q_tokens = 1;
     if (q_tokens > kAp8Rows) q_tokens = kAp8Rows;
-    const int kv_wgs = 2 * ((S.nkv + kAp8Waves - 1) / kAp8Waves), kv_blocks = (n + rows - 1) / rows * kv_wgs;
+    const bool f32 = io.append.dtype == ETC_FP32, shared = (1 << S.page_shift) > 2 * kAp8Rows;
+    const int kv_wgs = 2 * (shared ? S.nkv : (S.nkv + kAp8Waves - 1) / kAp8Waves), kv_blocks = (n + rows - 1) / rows * kv_wgs;
     const dim3 grid((unsigned)(kv_blocks + (n + q_tokens - 1) / q_tokens)), block(kAp8Threads);
-    const bool f32 = io.append.dtype == ETC_FP32;
-    if (S.d == 128) {
-        if (f32) hipLaunchKernelGGL((serving_append_codes_kernel<128, true>), grid, block, 0, s, S, io, rows, kv_wgs, kv_blocks, q_tokens);
-        else hipLaunchKernelGGL((serving_append_codes_kernel<128, false>), grid, block, 0, s, S, io, rows, kv_wgs, kv_blocks, q_tokens);
-    } else {
-        if (f32) hipLaunchKernelGGL((serving_append_codes_kernel<64, true>), grid, block, 0, s, S, io, rows, kv_wgs, kv_blocks, q_tokens);
-        else hipLaunchKernelGGL((serving_append_codes_kernel<64, false>), grid, block, 0, s, S, io, rows, kv_wgs, kv_blocks, q_tokens);
-    }
+    auto launch = [&](auto d, auto is_f32, auto is_shared) {
+        hipLaunchKernelGGL((serving_append_codes_kernel<decltype(d)::value, decltype(is_f32)::value, decltype(is_shared)::value>), grid, block, 0, s, S, io, rows, kv_wgs, kv_blocks, q_tokens);
+    };
+    auto of_type = [&](auto d, auto is_f32) { shared ? launch(d, is_f32, std::true_type()) : launch(d, is_f32, std::false_type()); };
+    auto of_heads = [&](auto d) { f32 ? of_type(d, std::true_type()) : of_type(d, std::false_type()); };
+    S.d == 128 ? of_heads(std::integral_constant<int, 128>()) : of_heads(std::integral_constant<int, 64>());
     return hipGetLastError();
 }
 
