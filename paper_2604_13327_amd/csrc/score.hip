@@ -255,6 +255,7 @@ __global__ __launch_bounds__(kScoreThreads) void serving_score_kernel(ServingDev
     float from_ref = INFINITY;                           // -in_log2(s.ref)
     float best = -INFINITY;                              // of what this lane has read
     int fed = 0;
+    const bool short_row = nv < THREADS;
     auto feed = [&](const u32x4 (&w)[U], int id) {       // vector u: tokens id + u * THREADS * E ..; out of range: NaN
         float most[U], all = -INFINITY;
 #pragma unroll
@@ -286,16 +287,16 @@ __global__ __launch_bounds__(kScoreThreads) void serving_score_kernel(ServingDev
         s.l += l;
         s.t += t;
         if (top == 0) return;
-        // The wavefronts' lanes together: `top` of them reach the least of this.  Found again behind the second, fourth, eighth .. load (another
+        // The wavefronts' lanes together: `top` of them reach the least of this (of a row that has no vector for each of them: one wavefront's do).  Found again behind the second, fourth, eighth .. load (another
         // wavefront's number may be an older one then, which holds as well): 512 rows of 128256 in bf16 with 5 alternatives, 35.8 us -> 32.3.
         best = fmaxf(best, all);
         if (fed != 1 && (fed & (fed - 1)) == 0) {
-            const uint64_t t = TopList::reached(best, (top + WAVES - 1) / WAVES);
+            const uint64_t t = TopList::reached(best, short_row ? top : (top + WAVES - 1) / WAVES);
             if (lane == 0) s_begin[wave] = t;
             if (fed == 0) __syncthreads(); else in_order();
             uint64_t least = s_begin[0];
 #pragma unroll
-            for (int i = 1; i < WAVES; ++i) least = min(least, s_begin[i]);
+            for (int i = 1; i < WAVES; ++i) least = short_row ? max(least, s_begin[i]) : min(least, s_begin[i]);
             if (least > list.threshold) list.set(least);
         }
         ++fed;
