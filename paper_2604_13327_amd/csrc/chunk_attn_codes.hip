@@ -120,7 +120,7 @@ struct Rows8 {
 // ---- a block of more than 64 rows ------------------------------------------------------------------------------------------
 // 32 rows to a wavefront, all wavefronts over the same tiles of 64 keys, in three buffers of LDS: while tile t is being read, t + 1 comes to LDS
 // from registers, 16 bytes of K and of V to a thread, and t + 2 is on its way there.
-// Bound by the matrix units and the power they take: 4001 tokens behind 30000 keys, 64 heads of 128 on 8 (4.2 TFLOP), take 3.5 to 3.6 ms, 1.20
+// Bound by the matrix units and the power they take: 4001 tokens behind 30000 keys, 64 heads of 128 on 8 (4.2 TFLOP), take 3.5 to 3.6 ms, 1.2
 // PFLOP/s where a large bf16 product of a library reaches 1.29; the units are busy for half of the cycles.  Tried and slower there: K's fragments
 // all asked for in front of their products (1 %), exponentials placed between the products by hand (5 %), the next tile to LDS in front of the
 // products (6 %), a higher wave priority for either half of a tile (1 to 3 %).
@@ -219,8 +219,8 @@ __device__ __forceinline__ void wide_piece_codes(const ServingDev &S, const etc_
     uint32_t buf = 0;
     const int n_seen = min(first_masked, n_tiles);
     // Tiles that all rows see whole.  A SIMD has a wavefront of the upper and one of the lower half of the rows: the lower ones are half a tile late, so
-    // that one's products keep the matrix units busy while the other computes exponentials (7 % fewer cycles; 3605 -> 3490 us for 4001 tokens behind
-    // 30000 keys, 163 -> 153 for 1500 behind 4000, 32 heads of 128 on 4).
+    // that one's products keep the matrix units busy while the other computes exponentials (7 % fewer cycles; 3 % of the time of 4001 tokens behind
+    // 30000 keys, where power binds, 6 % of 1500 behind 4000, 32 heads of 128 on 4).
     const bool late = wave >= kCaWaves / 2;
     while (tile < n_seen) {
         const int stop = min(n_seen, whole_tiles);
@@ -287,8 +287,8 @@ __device__ __forceinline__ void wide_piece_codes(const ServingDev &S, const etc_
 // ---- a block of at most 64 rows --------------------------------------------------------------------------------------------
 // Bound by the rows of the cache.  Every wavefront goes through keys of its own, 32 at a time, every eighth such step, without a barrier: codes go to
 // its own part of LDS, two steps of them on their way or at hand, and from there to registers as they are, K's as rows, V's transposed, so that a
-// step's place is free for the one behind the next while it is worked on.  64 tokens over 4081 to 7935 keys, 32 heads of 128 on 8 (778 MB), take 159 to
-// 165 us, 4.9 TB/s; without any arithmetic 148: a head's row is 128 bytes in every 1024.  Rows pass the caches by (non-temporal loads): 164 us, 175
+// step's place is free for the one behind the next while it is worked on.  64 tokens over 4081 to 7935 keys, 32 heads of 128 on 8 (778 MB), take 160 to
+// 163 us, 4.8 TB/s; without any arithmetic 148: a head's row is 128 bytes in every 1024.  Rows pass the caches by (non-temporal loads): 164 us, 175
 // without, and 94 against 101 for half as many keys.  With K straight to registers and V through them to LDS, as bf16, it took 544.
 // V's codes become bf16 without their scales, which the probabilities take (keys of one instruction may lie in several pages).
 // The wavefronts' results are joined in LDS.
@@ -587,8 +587,8 @@ __device__ __forceinline__ void narrow_piece_codes(const ServingDev &S, const et
 
 // The pieces of a workgroup, one after the other, in groups of kXcds so that piece p stays with die p % kXcds: whole blocks' first, which take up to
 // 45 us, then narrow ones (2 to 30).  A workgroup's first piece is its own; of the others each takes the die's next one when it has none.  Dealt out in
-// advance, narrow pieces among the others, 32 mixed sequences took 67 us, not 62, and 40 of heads of 8 to 4 262, not 156; taken in turn in that
-// order 65 and 171.
+// advance, narrow pieces among the others, 32 mixed sequences (57 us) took 8 % longer and 40 of heads of 4 to 1 (150 us) 68 %; taken in turn in
+// that order 5 % and 10 %.
 template <class F>
 __device__ __forceinline__ void take_pieces(const ServingDev &S, const etc_serving_attention_io &io, ETC_AS_LDS CaLds &L, ETC_AS_LDS int *next, int n_pieces, F f)
 {
