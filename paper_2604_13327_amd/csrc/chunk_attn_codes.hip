@@ -82,8 +82,14 @@ __device__ __forceinline__ f32x16 scores_of(const u32x4 (&k)[D / 32], int k_scal
 // is left of a launch that takes its pieces one after the other when the first workgroup finds none, by the average piece.  Fitted to the times of all
 // candidates in 34 calls (1 to 200 sequences, chunks of 1 to 4096, caches to 30000): what it chooses is 2 % behind the fastest in the mean,
 // 15 % at worst (a prompt of 2000, 66 us without a cut, 57 with 1.5 shares).
+// Items of up to WHOLE tiles are not cut, nor is a cut estimated; whole and as the estimate has it, in us, calls back to back:
+//   tiles of the longest                          7           8          10          12          14          16
+//   3 single tokens, 4 heads of 64 on 2       10.4  11.8  10.3  11.9  10.8  12.3  11.4  12.3  11.6  12.8  12.5  12.2
+//   1 single token, 64 heads of 128 on 8      14.4  15.6  14.6  15.6  15.0  16.1  16.0  16.1  16.4  16.8  17.4  16.1
+//   300 tokens, 32 heads of 128 on 8          24.9  26.1  26.4  28.3  29.5  34.1  32.5  29.7  35.7  35.0  38.6  31.1
 struct CodesPrices {
     static constexpr bool OWN = true;
+    static constexpr int WHOLE = 10;
     static __device__ __forceinline__ float factor(int w) { return w == 1 ? 4.f : w == 2 ? 2.f : w == 3 ? 1.5f : w == 4 ? 1.25f : w == 5 ? 1.1f : w == 6 ? 1.f : 0.85f; }
     static __device__ __forceinline__ float tile(bool narrow) { return narrow ? 0.44f : 1.f; }
     static __device__ __forceinline__ float alone(bool narrow) { return narrow ? 0.39f : 1.07f; }

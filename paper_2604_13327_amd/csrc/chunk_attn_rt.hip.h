@@ -97,6 +97,7 @@ __device__ __forceinline__ int wave_max_i(int v)
 // in wide tiles; without OWN those are as cut() has them.
 struct CutPrices {
     static constexpr bool OWN = false;
+    static constexpr int WHOLE = kCaWholeTiles;          // tiles of an item up to which none is cut
     static __device__ __forceinline__ float factor(int w) { return w == 1 ? 4.f : w == 2 ? 3.f : w == 3 ? 2.f : w == 4 ? 1.5f : w == 5 ? 1.25f : w == 6 ? 1.1f : 1.f; }
 };
 
@@ -155,7 +156,7 @@ __device__ __forceinline__ int cut(const ServingDev &S, const etc_serving_attent
     };
     int best = 0, longest_piece = most;
     int longest_narrow = 0;                              // (OWN; longest_piece is that of wide sequences then)
-    if (most > kCaWholeTiles) {
+    if (most > Prices::WHOLE) {
         float pieces = 0.f, slots = 0.f;
         int longest = 0, parts = 1;
         bool whole = false;
