@@ -269,12 +269,25 @@ __device__ __forceinline__ void wide_piece_codes(const ServingDev &S, const etc_
     l = partner_sum(l);
     if (P.parts == 1) {
         if (!wave_live) return;
+        // By way of LDS, where everyone is done with the tiles: a lane has 4 elements of a row next to its partner's 4, and writes 8 of one.
         const float inv = 1.0f / l;
+        const uint32_t rows_at = (uint32_t)(uintptr_t)&B.rows[0] + wave * 32 * D * 2;
+        auto piece_at = [&](int r, int piece) { return rows_at + r * D * 2 + (piece ^ (r & (D / 8 - 1))) * 16; };
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-                put_out<D>(S, io, P, row, dt * 4 + q, half, f32x4{o[dt][4 * q] * inv, o[dt][4 * q + 1] * inv, o[dt][4 * q + 2] * inv, o[dt][4 * q + 3] * inv});
+                *reinterpret_cast<ETC_AS_LDS u32x2 *>(piece_at(col, dt * 4 + q) + half * 8) =
+                    u32x2{to_bf16x2(o[dt][4 * q] * inv, o[dt][4 * q + 1] * inv), to_bf16x2(o[dt][4 * q + 2] * inv, o[dt][4 * q + 3] * inv)};
+        in_order();
+        constexpr int AT_ONCE = 64 / (D / 8);            // rows
+#pragma unroll
+        for (int i = 0; i < 32 / AT_ONCE; ++i) {
+            const int lr = i * AT_ONCE + lane / (D / 8), piece = lane % (D / 8), r = P.r0 + wave * 32 + lr, rt = r / P.grp;
+            const u32x4 w = *reinterpret_cast<ETC_AS_LDS const u32x4 *>(piece_at(lr, piece));
+            if (r < P.rows)
+                *as_global(reinterpret_cast<u32x4 *>((uint16_t *)io.out + ((int64_t)(P.seq.q0 + rt) * S.nq + P.kvh * P.grp + (r - rt * P.grp)) * D + piece * 8)) = w;
+        }
         return;
     }
     if (wave_live) {
