@@ -287,8 +287,9 @@ __global__ __launch_bounds__(kScoreThreads) void serving_score_kernel(ServingDev
         s.l += l;
         s.t += t;
         if (top == 0) return;
-        // The wavefronts' lanes together: `top` of them reach the least of this (of a row that has no vector for each of them: one wavefront's do).  Found again behind the second, fourth, eighth .. load (another
-        // wavefront's number may be an older or a newer one then, which hold as well; their lower words are always 0): 512 rows of 128256 in bf16 with 5 alternatives, 35.8 us -> 32.3.
+        // The wavefronts' lanes together: `top` of them reach the least of this (of a row that has no vector for each of them: one wavefront's do).  Found
+        // again behind the second, fourth, eighth .. load: 512 rows of 128256 in bf16 with 5 alternatives, 35.8 us -> 32.3.  Another wavefront's number
+        // may be an older or a newer one then, which hold as well, and its lower word is always 0.
         best = fmaxf(best, all);
         if (fed != 1 && (fed & (fed - 1)) == 0) {
             const uint64_t t = TopList::reached(best, short_row ? top : (top + WAVES - 1) / WAVES);
