@@ -18,6 +18,7 @@ constexpr int kAp8Rows = 16;                // of the angles in LDS, and of a ru
 constexpr int kAp8Heads = 2;                // queries of a lane at once
 constexpr int kAp8LowByte = 127 - 40;       // of a scale
 constexpr int kAp8HighByte = 127 + 120;     // of 2^128 / 448
+constexpr int kAp8GridX = 1 << 23;          // workgroups in a row of the grid: a dimension takes less than 2^32 threads (2^20 rows of 128 KV heads ask for more)
 
 template <int D, int ROWS>
 struct Angles { float c[ROWS][D / 2], s[ROWS][D / 2]; };
@@ -91,8 +92,8 @@ __device__ __forceinline__ void rotate_head(float (&a)[8], float (&b)[8], ETC_AS
     }
 }
 
-// Blocks [0, kv_blocks): runs that begin in rows [g * rows_per_wg, ..), of K or V, and SHARED: a head, whose runs the wavefronts share, 16 rows of
-// 64 each; else heads 4 h .., one to a wavefront.  Blocks behind: queries.
+// Workgroups [0, kv_blocks): runs that begin in rows [g * rows_per_wg, ..), of K or V, and SHARED: a head, whose runs the wavefronts share, 16 rows of
+// 64 each; else heads 4 h .., one to a wavefront.  Those behind: queries.
 // SHARED is for pages of more than 32 tokens: 8192 rows of a prompt, 32 + 2 * 8 heads of 128, not shared and shared, in us, by the page's tokens:
 // 16 34 and -, 32 55 and 69, 64 89 and 59, 128 162 and 85, 256 163 and 93, 1024 604 and 230 (and of smaller pages 4 45 and -, 1 107 and -).
 template <int D, bool F32, bool SHARED>
@@ -107,9 +108,11 @@ __global__ __launch_bounds__(kAp8Threads) void serving_append_codes_kernel(Servi
     const etc_serving_append_io &io = io8.append;
     const int tid = (int)threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id());
     const int psh = S.page_shift, pmask = (1 << psh) - 1, n_slots = (int)(io.n_pages << psh), c = (lane % LPH) * 8;
+    const int wg = (int)(blockIdx.y * gridDim.x + blockIdx.x);
 
-    if ((int)blockIdx.x >= kv_blocks) {                  // queries
-        const int t0 = ((int)blockIdx.x - kv_blocks) * q_tokens, nt = min(q_tokens, io.n_tokens - t0);
+    if (wg >= kv_blocks) {                               // queries
+        const int t0 = (wg - kv_blocks) * q_tokens, nt = min(q_tokens, io.n_tokens - t0);
+        if (nt <= 0) return;                             // the rest of the grid's last row
         const double freq = *as_global(S.inv_freq + tid % (D / 2));
         bool there = false;
         for (int r0 = tid / LPH; r0 < (nt * S.nq + RPP - 1) / RPP * RPP; r0 += RPP * kAp8Heads) {
@@ -143,7 +146,7 @@ __global__ __launch_bounds__(kAp8Threads) void serving_append_codes_kernel(Servi
         return;
     }
 
-    const int part = (int)blockIdx.x % kv_wgs, group = (int)blockIdx.x / kv_wgs, head_groups = kv_wgs / 2;
+    const int part = wg % kv_wgs, group = wg / kv_wgs, head_groups = kv_wgs / 2;
     const bool is_v = part >= head_groups;
     const int first = is_v ? part - head_groups : part, h = SHARED ? first : first * kAp8Waves + wave;
     const int u0 = SHARED ? wave * kAp8Rows : 0;         // this wavefront's part of ROWS
@@ -298,7 +301,8 @@ hipError_t launch_serving_append_codes(const ServingDev &S, const etc_serving_ap
     if (q_tokens > kAp8Rows) q_tokens = kAp8Rows;
     const bool f32 = io.append.dtype == ETC_FP32, shared = (1 << S.page_shift) > 2 * kAp8Rows;
     const int kv_wgs = 2 * (shared ? S.nkv : (S.nkv + kAp8Waves - 1) / kAp8Waves), kv_blocks = (n + rows - 1) / rows * kv_wgs;
-    const dim3 grid((unsigned)(kv_blocks + (n + q_tokens - 1) / q_tokens)), block(kAp8Threads);
+    const int wgs = kv_blocks + (n + q_tokens - 1) / q_tokens;      // at most 2^16 * 2048 + 2^20
+    const dim3 grid((unsigned)(wgs < kAp8GridX ? wgs : kAp8GridX), (unsigned)((wgs + kAp8GridX - 1) / kAp8GridX)), block(kAp8Threads);
     auto launch = [&](auto d, auto is_f32, auto is_shared) {
         hipLaunchKernelGGL((serving_append_codes_kernel<decltype(d)::value, decltype(is_f32)::value, decltype(is_shared)::value>), grid, block, 0, s, S, io, rows, kv_wgs, kv_blocks, q_tokens);
     };

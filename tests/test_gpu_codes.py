@@ -379,3 +379,33 @@ def test_attention_refuses(etc, why):
     assert sv.read_error() == (0, 0, 0, 0)
     ref.check_attention(out, want, size)
     sv.close()
+
+
+# ---- ends of what is allowed ------------------------------------------------------------------------------------------
+def test_append_of_the_most_blocks(etc):
+    """2^20 rows of 128 KV heads in pages that workgroups share: more workgroups of K and V than one dimension of a launch takes, the queries'
+    behind them.  Nearly all rows are left out."""
+    s, rows = ref.shape(128, 128, 64, page=64), 1 << 20
+    live = np.concatenate((np.arange(3), np.arange(rows - 70, rows)))
+    where = np.concatenate((np.arange(5, 8), np.arange(64 + 60, 64 + 60 + 70)))
+    slots = np.full(rows, -1, np.int32)
+    slots[live] = where
+    x = torch.empty(rows, 128 * 64, dtype=torch.bfloat16, device="cuda")
+    q = torch.empty(rows, 128, 64, dtype=torch.bfloat16, device="cuda")
+    some = randn(1, len(live), 128 * 64)
+    x[torch.as_tensor(live).cuda()] = some.cuda()
+    q[3], q[rows - 71] = 7.0, 7.0
+    (k0, ks0), (v0, vs0) = codes.pools(2, 4, 64, 128, 64), codes.pools(3, 4, 64, 128, 64)
+    k, ks, v, vs = [t.cuda() for t in (k0, ks0, v0, vs0)]
+    pos = np.arange(rows) % 5000
+    sv = etc.Serving(s, max_seqs=1, max_tokens=rows, max_kv_len=100)
+    sv.append_codes(x, x, x, i32(pos), i32(slots), q, k, v, ks, vs)
+    assert sv.read_error() == (0, 0, 0, 0)
+    sv.close()
+    heads = some.view(-1, 128, 64)
+    want, size = ref.rotate(s, heads, pos[live])
+    got = q[torch.as_tensor(live).cuda()].cpu().double()
+    assert bool(((got - want).abs() <= 2.0 ** -8 * want.abs() + FP32 * size).all())
+    assert bool((q[3] == 7.0).all()) and bool((q[rows - 71] == 7.0).all())
+    codes.check_append(64, where, want, FP32 * size, k0, ks0, k, ks)
+    codes.check_append(64, where, heads.double(), torch.zeros(heads.shape, dtype=torch.float64), v0, vs0, v, vs)
