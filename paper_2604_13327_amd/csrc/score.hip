@@ -24,7 +24,9 @@ constexpr int kScoreSlices = 32;            // of a row, at most
 constexpr int kIdBits = 20;
 static_assert(kServingMaxVocab <= 1 << kIdBits, "ids");
 constexpr float kScoreLag = 6.f;            // weights up to e^6 lose nothing
-constexpr float kScoreHuge = 1e38f;         // references from here on leave no room for their multiple by 1 / ln 2
+// References from 2^30 on (of either sign): neighbours of theirs differ by 64 at least, so that only the logits equal to the largest have weight, and
+// are counted.  In front of that a multiple by 1 / ln 2 is rounded by 64 at most, as far as exponents go.
+constexpr float kScoreHuge = 0x1p30f;
 constexpr float kLog2E = 1.44269504088896f;
 constexpr double kPerLog2E = 1.0 / (double)kLog2E;      // of that very number: what it is off by scales all logits, not their differences
 constexpr int kScoreMinSlice = 4096;        // tokens (one row of 32000 in bf16: 8.8 us, 8.8 with 2048, 9.3 with 8192, 9.8 with 16384)
@@ -213,7 +215,7 @@ __device__ __forceinline__ Sums wave_total(Sums s)
     if (s.ref == ref) {
         l = s.l;
         t = s.t;
-    } else if (s.ref > -INFINITY && fabsf(ref) < kScoreHuge) {      // (numbers of that size differ by far more than an exponential can tell)
+    } else if (fabsf(s.ref) < kScoreHuge && fabsf(ref) < kScoreHuge) {      // (others differ by more than an exponential can tell; -inf too)
         const float by = log2_between(s.ref, ref), f = __builtin_amdgcn_exp2f(by);
         l = f * s.l;
         t = f * __builtin_fmaf(s.l, by, s.t);
@@ -279,7 +281,7 @@ __global__ __launch_bounds__(kScoreThreads) void serving_score_kernel(ServingDev
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                // NaN and -inf: 0; against a reference of the type's lowest values, which is -inf in powers of two: a number, of no weight in the end
+                // NaN and -inf: 0; against huge references, some -inf or inf in powers of two: a number, which is not used
                 const float y = __builtin_amdgcn_fmed3f(__builtin_fmaf(Vec<F32>::at(w[u], e), kLog2E, from_ref), -160.f, 64.f), p = __builtin_amdgcn_exp2f(y);
                 l += p;
                 t = __builtin_fmaf(p, y, t);
@@ -415,7 +417,7 @@ __global__ __launch_bounds__(kScoreThreads) void serving_score_kernel(ServingDev
     const double log_l = T.ref == -INFINITY ? 0.0 : log((double)T.l);
     auto logprob = [&](float x) {                        // of a logit
         if (!(x > -INFINITY) || T.ref == -INFINITY) return -INFINITY;
-        if (fabsf(T.ref) >= kScoreHuge) return x == T.ref ? (float)-log_l : (float)((double)x - (double)T.ref);
+        if (fabsf(T.ref) >= kScoreHuge) return (float)((x == T.ref ? 0.0 : (double)x - (double)T.ref) - log_l);
         return (float)((double)x - ((double)in_log2(T.ref) * kPerLog2E + log_l));
     };
     if (wave == WAVES - 1 && lane == 0) {

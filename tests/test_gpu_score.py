@@ -155,3 +155,35 @@ def test_score_after_and_before_sample(etc):
         assert np.allclose(drawn, again["lp"], atol=2.0 ** -16)          # without filters both are the same share
     assert sv.read_error() == (0, 0, 0, 0)
     sv.close()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocab", [1, 300, 16000, 40000])
+def test_score_large_logits(etc, vocab, dtype):
+    """Logits far from zero, neighbours in their type: from about 2^27 on those differ by more than an exponential tells apart, and a multiple of
+    one by 1 / ln 2 is rounded by as much.  The rounding of a reference, 2^-24 of it and 64 at most where sums count from it (2^30), is what
+    sums of p ln p are counted from: their roundings (as in _check) are relative to it too."""
+    g = torch.Generator().manual_seed(vocab)
+    bits = torch.int32 if dtype == torch.float32 else torch.int16
+    rows = []
+    for e in (20, 24, 26, 27, 28, 29, 30, 31, 33, 40, 64, 100, 126):
+        for m in (1.0, 1.4, 1.96):
+            for sign in (1, -1):
+                most = torch.tensor([sign * m * 2.0 ** e]).to(dtype).view(bits)
+                rows.append((most - sign * torch.randint(0, 40, (vocab,), generator=g).to(bits)).view(dtype))
+    for sign in (1, -1):                                 # both sides of 2^30, by parts of a row and mixed
+        edge = torch.tensor([sign * 2.0 ** 30]).to(dtype).view(bits)
+        for up in ([vocab // 2], [0, vocab - 1], list(range(0, vocab, 3))):
+            k = torch.zeros(vocab, dtype=bits)
+            k[up] = sign
+            rows += [(edge + k).view(dtype), (edge - k).view(dtype)]
+    x = torch.stack(rows)
+    tokens = torch.where(torch.arange(len(rows)) % 2 == 0, x.double().argmax(1), torch.randint(0, vocab, (len(rows),), generator=g)).numpy()
+    got = _run(etc, x, tokens, 9)
+    entropy = got["entropy"].copy()
+    got["entropy"][:] = 55.0
+    _check(x, tokens, 9, got)
+    for r in range(len(rows)):
+        want = codes.score(x[r].double().numpy(), None, 0)[1]
+        off = min(64.0, 1.4427 * 2.0 ** -24 * float(x[r].double().abs().max()))
+        assert abs(entropy[r] - want) <= 2.0 ** -17 * (8 + off + want), (r, entropy[r], want)
