@@ -415,10 +415,10 @@ __global__ __launch_bounds__(kScoreThreads) void serving_score_kernel(ServingDev
     }
     // ---- the row's outputs
     const double log_l = T.ref == -INFINITY ? 0.0 : log((double)T.l);
-    auto logprob = [&](float x) {                        // of a logit
+    auto logprob = [&](float x) {                        // of a logit; never positive, whatever l was rounded by
         if (!(x > -INFINITY) || T.ref == -INFINITY) return -INFINITY;
         if (fabsf(T.ref) >= kScoreHuge) return (float)((x == T.ref ? 0.0 : (double)x - (double)T.ref) - log_l);
-        return (float)((double)x - ((double)in_log2(T.ref) * kPerLog2E + log_l));
+        return (float)fmin((double)x - ((double)in_log2(T.ref) * kPerLog2E + log_l), 0.0);
     };
     if (wave == WAVES - 1 && lane == 0) {
         if (io.entropy_out) *as_global(io.entropy_out + row) = T.ref == -INFINITY ? 0.f : (float)fmax(log_l - (double)(T.t / T.l) * 0.6931471805599453, 0.0);

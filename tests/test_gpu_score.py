@@ -187,3 +187,20 @@ def test_score_large_logits(etc, vocab, dtype):
         want = codes.score(x[r].double().numpy(), None, 0)[1]
         off = min(64.0, 1.4427 * 2.0 ** -24 * float(x[r].double().abs().max()))
         assert abs(entropy[r] - want) <= 2.0 ** -17 * (8 + off + want), (r, entropy[r], want)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocab", [1, 300, 16000, 40000])
+def test_score_is_no_more_than_certain(etc, vocab, dtype):
+    """Rows of one likely token, alone or far above the others: a logarithm of a probability is not above 0, whatever was rounded on the way."""
+    g = torch.Generator().manual_seed(vocab)
+    rows = 64
+    tokens = torch.randint(0, vocab, (rows,), generator=g)
+    most = torch.randn(rows, generator=g) * torch.tensor([1.0, 30.0, 1e4, 1e8]).repeat(rows // 4)
+    most[4], most[9] = 2.5e38, -3e38
+    x = torch.full((rows, vocab), -math.inf)
+    x[::2] = most[::2, None] - 40 - 3 * torch.rand(rows // 2, vocab, generator=g)
+    x = x.scatter(1, tokens[:, None], most[:, None]).to(dtype)
+    got = _run(etc, x, tokens.numpy(), 5)
+    _check(x, tokens.numpy(), 5, got)
+    assert (got["logprob"] <= 0).all() and (got["tops"] <= 0).all() and (got["entropy"] >= 0).all()
