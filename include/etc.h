@@ -522,8 +522,10 @@ etc_status etc_serving_append_codes(etc_serving *s, const etc_serving_append_cod
 /* etc_serving_attention over such pools.  The scores are products of q and the values that the codes stand for: q goes through the
  * matrix units as two codes of 4 bits each, at scales of its row, exact to 2^-21 of the row's largest element.  The rest as there: sums
  * and softmax statistics in fp32, probabilities rounded to bf16 for sequences of more than 64 rows in the call and of 15 bits for others,
- * nothing outside a row's keys reaches it, NaN codes included.  Scale bytes 27 to 227 are supported (append writes 87 to 247 for values
- * up to 2^128, and none above 227 for values up to 2^108). */
+ * nothing outside a row's keys reaches it, NaN codes included.  Scale bytes from 27 on are supported, of K up to 227 where
+ * |q . k| / sqrt(head_dim) stays below 2^21, of V up to 238 - ceil(log2 n) for sequences of n keys, at most 227: sums of n values with
+ * weights up to 2^8 have to be fp32 (208 for 2^30 keys).
+ * Append writes 87 to 247 for values up to 2^128, and none above 208 for values up to 2^89. */
 typedef struct {
     etc_serving_attention_io attention;      /* k_pages, v_pages: codes, as in etc_serving_append_codes */
     const void *k_scale, *v_scale;

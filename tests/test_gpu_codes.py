@@ -409,3 +409,40 @@ def test_append_of_the_most_blocks(etc):
     assert bool((q[3] == 7.0).all()) and bool((q[rows - 71] == 7.0).all())
     codes.check_append(64, where, want, FP32 * size, k0, ks0, k, ks)
     codes.check_append(64, where, heads.double(), torch.zeros(heads.shape, dtype=torch.float64), v0, vs0, v, vs)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n_seqs,new,keys", [(40, 1, 4096), (40, 20, 2048), (20, 129, 4096)])
+@pytest.mark.parametrize("top", [False, True])
+def test_attention_ends_of_scales(etc, d, n_seqs, new, keys, top):
+    """The least scale and, for so many keys, the largest.  The first keys, 32 of every wavefront, score nearly 2^8 below the
+    others, so that those have weights near 2^8, the most that a reference that lags lets through; the largest case has values of 384 to 448 of one sign in every column.
+    Sequences share their pages, and there are enough of them that none is cut."""
+    s, page = ref.shape(16, 8, d), 16
+    n_pages = keys // page
+    v_byte = 238 - int(math.log2(keys)) if top else 27
+    k_byte = 227 if top else 27
+    table, _ = ref.paged([keys], page, 3, extra=0)
+    k0 = torch.zeros(n_pages, page, 8, d)
+    k0[torch.as_tensor(table[0, 256 // page:n_pages]).long(), :, :, 0] = 44.0 if d == 64 else 60.0      # times 1 / ln 2 / sqrt(d): 7.93, 7.65
+    g = torch.Generator().manual_seed(d)
+    v0 = (384 + 32 * torch.randint(0, 3, (n_pages, page, 8, d), generator=g)) * (torch.randint(0, 2, (8, d), generator=g) * 2 - 1) if top else \
+        torch.randn(n_pages, page, 8, d, generator=g) * 100
+    k, v = k0.to(torch.float8_e4m3fn), v0.float().clamp(-448, 448).to(torch.float8_e4m3fn)
+    ks, vs = [torch.full((n_pages, 8), b, dtype=torch.uint8) for b in (k_byte, v_byte)]
+    q = torch.zeros(new, 16, d)
+    q[..., 0] = 2.0 ** (127 - k_byte)
+    rows = n_seqs * new
+    out = torch.zeros(rows, 16, d, dtype=torch.bfloat16, device="cuda")
+    sv = etc.Serving(s, max_seqs=n_seqs, max_tokens=rows, max_kv_len=keys)
+    sv.attention_codes(q.bfloat16().repeat(n_seqs, 1, 1).cuda(), out, i32(new * np.arange(n_seqs + 1)), i32([keys - new] * n_seqs), i32(np.repeat(table, n_seqs, 0)),
+                       k.cuda(), v.cuda(), ks.cuda(), vs.cuda())
+    assert sv.read_error() == (0, 0, 0, 0)
+    sv.close()
+    want, size = ref.attention(s, q.bfloat16(), codes.values(k, ks), codes.values(v, vs), [0, new], [keys - new], table)
+    got = out.cpu().double().view(n_seqs, new, 16, d)
+    # as _attention's; and what is below 2^-126 of a probability times a scale, or of a product, is lost: at most 448 * 2^-126 of a key, twice
+    few = new * 2 <= 64
+    bound = 2.0 ** -8 * want.abs() + (2.0 ** -12 + (0 if few else 2.0 ** -8)) * size + keys * 2.0 ** -116
+    worst = float(((got - want).abs() / bound).max())
+    assert worst <= 1.0, f"worst error / bound {worst:.3f}"
