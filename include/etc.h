@@ -537,7 +537,8 @@ etc_status etc_serving_attention_codes(etc_serving *s, const etc_serving_attenti
  * -sum p ln p.  The likeliest are the first n_top in the order larger logit first, equal logits by lower id, without the banned ones;
  * where fewer are left the places behind them hold token -1, log-probability -inf.  A row with nothing left: log-probability -inf, entropy
  * 0.  A row whose token is negative is left out, its outputs stay as they were; one whose token is vocab or more as well, and is reported.
- * Weights and sums are fp32, the logarithm fp64 (no log-probability comes out above 0, no entropy below); sums are added in an order that the call's shape gives, the same at every run. */
+ * Weights and sums are fp32, the logarithm fp64 (no log-probability comes out above 0, no entropy below); sums are added in an order
+ * given by the call's shape and by where a row begins, modulo 16 bytes: the same pointers give the same bits, rows alike in both do too. */
 typedef struct {
     int32_t n_rows, dtype;          /* up to max_tokens; etc_dtype of logits */
     const void *logits;             /* [n_rows][vocab], rows row_stride elements apart; any alignment of the type */

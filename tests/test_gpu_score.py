@@ -204,3 +204,21 @@ def test_score_is_no_more_than_certain(etc, vocab, dtype):
     got = _run(etc, x, tokens.numpy(), 5)
     _check(x, tokens.numpy(), 5, got)
     assert (got["logprob"] <= 0).all() and (got["tops"] <= 0).all() and (got["entropy"] >= 0).all()
+
+
+def test_score_repeats(etc):
+    """The same pointers give the same bits, and so do rows that lie alike in memory (their first elements' places modulo 16 bytes)."""
+    for vocab, dtype, rows, stride in ((30001, torch.bfloat16, 24, 0), (30001, torch.float32, 9, 0), (30001, torch.bfloat16, 9, 7), (1003, torch.float32, 530, 0)):
+        one = _logits(vocab, 1, vocab, dtype)
+        x = one.repeat(rows, 1)
+        tokens = np.full(rows, 77)
+        sv = etc.Serving(ref.shape(vocab=vocab), max_seqs=rows if rows <= 1024 else 1024, max_tokens=rows, max_kv_len=1)
+        first = _run(etc, x, tokens, 7, stride=stride, serving=sv)
+        again = _run(etc, x, tokens, 7, stride=stride, serving=sv)
+        assert all(np.array_equal(first[k], again[k]) for k in first)
+        _check(x, tokens, 7, first, rows=range(0, rows, 5))
+        alike = 16 // dtype.itemsize // math.gcd(vocab + stride, 16 // dtype.itemsize)
+        for r in range(rows - alike):
+            assert all(np.array_equal(first[k][r], first[k][r + alike]) for k in first), r
+        assert sv.read_error() == (0, 0, 0, 0)
+        sv.close()
