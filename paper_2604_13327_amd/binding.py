@@ -533,7 +533,8 @@ class Serving:
         self._i32, self._f32, self._bf16 = (torch.int32,), (torch.float32,), (torch.bfloat16,)
         self._float = (torch.bfloat16, torch.float32)
         self._code = {torch.bfloat16: 0, torch.float32: 1}
-        self._f8, self._e8 = (torch.float8_e4m3fn,), (torch.float8_e8m0fnu, torch.uint8)
+        of_8 = lambda name: (getattr(torch, name),) if hasattr(torch, name) else ()      # noqa: E731  older torch lacks some: calls that need one refuse
+        self._f8, self._e8 = of_8("float8_e4m3fn"), of_8("float8_e8m0fnu") + (torch.uint8,)
 
     def _call(self, fn, io, stream):
         st = fn(self._h, C.byref(io), self._stream(self._device) if stream is None else stream.cuda_stream)

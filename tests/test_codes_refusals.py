@@ -97,3 +97,36 @@ def test_binding_checks():
     with pytest.raises(ValueError):
         s.score(_z(3, 51, dtype=f32), tokens, lp)
     assert len(called) == 4
+
+
+@pytest.mark.parametrize("missing", [(), ("float8_e8m0fnu",), ("float8_e8m0fnu", "float8_e4m3fn")])
+def test_a_torch_without_types_of_8_bits(monkeypatch, missing):
+    """A handle is made and its other operators work; scales may be bytes; what needs a type that is not there is refused."""
+    calls = []
+    names = [n for n in binding.EXPORTS if n.startswith("etc_serving_")]
+    stub = SimpleNamespace(**{n: (lambda *a, n=n: calls.append(n) or 0) for n in names})
+    monkeypatch.setattr(binding, "lib", lambda: stub)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    bf, f8 = torch.bfloat16, torch.float8_e4m3fn
+    q, k, slots, out = _z(3, 256, dtype=bf), _z(3, 128, dtype=bf), _z(3), _z(3, 4, 64, dtype=bf)
+    pool, codes, scale = _z(5, 16, 2, 64, dtype=bf), _z(5, 16, 2, 64, dtype=f8), _z(5, 2, dtype=torch.uint8)
+    logits, entropy, out2, one, table = _z(3, 50, dtype=torch.float32), _z(3, dtype=torch.float32), _z(3, 4, 64, dtype=bf), _z(1), _z(1, 5)
+    indptr = _z(2)
+    for name in missing:
+        monkeypatch.delattr(torch, name)
+    s = etc.Serving(ref.shape(4, 2, 64, vocab=50), max_seqs=1, max_tokens=3, max_kv_len=9)
+    stream = SimpleNamespace(cuda_stream=None)
+    s.append(q, k, k, slots, slots, out, pool, pool, stream=stream)
+    s.score(logits, entropy_out=entropy, stream=stream)
+    assert calls[-2:] == ["etc_serving_append", "etc_serving_score"]
+    many = len(calls)
+    if "float8_e4m3fn" in missing:
+        with pytest.raises(ValueError, match="k_pages"):
+            s.append_codes(q, k, k, slots, slots, out, codes, codes, scale, scale, stream=stream)
+        with pytest.raises(ValueError, match="k_pages"):
+            s.attention_codes(out, out2, indptr, one, table, codes, codes, scale, scale, stream=stream)
+        assert len(calls) == many
+    else:
+        s.append_codes(q, k, k, slots, slots, out, codes, codes, scale, scale, stream=stream)
+        assert calls[many:] == ["etc_serving_append_codes"]
+    s.close()
