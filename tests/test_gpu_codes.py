@@ -446,3 +446,19 @@ def test_attention_ends_of_scales(etc, d, n_seqs, new, keys, top):
     bound = 2.0 ** -8 * want.abs() + (2.0 ** -12 + (0 if few else 2.0 ** -8)) * size + keys * 2.0 ** -116
     worst = float(((got - want).abs() / bound).max())
     assert worst <= 1.0, f"worst error / bound {worst:.3f}"
+
+
+@pytest.mark.parametrize("page", [1, 2, 4])
+@pytest.mark.parametrize("nq,nkv,d", [(4, 2, 64), (6, 2, 128), (8, 1, 128)])
+def test_attention_pairs_with_windows(etc, page, nq, nkv, d):
+    """Blocks of 33 to 64 rows, whose wavefronts share a ring, over more pages than a window of their ids holds; NaN codes among what no row sees."""
+    rows = 64 // (nq // nkv)
+    _attention(etc, ref.shape(nq, nkv, d, page=page), [600 - rows], [rows])                  # one piece, three windows of single tokens
+    _attention(etc, ref.shape(nq, nkv, d, page=page), [5000, 255, 590, 9000], [rows, rows // 2 + 1, rows - 1, rows], seed=7)
+
+
+@pytest.mark.parametrize("nq,nkv,d", [(4, 2, 64), (6, 2, 128)])
+def test_attention_pairs_with_windows_not_cut(etc, nq, nkv, d):
+    """The same in pieces of several thousand keys."""
+    rows = 64 // (nq // nkv)
+    _attention(etc, ref.shape(nq, nkv, d, page=2), [1500 + 7 * b for b in range(150)], [rows - b % 3 for b in range(150)])

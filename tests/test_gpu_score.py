@@ -222,3 +222,22 @@ def test_score_repeats(etc):
             assert all(np.array_equal(first[k][r], first[k][r + alike]) for k in first), r
         assert sv.read_error() == (0, 0, 0, 0)
         sv.close()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,vocab,top", [(513, 128256, 5), (600, 70001, 64), (520, 16385, 0)])
+def test_score_long_rows_not_cut(etc, dtype, rows, vocab, top):
+    """More rows than are cut: a workgroup goes through a long row, its threshold found again many times."""
+    x, tokens = _logits(rows, rows, vocab, dtype), _tokens(rows, rows, vocab)
+    n = torch.arange(vocab).float() / vocab
+    x[0], x[1], x[2], x[3] = 10 * n, -10 * n, 2.0, (7 * n).round()          # rising, falling, flat, ties that rise
+    x[4], x[4, -9:], x[5, ::2] = -math.inf, 1.0, math.nan
+    _check(x, tokens, top, _run(etc, x, tokens, top), rows=[*range(7), *range(7, rows, 40), rows - 1])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,vocab,top", [(300, 20001, 64), (512, 16384, 9), (40, 128256, 64), (513, 20001, 5)])
+def test_score_more_rows_than_sequences(etc, dtype, rows, vocab, top):
+    """The workspace of the smallest handle, and scores of many rows in it."""
+    x, tokens = _logits(rows, rows, vocab, dtype), _tokens(rows, rows, vocab)
+    _check(x, tokens, top, _run(etc, x, tokens, top, max_seqs=1), rows=[*range(0, rows, 20), rows - 1])
