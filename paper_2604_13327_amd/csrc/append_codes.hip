@@ -5,7 +5,7 @@
 // by lane moves, and writes codes; longer runs are gone through twice.  Pages of more than 32 tokens are a workgroup's.  Queries have no scale: they are rows as in serving_append_kernel, in workgroups of
 // their own behind the others (in front of them, and of the runs' chains of loads, 66 us instead of 60 for the 7328 rows below).
 // Bound by memory: 7328 rows in bf16 of 64 + 2 * 8 heads of 128 take 60 us, 4.8 TB/s of the 285 MB that they read and write, a large copy's rate; 1000
-// rows of 32 + 2 * 8 heads 11 us (22.5 MB: 4.6), and three tokens 4.5: there a chain of slots, rows, angles and a largest value.
+// rows of 32 + 2 * 8 heads 11 us (22.5 MB: 4.6), and three tokens 4.3: there a chain of slots, rows, angles and a largest value.
 #ifndef ETC_GENERIC_ONLY
 #include <type_traits>
 
@@ -24,7 +24,8 @@ template <int D, int ROWS>
 struct Angles { float c[ROWS][D / 2], s[ROWS][D / 2]; };
 
 // Sine and cosine of n rows (at most ROWS), whose positions are position(row); a thread has one frequency.  The angle in fp64, reduced to half
-// a turn: positions run into the millions.
+// a turn, since positions run into the millions, and rounded to fp32 there: 2^-25 of half a turn at most, about what a rotation's
+// products and sum are rounded by.
 template <int D, int ROWS, class Position>
 __device__ __forceinline__ void fill_angles(ETC_AS_LDS Angles<D, ROWS> &A, double freq, int n, Position position)
 {

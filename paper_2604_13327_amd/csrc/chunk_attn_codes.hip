@@ -126,8 +126,8 @@ struct Rows8 {
 // ---- a block of more than 64 rows ------------------------------------------------------------------------------------------
 // 32 rows to a wavefront, all wavefronts over the same tiles of 64 keys, in three buffers of LDS: while tile t is being read, t + 1 comes to LDS
 // from registers, 16 bytes of K and of V to a thread, and t + 2 is on its way there.
-// Bound by the matrix units and the power they take: 4001 tokens behind 30000 keys, 64 heads of 128 on 8 (4.2 TFLOP), take 3.5 to 3.6 ms, 1.2
-// PFLOP/s where a large bf16 product of a library reaches 1.29; the units are busy for half of the cycles.  Tried and slower there: K's fragments
+// Bound by the matrix units and the power they take: 4001 tokens behind 30000 keys, 64 heads of 128 on 8 (4.2 TFLOP), take 3.46 to 3.72 ms on
+// different machines, 1.13 to 1.21 PFLOP/s where a large bf16 product of a library reaches 1.29; the units are busy for half of the cycles.  Tried and slower there: K's fragments
 // all asked for in front of their products (1 %), exponentials placed between the products by hand (5 %), the next tile to LDS in front of the
 // products (6 %), a higher wave priority for either half of a tile (1 to 3 %).
 template <int D>

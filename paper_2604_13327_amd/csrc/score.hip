@@ -8,7 +8,7 @@
 // Few rows are cut into slices; the workgroup that arrives last at a row joins them.
 // Bound by memory where rows are many: 4096 of 128256 in bf16 (1.05 GB) with 5 alternatives take 187 to 196 us, 5.5 TB/s.  301 such rows with 10 take 28
 // (77 MB: 16 us at a copy's rate): two slices to a row, and behind them 8 us of lists, join and ranks that no load covers; without alternatives 21.
-// 16 rows in fp32 with 20 take 10.2, one row of 1024 with 5 6.8, of which a launch is 2.  With lists that take elements one by one, and are
+// 16 rows in fp32 with 20 take 9.8 to 10.2, one row of 1024 with 5 7.0, of which a launch is 2.  With lists that take elements one by one, and are
 // cut by ranks, 131 us for those 16 rows, 59 for the 301.
 #ifndef ETC_GENERIC_ONLY
 #include <type_traits>
