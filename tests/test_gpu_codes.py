@@ -409,6 +409,8 @@ def test_append_of_the_most_blocks(etc):
     assert bool((q[3] == 7.0).all()) and bool((q[rows - 71] == 7.0).all())
     codes.check_append(64, where, want, FP32 * size, k0, ks0, k, ks)
     codes.check_append(64, where, heads.double(), torch.zeros(heads.shape, dtype=torch.float64), v0, vs0, v, vs)
+    del x, q
+    torch.cuda.empty_cache()                             # 34 GB that no other test asks for
 
 
 @pytest.mark.parametrize("d", [64, 128])
